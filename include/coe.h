@@ -276,6 +276,98 @@ int coe_debug_last_chunks(coe_ctx* ctx, int32_t cap, int32_t* chunks, int32_t* n
 int coe_regroup_static(int32_t n, const int32_t* cur, int32_t n_experts, int32_t* cnt, int32_t* off, int32_t* perm,
                        int32_t* inv, void* stream);
 
+/* ---- token-generating experts: paged key/value cache, attention over it, sampling ----------------------------------------
+ * Transformer-shaped experts that answer with tokens keep the keys and values of their requests in a cache of fixed-size
+ * blocks.  A step of such an expert is: coe_kv_plan (which blocks every request owns, where each new token's row goes); per
+ * layer coe_kv_append and coe_kv_attention; coe_sample_tokens on the logits.  Like coe_regroup_static these calls take no
+ * context: every array is a DEVICE pointer owned by the caller (a parameter said to be a host value is one), the kernels are
+ * enqueued on `stream` (a hipStream_t, NULL = the default stream) of the current device and the call returns without waiting.
+ * They allocate, free and synchronise nothing, read no device data on the host and may be captured into a HIP graph.
+ * Scratch memory is the caller's: the *_workspace functions say how many bytes; it needs no clearing, holds nothing between
+ * calls, and calls that overlap (two streams) need one each.  Arguments are checked on the host (COE_EINVAL; COE_ERANGE for
+ * a workspace that is too small; COE_EDEVICE when a launch fails; coe_last_error(NULL) holds the message, per thread);
+ * lengths, block ids and slots on the device are checked by the kernels, which never leave the arrays described here.
+ * A call with nothing to do (no requests, no tokens, no rows) succeeds. */
+
+/* A step's block tables and slot map, built from request lengths.
+ * Request r has have[r] >= 0 cached tokens in blocks table[r][0 .. ceil(have / block_size) - 1] (table: [n_requests][max_blocks])
+ * and is to grow by add[r] >= 0 tokens; add[r] < 0 marks a finished request, whose blocks are given back.
+ * Free block ids lie in a ring: ring_state = {head, count}, the ids ring[(head + i) % n_blocks] for i < count.  Requests are
+ * served in order: a request takes the blocks that its new tokens need from the ring's front, and writes them into its row of
+ * the table.  The first request that would need more blocks than are left, more than token_cap new tokens so far, or more
+ * than max_blocks blocks closes the step: it and every later one does not grow (none overtakes).  Finished requests anywhere
+ * give their blocks to the ring's end, in request order; they can be taken from the next call on.
+ * Written: seq_len[r] = tokens after the step (0 for a finished request); q_off[n_requests + 1] = first new token of every
+ * request in the step's token order; for token t of them position[t] (its place in its request, from 0) and slot[t] =
+ * block * block_size + position % block_size, both -1 from the last token up to token_cap; next_state = {head, count,
+ * requests before the one that closed the step (n_requests if none did), new tokens}.  Nothing that the next call's inputs
+ * need is written in place but the table and the ring: seq_len and next_state serve as have and ring_state then, and must
+ * not alias them.  The same inputs give the same outputs, ids included; repeating a call is harmless.
+ * A negative have counts as 0, one beyond max_blocks * block_size as that.
+ * block_size: a power of two in 8..1024; n_requests <= COE_KV_MAX_REQUESTS; n_blocks * block_size < 2^31. */
+#define COE_KV_MAX_REQUESTS 16384
+int coe_kv_plan(int32_t n_requests, int32_t block_size, int32_t n_blocks, int32_t max_blocks, int32_t token_cap,
+                const int32_t* have, const int32_t* add, int32_t* ring, const int32_t* ring_state, int32_t* table,
+                int32_t* seq_len, int32_t* q_off, int32_t* slot, int32_t* position, int32_t* next_state, void* stream);
+
+/* One layer's cache: the key (value) of token i of block b and head h is head_dim contiguous channels at
+ * k (v) + b * block_stride + i * token_stride + h * head_stride, in elements of dtype.  Any order of the axes that keeps
+ * channels innermost will do, keys and values interleaved in one tensor included.  dtype: COE_DT_BF16.  head_dim: a multiple
+ * of 8 in 8..128; k and v 16-byte aligned, strides multiples of 8; block_size as in coe_kv_plan; a block's rows lie within
+ * 2^31 bytes, the cache may be of any size. */
+typedef struct {
+    int32_t dtype, n_blocks, block_size, kv_heads, head_dim;
+    void *k, *v;
+    int64_t block_stride, token_stride, head_stride;
+} coe_kv_cache;
+
+/* Copy n_tokens new rows into the cache: row t of k and v (head h at t * token_stride + h * head_stride elements; 16-byte
+ * aligned, strides multiples of 8) goes to cache slot slot[t] = block * block_size + row.  Slots outside the cache (-1: the
+ * padding of coe_kv_plan) are skipped.  The cache struct is a host value, read during the call.  Two tokens must not share a
+ * slot. */
+int coe_kv_append(const coe_kv_cache* cache, int32_t n_tokens, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                  const void* v, int64_t v_token_stride, int64_t v_head_stride, const int32_t* slot, void* stream);
+
+/* Attention of every request's new tokens over its cached ones, the new ones included (append first).
+ * Request r's new tokens are rows q_off[r] .. q_off[r + 1] - 1 of q (at most max_new of them; n_tokens rows in all; q_off and
+ * seq_len as coe_kv_plan writes them); with m of them, row i stands at position p = seq_len[r] - m + i and sees the cached
+ * tokens j <= p, with window > 0 only those with j > p - window.  Query head h reads cache head h / (heads / kv_heads).
+ *   out = softmax_j(scale * q . k_j) v_j      lse = ln sum_j exp(scale * q . k_j)
+ * A row that sees nothing (p < 0) gets out = 0 and lse = -inf.  What a row does not see does not reach it, whatever its bits.
+ * q and out: row t, head h at t * token_stride + h * head_stride elements of the cache's dtype, 16-byte aligned, strides
+ * multiples of 8.  lse: [n_tokens][heads] fp32, or NULL.  table: [n_requests][max_blocks] block ids; a cached token whose
+ * block id is outside the cache reads as zeros; seq_len is limited to max_blocks * block_size.
+ * Numerics: products and sums in fp32, exponentials relative to a running maximum, the probabilities rounded to bf16 before
+ * they meet the values, one rounding of the result to bf16.  The same inputs give the same bits.
+ * heads: a multiple of kv_heads.  workspace: coe_kv_attention_workspace bytes for the same sizes, 16-byte aligned. */
+int64_t coe_kv_attention_workspace(int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads, int32_t kv_heads,
+                                   int32_t head_dim);
+int coe_kv_attention(const coe_kv_cache* cache, int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads,
+                     int32_t window, float scale, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                     const int32_t* q_off, const int32_t* seq_len, const int32_t* table, int32_t max_blocks, void* out,
+                     int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace, int64_t workspace_bytes,
+                     void* stream);
+
+/* Draw a token from every row of logits [n_rows][vocab] (COE_DT_F32 or COE_DT_BF16, rows logits_stride elements apart).
+ * Per row (arrays [n_rows], each may be NULL = off for all rows): temperature T (NULL: 1), top_k (<= 0: off), top_p (>= 1: off),
+ * min_p (<= 0: off).  With the tokens in descending order of their logits, equal ones by ascending index, weights
+ * w = exp((x - max x) / T), and M the weight of the first top_k tokens, a token is kept when its place is below top_k, the
+ * weights before it sum to less than top_p * M, and w >= min_p; the first token is always kept, a logit of -inf or NaN never.
+ * Among the kept tokens the row's random numbers decide: noise [n_rows][vocab] fp32 (rows noise_stride apart) holds
+ * exponentially distributed numbers E, and token[r] is the index with the largest (x - max x) / T - ln E (the lowest among
+ * equals; numbers that are negative or NaN never win), which draws every kept token with its renormalised probability.  If no
+ * kept token has a usable number, and where T <= 0 (greedy: the noise is not read), the first token of the order is taken.
+ * noise may be NULL when every row is greedy, which only T == NULL rules out on the host: other rows then take the first token.
+ * logprob[r] (nullable): ln of the token's probability under softmax(logits / T), before any filter (T <= 0: T = 1).
+ * A row without a logit above -inf gets token -1 and logprob -inf.
+ * Numerics: fp32; comparisons of logits are exact.  The same inputs give the same tokens.
+ * workspace: coe_sample_workspace bytes (may be 0), 16-byte aligned. */
+int64_t coe_sample_workspace(int32_t n_rows, int32_t vocab);
+int coe_sample_tokens(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits, int64_t logits_stride,
+                      const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                      const float* noise, int64_t noise_stride, int32_t* token, float* logprob, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
 /* Launch sequences of the last step in launch order: the first expert of each, its predicted cost and the executor it ran
  * on.  Writes at most cap entries (arrays nullable); *n_units receives the total. */
 int coe_debug_last_assignment(coe_ctx* ctx, int32_t cap, int32_t* first_expert, int64_t* cost_ns, int32_t* executor,

@@ -27,7 +27,10 @@ EXPORTS = [
     "coe_policy_stage", "coe_policy_resident", "coe_policy_set_eviction", "coe_policy_set_in_use_depth", "coe_set_arranging", "coe_arrange_defer", "coe_set_latency_model", "coe_assign_executors", "coe_debug_last_assignment",
     "coe_regroup_static", "coe_debug_last_chunks", "coe_set_host_tier", "coe_debug_host_log", "coe_profiler_memory_scores", "coe_profiler_expert_budget", "coe_profiler_executable_batch", "coe_profiler_usage_probabilities",
     "coe_profiler_fit_latency", "coe_profiler_max_batch", "coe_profiler_arranging_window", "coe_profiler_window_step",
+    "coe_kv_plan", "coe_kv_append", "coe_kv_attention_workspace", "coe_kv_attention", "coe_sample_workspace", "coe_sample_tokens",
 ]
+COE_DT_F32, COE_DT_BF16 = 0, 1
+COE_KV_MAX_REQUESTS = 16384
 
 
 class coe_layer(C.Structure):
@@ -52,6 +55,12 @@ class coe_step_stats(C.Structure):
                 ("n_deferred_groups", C.c_int32), ("n_deferred_requests", C.c_int32), ("n_executors_used", C.c_int32),
                 ("n_device_allocs", C.c_int32), ("n_host_misses", C.c_int32), ("bytes_read", C.c_int64),
                 ("read_us", C.c_double)]
+
+
+class coe_kv_cache(C.Structure):
+    """One layer's paged cache; k and v are device addresses, strides in elements."""
+    _fields_ = [("dtype", C.c_int32), ("n_blocks", C.c_int32), ("block_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("block_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class coe_window_state(C.Structure):
@@ -114,6 +123,12 @@ def _load():
     L.coe_profiler_usage_probabilities.argtypes = [i32, i32, vp, i32, vp]
     L.coe_profiler_window_step.argtypes = [i32, C.c_double, C.c_double, i32, i32, vp, C.POINTER(coe_window_state)]
     L.coe_regroup_static.argtypes = [i32, vp, i32, vp, vp, vp, vp, vp]
+    L.coe_kv_plan.argtypes = [i32] * 5 + [vp] * 11
+    L.coe_kv_append.argtypes = [C.POINTER(coe_kv_cache), i32, vp, i64, i64, vp, i64, i64, vp, vp]
+    L.coe_kv_attention_workspace.argtypes = [i32] * 6; L.coe_kv_attention_workspace.restype = i64
+    L.coe_kv_attention.argtypes = [C.POINTER(coe_kv_cache)] + [i32] * 5 + [C.c_float, vp, i64, i64, vp, vp, vp, i32, vp, i64, i64, vp, vp, i64, vp]
+    L.coe_sample_workspace.argtypes = [i32, i32]; L.coe_sample_workspace.restype = i64
+    L.coe_sample_tokens.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
     return L
 
 
@@ -140,6 +155,52 @@ def coe_regroup_static(n: int, cur: int, n_experts: int, cnt: int, off: int, per
                                 _ptr(inv or None), C.c_void_p(stream or None))
     if rc < 0:
         raise CoEError(rc, lib.coe_last_error(None).decode())
+
+
+# ---- token-generating experts: device addresses are integers (0 = NULL), as a tensor's data_ptr() gives them -------------------
+def _static(rc: int) -> int:
+    if rc < 0:
+        raise CoEError(rc, lib.coe_last_error(None).decode())
+    return rc
+
+
+def coe_kv_plan(n_requests: int, block_size: int, n_blocks: int, max_blocks: int, token_cap: int, have: int, add: int, ring: int, ring_state: int,
+                table: int, seq_len: int, q_off: int, slot: int, position: int, next_state: int, stream: int = 0) -> None:
+    """A step's block tables and slot map from the requests' lengths; enqueued on `stream`."""
+    _static(lib.coe_kv_plan(n_requests, block_size, n_blocks, max_blocks, token_cap, have or None, add or None, ring or None, ring_state or None,
+                            table or None, seq_len or None, q_off or None, slot or None, position or None, next_state or None, stream or None))
+
+
+def coe_kv_append(cache: coe_kv_cache, n_tokens: int, k: int, k_token_stride: int, k_head_stride: int, v: int, v_token_stride: int,
+                  v_head_stride: int, slot: int, stream: int = 0) -> None:
+    """New keys and values into their cache slots; enqueued on `stream`."""
+    _static(lib.coe_kv_append(C.byref(cache), n_tokens, k or None, k_token_stride, k_head_stride, v or None, v_token_stride, v_head_stride,
+                              slot or None, stream or None))
+
+
+def coe_kv_attention_workspace(n_requests: int, n_tokens: int, max_new: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return _static(lib.coe_kv_attention_workspace(n_requests, n_tokens, max_new, heads, kv_heads, head_dim))
+
+
+def coe_kv_attention(cache: coe_kv_cache, n_requests: int, n_tokens: int, max_new: int, heads: int, window: int, scale: float, q: int,
+                     q_token_stride: int, q_head_stride: int, q_off: int, seq_len: int, table: int, max_blocks: int, out: int,
+                     out_token_stride: int, out_head_stride: int, lse: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """The new tokens' attention over the paged cache; enqueued on `stream`."""
+    _static(lib.coe_kv_attention(C.byref(cache), n_requests, n_tokens, max_new, heads, window, scale, q or None, q_token_stride, q_head_stride,
+                                 q_off or None, seq_len or None, table or None, max_blocks, out or None, out_token_stride, out_head_stride, lse or None,
+                                 workspace or None, workspace_bytes, stream or None))
+
+
+def coe_sample_workspace(n_rows: int, vocab: int) -> int:
+    return _static(lib.coe_sample_workspace(n_rows, vocab))
+
+
+def coe_sample_tokens(n_rows: int, vocab: int, dtype: int, logits: int, logits_stride: int, temperature: int, top_k: int, top_p: int, min_p: int,
+                      noise: int, noise_stride: int, token: int, logprob: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """A token from every row of logits; enqueued on `stream`."""
+    _static(lib.coe_sample_tokens(n_rows, vocab, dtype, logits or None, logits_stride, temperature or None, top_k or None, top_p or None,
+                                  min_p or None, noise or None, noise_stride, token or None, logprob or None, workspace or None, workspace_bytes,
+                                  stream or None))
 
 
 def coe_profiler_fit_latency(batch, latency_us) -> Tuple[float, float]:

@@ -1208,6 +1208,17 @@ static_assert(COE_STATIC_SCRATCH_BYTES == sizeof(int32_t) * (size_t)coe::k::kReg
 
 // message of the last failed call that takes no context (per thread)
 static thread_local std::string g_err;
+}
+int coe::context_free_error(int code, const char* message) noexcept
+{
+    try {
+        g_err = message;
+    } catch (...) {
+        g_err.clear();
+    }
+    return code;
+}
+extern "C" {
 
 const char* coe_last_error(const coe_ctx* ctx) { return ctx ? ctx->err.c_str() : g_err.c_str(); }
 

@@ -7,6 +7,10 @@
 #include <cstdint>
 
 namespace coe {
+
+// keeps the message that coe_last_error(NULL) returns on this thread; returns `code`
+int context_free_error(int code, const char* message) noexcept;
+
 namespace k {
 
 constexpr int kRegroupTile = 256;     // the histogram scratch is sized for one histogram per so many requests
@@ -181,6 +185,47 @@ hipError_t head_cls(const void* x, const float* gamma, const float* beta, const 
 // grouped form: the four tensors at weights[g] + off[0..3]; r and routes as in head_gap_fc_grouped
 hipError_t head_cls_grouped(const void* x, const GroupTable& groups, const size_t off[4], int32_t N, int32_t T, int32_t D, int32_t ncls,
                             const RouteArgs& r, const GroupRoutes& routes, hipStream_t stream);
+
+// ---- token-generating experts (bf16 only) ------------------------------------------------------------------------
+// Block tables and slot map of a step; the arguments of coe_kv_plan.
+constexpr int kPlanMaxRequests = 16384;
+hipError_t kv_plan(int32_t n_requests, int32_t block_shift, int32_t n_blocks, int32_t max_blocks, int32_t token_cap, const int32_t* have,
+                   const int32_t* add, int32_t* ring, const int32_t* ring_state, int32_t* table, int32_t* seq_len, int32_t* q_off,
+                   int32_t* slot, int32_t* position, int32_t* next_state, hipStream_t stream);
+
+// Strides in elements; block_size = 1 << block_shift.
+struct KvCache {
+    uint16_t *k, *v;
+    int64_t block_stride, token_stride, head_stride;
+    int32_t n_blocks, block_shift, kv_heads, head_dim;
+};
+hipError_t kv_append(const KvCache& cache, int32_t n_tokens, const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+                     const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride, const int32_t* slot, hipStream_t stream);
+
+struct KvAttention {
+    int32_t n_requests, n_tokens, max_new, heads, window, max_blocks;
+    float scale;
+    const uint16_t* q;
+    int64_t q_token_stride, q_head_stride;
+    const int32_t *q_off, *seq_len, *table;
+    uint16_t* out;
+    int64_t out_token_stride, out_head_stride;
+    float* lse;
+};
+int64_t kv_attention_workspace(int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads, int32_t kv_heads, int32_t head_dim);
+hipError_t kv_attention(const KvCache& cache, const KvAttention& a, void* workspace, hipStream_t stream);
+
+struct Sampling {
+    const void* logits;
+    int64_t logits_stride, noise_stride;
+    const float *temperature, *top_p, *min_p, *noise;
+    const int32_t* top_k;
+    int32_t* token;
+    float* logprob;
+    int32_t vocab;
+};
+int64_t sample_workspace(int32_t n_rows, int32_t vocab);
+hipError_t sample_tokens(int dtype, int32_t n_rows, const Sampling& s, void* workspace, hipStream_t stream);
 
 }  // namespace k
 }  // namespace coe

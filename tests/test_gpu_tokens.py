@@ -1,0 +1,633 @@
+"""The calls for token-generating experts against their 64-bit statement: lengths, masks, layouts and values where they can go wrong."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import tokens as T
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2503_02354_amd import binding
+    return binding
+
+
+def _dev(a):
+    import torch
+    a = np.ascontiguousarray(a)
+    return torch.from_numpy(a.view(np.int16) if a.dtype == np.uint16 else a).cuda()
+
+
+def _bf16(a):
+    """Round float64 to bf16 bits (to nearest even)."""
+    b = np.asarray(a, np.float32).view(np.uint32)
+    return ((b + 0x7FFF + ((b >> 16) & 1)) >> 16).astype(np.uint16)
+
+
+def _stream():
+    import torch
+    return torch.cuda.current_stream().cuda_stream
+
+
+# ---- plan -------------------------------------------------------------------------------------------------------
+def _plan_gpu(B, block, n_blocks, max_blocks, cap, have, add, ring, state, table):
+    import torch
+    n = len(have)
+    d = dict(have=_dev(np.asarray(have, np.int32)), add=_dev(np.asarray(add, np.int32)), ring=_dev(ring), state=_dev(np.asarray(state, np.int32)),
+             table=_dev(table))
+    out = {k: torch.full((size,), -77, dtype=torch.int32, device="cuda") for k, size in
+           (("seq_len", max(n, 1)), ("q_off", n + 1), ("slot", max(cap, 1)), ("position", max(cap, 1)), ("next_state", 4))}
+    B.coe_kv_plan(n, block, n_blocks, max_blocks, cap, *(d[k].data_ptr() for k in ("have", "add", "ring", "state", "table")),
+                  *(out[k].data_ptr() for k in ("seq_len", "q_off", "slot", "position", "next_state")), _stream())
+    got = {k: v.cpu().numpy() for k, v in out.items()}
+    got["seq_len"], got["slot"], got["position"] = got["seq_len"][:n], got["slot"][:cap], got["position"][:cap]
+    got["table"], got["ring"] = d["table"].cpu().numpy(), d["ring"].cpu().numpy()
+    return got
+
+
+def _pool(rng, have, block, n_blocks, max_blocks):
+    """Random tables for `have` cached tokens, the rest of the ids in a ring that starts anywhere."""
+    order = rng.permutation(n_blocks).astype(np.int32)
+    table = np.full((len(have), max_blocks), -9, np.int32)
+    at = 0
+    for r, h in enumerate(have):
+        b = -(-int(h) // block)
+        table[r, :b] = order[at:at + b]
+        at += b
+    assert at <= n_blocks
+    head = int(rng.integers(n_blocks))
+    ring = np.full(n_blocks, -5, np.int32)
+    ring[(head + np.arange(n_blocks - at)) % n_blocks] = order[at:]
+    return table, ring, [head, n_blocks - at]
+
+
+@pytest.mark.parametrize("n,block,most,new,done,spare,cap", [
+    (0, 16, 1, 1, 0.0, 3, 4),            # no requests: offsets and state all the same
+    (1, 8, 40, 1, 0.0, 3, 1),
+    (1, 8, 0, 9000, 0.0, 2000, 9000),    # one long prompt, many workgroups
+    (7, 16, 100, 40, 0.3, 200, 500),
+    (255, 16, 300, 1, 0.1, 300, 256), (256, 32, 300, 2, 0.1, 600, 600), (257, 64, 300, 70, 0.1, 600, 20000),
+    (300, 16, 64, 33, 0.0, 100, 20000),  # the pool runs out part of the way
+    (300, 16, 64, 33, 0.2, 4000, 1000),  # the token room runs out
+    (1000, 16, 64, 0, 0.0, 0, 10),       # nothing grows
+    (16384, 8, 30, 3, 0.05, 16384, 60000),
+])
+def test_plan(B, n, block, most, new, done, spare, cap):
+    rng = np.random.default_rng(n + block + most)
+    have = rng.integers(0, most + 1, n).astype(np.int32)
+    add = rng.integers(0, new + 1, n).astype(np.int32) if new > 1 else np.full(n, new, np.int32)
+    add[rng.random(n) < done] = -1
+    if new == 9000:
+        add[:] = 9000
+    max_blocks = -(-(most + new) // block) + 1
+    n_blocks = int(sum(-(-have // block))) + spare + 1 if n else spare
+    n_blocks = int((-(-have // block)).sum()) + spare + 1
+    table, ring, state = _pool(rng, have, block, n_blocks, max_blocks)
+    want = T.plan(block, n_blocks, max_blocks, cap, have, add, ring, state, table)
+    got = _plan_gpu(B, block, n_blocks, max_blocks, cap, have, add, ring, state, table)
+    for k in want:
+        assert np.array_equal(got[k], want[k]), k
+
+
+def test_plan_values_out_of_range(B):
+    """Negative and overlong lengths, a request too long for its row, sums beyond 32 bits: clamped or refused, never followed."""
+    block, n_blocks, max_blocks = 16, 50, 4
+    have = np.array([-5, 30, 1000, 10, 3, 20], np.int32)
+    add = np.array([3, 2, -1, 55, 1, -7], np.int32)
+    rng = np.random.default_rng(0)
+    table = rng.permutation(n_blocks)[:24].reshape(6, 4).astype(np.int32)
+    ring = rng.permutation(n_blocks).astype(np.int32)
+    for state in ([48, 20], [0, 0]):
+        want = T.plan(block, n_blocks, max_blocks, 9, have, add, ring, state, table)
+        assert want["next_state"][2] == (3 if state[1] else 0)
+        got = _plan_gpu(B, block, n_blocks, max_blocks, 9, have, add, ring, state, table)
+        for k in want:
+            assert np.array_equal(got[k], want[k]), k
+    add = np.full(6, 2 ** 31 - 1, np.int32)
+    want = T.plan(block, n_blocks, max_blocks, 9, have, add, ring, [3, 20], table)
+    got = _plan_gpu(B, block, n_blocks, max_blocks, 9, have, add, ring, [3, 20], table)
+    for k in want:
+        assert np.array_equal(got[k], want[k]), k
+
+
+def test_plan_many_steps_conserve_blocks(B):
+    """A service that runs for a while: outputs of a step are the inputs of the next; no block is lost or owned twice."""
+    rng = np.random.default_rng(5)
+    n, block, n_blocks, max_blocks, cap = 40, 8, 300, 32, 400
+    have = np.zeros(n, np.int32)
+    table, ring, state = _pool(rng, have, block, n_blocks, max_blocks)
+    refused = 0
+    for _ in range(60):
+        add = np.where(have == 0, rng.integers(0, 60, n), 1).astype(np.int32)
+        add[(have > 0) & (rng.random(n) < 0.08)] = -1
+        add[have + np.maximum(add, 0) > max_blocks * block] = -1
+        want = T.plan(block, n_blocks, max_blocks, cap, have, add, ring, state, table)
+        got = _plan_gpu(B, block, n_blocks, max_blocks, cap, have, add, ring, state, table)
+        for k in want:
+            assert np.array_equal(got[k], want[k]), k
+        refused += got["next_state"][2] < n
+        have, table, ring, state = got["seq_len"], got["table"], got["ring"], got["next_state"][:2]
+        owned = np.concatenate([table[r, :-(-int(h) // block)] for r, h in enumerate(have)])
+        free = ring[(state[0] + np.arange(state[1])) % n_blocks]
+        assert sorted(np.concatenate([owned, free]).tolist()) == list(range(n_blocks))
+    assert refused > 0
+
+
+# ---- append -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("tokens,kv,dim,block,layout", [(1, 1, 8, 8, "token"), (3, 12, 64, 16, "head"), (100, 5, 80, 32, "pair"), (257, 8, 128, 64, "token"),
+                                                        (33, 40, 128, 16, "head"), (2000, 2, 24, 1024, "token")])
+def test_append(B, tokens, kv, dim, block, layout):
+    """Every row lands in its slot, bit for bit (NaN bits too); padding and slots outside the cache are skipped; nothing else changes."""
+    import torch
+    rng = np.random.default_rng(tokens)
+    n_blocks = -(-tokens // block) + 2
+    new = rng.integers(0, 65536, (tokens, 3 * kv, dim)).astype(np.uint16)
+    slots = rng.permutation(n_blocks * block)[:tokens].astype(np.int32)
+    skip = rng.random(tokens) < 0.2
+    slot = np.where(skip, rng.choice([-1, -2 ** 31, n_blocks * block, 2 ** 31 - 1], tokens), slots).astype(np.int32)
+    k, v, cache = _make_cache(B, rng.integers(0, 65536, (2, n_blocks, block, kv, dim)).astype(np.uint16), layout)
+    want = [k.cpu().numpy().view(np.uint16).copy(), v.cpu().numpy().view(np.uint16).copy()]
+    for i, w in enumerate(want):
+        for t in np.nonzero(~skip)[0]:
+            w[slots[t] // block, slots[t] % block] = new[t, (1 + i) * kv:(2 + i) * kv]
+    d, s = _dev(new), _dev(slot)
+    B.coe_kv_append(cache, tokens, d.data_ptr() + 2 * kv * dim, 3 * kv * dim, dim, d.data_ptr() + 4 * kv * dim, 3 * kv * dim, dim, s.data_ptr(), _stream())
+    torch.cuda.synchronize()
+    assert np.array_equal(k.cpu().numpy().view(np.uint16), want[0]) and np.array_equal(v.cpu().numpy().view(np.uint16), want[1])
+
+
+def _make_cache(B, bits, layout):
+    """bits [2][blocks][block][kv][dim] -> (k, v as [block][token][head][channel] views, the struct)."""
+    import torch
+    _, n_blocks, block, kv, dim = bits.shape
+    if layout == "token":
+        k, v = _dev(bits[0]), _dev(bits[1])
+    elif layout == "head":
+        k, v = (_dev(b.transpose(0, 2, 1, 3)).permute(0, 2, 1, 3) for b in bits)
+    elif layout == "pair":                      # key and value of a token side by side
+        both = _dev(bits.transpose(1, 2, 0, 3, 4))
+        k, v = both[:, :, 0], both[:, :, 1]
+    else:                                       # blocks innermost but for the channels
+        k, v = (_dev(b.transpose(2, 1, 0, 3)).permute(2, 1, 0, 3) for b in bits)
+    s = k.stride()
+    assert s == v.stride()
+    return k, v, B.coe_kv_cache(B.COE_DT_BF16, n_blocks, block, kv, dim, k.data_ptr(), v.data_ptr(), s[0], s[1], s[2])
+
+
+# ---- attention --------------------------------------------------------------------------------------------------
+class Attend:
+    """Inputs of a call from a list of (cached tokens, new tokens) and a device run of it."""
+
+    def __init__(self, B, lengths, heads, kv, dim, block=16, window=0, layout="token", seed=0, scale=None, sharp=1.0, gaps=False):
+        self.B, self.heads, self.kv, self.dim, self.block, self.window, self.layout = B, heads, kv, dim, block, window, layout
+        rng = np.random.default_rng(seed)
+        self.scale = scale if scale is not None else 1 / math.sqrt(dim)
+        self.total = np.array([h + m for h, m in lengths], np.int32)
+        self.new = np.array([m for _, m in lengths], np.int32)
+        self.off = np.concatenate([[0], np.cumsum(self.new)]).astype(np.int32)
+        owned = [-(-max(int(t), 0) // block) for t in self.total]
+        self.n_blocks = sum(owned) + 3
+        order = rng.permutation(self.n_blocks).astype(np.int32)
+        self.max_blocks = max(owned) + 2
+        self.table = rng.integers(-3, self.n_blocks + 3, (len(lengths), self.max_blocks)).astype(np.int32)     # unused entries: anything
+        at = 0
+        for r, b in enumerate(owned):
+            self.table[r, :b] = order[at:at + b]
+            at += b
+        tokens = int(self.off[-1])
+        self.q = _bf16(sharp * rng.standard_normal((tokens, heads, dim)))
+        self.bits = np.full((2, self.n_blocks, block, kv, dim), 0x7FC0, np.uint16)      # rows nobody has written: NaN
+        for r, t in enumerate(self.total):
+            for j in range(max(int(t), 0)):
+                self.bits[:, self.table[r, j // block], j % block] = _bf16(rng.standard_normal((2, kv, dim)))
+
+    def at(self, r, j):
+        return self.table[r, j // self.block], j % self.block
+
+    def run(self, max_new=None, lse=True, extra=0, poison=0xFFC0):
+        import torch
+        B, tokens = self.B, int(self.off[-1])
+        k, v, cache = _make_cache(B, self.bits, self.layout)
+        q = _dev(np.concatenate([self.q, self.q[:, :2]], 1))         # rows farther apart than they are long
+        out = _dev(np.full((tokens + extra, self.heads + 1, self.dim), poison, np.uint16))
+        logs = torch.full((tokens + extra, self.heads), 7.5, device="cuda")
+        most = int(self.new.max()) if max_new is None else max_new
+        need = B.coe_kv_attention_workspace(len(self.new), tokens + extra, most, self.heads, self.kv, self.dim)
+        work = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+        off, total, table = _dev(self.off), _dev(self.total), _dev(self.table)
+        if extra:
+            q = torch.cat([q, q[:1].expand(extra, -1, -1)])
+        B.coe_kv_attention(cache, len(self.new), tokens + extra, most, self.heads, self.window, self.scale, q.data_ptr(), q.stride(0), q.stride(1),
+                           off.data_ptr(), total.data_ptr(), table.data_ptr(), self.max_blocks, out.data_ptr(), out.stride(0), out.stride(1),
+                           logs.data_ptr() if lse else 0, work.data_ptr(), need, _stream())
+        torch.cuda.synchronize()
+        got = out.cpu().numpy().view(np.uint16)
+        assert (got[:, -1] == poison).all() and (got[tokens:] == poison).all(), "wrote outside its rows"
+        return got[:tokens, :-1], logs.cpu().numpy()[:tokens] if lse else None
+
+    def check(self, got, logs=None, clean=None):
+        bits = self.bits if clean is None else clean
+        with np.errstate(invalid="ignore"):
+            out, lse, size = T.attention(T.bf16_to_f64(self.q), T.bf16_to_f64(bits[0]), T.bf16_to_f64(bits[1]), self.total, self.off, self.table,
+                                         self.block, self.window, self.scale)
+        g = T.bf16_to_f64(got)
+        # bf16 holds 8 bits: a probability is rounded to it (2^-8 of itself at most), as is the result (2^-8); the scores carry fp32 errors: at most
+        # (dim + 2) 2^-24 sum|q k| * scale, under 1e-4 for these inputs' scores (sharp rows have larger ones: checked as given),
+        # and so do sums over the keys.  Per element |error| <= 2^-8 |out| + (2^-8 + 1e-3) sum p |v|; over all of them the
+        # roundings are independent: about 1.7e-3 of the norm, where 4e-3 is allowed.
+        bound = 2.0 ** -8 * np.abs(out) + (2.0 ** -8 + 1e-3) * size + 1e-30
+        assert np.isfinite(g).all()
+        assert (np.abs(g - out) <= bound).all(), float((np.abs(g - out) / bound).max())
+        if out.size >= 4096:
+            assert np.linalg.norm(g - out) <= 4e-3 * np.linalg.norm(out)
+        if logs is not None:
+            assert np.array_equal(np.isinf(logs), np.isinf(lse))
+            ok = np.isfinite(lse)
+            assert (np.abs(logs[ok] - lse[ok]) <= 2e-4 + 2e-6 * np.abs(lse[ok])).all()
+
+
+SHAPES = [(12, 12, 64), (32, 8, 128), (8, 1, 64), (6, 2, 80), (24, 8, 96), (7, 7, 8), (5, 5, 40), (14, 2, 128), (16, 1, 128), (33, 1, 64), (80, 2, 128)]
+
+
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+def test_attention_single_tokens(B, heads, kv, dim):
+    """One new token per request, histories of every remainder of a tile and of a block."""
+    lengths = [(h, 1) for h in (0, 1, 7, 8, 15, 16, 17, 30, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 300)]
+    a = Attend(B, lengths, heads, kv, dim, seed=heads + dim)
+    a.check(*a.run())
+
+
+@pytest.mark.parametrize("block,layout", [(8, "token"), (16, "head"), (32, "pair"), (64, "inner"), (128, "token"), (1024, "head")])
+def test_attention_blocks_and_layouts(B, block, layout):
+    for lengths in ([(500, 1), (0, 1), (77, 1), (1024, 1)], [(300, 40), (0, 90), (129, 1), (5, 130)]):
+        for heads, kv, dim in ((8, 2, 128), (6, 6, 64)):
+            a = Attend(B, lengths, heads, kv, dim, block=block, layout=layout, seed=block)
+            a.check(*a.run())
+
+
+@pytest.mark.parametrize("lengths", [
+    [(0, 1)], [(0, 2)], [(0, 31)], [(0, 33)], [(0, 64), (0, 65)], [(0, 127), (0, 128), (0, 129)], [(100, 257)], [(64, 3), (200, 5), (3, 8), (0, 9)],
+    [(0, 0), (50, 1), (0, 0), (33, 40), (0, 0)],                    # requests with no new tokens between others
+    [(-3, 5), (-5, 5), (-40, 60), (10, 2)],                         # rows before the first cached token see nothing
+    [(0, 300), (700, 1), (700, 20), (31, 1), (1000, 64)],
+])
+@pytest.mark.parametrize("heads,kv,dim", [(4, 4, 64), (8, 2, 128), (12, 4, 96), (5, 1, 80)])
+def test_attention_chunks(B, lengths, heads, kv, dim):
+    a = Attend(B, lengths, heads, kv, dim, seed=len(lengths) + dim)
+    a.check(*a.run())
+
+
+@pytest.mark.parametrize("window", [1, 2, 31, 32, 33, 64, 100, 129, 5000])
+def test_attention_window(B, window):
+    for lengths in ([(0, 1), (31, 1), (32, 1), (500, 1), (1000, 1)], [(0, 200), (300, 150), (64, 1), (1000, 30)]):
+        for heads, kv, dim in ((8, 2, 128), (12, 12, 64)):
+            a = Attend(B, lengths, heads, kv, dim, window=window, seed=window)
+            a.check(*a.run())
+
+
+def test_attention_long_histories_are_split(B):
+    """Few requests with long histories beside short ones: parts of a history are joined again."""
+    for lengths in ([(9000, 1)], [(5000, 1), (3, 1), (7777, 1)], [(6000, 2), (6001, 3)], [(5000, 40), (10, 1)]):
+        for heads, kv, dim in ((8, 1, 128), (4, 4, 64)):
+            a = Attend(B, lengths, heads, kv, dim, block=64, seed=3)
+            a.check(*a.run())
+
+
+def test_attention_sharp_and_flat_scores(B):
+    """Scores of some hundreds (one key takes all), all equal (a plain mean), and a running maximum that rises with every key."""
+    a = Attend(B, [(400, 1), (300, 70)], 4, 2, 128, seed=1, sharp=40.0, scale=0.5)
+    got, logs = a.run()
+    out, lse, size = T.attention(T.bf16_to_f64(a.q), T.bf16_to_f64(a.bits[0]), T.bf16_to_f64(a.bits[1]), a.total, a.off, a.table, 16, 0, a.scale)
+    # sum|q k| * scale reaches 40 * 128 * 0.64 * 0.5 = 1640, so a score may be off by 130 * 2^-24 * 1640 = 0.013 at most
+    g = T.bf16_to_f64(got)
+    assert (np.abs(g - out) <= 2.0 ** -8 * np.abs(out) + (2.0 ** -8 + 0.026) * size + 1e-30).all()
+    assert (np.abs(logs - lse) <= 0.013 + 1e-6 * np.abs(lse)).all()
+    a = Attend(B, [(400, 1), (300, 70)], 4, 2, 64, seed=2, scale=0.0)
+    a.check(*a.run())
+    for sign in (1.0, -1.0):
+        a = Attend(B, [(700, 1), (200, 80)], 4, 2, 64, seed=3)
+        a.q[:] = _bf16(np.ones_like(a.q, np.float64))
+        for r, t in enumerate(a.total):
+            for j in range(t):
+                b, row = a.at(r, j)
+                a.bits[0, b, row] = _bf16(np.full((2, 64), sign * j / 64.0))
+        a.check(*a.run())
+
+
+@pytest.mark.parametrize("value", [0x7F80, 0xFF80, 0x7FC0, 0x7F7F, 0xFF7F])     # inf, -inf, NaN, the largest, the lowest
+@pytest.mark.parametrize("window", [0, 50])
+def test_attention_keeps_what_is_masked_out(B, value, window):
+    """Keys and values that a row does not see leave its bits alone, whatever they hold."""
+    for lengths, bad in ([[(300, 1), (40, 1), (63, 1)], []], [[(60, 150), (0, 70), (90, 1)], [(0, 130), (0, 209), (1, 33), (1, 69)]]):
+        for heads, kv, dim in ((8, 2, 128), (4, 4, 64)):
+            a = Attend(B, lengths, heads, kv, dim, window=window, seed=9)
+            if window:
+                bad = bad + [(0, 5)]
+            base, base_lse = a.run()
+            clean = a.bits.copy()
+            for r, j in bad:
+                a.bits[(slice(None),) + a.at(r, j)] = value
+            a.bits[clean == 0x7FC0] = value                            # rows nobody has written
+            got, lse = a.run()
+            seen = np.zeros(len(got), bool)                            # rows that do see a bad token
+            for r, j in bad:
+                for i in range(a.new[r]):
+                    pos = a.total[r] - a.new[r] + i
+                    seen[a.off[r] + i] |= j <= pos and (window == 0 or j > pos - window)
+            assert np.array_equal(got[~seen], base[~seen]) and np.array_equal(lse[~seen], base_lse[~seen])
+            if value in (0x7F80, 0xFF80, 0x7FC0) and seen.any():
+                assert not np.isfinite(T.bf16_to_f64(got[seen])).all()
+
+
+def test_attention_unknown_blocks_read_as_zeros(B):
+    a = Attend(B, [(200, 1), (90, 64)], 8, 2, 64, seed=4)
+    a.table[0, 3], a.table[0, 5], a.table[1, 0] = -1, a.n_blocks, 2 ** 31 - 1
+    a.check(*a.run())
+
+
+def test_attention_length_beyond_the_table(B):
+    """seq_len is limited to what the table holds."""
+    a = Attend(B, [(100, 1), (63, 1)], 4, 2, 64, seed=4)              # full blocks: every row that comes into reach is written
+    a.max_blocks = 7
+    a.table = a.table[:, :7].copy()
+    a.table[1, 4:] = a.table[0, :3]
+    a.total[1] = 10 ** 6
+    got, lse = a.run()
+    a.total[1] = 112
+    a.total[0] = 101
+    a.check(got, lse)
+
+
+def test_attention_fewer_new_tokens_than_announced_and_padding_rows(B):
+    a = Attend(B, [(100, 3), (50, 1), (7, 0)], 8, 2, 128, seed=4)
+    base = a.run()
+    for most, extra in ((3, 5), (200, 0), (300, 9)):
+        got, lse = a.run(max_new=most, extra=extra)
+        a.check(got, lse)
+    assert np.array_equal(a.run(lse=False)[0], base[0])
+
+
+def test_attention_cache_beyond_4_gib(B):
+    """Blocks whose bytes begin past 2^32: the same bits as in a small cache."""
+    import torch
+    a = Attend(B, [(500, 1), (130, 1), (200, 60)], 8, 2, 128, block=64, seed=5)
+    base, base_lse = a.run()
+    # the same blocks, 2^20 * 300 elements (600 MiB) apart: the last one begins beyond 2^32 bytes and 2^32 elements
+    apart = (1 << 20) * 300
+    row = 64 * 2 * 128
+    assert a.n_blocks * apart > 2 ** 32
+    room = torch.empty(2 * (a.n_blocks - 1) * apart + 4 * row, dtype=torch.int16, device="cuda")
+    k = room[:].as_strided((a.n_blocks, row), (apart, 1), 0)
+    v = room[:].as_strided((a.n_blocks, row), (apart, 1), (a.n_blocks - 1) * apart + row)
+    k.copy_(_dev(a.bits[0].reshape(a.n_blocks, row)))
+    v.copy_(_dev(a.bits[1].reshape(a.n_blocks, row)))
+    cache = B.coe_kv_cache(B.COE_DT_BF16, a.n_blocks, 64, 2, 128, k.data_ptr(), v.data_ptr(), apart, 256, 128)
+    tokens = int(a.off[-1])
+    q, out, lse = _dev(a.q), _dev(np.zeros_like(a.q)), torch.zeros(tokens, 8, device="cuda")
+    need = B.coe_kv_attention_workspace(3, tokens, 60, 8, 2, 128)
+    work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    off, total, table = _dev(a.off), _dev(a.total), _dev(a.table)
+    B.coe_kv_attention(cache, 3, tokens, 60, 8, 0, a.scale, q.data_ptr(), q.stride(0), q.stride(1), off.data_ptr(), total.data_ptr(), table.data_ptr(),
+                       a.max_blocks, out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(), work.data_ptr(), need, _stream())
+    assert np.array_equal(out.cpu().numpy().view(np.uint16), base) and np.array_equal(lse.cpu().numpy(), base_lse)
+    # and an append there
+    slot = _dev(np.array([(a.n_blocks - 1) * 64 + 63], np.int32))
+    new = _dev(np.full((1, 2, 128), 0x4040, np.uint16))
+    B.coe_kv_append(cache, 1, new.data_ptr(), 256, 128, new.data_ptr(), 256, 128, slot.data_ptr(), _stream())
+    assert (k[-1, -256:] == 0x4040).all() and (v[-1, -256:] == 0x4040).all()
+
+
+def test_attention_repeats_its_bits(B):
+    a = Attend(B, [(3000, 1), (100, 1), (900, 90), (0, 300)], 8, 2, 128, seed=6)
+    base = a.run()
+    for _ in range(3):
+        got = a.run()
+        assert np.array_equal(got[0], base[0]) and np.array_equal(got[1], base[1])
+
+
+# ---- sampling ---------------------------------------------------------------------------------------------------
+def _sample_gpu(B, x, temperature=None, top_k=None, top_p=None, min_p=None, noise=None, pad=3, logprob=True):
+    """x float32 or uint16 (bf16 bits) [rows][vocab]; garbage between the rows."""
+    import torch
+    rows, vocab = x.shape
+    wide = np.full((rows, vocab + pad), 0x7F80 if x.dtype == np.uint16 else np.inf, x.dtype)
+    wide[:, :vocab] = x
+    d = _dev(wide)
+    nz = None
+    if noise is not None:
+        nz = np.zeros((rows, vocab + 1), np.float32)
+        nz[:, :vocab] = noise
+        nz = _dev(nz)
+    args = [None if a is None else _dev(np.broadcast_to(np.asarray(a, t), (rows,)).copy()) for a, t in
+            ((temperature, np.float32), (top_k, np.int32), (top_p, np.float32), (min_p, np.float32))]
+    token = torch.full((rows,), -99, dtype=torch.int32, device="cuda")
+    lp = torch.full((rows,), 7.0, device="cuda")
+    need = B.coe_sample_workspace(rows, vocab)
+    work = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.coe_sample_tokens(rows, vocab, B.COE_DT_BF16 if x.dtype == np.uint16 else B.COE_DT_F32, d.data_ptr(), vocab + pad,
+                        *(0 if a is None else a.data_ptr() for a in args), 0 if nz is None else nz.data_ptr(), vocab + 1, token.data_ptr(),
+                        lp.data_ptr() if logprob else 0, work.data_ptr(), need, _stream())
+    return token.cpu().numpy(), lp.cpu().numpy()
+
+
+def _at(a, r, off):
+    return off if a is None else float(np.broadcast_to(np.asarray(a), (r + 1,) if np.ndim(a) == 0 else np.shape(a))[r])
+
+
+def _check_sample(B, x, temperature=None, top_k=None, top_p=None, min_p=None, noise=None):
+    token, lp = _sample_gpu(B, x, temperature, top_k, top_p, min_p, noise)
+    x64 = T.bf16_to_f64(x) if x.dtype == np.uint16 else x.astype(np.float64)
+    f = lambda a: None if a is None else np.asarray(a, np.float32).astype(np.float64)
+    temperature, top_p, min_p = f(temperature), f(top_p), f(min_p)
+    for r in range(len(x)):
+        # scores: (x - max) / T and ln E in fp32, at most 2^-22 of values up to 100: 5e-5 together; masses: sums of up to 10^5 fp32
+        # terms by 1024 lanes, 1e-5 of them at most
+        near, ln = T.sample(x64[r], _at(temperature, r, 1.0), int(_at(top_k, r, 0)), _at(top_p, r, 1.0), _at(min_p, r, 0.0),
+                            None if noise is None else noise[r], slack=1e-4)
+        assert int(token[r]) in near, (r, int(token[r]), near)
+        if ln is None:
+            assert lp[r] == -np.inf
+        else:
+            assert abs(lp[r] - ln[token[r]]) <= 1e-5 * (1 + abs(ln[token[r]])), r
+    return token
+
+
+def _noise(rng, shape):
+    return rng.standard_exponential(shape).astype(np.float32)
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 63, 64, 65, 1000, 1023, 1024, 1025, 4097, 32003, 50001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sample_sizes(B, vocab, dtype):
+    """Every filter and several at once, at vocabularies around the workgroup's stride."""
+    rng = np.random.default_rng(vocab)
+    settings = [(0.0, 0, 1.0, 0.0), (1.0, 0, 1.0, 0.0), (0.7, 1, 1.0, 0.0), (1.3, 5, 1.0, 0.0), (1.0, 40, 0.9, 0.0), (1.0, vocab - 1, 0.95, 0.0),
+                (1.0, vocab, 0.5, 0.0), (1.0, vocab + 7, 1.0, 0.0), (0.8, 0, 0.9, 0.0), (2.0, 0, 0.3, 0.0), (1.0, 0, 1e-6, 0.0), (1.0, 0, 0.0, 0.0),
+                (1.0, 0, 1.0, 0.05), (1.0, 0, 1.0, 1.0), (1.0, 50, 0.99, 0.1), (0.05, 700, 0.999, 0.0), (1.0, 1000, 0.8, 0.001), (1.0, -3, 1.5, -1.0)]
+    rows = len(settings)
+    x = (3 * rng.standard_normal((rows, vocab))).astype(np.float32)
+    if dtype == "bf16":
+        x = _bf16(x)
+    t, k, p, m = (np.array(c) for c in zip(*settings))
+    _check_sample(B, x, t, k, p, m, _noise(rng, (rows, vocab)))
+
+
+@pytest.mark.parametrize("case", ["equal", "two values", "ascending", "descending", "steps", "one large", "lowest", "far below", "zeros"])
+@pytest.mark.parametrize("vocab", [70, 3000, 20001])
+def test_sample_ties_and_masks(B, case, vocab):
+    """Ties go by index, also across the cut of a filter; masks of -inf, of the type's lowest value, and far-off values."""
+    rng = np.random.default_rng(vocab)
+    one = {"equal": np.full(vocab, 2.5), "two values": rng.integers(0, 2, vocab) * 1.0, "ascending": np.arange(vocab) * 0.01,
+           "descending": -np.arange(vocab) * 0.01, "steps": np.floor(rng.standard_normal(vocab) * 4), "one large": np.where(np.arange(vocab) == 11, 50.0, 0.0),
+           "lowest": np.where(rng.random(vocab) < 0.9, -3.4028235e38, rng.standard_normal(vocab)),
+           "far below": np.where(rng.random(vocab) < 0.99, -1e30, rng.standard_normal(vocab)),
+           "zeros": np.where(rng.random(vocab) < 0.5, 0.0, -0.0)}[case].astype(np.float32)
+    settings = [(0.0, 0, 1.0, 0.0), (1.0, 0, 1.0, 0.0), (1.0, 3, 1.0, 0.0), (1.0, 33, 0.7, 0.0), (1.0, 0, 0.5, 0.0), (0.3, 0, 0.9, 0.2), (1.0, vocab - 2, 0.99, 0.0),
+                (1.0, 2000, 1.0, 0.0)]
+    x = np.repeat(one[None], len(settings), 0)
+    masked = x.copy()
+    masked[:, rng.random(vocab) < 0.6] = -np.inf
+    masked[:, 7] = 1.0
+    t, k, p, m = (np.array(c) for c in zip(*settings))
+    for v in (x, masked, _bf16(x), _bf16(masked)):
+        _check_sample(B, v, t, k, p, m, _noise(rng, x.shape))
+
+
+def test_sample_exact_cuts(B):
+    """Weights and masses that fp32 holds exactly: the cut falls where the definition says, not one further."""
+    vocab = 64
+    x = np.full((vocab, vocab), -np.inf, np.float32)
+    x[:, ::8] = 0.0                                   # eight equal tokens at 0, 8, ..., 56
+    noise = np.full((vocab, vocab), 1.0, np.float32)
+    for r in range(vocab):
+        noise[r, 8 * (r % 8)] = 1e-6                  # token r % 8 of them wins if it is kept, else the first
+    for p, kept in ((0.5, 4), (0.51, 5), (0.125, 1), (0.126, 2), (0.875, 7), (0.99, 8)):
+        token, _ = _sample_gpu(B, x, 1.0, None, p, None, noise)
+        assert [int(v) for v in token] == [8 * (r % 8) if r % 8 < kept else 0 for r in range(vocab)], p
+    for k in range(1, 9):
+        token, _ = _sample_gpu(B, x, 1.0, k, None, None, noise)
+        assert [int(v) for v in token] == [8 * (r % 8) if r % 8 < k else 0 for r in range(vocab)], k
+    for k, p, kept in ((4, 0.5, 2), (4, 0.51, 3), (6, 0.5, 3), (2, 0.4, 1)):        # the nucleus of what top_k left
+        token, _ = _sample_gpu(B, x, 1.0, k, p, None, noise)
+        assert [int(v) for v in token] == [8 * (r % 8) if r % 8 < kept else 0 for r in range(vocab)], (k, p)
+    x[:, 8] = 0.75                                    # orders that differ in the last bits only
+    x[:, 16] = np.nextafter(np.float32(0.75), np.float32(1))
+    token, _ = _sample_gpu(B, x, 1.0, 1, None, None, noise)
+    assert (token == 16).all()
+    tiny = np.zeros((1, 3000), np.float32)
+    tiny[0, 0], tiny[0, 100], tiny[0, 200] = 10.0, 1e-9, 2e-9
+    n = np.full((1, 3000), 1.0, np.float32)
+    n[0, 100], n[0, 200] = 1e-12, 1e-10
+    assert _sample_gpu(B, tiny, 1.0, 2, None, None, n)[0][0] == 200 and _sample_gpu(B, tiny, 1.0, 3, None, None, n)[0][0] == 100
+
+
+def test_sample_values_that_are_no_numbers(B):
+    rng = np.random.default_rng(3)
+    vocab = 2500
+    x = rng.standard_normal((12, vocab)).astype(np.float32)
+    x[0] = -np.inf                                    # nothing to draw
+    x[1] = np.nan
+    x[2, :] = -np.inf
+    x[2, 1777] = -5.0                                 # a single token
+    x[3, rng.random(vocab) < 0.5] = np.nan
+    x[4, [100, 7, 2000]] = np.inf                     # shares everything among three
+    x[5, 3] = np.inf
+    x[6] = 3.4028235e38
+    x[7, 5] = 3.4028235e38
+    noise = _noise(rng, x.shape)
+    noise[8] = np.nan                                 # no usable number: the first token
+    noise[9] = -1.0
+    noise[10] = np.inf
+    noise[11, [40, 50]] = 0.0                         # certain winners, the lower index of the two
+    for t, k, p, m in ((1.0, 0, 1.0, 0.0), (0.7, 10, 1.0, 0.0), (1.0, 0, 0.8, 0.0), (1.0, 600, 0.9, 0.01), (0.0, 0, 1.0, 0.0), (np.nan, 0, 1.0, 0.0)):
+        token = _check_sample(B, x, t, k, p, m, noise)
+        assert token[0] == -1 and token[1] == -1 and token[2] == 1777
+        if t == 1.0 and k == 0 and p == 1.0:
+            assert token[11] == 40 and token[8] == np.argmax(x[8])
+    _check_sample(B, x, np.inf, 0, 1.0, 0.0, noise)
+    _check_sample(B, x, 0.0, None, None, None, None)  # greedy needs no numbers
+    token, _ = _sample_gpu(B, x, None, None, None, None, noise, logprob=False)
+    assert token[2] == 1777
+
+
+def test_sample_many_rows_have_their_probabilities(B):
+    """20,000 draws from one row: counts within five standard deviations of the renormalised probabilities."""
+    rng = np.random.default_rng(11)
+    rows, vocab = 20000, 300
+    one = (2 * rng.standard_normal(vocab)).astype(np.float32)
+    x = np.repeat(one[None], rows, 0)
+    token, _ = _sample_gpu(B, x, 0.9, 50, 0.9, 0.01, _noise(rng, x.shape))
+    z = one.astype(np.float64) / np.float64(np.float32(0.9))
+    w = np.exp(z - z.max())
+    order = np.argsort(-one, kind="stable")[:50]
+    before = np.cumsum(w[order]) - w[order]
+    order = order[(before < 0.9 * w[order].sum()) & (w[order] >= 0.01)]
+    p = w[order] / w[order].sum()
+    count = np.bincount(token, minlength=vocab)
+    assert count.sum() == count[order].sum() == rows
+    assert (np.abs(count[order] - rows * p) <= 5 * np.sqrt(rows * p * (1 - p)) + 1).all()
+
+
+# ---- streams and graphs ------------------------------------------------------------------------------------------
+def test_a_step_on_another_stream_and_in_a_graph(B):
+    """Plan, append, attention and sampling of a step on a stream of their own, then captured: every replay equals the eager run."""
+    import torch
+    rng = np.random.default_rng(2)
+    n, block, n_blocks, max_blocks, cap, heads, kv, dim, vocab = 9, 16, 300, 40, 64, 8, 2, 64, 3000
+    have = rng.integers(0, 500, n).astype(np.int32)
+    add = np.array([1, 1, 5, 1, 0, -1, 20, 1, 3], np.int32)
+    table, ring, state = _pool(rng, have, block, n_blocks, max_blocks)
+    d = {k: _dev(np.asarray(v, np.int32)) for k, v in dict(have=have, add=add, ring=ring, state=state, table=table).items()}
+    i32 = dict(dtype=torch.int32, device="cuda")
+    o = dict(seq_len=torch.zeros(n, **i32), q_off=torch.zeros(n + 1, **i32), slot=torch.zeros(cap, **i32), position=torch.zeros(cap, **i32),
+             next=torch.zeros(4, **i32), token=torch.zeros(n, **i32))
+    k, v, cache = _make_cache(B, _bf16(rng.standard_normal((2, n_blocks, block, kv, dim))), "token")
+    qkv = _dev(_bf16(rng.standard_normal((cap, heads + 2 * kv, dim))))
+    out, lse = torch.zeros(cap, heads, dim, dtype=torch.int16, device="cuda"), torch.zeros(cap, heads, device="cuda")
+    logits, noise = torch.randn(n, vocab, device="cuda"), torch.empty(n, vocab, device="cuda").exponential_()
+    w1, w2 = B.coe_kv_attention_workspace(n, cap, 20, heads, kv, dim), B.coe_sample_workspace(n, vocab)
+    work, work2 = torch.empty(max(w1, 16), dtype=torch.uint8, device="cuda"), torch.empty(max(w2, 16), dtype=torch.uint8, device="cuda")
+    top_k = torch.full((n,), 30, **i32)
+    p = lambda t: t.data_ptr()
+
+    def step(stream):
+        B.coe_kv_plan(n, block, n_blocks, max_blocks, cap, p(d["have"]), p(d["add"]), p(d["ring"]), p(d["state"]), p(d["table"]), p(o["seq_len"]), p(o["q_off"]),
+                      p(o["slot"]), p(o["position"]), p(o["next"]), stream)
+        row = (heads + 2 * kv) * dim
+        B.coe_kv_append(cache, cap, p(qkv) + 2 * heads * dim, row, dim, p(qkv) + 2 * (heads + kv) * dim, row, dim, p(o["slot"]), stream)
+        B.coe_kv_attention(cache, n, cap, 20, heads, 0, 0.125, p(qkv), row, dim, p(o["q_off"]), p(o["seq_len"]), p(d["table"]), max_blocks, p(out), heads * dim, dim,
+                           p(lse), p(work), w1, stream)
+        B.coe_sample_tokens(n, vocab, B.COE_DT_F32, p(logits), vocab, 0, p(top_k), 0, 0, p(noise), vocab, p(o["token"]), 0, p(work2), w2, stream)
+
+    outputs = [out, lse, k, v, d["table"], d["ring"], *o.values()]
+    torch.cuda.synchronize()
+    step(_stream())
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outputs]
+    for t in (out, lse, *o.values()):
+        t.zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    step(side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outputs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(torch.cuda.current_stream().cuda_stream)
+    for i in range(4):
+        for t in (out, lse, *o.values()):
+            t.fill_(i)
+        work.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        used = int(o["q_off"][-1])               # rows of no request are not written
+        for a, b in zip(outputs, want):
+            if a is out or a is lse:
+                a, b = a[:used], b[:used]
+            assert torch.equal(a, b)
