@@ -1,5 +1,14 @@
 // gfx950 kernels for attention over the paged key/value cache of token-generating experts (bf16).
+//
+// A request with m new tokens and `heads / kv_heads` = G query heads to a cache head has m G query rows per cache head that look at
+// the same keys and values.  Scores are computed transposed, S^T = K Q^T, so that a lane holds ONE query row (column l % 32) and of a
+// block of 32 keys the keys 8 (v / 4) + 4 (l / 32) + v % 4: the running maximum and sum of a row live in lanes l and l ^ 32, and the
+// exponentials, rounded to bf16, are the second operand of O^T = V^T P^T as they lie.  V^T comes from the transposing LDS read.
+//   m' = max(m, max s)    l' = l 2^(m - m') + sum 2^(s - m')    o' = o 2^(m - m') + sum 2^(s - m') v        (s in units of ln 2)
+// All three are fp32; only 2^(s - m') is rounded to bf16, for the matrix cores.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "kernels.h"
 
@@ -8,17 +17,433 @@ namespace k {
 
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kKeys = 32;                 // keys of a tile
+constexpr int kFewRows = 32;              // query rows of a request and cache head that the kernel for few rows takes
+constexpr int kFewWaves = 4;
+constexpr int kFewGroups = 512;           // its workgroups: two per compute unit
+constexpr float kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    f32x2 f = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));   // round to nearest even
+}
+// the larger (the sum) of a value and that of lane ^ 32
+__device__ __forceinline__ float max_halves(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+#endif
+    return v;
+}
+__device__ __forceinline__ float sum_halves(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+#endif
+    return v;
+}
+__device__ __forceinline__ float exp2_fast(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(v);
+#else
+    return v;
+#endif
+}
+
+// A request's new tokens and the cached tokens [begin, end) that at least one of them sees.
+struct Span {
+    int m, rows, first_pos, begin, end;   // new tokens taken, query rows per cache head, position of the first new token
+    __device__ __forceinline__ int first_tile() const { return begin / kKeys; }
+    __device__ __forceinline__ int tiles() const { return rows == 0 ? 0 : max(1, (end + kKeys - 1) / kKeys - begin / kKeys); }
+};
+__device__ __forceinline__ Span span_of(const KvAttention& a, int r, int group, int table_tokens)
+{
+    const int q0 = max(0, min(a.q_off[r], a.n_tokens)), q1 = max(q0, min(a.q_off[r + 1], a.n_tokens));
+    const int len = max(0, min(a.seq_len[r], table_tokens)), m_all = q1 - q0;
+    Span s;
+    s.m = min(m_all, a.max_new);
+    s.rows = s.m * group;
+    s.first_pos = len - m_all;
+    s.end = max(0, min(len, s.first_pos + s.m));
+    s.begin = a.window > 0 ? min(s.end, max(0, s.first_pos - a.window + 1)) : 0;
+    return s;
+}
+
+// Where 16-byte chunk c of row r of a V tile lies: rows of DH channels, chunks in an order that spreads both the writes (sixteen rows of
+// one chunk) and the transposing reads (four rows of four chunks) over all LDS banks.
+template <int DH> __device__ __forceinline__ uint32_t v_slot(int r, int c)
+{
+    const int f = DH == 128 ? (r & 3) * 4 + ((r >> 2) & 3) : ((r >> 1) & 1) * 4 + ((r >> 2) & 3);
+    return (uint32_t)(r * DH * 2 + ((c ^ f) & (DH / 8 - 1)) * 16);
+}
+
+// acc += V^T P^T for 16 keys of a tile.  at: this lane's addresses of the transposing reads of keys 0..7 and 8..15, per 32 channels.
+// careful: a key may be hidden from some rows, and 0 * inf would reach them through the matrix core: values that are not finite are
+// then taken out of the operand and added one by one to the rows that see them (`sees(key of the 16)` says for this lane's row).
+template <int DH, class Sees>
+__device__ __forceinline__ void add_values(f32x16 (&acc)[DH / 32], const char* const (&at)[DH / 32][2], int offset, bf16x8 pf, bool careful, Sees sees)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+    for (int db = 0; db < DH / 32; ++db) {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at[db][0] + offset));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at[db][1] + offset));
+        u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        if (careful) {
+            uint32_t odd = 0;                 // bit e: element e is inf or NaN
+#pragma unroll
+            for (int e = 0; e < 8; ++e) odd |= ((w[e >> 1] >> (16 * (e & 1))) & 0x7F80u) == 0x7F80u ? 1u << e : 0u;
+            const u32x4 all = w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (odd >> e & 1) w[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+            const u32x4 p = __builtin_bit_cast(u32x4, pf);
+            for (unsigned long long left = __ballot(odd != 0); left; left &= left - 1) {
+                const int src = __builtin_ctzll(left), row = src & 31, kh = src >> 5;
+                const uint32_t which = __builtin_amdgcn_readlane(odd, src);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (!(which >> e & 1)) continue;
+                    const uint32_t bits = __builtin_amdgcn_readlane(all[e >> 1], src), word = __shfl(p[e >> 1], (lane & 31) + 32 * kh, 64);
+                    const float v = __uint_as_float(e & 1 ? bits & 0xFFFF0000u : bits << 16), q = __uint_as_float(e & 1 ? word & 0xFFFF0000u : word << 16);
+                    const bool mine = half == ((row >> 2) & 1) && sees(8 * (e >> 2) + 4 * kh + (e & 3));
+#pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        if (x == 4 * (row >> 3) + (row & 3) && mine) acc[db][x] += q * v;
+                }
+            }
+        }
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, acc[db], 0, 0, 0);
+    }
+#endif
+}
+
+// ---- few query rows (single tokens): at most 32 per request and cache head ------------------------------------------------
+// The work is the list of all 32-key tiles, (request, cache head, tile) in that order; every workgroup takes an equal stretch of
+// it, so that lengths of any mix fill the chip evenly.  A stretch may begin and end inside a history (a "part"): such parts go to the
+// workspace as (maximum, sum, unnormalised output) and kv_attention_join_kernel adds them up; a history inside one stretch is
+// finished here.  Inside a stretch the four wavefronts take tiles in turn, each for itself: keys go from memory straight into
+// registers (they are the first operand as they lie), values through registers into LDS of the wavefront's own, and the next tile's
+// are on their way while this one is multiplied.
+// What bounds it: HBM, keys and values once.
+struct FewHeader {                        // at the workspace's start, for the joining kernel
+    unsigned long long per;               // tiles of a stretch
+    unsigned long long base[1];           // [n_requests + 1] tiles before request r, of one cache head
+};
+__host__ __device__ constexpr int64_t few_header_bytes(int n_requests) { return (16 + 8 * (int64_t)(n_requests + 1) + 255) / 256 * 256; }
+// a part: maxima and sums [2][32], then the output [32][DH]
+template <int DH> constexpr int kPartFloats = 2 * kFewRows + kFewRows * DH;
+
+template <int DH> constexpr int kMergeRow = DH + 4;          // floats between the rows of a wavefront's output in LDS
+template <int DH> constexpr size_t kFewLds = (size_t)kFewWaves * kFewRows * kMergeRow<DH> * 4;
+
+template <int DH, bool PAD>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvCache c, KvAttention a, char* workspace)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int kSteps = DH / 16, kBlocks = DH / 32;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    __shared__ float stat[2][kFewWaves][kFewRows];
+    __shared__ unsigned long long part_sum[kFewWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int group = a.heads / c.kv_heads, table_tokens = a.max_blocks << c.block_shift, n = a.n_requests;
+
+    // tiles before every request
+    unsigned long long* const base = (unsigned long long*)lds;
+    unsigned long long carry = 0;
+    for (int r0 = 0; r0 < n; r0 += 64 * kFewWaves) {
+        unsigned long long v = 0;
+        if (r0 + tid < n) {
+            const Span s = span_of(a, r0 + tid, group, table_tokens);
+            v = s.rows <= kFewRows ? (unsigned long long)s.tiles() : 0;
+        }
+        unsigned long long sum = v;
+        for (int d = 1; d < 64; d <<= 1) {
+            const unsigned long long u = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += u;
+        }
+        if (lane == 63) part_sum[wid] = sum;
+        __syncthreads();
+        unsigned long long before = carry;
+        for (int w = 0; w < kFewWaves; ++w) {
+            if (w < wid) before += part_sum[w];
+            carry += part_sum[w];
+        }
+        if (r0 + tid < n) base[r0 + tid] = before + sum - v;
+        __syncthreads();
+    }
+    if (tid == 0) base[n] = carry;
+    __syncthreads();
+    const unsigned long long total = carry * (unsigned)c.kv_heads;
+    const unsigned long long share = (total + gridDim.x - 1) / gridDim.x, per = max(4ull, (share + 3) / 4 * 4);
+    if (blockIdx.x == 0) {
+        FewHeader* h = (FewHeader*)workspace;
+        for (int r = tid; r <= n; r += 64 * kFewWaves) h->base[r] = base[r];
+        if (tid == 0) h->per = per;
+    }
+    unsigned long long now = blockIdx.x * per;
+    const unsigned long long stop = min(total, now + per);
+    if (now >= stop) return;
+    int r = 0;
+    for (int hi = n; hi - r > 1;) {       // the last request that begins at or before `now`
+        const int mid = (r + hi) >> 1;
+        if (base[mid] * (unsigned)c.kv_heads <= now) r = mid;
+        else hi = mid;
+    }
+    r = __builtin_amdgcn_readfirstlane(r);
+    unsigned long long into = now - base[r] * (unsigned)c.kv_heads;       // tiles of this request that others did
+    __syncthreads();
+
+    const int chunks = c.head_dim >> 3;
+    const float scale2 = a.scale * 1.44269504088896340736f;
+    char* const v_lds = lds + wid * (kKeys * DH * 2);
+    const char* v_at[kBlocks][2];
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            v_at[db][i] = v_lds + v_slot<DH>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+    const unsigned long long start = now;
+
+    while (now < stop && r < n) {
+        Span s = span_of(a, r, group, table_tokens);
+        int tiles = s.rows <= kFewRows ? s.tiles() : 0;
+        if (into >= (unsigned long long)tiles * (unsigned)c.kv_heads) {
+            into = 0;
+            ++r;
+            continue;
+        }
+        const int kvh = (int)(into / (unsigned)tiles), t_begin = (int)(into - (unsigned long long)kvh * (unsigned)tiles);
+        const int t_end = (int)min((unsigned long long)tiles, t_begin + (stop - now)), first = s.first_tile();
+        const int q0 = max(0, min(a.q_off[r], a.n_tokens));
+
+        // this lane's query row
+        const int row = l32, token = row / group, head = kvh * group + (row - token * group);
+        const bool row_ok = row < s.rows;
+        const int pos = s.first_pos + token, from = a.window > 0 ? pos - a.window : -1;       // sees keys from < j <= pos
+        bf16x8 qf[kSteps];
+        {
+            const uint16_t* qp = a.q + (int64_t)(q0 + (row_ok ? token : 0)) * a.q_token_stride + (int64_t)(row_ok ? head : 0) * a.q_head_stride + half * 8;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) {
+                u32x4 w = {0, 0, 0, 0};
+                if (row_ok && (!PAD || 2 * ks + half < chunks)) w = *(const u32x4*)(qp + ks * 16);
+                qf[ks] = __builtin_bit_cast(bf16x8, w);
+            }
+        }
+        float m = -INFINITY, l = 0.f;
+        f32x16 o[kBlocks];
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[db][x] = 0.f;
+
+        const int32_t* const ids = a.table + (size_t)r * a.max_blocks;
+        const uint16_t *const k_base = c.k + kvh * c.head_stride + half * 8, *const v_base = c.v + kvh * c.head_stride + half * 8;
+        auto id_of = [&](int tile) {      // block of this lane's key of a tile; -1: reads as zeros
+            const int key = tile * kKeys + l32;
+            int id = -1;
+            if (key >= s.begin && key < s.end) id = ids[key >> c.block_shift];
+            return (uint32_t)id < (uint32_t)c.n_blocks ? id : -1;
+        };
+        auto offset_of = [&](int tile, int id) {
+            const int key = tile * kKeys + l32;
+            return id < 0 ? (int64_t)0 : id * c.block_stride + (key & ((1 << c.block_shift) - 1)) * c.token_stride;
+        };
+        auto fetch = [&](const uint16_t* p, u32x4 (&w)[kSteps]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) {
+                if (PAD) {
+                    w[ks] = u32x4{0, 0, 0, 0};
+                    if (2 * ks + half < chunks) w[ks] = *(const u32x4*)(p + ks * 16);
+                } else
+                    w[ks] = *(const u32x4*)(p + ks * 16);
+            }
+        };
+        u32x4 kw[kSteps], vw[kSteps];
+        int tile = first + t_begin + wid;
+        const int tile_stop = first + t_end;
+        int id = -1, id_next = -1;
+        if (tile < tile_stop) {
+            id = id_of(tile);
+            const int64_t at = offset_of(tile, id);
+            fetch(k_base + at, kw);
+            fetch(v_base + at, vw);
+            if (tile + kFewWaves < tile_stop) id_next = id_of(tile + kFewWaves);
+        }
+        for (; tile < tile_stop; tile += kFewWaves) {
+            const bool more = tile + kFewWaves < tile_stop;
+            if (__any(id < 0)) {          // rows outside the history, blocks outside the cache
+#pragma unroll
+                for (int ks = 0; ks < kSteps; ++ks) {
+                    kw[ks] = id < 0 ? u32x4{0, 0, 0, 0} : kw[ks];
+                    vw[ks] = id < 0 ? u32x4{0, 0, 0, 0} : vw[ks];
+                }
+            }
+            f32x16 sc;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw[ks]), qf[ks], sc, 0, 0, 0);
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) *(u32x4*)(v_lds + v_slot<DH>(l32, 2 * ks + half)) = vw[ks];
+            if (more) {
+                id = id_next;
+                const int64_t at = offset_of(tile + kFewWaves, id);
+                fetch(k_base + at, kw);
+                fetch(v_base + at, vw);
+                if (tile + 2 * kFewWaves < tile_stop) id_next = id_of(tile + 2 * kFewWaves);
+            }
+            const int key0 = tile * kKeys;
+            const bool masked = key0 + kKeys - 1 > s.first_pos || key0 < s.begin || (a.window > 0 && key0 <= s.first_pos + s.m - 1 - a.window);
+            float top = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                sc[x] *= scale2;
+                const int key = key0 + 8 * (x >> 2) + 4 * half + (x & 3);
+                if (masked) sc[x] = row_ok && key <= pos && key > from && key >= 0 ? sc[x] : -INFINITY;
+                top = fmaxf(top, sc[x]);
+            }
+            top = max_halves(top);
+            const float m_new = fmaxf(m, top);
+            if (__any(m_new > m)) {
+                const float shrink = m_new == m ? 1.f : exp2_fast(m - m_new);
+                l *= shrink;
+#pragma unroll
+                for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[db][x] *= shrink;
+                m = m_new;
+            }
+            const float m_use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                sc[x] = exp2_fast(sc[x] - m_use);
+                l += sc[x];
+            }
+            const bool careful = masked && s.m > 1;
+#pragma unroll
+            for (int t2 = 0; t2 < 2; ++t2) {
+                u32x4 pw;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16(sc[8 * t2 + 2 * e], sc[8 * t2 + 2 * e + 1]);
+                add_values<DH>(o, v_at, t2 * 16 * DH * 2, __builtin_bit_cast(bf16x8, pw), careful, [&](int j) {
+                    const int key = key0 + 16 * t2 + j;
+                    return row_ok && key <= pos && key > from;
+                });
+            }
+        }
+        l = sum_halves(l);
+
+        // the four wavefronts' results
+        __syncthreads();
+        float* const mine = (float*)lds + wid * kFewRows * kMergeRow<DH> + l32 * kMergeRow<DH>;
+        if (row_ok) {
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(float4*)(mine + db * 32 + g * 8 + half * 4) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+        }
+        if (half == 0) {
+            stat[0][wid][l32] = m;
+            stat[1][wid][l32] = l;
+        }
+        __syncthreads();
+        const bool whole = t_begin == 0 && t_end == tiles;
+        float* const part = (float*)(workspace + few_header_bytes(n)) + ((size_t)blockIdx.x * 2 + (now != start)) * kPartFloats<DH>;
+        for (int i = tid; i < s.rows * (DH / 4); i += 64 * kFewWaves) {
+            const int rw = i / (DH / 4), ch = (i - rw * (DH / 4)) * 4;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) mx = fmaxf(mx, stat[0][w][rw]);
+            float sum = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) {
+                const float mw = stat[0][w][rw];
+                if (mw == -INFINITY) continue;
+                const float f = mw == mx ? 1.f : exp2_fast(mw - mx);
+                const float4 v = *(const float4*)((const float*)lds + (w * kFewRows + rw) * kMergeRow<DH> + ch);
+                sum += f * stat[1][w][rw];
+                acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
+            }
+            const int tk = rw / group, hd = kvh * group + (rw - tk * group);
+            if (whole) {
+                const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+                if (!PAD || ch < c.head_dim)
+                    *(uint2*)(a.out + (int64_t)(q0 + tk) * a.out_token_stride + (int64_t)hd * a.out_head_stride + ch) =
+                        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                if (a.lse && ch == 0) a.lse[(int64_t)(q0 + tk) * a.heads + hd] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+            } else {
+                *(float4*)(part + 2 * kFewRows + rw * DH + ch) = acc;
+                if (ch == 0) {
+                    part[rw] = mx;
+                    part[kFewRows + rw] = sum;
+                }
+            }
+        }
+        __syncthreads();
+        now += (unsigned)(t_end - t_begin);
+        into += (unsigned)(t_end - t_begin);
+    }
+#endif
+}
+
+// Adds up the parts of a history that several workgroups shared; a workgroup per request and cache head.
+template <int DH>
+__global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAttention a, const char* workspace)
+{
+    const FewHeader* const h = (const FewHeader*)workspace;
+    const int r = blockIdx.x / c.kv_heads, kvh = blockIdx.x - r * c.kv_heads, group = a.heads / c.kv_heads;
+    const unsigned long long tiles = h->base[r + 1] - h->base[r], per = h->per;
+    if (tiles == 0) return;
+    const unsigned long long begin = h->base[r] * (unsigned)c.kv_heads + (unsigned)kvh * tiles, end = begin + tiles;
+    const unsigned long long w0 = begin / per, w1 = (end - 1) / per;
+    if (w0 == w1) return;
+    const Span s = span_of(a, r, group, a.max_blocks << c.block_shift);
+    const int q0 = max(0, min(a.q_off[r], a.n_tokens));
+    const float* const parts = (const float*)(workspace + few_header_bytes(a.n_requests));
+    // a stretch's first history leaves the first part, its last one the second
+    auto part_of = [&](unsigned long long w) { return parts + (w * 2 + (begin > w * per)) * kPartFloats<DH>; };
+    for (int i = threadIdx.x; i < s.rows * (DH / 4); i += 256) {
+        const int rw = i / (DH / 4), ch = (i - rw * (DH / 4)) * 4;
+        float mx = -INFINITY, sum = 0.f;
+        for (unsigned long long w = w0; w <= w1; ++w) mx = fmaxf(mx, part_of(w)[rw]);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (unsigned long long w = w0; w <= w1; ++w) {
+            const float* const p = part_of(w);
+            const float mw = p[rw];
+            if (mw == -INFINITY) continue;
+            const float f = mw == mx ? 1.f : exp2f(mw - mx);
+            const float4 v = *(const float4*)(p + 2 * kFewRows + rw * DH + ch);
+            sum += f * p[kFewRows + rw];
+            acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
+        }
+        const int tk = rw / group, hd = kvh * group + (rw - tk * group);
+        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+        if (ch < c.head_dim)
+            *(uint2*)(a.out + (int64_t)(q0 + tk) * a.out_token_stride + (int64_t)hd * a.out_head_stride + ch) =
+                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (a.lse && ch == 0) a.lse[(int64_t)(q0 + tk) * a.heads + hd] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+    }
+}
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-__device__ __forceinline__ uint16_t to_bf16(float v)
-{
-    f32x2 f = {v, 0.f};
-    return (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));   // round to nearest even
-}
-
 // One wavefront per query row: 64 keys at a time, a lane scores one of them; then a lane sums two channels over the 64 values.
 __global__ __launch_bounds__(64) void kv_attention_rows_kernel(KvCache c, KvAttention a)
 {
@@ -32,6 +457,7 @@ __global__ __launch_bounds__(64) void kv_attention_rows_kernel(KvCache c, KvAtte
         if (a.q_off[mid] <= t) lo = mid;
         else hi = mid;
     }
+    if ((a.q_off[lo + 1] - a.q_off[lo]) * (a.heads / c.kv_heads) <= kFewRows) return;
     const int r = lo, bs = 1 << c.block_shift, dim = c.head_dim;
     const int len = max(0, min(a.seq_len[r], a.max_blocks << c.block_shift));
     const int pos = len - (a.q_off[r + 1] - t);
@@ -67,7 +493,7 @@ __global__ __launch_bounds__(64) void kv_attention_rows_kernel(KvCache c, KvAtte
         for (int d = 32; d > 0; d >>= 1) part += __shfl_xor(part, d, 64);
         sum = sum * shrink + part;
         m = m_new;
-        p[lane] = __uint_as_float((uint32_t)to_bf16(e) << 16);
+        p[lane] = __uint_as_float((uint32_t)(pack_bf16(e, 0.f) & 0xFFFF) << 16);
         __syncthreads();
         o[0] *= shrink;
         o[1] *= shrink;
@@ -81,18 +507,38 @@ __global__ __launch_bounds__(64) void kv_attention_rows_kernel(KvCache c, KvAtte
     }
     const float inv = end > begin ? 1.f / sum : 0.f;
     for (int d = lane, x = 0; d < dim; d += 64, ++x)
-        a.out[t * a.out_token_stride + head * a.out_head_stride + d] = end > begin ? to_bf16(o[x] * inv) : 0;
+        a.out[t * a.out_token_stride + head * a.out_head_stride + d] = end > begin ? (uint16_t)pack_bf16(o[x] * inv, 0.f) : 0;
     if (a.lse && lane == 0) a.lse[(int64_t)t * a.heads + head] = end > begin ? m + logf(sum) : -INFINITY;
+}
+
+
+template <int DH> hipError_t launch_few(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
+{
+    const size_t lds = std::max(kFewLds<DH>, ((size_t)a.n_requests + 1) * 8);
+    constexpr int kMost = 144 * 1024;
+    static const hipError_t configured[2] = {
+        hipFuncSetAttribute((const void*)kv_attention_few_kernel<DH, false>, hipFuncAttributeMaxDynamicSharedMemorySize, kMost),
+        hipFuncSetAttribute((const void*)kv_attention_few_kernel<DH, true>, hipFuncAttributeMaxDynamicSharedMemorySize, kMost)};
+    if (configured[0] != hipSuccess || configured[1] != hipSuccess) return configured[0] != hipSuccess ? configured[0] : configured[1];
+    if (c.head_dim == DH) hipLaunchKernelGGL((kv_attention_few_kernel<DH, false>), dim3(kFewGroups), dim3(64 * kFewWaves), lds, stream, c, a, workspace);
+    else hipLaunchKernelGGL((kv_attention_few_kernel<DH, true>), dim3(kFewGroups), dim3(64 * kFewWaves), lds, stream, c, a, workspace);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kv_attention_join_kernel<DH>, dim3((unsigned)a.n_requests * c.kv_heads), dim3(256), 0, stream, c, a, workspace);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t kv_attention_workspace(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
-
-hipError_t kv_attention(const KvCache& c, const KvAttention& a, void*, hipStream_t stream)
+int64_t kv_attention_workspace(int32_t n_requests, int32_t, int32_t, int32_t, int32_t, int32_t head_dim)
 {
-    hipLaunchKernelGGL(kv_attention_rows_kernel, dim3((unsigned)(a.n_tokens * a.heads)), dim3(64), 0, stream, c, a);
-    return hipGetLastError();
+    return few_header_bytes(n_requests) + (int64_t)kFewGroups * 2 * (head_dim <= 64 ? kPartFloats<64> : kPartFloats<128>) * 4;
+}
+
+hipError_t kv_attention(const KvCache& c, const KvAttention& a, void* workspace, hipStream_t stream)
+{
+    if ((long long)a.max_new * (a.heads / c.kv_heads) > kFewRows)
+        hipLaunchKernelGGL(kv_attention_rows_kernel, dim3((unsigned)(a.n_tokens * a.heads)), dim3(64), 0, stream, c, a);
+    return c.head_dim <= 64 ? launch_few<64>(c, a, (char*)workspace, stream) : launch_few<128>(c, a, (char*)workspace, stream);
 }
 
 }  // namespace k
