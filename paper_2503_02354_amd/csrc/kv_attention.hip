@@ -37,7 +37,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));   // round to nearest even
 }
 // the larger (the sum) of a value and that of lane ^ 32
-__device__ __forceinline__ float max_halves(float v)
+[[maybe_unused]] __device__ __forceinline__ float max_halves(float v)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -45,7 +45,7 @@ __device__ __forceinline__ float max_halves(float v)
 #endif
     return v;
 }
-__device__ __forceinline__ float sum_halves(float v)
+[[maybe_unused]] __device__ __forceinline__ float sum_halves(float v)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -53,7 +53,7 @@ __device__ __forceinline__ float sum_halves(float v)
 #endif
     return v;
 }
-__device__ __forceinline__ float exp2_fast(float v)
+[[maybe_unused]] __device__ __forceinline__ float exp2_fast(float v)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     return __builtin_amdgcn_exp2f(v);
@@ -442,75 +442,394 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
     }
 }
 
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-// One wavefront per query row: 64 keys at a time, a lane scores one of them; then a lane sums two channels over the 64 values.
-__global__ __launch_bounds__(64) void kv_attention_rows_kernel(KvCache c, KvAttention a)
+// ---- many query rows (chunks of prompts): more than 32 per request and cache head --------------------------------------------
+// Units of work are tiles of 128 query rows (32 to a wavefront) of a request and cache head, with all the 64-key tiles that one of
+// them sees.  A scheduling launch lists them, longest first, so that the last workgroups to start are short ones; where there are too
+// few units to fill the chip it cuts long ones into parts over the keys, which kv_attention_join_units_kernel adds up.  Block b
+// takes cache head b % kv_heads, so that with eight of them (or four, or two) the units of one head meet in the same second-level caches.
+// K and V tiles go from memory into LDS by DMA, two of them in turn; a wavefront reads every key and value of a tile for its 32
+// rows.  What bounds it: the matrix cores, with the softmax's vector instructions and 1 KiB of LDS reads per matrix instruction close by.
+constexpr int kManyRows = 128, kManyKeys = 64, kManyWaves = 4;
+constexpr int kManyGroups = 512;          // two workgroups per compute unit
+
+struct Unit {
+    int32_t request, first_row;           // request; first query row of the tile
+    int32_t tile, tiles;                  // 64-key tiles
+    int32_t part, pad[3];                 // -1, or the part of the workspace that takes the result (times kv_heads)
+};
+struct Joined { int32_t request, first_row, part, parts; };
+struct ManyHeader { int32_t units, joined, pad[62]; };
+
+__host__ __device__ constexpr int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
+// sizes of the workspace's pieces behind the few-row kernel's
+struct ManyLayout {
+    int64_t most_units, most_joined, header, units, joined, parts, end;
+};
+__host__ __device__ inline ManyLayout many_layout(int64_t begin, int32_t n_requests, int32_t n_tokens, int32_t heads, int32_t kv_heads, int32_t dh)
 {
-    __shared__ float q[128], p[64];
-    __shared__ int32_t blocks[64];
-    const int t = blockIdx.x / a.heads, head = blockIdx.x - t * a.heads, lane = threadIdx.x;
-    int lo = 0, hi = a.n_requests;
-    if (a.q_off[0] > t || a.q_off[hi] <= t) return;       // a row of no request
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.q_off[mid] <= t) lo = mid;
-        else hi = mid;
-    }
-    if ((a.q_off[lo + 1] - a.q_off[lo]) * (a.heads / c.kv_heads) <= kFewRows) return;
-    const int r = lo, bs = 1 << c.block_shift, dim = c.head_dim;
-    const int len = max(0, min(a.seq_len[r], a.max_blocks << c.block_shift));
-    const int pos = len - (a.q_off[r + 1] - t);
-    const int begin = a.window > 0 ? max(0, pos - a.window + 1) : 0, end = pos + 1;
-    for (int d = lane; d < dim; d += 64) q[d] = __uint_as_float((uint32_t)a.q[t * a.q_token_stride + head * a.q_head_stride + d] << 16);
-    __syncthreads();
-    const int64_t head_at = (head / (a.heads / c.kv_heads)) * c.head_stride;
-    float m = -INFINITY, sum = 0.f, o[2] = {0.f, 0.f};
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        const int j = j0 + lane;
-        float s = -INFINITY;
-        int32_t block = -1;
-        if (j < end) {
-            block = a.table[(size_t)r * a.max_blocks + (j >> c.block_shift)];
-            if (block < 0 || block >= c.n_blocks) block = -1;
-            s = 0.f;
-            if (block >= 0) {
-                const uint16_t* row = c.k + block * c.block_stride + (j & (bs - 1)) * c.token_stride + head_at;
-                for (int d = 0; d < dim; d += 8) {
-                    const uint4 w = *(const uint4*)(row + d);
-                    s += q[d] * bf16_lo(w.x) + q[d + 1] * bf16_hi(w.x) + q[d + 2] * bf16_lo(w.y) + q[d + 3] * bf16_hi(w.y) +
-                         q[d + 4] * bf16_lo(w.z) + q[d + 5] * bf16_hi(w.z) + q[d + 6] * bf16_lo(w.w) + q[d + 7] * bf16_hi(w.w);
-                }
-            }
-            s *= a.scale;
-        }
-        blocks[lane] = block;
-        float top = s;
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-        const float m_new = fmaxf(m, top), shrink = m == m_new ? 1.f : expf(m - m_new);
-        const float e = j < end ? expf(s - m_new) : 0.f;
-        float part = e;
-        for (int d = 32; d > 0; d >>= 1) part += __shfl_xor(part, d, 64);
-        sum = sum * shrink + part;
-        m = m_new;
-        p[lane] = __uint_as_float((uint32_t)(pack_bf16(e, 0.f) & 0xFFFF) << 16);
-        __syncthreads();
-        o[0] *= shrink;
-        o[1] *= shrink;
-        const int n = min(64, end - j0);
-        for (int i = 0; i < n; ++i) {
-            if (blocks[i] < 0) continue;
-            const uint16_t* row = c.v + blocks[i] * c.block_stride + ((j0 + i) & (bs - 1)) * c.token_stride + head_at;
-            for (int d = lane, x = 0; d < dim; d += 64, ++x) o[x] += p[i] * __uint_as_float((uint32_t)row[d] << 16);
-        }
-        __syncthreads();
-    }
-    const float inv = end > begin ? 1.f / sum : 0.f;
-    for (int d = lane, x = 0; d < dim; d += 64, ++x)
-        a.out[t * a.out_token_stride + head * a.out_head_stride + d] = end > begin ? (uint16_t)pack_bf16(o[x] * inv, 0.f) : 0;
-    if (a.lse && lane == 0) a.lse[(int64_t)t * a.heads + head] = end > begin ? m + logf(sum) : -INFINITY;
+    ManyLayout l;
+    const int64_t rows = (int64_t)n_tokens * (heads / kv_heads), cuts = (kManyGroups + kv_heads - 1) / kv_heads;
+    l.most_units = rows / kManyRows + n_requests + cuts;
+    l.most_joined = cuts;
+    l.header = begin;
+    l.units = begin + sizeof(ManyHeader);
+    l.joined = l.units + round256(l.most_units * (int64_t)sizeof(Unit));
+    l.parts = l.joined + round256(l.most_joined * (int64_t)sizeof(Joined));
+    l.end = l.parts + 2 * cuts * kv_heads * (int64_t)(2 * kManyRows + kManyRows * dh) * 4;
+    return l;
 }
 
+// 64-key tiles that the query rows [row, row + 128) of a request see
+__device__ __forceinline__ void tiles_of(const Span& s, int window, int group, int row, int& first, int& count)
+{
+    const int last = min(s.rows, row + kManyRows) - 1;
+    const int end = max(0, s.first_pos + last / group + 1), begin = window > 0 ? min(end, max(0, s.first_pos + row / group - window + 1)) : 0;
+    first = begin / kManyKeys;
+    count = max(1, (end + kManyKeys - 1) / kManyKeys - first);
+}
+
+constexpr int kSchedThreads = 1024, kSchedBins = 2048;
+__global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(KvCache c, KvAttention a, char* workspace, ManyLayout at)
+{
+    extern __shared__ int32_t first_segment[];            // [n_requests + 1] row tiles before request r
+    __shared__ unsigned long long wave_sum[kSchedThreads / 64];
+    __shared__ int32_t bins[kSchedBins];
+    __shared__ int32_t n_parts, n_joined;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n = a.n_requests;
+    const int group = a.heads / c.kv_heads, table_tokens = a.max_blocks << c.block_shift;
+    auto sum_before = [&](unsigned long long v, unsigned long long& all) {
+        unsigned long long sum = v;
+        for (int d = 1; d < 64; d <<= 1) {
+            const unsigned long long u = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += u;
+        }
+        __syncthreads();
+        if (lane == 63) wave_sum[wid] = sum;
+        __syncthreads();
+        unsigned long long before = sum - v;
+        all = 0;
+        for (int w = 0; w < kSchedThreads / 64; ++w) {
+            if (w < wid) before += wave_sum[w];
+            all += wave_sum[w];
+        }
+        return before;
+    };
+    unsigned long long segments = 0;
+    for (int r0 = 0; r0 < n; r0 += kSchedThreads) {
+        int v = 0;
+        if (r0 + tid < n) {
+            const Span s = span_of(a, r0 + tid, group, table_tokens);
+            v = s.rows > kFewRows ? (s.rows + kManyRows - 1) / kManyRows : 0;
+        }
+        unsigned long long all;
+        const unsigned long long before = segments + sum_before((unsigned)v, all);
+        if (r0 + tid < n) first_segment[r0 + tid] = (int32_t)min(before, (unsigned long long)at.most_units);
+        segments += all;
+    }
+    const int count = (int)min(segments, (unsigned long long)at.most_units);      // the sum of the requests' rows is at most n_tokens * group
+    if (tid == 0) first_segment[n] = count;
+    for (int i = tid; i < kSchedBins; i += kSchedThreads) bins[i] = 0;
+    if (tid == 0) n_parts = n_joined = 0;
+    __syncthreads();
+    auto segment = [&](int i, int& r, int& row, int& first, int& tiles) {
+        r = 0;
+        for (int hi = n; hi - r > 1;) {
+            const int mid = (r + hi) >> 1;
+            if (first_segment[mid] <= i) r = mid;
+            else hi = mid;
+        }
+        const Span s = span_of(a, r, group, table_tokens);
+        row = (i - first_segment[r]) * kManyRows;
+        tiles_of(s, a.window, group, row, first, tiles);
+    };
+    unsigned long long mine = 0, total;
+    for (int i = tid; i < count; i += kSchedThreads) {
+        int r, row, first, tiles;
+        segment(i, r, row, first, tiles);
+        mine += (unsigned)tiles;
+    }
+    (void)sum_before(mine, total);
+    // no part is shorter than 8 tiles, or than what fills the chip once
+    const int most = (int)max(8ull, (total * (unsigned)c.kv_heads + kManyGroups - 1) / kManyGroups);
+    // longest first: by length, the longer halves of the range in coarser steps
+    int scale = 0;
+    while ((most >> scale) >= kSchedBins) ++scale;
+    auto bin_of = [&](int tiles) { return kSchedBins - 1 - min(kSchedBins - 1, tiles >> scale); };
+    for (int i = tid; i < count; i += kSchedThreads) {
+        int r, row, first, tiles;
+        segment(i, r, row, first, tiles);
+        const int parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts;
+        atomicAdd(&bins[bin_of(each)], parts);
+    }
+    __syncthreads();
+    {                                         // exclusive sums of the bins
+        constexpr int kPer = kSchedBins / kSchedThreads;
+        int own[kPer], sum = 0;
+        for (int j = 0; j < kPer; ++j) {
+            own[j] = bins[tid * kPer + j];
+            sum += own[j];
+        }
+        unsigned long long all;
+        int before = (int)sum_before((unsigned)sum, all);
+        for (int j = 0; j < kPer; ++j) {
+            bins[tid * kPer + j] = before;
+            before += own[j];
+        }
+        if (tid == 0) ((ManyHeader*)(workspace + at.header))->units = (int32_t)min(all, (unsigned long long)at.most_units);
+    }
+    __syncthreads();
+    Unit* const units = (Unit*)(workspace + at.units);
+    Joined* const joined = (Joined*)(workspace + at.joined);
+    for (int i = tid; i < count; i += kSchedThreads) {
+        int r, row, first, tiles;
+        segment(i, r, row, first, tiles);
+        const int parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts;
+        const int to = atomicAdd(&bins[bin_of(each)], parts);
+        int part = -1;
+        if (parts > 1) {
+            part = atomicAdd(&n_parts, parts);
+            const int j = atomicAdd(&n_joined, 1);
+            if (j < at.most_joined) joined[j] = {r, row, part, parts};
+        }
+        for (int p = 0; p < parts; ++p) {
+            const int t0 = p * each, t1 = min(tiles, t0 + each);
+            if (to + p < at.most_units) units[to + p] = {r, row, first + t0, max(0, t1 - t0), part < 0 ? -1 : part + p, {0, 0, 0}};
+        }
+    }
+    __syncthreads();
+    if (tid == 0) ((ManyHeader*)(workspace + at.header))->joined = min(n_joined, (int)at.most_joined);
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(4))) int32_t constant_int;
+[[maybe_unused]] constexpr uint32_t kOutOfRange = 0x80000000u;   // buffer offset beyond any block: loads return zeros
+
+template <int DH> constexpr int kManyTile = kManyKeys * DH * 2;  // bytes of a K (or V) tile
+
+template <int DH>
+__global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(KvCache c, KvAttention a, char* workspace, ManyLayout layout)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int kSteps = DH / 16, kBlocks = DH / 32, kTile = kManyTile<DH>;
+    constexpr int kRowsPerLoad = 1024 / (DH * 2), kLoads = kManyKeys / kRowsPerLoad / kManyWaves;     // of K, and the same of V
+    extern __shared__ __attribute__((aligned(1024))) char lds[];          // two buffers of a K and a V tile
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int kvh = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
+    if (index >= ((const ManyHeader*)(workspace + layout.header))->units) return;
+    const Unit* const up = (const Unit*)(workspace + layout.units) + index;
+    const int r = __builtin_amdgcn_readfirstlane(up->request), row0 = __builtin_amdgcn_readfirstlane(up->first_row);
+    const int tile0 = __builtin_amdgcn_readfirstlane(up->tile), tiles = __builtin_amdgcn_readfirstlane(up->tiles), part = __builtin_amdgcn_readfirstlane(up->part);
+    const int group = a.heads / c.kv_heads, table_tokens = a.max_blocks << c.block_shift;
+    const Span s = span_of(a, r, group, table_tokens);
+    const int q0 = max(0, min(a.q_off[r], a.n_tokens));
+    const int chunks = c.head_dim >> 3;
+
+    // this lane's query row; a negative scale moves to the queries
+    const int row = row0 + wid * 32 + l32, token = row / group, head = kvh * group + (row - token * group);
+    const bool row_ok = row < s.rows;
+    const int pos = s.first_pos + token, from = a.window > 0 ? pos - a.window : -1;
+    // positions of this wavefront's first and last row
+    const int low = __builtin_amdgcn_readfirstlane(s.first_pos + (row0 + wid * 32) / group);
+    const int high = __builtin_amdgcn_readfirstlane(s.first_pos + (min(s.rows, row0 + wid * 32 + 32) - 1) / group);
+    const bool works = row0 + wid * 32 < s.rows;
+    bf16x8 qf[kSteps];
+    {
+        const uint16_t* qp = a.q + (int64_t)(q0 + (row_ok ? token : 0)) * a.q_token_stride + (int64_t)(row_ok ? head : 0) * a.q_head_stride + half * 8;
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) {
+            u32x4 w = {0, 0, 0, 0};
+            if (row_ok && 2 * ks + half < chunks) w = *(const u32x4*)(qp + ks * 16) ^ flip;
+            qf[ks] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+    const float scale2 = fabsf(a.scale) * 1.44269504088896340736f;
+
+    // Lane i of a load fills slot i % (DH / 8) of row i / (DH / 8) of its rows, and fetches the chunk that belongs there.
+    const int ld_row = lane / (DH / 8), ld_slot = lane % (DH / 8);
+    const uint32_t row_bytes = (uint32_t)c.token_stride * 2u;
+    constant_int* const ids = (constant_int*)(uint64_t)(a.table + (size_t)r * a.max_blocks);
+    const uint64_t head_bytes = (uint64_t)kvh * (uint64_t)c.head_stride * 2u;
+    const int block_mask = (1 << c.block_shift) - 1;
+    auto load_tile = [&](int tile, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int in_tile = (wid * kLoads + j) * kRowsPerLoad, key = __builtin_amdgcn_readfirstlane(tile * kManyKeys + in_tile);
+            const int chunk = (int)(v_slot<DH>(in_tile + ld_row, ld_slot) / 16) & (DH / 8 - 1);       // the order is its own inverse
+            const bool ok = chunk < chunks && key + ld_row < s.end && key + ld_row >= s.begin;
+            const uint32_t at = ok ? (uint32_t)ld_row * row_bytes + (uint32_t)chunk * 16u : kOutOfRange;
+            const int id = key < s.end ? ids[key >> c.block_shift] : -1;
+            const bool known = (uint32_t)id < (uint32_t)c.n_blocks;
+            const uint64_t block = (uint64_t)(known ? id : 0) * (uint64_t)c.block_stride * 2u + head_bytes + (uint64_t)(key & block_mask) * row_bytes;
+            const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.k + block, 0, known ? 0x7FFFFFFF : 0, 0x00020000);
+            const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.v + block, 0, known ? 0x7FFFFFFF : 0, 0x00020000);
+            char* const to = lds + buf * (2 * kTile) + in_tile * (DH * 2);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)to, 16, at, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(to + kTile), 16, at, 0, 0, 0);
+        }
+    };
+    // operand addresses inside a buffer
+    uint32_t k_at[kSteps], v_at[kBlocks][2];
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks) k_at[ks] = v_slot<DH>(l32, 2 * ks + half);
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            v_at[db][i] = kTile + v_slot<DH>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+
+    float m = -INFINITY, l = 0.f;
+    f32x16 o[kBlocks];
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[db][x] = 0.f;
+
+    int buf = 0;
+    if (tiles > 0) load_tile(tile0, 0);
+    for (int t = 0; t < tiles; ++t, buf ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));              // this tile's loads have landed, the last one's reads are done
+        __builtin_amdgcn_s_barrier();
+        if (t + 1 < tiles) load_tile(tile0 + t + 1, buf ^ 1);
+        const int key0 = (tile0 + t) * kManyKeys;
+        if (!works || key0 > high || (a.window > 0 && key0 + kManyKeys - 1 <= low - a.window)) continue;      // nothing here for these rows
+        const char* const kv = lds + buf * (2 * kTile);
+        f32x16 sc[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sc[kb][x] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) {
+                const bf16x8 kf = *(const bf16x8*)(kv + k_at[ks] + kb * 32 * DH * 2);
+                sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sc[kb], 0, 0, 0);
+            }
+        }
+        const bool masked = key0 + kManyKeys - 1 > low || (a.window > 0 && key0 <= high - a.window);
+        if (masked) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const int key = key0 + kb * 32 + 8 * (x >> 2) + 4 * half + (x & 3);
+                    if (!(row_ok && key <= pos && key > from)) sc[kb][x] = -INFINITY;
+                }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[kb][x]);
+        top = max_halves(top);
+        // scale2 >= 0 keeps the order; 0 times -inf would not be a mask any more
+        top = top == -INFINITY ? top : top * scale2;
+        // The reference moves only when a score exceeds it by 2^8: exponentials up to 2^8 are as exact as up to 1, and moving it costs a
+        // multiplication of the whole output.
+        if (__any(top > m + 8.f)) {
+            const float m_new = fmaxf(m, top), shrink = m_new == m ? 1.f : exp2_fast(m - m_new);
+            l *= shrink;
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[db][x] *= shrink;
+            m = m_new;
+        }
+        const float m_use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                float p = exp2_fast(__builtin_fmaf(sc[kb][x], scale2, -m_use));
+                if (masked && sc[kb][x] == -INFINITY) p = 0.f;            // scale2 = 0
+                sc[kb][x] = p;
+                l += p;
+            }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int t2 = 0; t2 < 2; ++t2) {
+                u32x4 pw;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16(sc[kb][8 * t2 + 2 * e], sc[kb][8 * t2 + 2 * e + 1]);
+                const char* at[kBlocks][2];
+#pragma unroll
+                for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) at[db][i] = kv + v_at[db][i];
+                add_values<DH>(o, at, (kb * 32 + t2 * 16) * DH * 2, __builtin_bit_cast(bf16x8, pw), masked, [&](int j) {
+                    const int key = key0 + kb * 32 + t2 * 16 + j;
+                    return row_ok && key <= pos && key > from;
+                });
+            }
+    }
+    l = sum_halves(l);
+    if (!row_ok) return;
+    if (part < 0) {
+        const float inv = m == -INFINITY ? 0.f : 1.f / l;
+        uint16_t* const to = a.out + (int64_t)(q0 + token) * a.out_token_stride + (int64_t)head * a.out_head_stride + half * 4;
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (db * 32 + g * 8 < c.head_dim)
+                    *(uint2*)(to + db * 32 + g * 8) = make_uint2(pack_bf16(o[db][4 * g] * inv, o[db][4 * g + 1] * inv), pack_bf16(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv));
+        if (a.lse && half == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+    } else {
+        float* const to = (float*)(workspace + layout.parts) + ((size_t)part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * DH);
+        const int rw = wid * 32 + l32;
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(float4*)(to + 2 * kManyRows + rw * DH + db * 32 + g * 8 + half * 4) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+        if (half == 0) {
+            to[rw] = m;
+            to[kManyRows + rw] = l;
+        }
+    }
+#endif
+}
+
+// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.
+template <int DH>
+__global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c, KvAttention a, const char* workspace, ManyLayout layout)
+{
+    const int kvh = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
+    if (index >= ((const ManyHeader*)(workspace + layout.header))->joined) return;
+    const Joined u = ((const Joined*)(workspace + layout.joined))[index];
+    const int group = a.heads / c.kv_heads;
+    const Span s = span_of(a, u.request, group, a.max_blocks << c.block_shift);
+    const int q0 = max(0, min(a.q_off[u.request], a.n_tokens));
+    const size_t stride = (size_t)c.kv_heads * (2 * kManyRows + kManyRows * DH);
+    const float* const parts = (const float*)(workspace + layout.parts) + ((size_t)u.part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * DH);
+    for (int i = threadIdx.x; i < 16 * (DH / 4); i += 256) {
+        const int rw = blockIdx.y * 16 + i / (DH / 4), ch = i % (DH / 4) * 4, row = u.first_row + rw;
+        if (row >= s.rows) continue;
+        float mx = -INFINITY, sum = 0.f;
+        for (int p = 0; p < u.parts; ++p) mx = fmaxf(mx, parts[p * stride + rw]);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 0; p < u.parts; ++p) {
+            const float* const from = parts + p * stride;
+            const float mw = from[rw];
+            if (mw == -INFINITY) continue;
+            const float f = mw == mx ? 1.f : exp2f(mw - mx);
+            const float4 v = *(const float4*)(from + 2 * kManyRows + rw * DH + ch);
+            sum += f * from[kManyRows + rw];
+            acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
+        }
+        const int token = row / group, head = kvh * group + (row - token * group);
+        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+        if (ch < c.head_dim)
+            *(uint2*)(a.out + (int64_t)(q0 + token) * a.out_token_stride + (int64_t)head * a.out_head_stride + ch) =
+                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (a.lse && ch == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+    }
+}
+
+template <int DH> int64_t few_bytes(int32_t n_requests)
+{
+    return few_header_bytes(n_requests) + (int64_t)kFewGroups * 2 * kPartFloats<DH> * 4;
+}
 
 template <int DH> hipError_t launch_few(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
 {
@@ -527,18 +846,40 @@ template <int DH> hipError_t launch_few(const KvCache& c, const KvAttention& a, 
     return hipGetLastError();
 }
 
+template <int DH> hipError_t launch_many(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
+{
+    constexpr int kLds = 4 * kManyTile<DH>;
+    static const hipError_t configured[2] = {
+        hipFuncSetAttribute((const void*)kv_attention_many_kernel<DH>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds),
+        hipFuncSetAttribute((const void*)kv_attention_schedule_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (kPlanMaxRequests + 1) * 4)};
+    if (configured[0] != hipSuccess || configured[1] != hipSuccess) return configured[0] != hipSuccess ? configured[0] : configured[1];
+    const ManyLayout at = many_layout(few_bytes<DH>(a.n_requests), a.n_requests, a.n_tokens, a.heads, c.kv_heads, DH);
+    if (at.most_units * c.kv_heads > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kv_attention_schedule_kernel, dim3(1), dim3(kSchedThreads), (a.n_requests + 1) * 4, stream, c, a, workspace, at);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kv_attention_many_kernel<DH>, dim3((unsigned)(at.most_units * c.kv_heads)), dim3(64 * kManyWaves), kLds, stream, c, a, workspace, at);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kv_attention_join_units_kernel<DH>, dim3((unsigned)(at.most_joined * c.kv_heads), kManyRows / 16), dim3(256), 0, stream, c, a, workspace, at);
+    return hipGetLastError();
+}
+
 }  // namespace
 
-int64_t kv_attention_workspace(int32_t n_requests, int32_t, int32_t, int32_t, int32_t, int32_t head_dim)
+int64_t kv_attention_workspace(int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads, int32_t kv_heads, int32_t head_dim)
 {
-    return few_header_bytes(n_requests) + (int64_t)kFewGroups * 2 * (head_dim <= 64 ? kPartFloats<64> : kPartFloats<128>) * 4;
+    const int64_t few = head_dim <= 64 ? few_bytes<64>(n_requests) : few_bytes<128>(n_requests);
+    if ((int64_t)std::min(max_new, n_tokens) * (heads / kv_heads) <= kFewRows) return few;
+    return many_layout(few, n_requests, n_tokens, heads, kv_heads, head_dim <= 64 ? 64 : 128).end;
 }
 
 hipError_t kv_attention(const KvCache& c, const KvAttention& a, void* workspace, hipStream_t stream)
 {
-    if ((long long)a.max_new * (a.heads / c.kv_heads) > kFewRows)
-        hipLaunchKernelGGL(kv_attention_rows_kernel, dim3((unsigned)(a.n_tokens * a.heads)), dim3(64), 0, stream, c, a);
-    return c.head_dim <= 64 ? launch_few<64>(c, a, (char*)workspace, stream) : launch_few<128>(c, a, (char*)workspace, stream);
+    const bool narrow = c.head_dim <= 64;
+    if ((int64_t)a.max_new * (a.heads / c.kv_heads) > kFewRows) {
+        const hipError_t e = narrow ? launch_many<64>(c, a, (char*)workspace, stream) : launch_many<128>(c, a, (char*)workspace, stream);
+        if (e != hipSuccess) return e;
+    }
+    return narrow ? launch_few<64>(c, a, (char*)workspace, stream) : launch_few<128>(c, a, (char*)workspace, stream);
 }
 
 }  // namespace k
