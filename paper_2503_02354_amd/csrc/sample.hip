@@ -21,7 +21,7 @@ __device__ __forceinline__ uint32_t key_of(float x)
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 __device__ __forceinline__ unsigned long long order_of(float x, uint32_t i) { return (unsigned long long)key_of(x) << 32 | (uint32_t)~i; }
 
-__device__ __forceinline__ float number(float x) { return fmaxf(x, -INFINITY); }        // NaN becomes -inf
+__device__ __forceinline__ float number(float x) { return x == x ? x : -INFINITY; }
 __device__ __forceinline__ float logit(const float* row, int i) { return number(row[i]); }
 __device__ __forceinline__ float logit(const uint16_t* row, int i) { return number(__uint_as_float((uint32_t)row[i] << 16)); }
 
@@ -29,23 +29,35 @@ __device__ __forceinline__ float logit(const uint16_t* row, int i) { return numb
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int kWidth = 4;
-    static __device__ __forceinline__ float at(const uint4& w, int e) { return number(__uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w)); }
+    static __device__ __forceinline__ float at(const uint4& w, int e) { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
 };
 template <> struct Vec<uint16_t> {
     static constexpr int kWidth = 8;
     static __device__ __forceinline__ float at(const uint4& w, int e)
     {
         const uint32_t d = e < 2 ? w.x : e < 4 ? w.y : e < 6 ? w.z : w.w;
-        return number(__uint_as_float(e & 1 ? d & 0xFFFF0000u : d << 16));
+        return __uint_as_float(e & 1 ? d & 0xFFFF0000u : d << 16);
     }
 };
 
+__device__ __forceinline__ float exp2_fast(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(v);         // one instruction; weights below 2^-126 are 0
+#else
+    return v;
+#endif
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));      // of any fp32 row
+
 struct Best { float score; uint32_t index; };
 constexpr uint32_t kNone = 0xFFFFFFFFu;
-__device__ __forceinline__ Best better(Best a, Best b) { return b.score > a.score || (b.score == a.score && b.index < a.index) ? b : a; }
+__device__ __forceinline__ bool better_than(float score, uint32_t index, Best a) { return (score > a.score) | ((score == a.score) & (index < a.index)); }
+__device__ __forceinline__ Best better(Best a, Best b) { return better_than(b.score, b.index, a) ? b : a; }
 
 // A row and the workgroup's shared memory; every method is called by all threads.
-constexpr int kMostCandidates = 2048, kMostTopK = 512, kSorted = 1024;
+constexpr int kMostCandidates = 3072, kMostTopK = 1536;
 template <int THREADS> struct Shared {
     static constexpr int kWaves = THREADS / 64;
     Best best[kWaves];
@@ -54,9 +66,9 @@ template <int THREADS> struct Shared {
     uint32_t hist[256];
     uint32_t pick[2];
     uint32_t n_candidates;
-    unsigned long long candidate[kMostCandidates];
-    float weight[kSorted];
-    uint32_t index[kSorted];
+    alignas(16) unsigned long long candidate[kMostCandidates + 4];
+    float weight[kMostTopK];
+    uint32_t index[kMostTopK];
 };
 
 template <int THREADS> __device__ __forceinline__ Best block_best(Best v, Shared<THREADS>& sh)
@@ -80,30 +92,36 @@ template <int THREADS> __device__ __forceinline__ float block_sum(float v, Share
     return v;
 }
 
-// The row in pieces of up to 16 bytes, this thread's share: f(x[], n, first index), n = W for whole vectors and 1 at the row's ends,
-// whose alignment may be any.
-template <int THREADS, typename T, class F> __device__ __forceinline__ void pieces(const T* row, int vocab, F f)
+// The row in batches, this thread's share: f(x[], n, first index) for n logits as they are (NaN too), W at a time from 16 bytes (in_batch
+// has their indices); n = 1 at the row's ends, whose alignment may be any.  A thread's indices ascend.
+template <int THREADS, typename T, class F> __device__ __forceinline__ void batches(const T* row, int vocab, F f)
 {
     constexpr int W = Vec<T>::kWidth, kAhead = 16 / W;
     const int tid = threadIdx.x;
     const int lead = min(vocab, (int)((-(uintptr_t)row & 15) / sizeof(T))), vecs = (vocab - lead) / W, tail = lead + vecs * W;
     const uint4* const body = (const uint4*)(row + lead);
-    float x[W];
+    float x[16];
     if (tid < lead) {
         x[0] = logit(row, tid);
         f(x, std::integral_constant<int, 1>(), (uint32_t)tid);
     }
     int v = tid;
+    uint4 next[kAhead];
+    if (v + (kAhead - 1) * THREADS < vecs)
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) next[j] = body[v + j * THREADS];
     for (; v + (kAhead - 1) * THREADS < vecs; v += kAhead * THREADS) {
         uint4 w[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) w[j] = body[v + j * THREADS];
+        for (int j = 0; j < kAhead; ++j) w[j] = next[j];
+        if (v + (2 * kAhead - 1) * THREADS < vecs)
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+            for (int j = 0; j < kAhead; ++j) next[j] = body[v + (kAhead + j) * THREADS];
 #pragma unroll
-            for (int e = 0; e < W; ++e) x[e] = Vec<T>::at(w[j], e);
-            f(x, std::integral_constant<int, W>(), (uint32_t)(lead + (v + j * THREADS) * W));
-        }
+        for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+            for (int e = 0; e < W; ++e) x[j * W + e] = Vec<T>::at(w[j], e);
+        f(x, std::integral_constant<int, 16>(), (uint32_t)(lead + v * W));
     }
     for (; v < vecs; v += THREADS) {
         const uint4 w = body[v];
@@ -116,12 +134,18 @@ template <int THREADS, typename T, class F> __device__ __forceinline__ void piec
         f(x, std::integral_constant<int, 1>(), (uint32_t)(tail + tid));
     }
 }
+// index of element e of a batch that begins at i
+template <int THREADS, typename T> __device__ __forceinline__ uint32_t in_batch(uint32_t i, int e)
+{
+    constexpr int W = Vec<T>::kWidth;
+    return i + (uint32_t)(e / W * THREADS * W + e % W);
+}
 // f(x, index) for every logit
 template <int THREADS, typename T, class F> __device__ __forceinline__ void each(const T* row, int vocab, F f)
 {
-    pieces<THREADS>(row, vocab, [&](const float (&x)[Vec<T>::kWidth], auto n, uint32_t i) {
+    batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
 #pragma unroll
-        for (int e = 0; e < n; ++e) f(x[e], i + e);
+        for (int e = 0; e < n; ++e) f(x[e], in_batch<THREADS, T>(i, e));
     });
 }
 
@@ -129,56 +153,134 @@ template <int THREADS, typename T, class F> __device__ __forceinline__ void each
 struct Front {
     float x;
     uint32_t end;
-    __device__ __forceinline__ bool holds(float v, uint32_t i) const { return v > x || (v == x && i < end); }
+    __device__ __forceinline__ bool holds(float v, uint32_t i) const { return (v > x) | ((v == x) & (i < end)); }
 };
 
 // What a row's weights are relative to, and in which unit.
 struct Scale {
     float top, per2;                          // largest logit; 1 / T in units of ln 2
-    // log2 of the weight: 0 for the largest itself, whatever it is
-    __device__ __forceinline__ float rel2(float x) const
-    {
-        const float d = x - top;
-        return x == top ? 0.f : d == -INFINITY ? d : d * per2;
-    }
-    __device__ __forceinline__ float weight(float x) const { return __builtin_exp2f(rel2(x)); }
+    // log2 of the weight: 0 for the largest itself, be it infinite, and -inf for others then
+    __device__ __forceinline__ float rel2(float x) const { return (x == top ? 0.f : x - top) * per2; }
+    __device__ __forceinline__ float weight(float x) const { return exp2_fast(rel2(x)); }
 };
 
-// The race among the tokens of a front, decided by what the filters say.  The race (largest (x - max) / T - ln E) needs no sorted row:
-// its winner among a set of tokens that holds all kept ones is the drawn token if it is kept itself, and whether it is takes one
-// sum over the tokens before it.  If it is not, no token from its place on is kept either, and the race is run again among those
-// before it.
+// The winner of the race among the tokens of a front: the largest log2(w) - log2 E.
 template <int THREADS, typename T>
-__device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t top_index, Front last, float top_p, float mass, float min_p, Scale scale,
+__device__ __attribute__((noinline)) Best winner_by_logs(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float least, Scale scale,
+                                                         Shared<THREADS>& sh)
+{
+    Best win{-INFINITY, kNone};
+    each<THREADS>(row, vocab, [&](float x, uint32_t i) {
+        if (!front.holds(x, i) | (x == -INFINITY)) return;
+        const float z = scale.rel2(x), score = z - log2f(noise[i]);
+        if (((z >= least) | (i == top_index)) & (score > -INFINITY)) win = better(win, Best{score, i});
+    });
+    return block_best(win, sh);
+}
+
+// The race decided by what the filters say.  It needs no sorted row: its winner among a front that holds all kept tokens is the drawn
+// token if it is kept itself, and whether it is takes one sum over the tokens before it.  If it is not, no token from its place on
+// is kept either, and the race is for the others.  The sums of the four best threads' winners are taken in one pass, since a row
+// whose winner falls to the nucleus would keep the launch waiting for another two.
+// w / E is compared by cross products; logarithms are taken of every thread's winner only.  Where fp32 may not hold the products
+// (random numbers below 2^-60, a winner below 2^-40, infinite logits), by logarithms after all.
+template <int THREADS, typename T>
+__device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float top_p, float mass, float min_p, Scale scale,
                          Shared<THREADS>& sh)
 {
+    constexpr int W = Vec<T>::kWidth, kFew = 4;
     const float least = min_p > 0.f ? log2f(min_p) : -INFINITY;
+    bool by_logs = !(scale.top < INFINITY);
     for (;;) {                                // the front shrinks with every round that goes on
-        Best win{-INFINITY, kNone};
-        pieces<THREADS>(row, vocab, [&](const float (&x)[Vec<T>::kWidth], auto n, uint32_t i) {
-            bool any = false;
+        Best c[kFew];
 #pragma unroll
-            for (int e = 0; e < n; ++e) any |= x[e] >= last.x;
-            if (!any) return;
-            float q[Vec<T>::kWidth];
+        for (int j = 0; j < kFew; ++j) c[j] = Best{-INFINITY, kNone};
+        if (!by_logs) {
+            uint32_t index = kNone;
+            float win_w = 0.f, win_q = 1.f, smallest = 1.f;
+            batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
+                float high = x[0];
 #pragma unroll
-            for (int e = 0; e < n; ++e) q[e] = noise[i + e];
+                for (int e = 1; e < n; ++e) high = fmaxf(high, x[e]);
+                if (!(high >= front.x)) return;
+                float q[16];
+                if constexpr (n == 1) q[0] = noise[i];
+                else {
 #pragma unroll
-            for (int e = 0; e < n; ++e) {
-                const float z = scale.rel2(x[e]), score = z - log2f(q[e]);
-                const bool in = last.holds(x[e], i + e) && x[e] > -INFINITY && (z >= least || i + e == top_index) && score > -INFINITY;
-                if (in) win = better(win, Best{score, i + e});
+                    for (int e = 0; e < n; e += 4) {
+                        const f32x4 v = *(const f32x4*)(noise + in_batch<THREADS, T>(i, e));
+                        q[e] = v[0], q[e + 1] = v[1], q[e + 2] = v[2], q[e + 3] = v[3];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < n; ++e) {
+                    const uint32_t at = in_batch<THREADS, T>(i, e);
+                    const float z = (x[e] - scale.top) * scale.per2, w = exp2_fast(z);
+                    smallest = fminf(smallest, q[e]);
+                    const bool wins = front.holds(x[e], at) & ((z >= least) | (at == top_index)) & (q[e] >= 0.f) & (w * win_q > win_w * q[e]);
+                    win_w = wins ? w : win_w;
+                    win_q = wins ? q[e] : win_q;
+                    index = wins ? at : index;
+                }
+            });
+            by_logs = __syncthreads_or(smallest < 0x1p-60f);
+            Best mine{index == kNone ? -INFINITY : log2f(win_w) - log2f(win_q), index};
+            c[0] = block_best(mine, sh);
+            by_logs |= !(c[0].score > -40.f);
+            if (!by_logs && top_p < 1.f && c[0].index != top_index) {
+#pragma unroll
+                for (int j = 1; j < kFew; ++j) {
+                    if (mine.index == c[j - 1].index) mine = Best{-INFINITY, kNone};
+                    c[j] = block_best(mine, sh);
+                }
             }
+        }
+        if (by_logs) c[0] = winner_by_logs<THREADS>(row, noise, vocab, top_index, front, least, scale, sh);
+        if (c[0].index == kNone) return top_index;
+        if (!(top_p < 1.f) || c[0].index == top_index) return c[0].index;
+
+        Front ahead[kFew];
+        float before[kFew];
+#pragma unroll
+        for (int j = 0; j < kFew; ++j) {
+            ahead[j] = c[j].index == kNone ? Front{INFINITY, 0} : Front{logit(row, c[j].index), c[j].index};
+            before[j] = 0.f;
+        }
+        each<THREADS>(row, vocab, [&](float x, uint32_t i) {
+            const float w = scale.weight(x);
+#pragma unroll
+            for (int j = 0; j < kFew; ++j) before[j] += ahead[j].holds(x, i) ? w : 0.f;
         });
-        win = block_best(win, sh);
-        if (win.index == kNone) return top_index;
-        if (!(top_p < 1.f) || win.index == top_index) return win.index;
-        const Front ahead{logit(row, win.index), win.index};
-        float before = 0.f;
-        each<THREADS>(row, vocab, [&](float x, uint32_t i) { before += ahead.holds(x, i) ? scale.weight(x) : 0.f; });
-        before = block_sum(before, sh);
-        if (before < top_p * mass) return win.index;
-        last = ahead;
+        int kept = kFew;
+        Front out{-INFINITY, kNone};          // in front of every token that turned out not to be kept
+#pragma unroll
+        for (int j = 0; j < kFew; ++j) {
+            before[j] = block_sum(before[j], sh);
+            if (kept < kFew || c[j].index == kNone) continue;
+            if (c[j].index == top_index || before[j] < top_p * mass) kept = j;
+            else if (!ahead[j].holds(out.x, out.end) || out.end == kNone) out = ahead[j];
+        }
+        if (kept == 0) return c[0].index;
+        if (kept < kFew) {
+            // A thread whose winner is not kept may hide another that is, and that beats the kept one: its share is looked through.
+            bool hidden = false;
+            const int lead = min(vocab, (int)((-(uintptr_t)row & 15) / sizeof(T))), vecs = (vocab - lead) / W, tail = lead + vecs * W;
+            const Best best = kept == 1 ? c[1] : kept == 2 ? c[2] : c[3];
+#pragma unroll
+            for (int j = 0; j < kFew - 1; ++j) {
+                if (j >= kept) continue;
+                const int at = (int)c[j].index, owner = at < lead ? at : at >= tail ? at - tail : (at - lead) / W % THREADS;
+                const int own_vecs = vecs > owner ? (vecs - owner + THREADS - 1) / THREADS : 0;
+                for (int k = threadIdx.x; k < own_vecs * W + 2; k += THREADS) {
+                    const int i = k < own_vecs * W ? lead + (owner + k / W * THREADS) * W + k % W : k == own_vecs * W ? (owner < lead ? owner : vocab) : tail + owner;
+                    if (i >= vocab) continue;
+                    const float x = logit(row, i), z = scale.rel2(x), score = z - log2f(noise[i]);
+                    if (out.holds(x, (uint32_t)i) && (z >= least || i == (int)top_index) && better_than(score, (uint32_t)i, best)) hidden = true;
+                }
+            }
+            if (!__syncthreads_or(hidden)) return best.index;
+        }
+        front = out;
     }
 }
 
@@ -191,7 +293,7 @@ template <int THREADS, typename T> __device__ Front front_of(const T* row, int v
         for (int b = tid; b < 256; b += THREADS) sh.hist[b] = 0;
         __syncthreads();
         each<THREADS>(row, vocab, [&](float x, uint32_t i) {
-            const unsigned long long o = order_of(x, i);
+            const unsigned long long o = order_of(number(x), i);
             if (shift == 56 || (o >> (shift + 8)) == (last >> (shift + 8))) atomicAdd(&sh.hist[(o >> shift) & 255], 1u);
         });
         __syncthreads();
@@ -210,21 +312,25 @@ template <int THREADS, typename T> __device__ Front front_of(const T* row, int v
     return {logit_of((uint32_t)(last >> 32)), ~(uint32_t)last + 1};
 }
 
-// Top_k up to 512 from a short list.  With at least top_k of the threads' largest logits at or above a bound, so are the first top_k
-// tokens: one pass collects what reaches the bound (little more than top_k tokens of 1024 threads), which then is ranked by
-// comparing all pairs, and the filters are decided on it.  Returns kNone where the list does not hold (more than 2048 tokens reach
-// the bound, because many are equal).
+// A small top_k from a short list.  Every thread has met the largest logits of four parts of its share; with at least top_k of all these
+// at or above a bound, so are the first top_k tokens.  One pass collects what reaches the bound (little more than top_k tokens),
+// which then is ranked by comparing all pairs, and the filters are decided on it.  Returns kNone where the list does not hold (more
+// tokens reach the bound, because many are equal).
 template <int THREADS, typename T>
-__device__ uint32_t from_list(const T* row, const float* noise, int vocab, float own_max, uint32_t top_k, float top_p, float min_p, Scale scale, Shared<THREADS>& sh)
+__device__ uint32_t from_list(const T* row, const float* noise, int vocab, const float (&own_max)[4], uint32_t top_k, float top_p, float min_p, Scale scale, Shared<THREADS>& sh)
 {
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     // the bound: two bytes of the top_k-th largest of the threads' maxima
-    const uint32_t own_key = key_of(own_max);
+    uint32_t own_key[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) own_key[j] = key_of(own_max[j]);
     uint32_t bound = 0, left = top_k;
     for (int shift = 24; shift >= 16; shift -= 8) {
         for (int b = tid; b < 256; b += THREADS) sh.hist[b] = 0;
         __syncthreads();
-        if (shift == 24 || own_key >> 24 == bound >> 24) atomicAdd(&sh.hist[(own_key >> shift) & 255], 1u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (shift == 24 || own_key[j] >> 24 == bound >> 24) atomicAdd(&sh.hist[(own_key[j] >> shift) & 255], 1u);
         __syncthreads();
         if (wid == 0) {                       // lane l holds bins 255 - 4 l .. 252 - 4 l
             uint32_t h[4], sum = 0;
@@ -249,21 +355,32 @@ __device__ uint32_t from_list(const T* row, const float* noise, int vocab, float
     }
     if (tid == 0) sh.n_candidates = 0;
     __syncthreads();
-    const float least = logit_of(bound);      // -inf where the bound's bits are no number's: everything
-    each<THREADS>(row, vocab, [&](float x, uint32_t i) {
-        if ((x >= least || !(least == least)) && x > -INFINITY) {
-            const uint32_t at = atomicAdd(&sh.n_candidates, 1u);
-            if (at < kMostCandidates) sh.candidate[at] = order_of(x, i);
-        }
+    const float edge = logit_of(bound), least = edge == edge ? edge : -INFINITY;      // bits below those of -inf are no number's
+    batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
+        float high = x[0];
+#pragma unroll
+        for (int e = 1; e < n; ++e) high = fmaxf(high, x[e]);
+        if (!(high >= least)) return;
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+            if (x[e] >= least && x[e] > -INFINITY) {
+                const uint32_t at = atomicAdd(&sh.n_candidates, 1u);
+                if (at < kMostCandidates) sh.candidate[at] = order_of(x[e], in_batch<THREADS, T>(i, e));
+            }
     });
     __syncthreads();
     const uint32_t n = sh.n_candidates;
     if (n > kMostCandidates) return kNone;
+    if (tid < 3) sh.candidate[n + tid] = 0;
+    __syncthreads();
     // rank of every candidate; the list's own order, which atomics made, has no say in anything below
     for (uint32_t c = tid; c < n; c += THREADS) {
         const unsigned long long o = sh.candidate[c];
         uint32_t rank = 0;
-        for (uint32_t j = 0; j < n; ++j) rank += sh.candidate[j] > o;
+        for (uint32_t j = 0; j < n; j += 4) {             // the places up to the next multiple of four hold zeros
+            const ulonglong2 a = *(const ulonglong2*)&sh.candidate[j], b = *(const ulonglong2*)&sh.candidate[j + 2];
+            rank += (a.x > o) + (a.y > o) + (b.x > o) + (b.y > o);
+        }
         if (rank < top_k) {
             sh.weight[rank] = scale.rel2(logit_of((uint32_t)(o >> 32)));
             sh.index[rank] = ~(uint32_t)o;
@@ -280,7 +397,7 @@ __device__ uint32_t from_list(const T* row, const float* noise, int vocab, float
     for (int round = 0; round < kRounds; ++round) {
         const uint32_t rank = round * THREADS + tid;
         z[round] = rank < kept ? sh.weight[rank] : -INFINITY;
-        w[round] = __builtin_exp2f(z[round]);
+        w[round] = exp2_fast(z[round]);
         float sum = w[round];
         for (int d = 1; d < 64; d <<= 1) {
             const float u = __shfl_up(sum, d, 64);
@@ -313,7 +430,7 @@ __device__ uint32_t from_list(const T* row, const float* noise, int vocab, float
 
 // A workgroup per row.
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 8) void sample_kernel(Sampling s)
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel(Sampling s)
 {
     __shared__ Shared<THREADS> sh;
     const int tid = threadIdx.x, vocab = s.vocab;
@@ -328,27 +445,56 @@ __global__ __launch_bounds__(THREADS, 8) void sample_kernel(Sampling s)
 
     // One pass: the largest logit and where it is, and the sum of the weights relative to it, which is scaled down whenever a thread
     // meets a larger one.
-    constexpr float kLowest = -3.402823466e38f;
-    const float unit = 1.44269504088896340736f / div;
-    float most = kLowest, sum = 0.f;
+    const float unit = fminf(fmaxf(1.44269504088896340736f / div, 1.4e-45f), 3.402823466e38f);      // neither 0 nor inf for any temperature
     Best top{-INFINITY, kNone};
-    pieces<THREADS>(row, vocab, [&](const float (&x)[Vec<T>::kWidth], auto n, uint32_t i) {
-        float high = x[0];
+    float part_max[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    // Weights relative to 2^at: x unit - at in one rounding, whatever number `at` is.  It follows the largest logit so far, but not below
+    // -2^20: masks of the type's lowest value weigh nothing then, and what a rounding of `at` leaves of the largest weight stays near 1.
+    constexpr float kFar = 1048576.f;
+    float at = 0.f, sum = 0.f;
+    batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
+        float high[4];
 #pragma unroll
-        for (int e = 1; e < n; ++e) high = fmaxf(high, x[e]);
-        if (high > top.score) {
-            uint32_t at = 0;
+        for (int e = 0; e < n; ++e) high[e / 4] = e % 4 ? fmaxf(high[e / 4], x[e]) : x[e];
+        constexpr int kParts = (n + 3) / 4;
 #pragma unroll
-            for (int e = n - 1; e >= 0; --e) at = x[e] == high ? e : at;
-            top = Best{high, i + at};
-            sum *= __builtin_exp2f((most - high) * unit);
-            most = fmaxf(high, kLowest);
+        for (int j = 0; j < kParts; ++j) part_max[j] = fmaxf(part_max[j], high[j]);
+#pragma unroll
+        for (int j = 1; j < kParts; ++j) high[0] = fmaxf(high[0], high[j]);
+        if (high[0] > top.score) {
+            uint32_t where = 0;
+#pragma unroll
+            for (int e = n - 1; e >= 0; --e) where = x[e] == high[0] ? in_batch<THREADS, T>(i, e) : where;
+            const float now = fmaxf(high[0] * unit, -kFar);
+            sum = top.index == kNone ? 0.f : sum * exp2_fast(at - now);
+            at = now;
+            top = Best{high[0], where};
         }
 #pragma unroll
-        for (int e = 0; e < n; ++e) sum += __builtin_exp2f((x[e] - most) * unit);
+        for (int e = 0; e < n; ++e) sum += exp2_fast(__builtin_fmaf(x[e], unit, -at));
     });
-    const float own_max = top.score;
+    const float own_top = top.score;
+    const bool odd = __syncthreads_or(!(sum < INFINITY));
     top = block_best(top, sh);
+    const float reference = top.score * unit;
+    float all = 0.f;
+    if (!odd && fabsf(reference) < kFar) {
+        all = block_sum(own_top == -INFINITY ? 0.f : sum * exp2_fast(at - reference), sh);
+        all *= exp2_fast(-__builtin_fmaf(top.score, unit, -reference));       // relative to the largest logit's weight
+    } else {
+        // NaN among the logits, infinite ones, or numbers too large for that
+        top = Best{-INFINITY, kNone};
+        each<THREADS>(row, vocab, [&](float raw, uint32_t i) {
+            const float x = number(raw);
+            if (x > top.score) top = Best{x, i};
+        });
+        part_max[0] = top.score;
+        part_max[1] = part_max[2] = part_max[3] = -INFINITY;
+        top = block_best(top, sh);
+        const Scale scale{top.score, unit};
+        each<THREADS>(row, vocab, [&](float raw, uint32_t) { all += number(raw) > -INFINITY ? scale.weight(raw) : 0.f; });
+        all = block_sum(all, sh);
+    }
     if (top.index == kNone) {
         if (tid == 0) {
             s.token[r] = -1;
@@ -357,26 +503,19 @@ __global__ __launch_bounds__(THREADS, 8) void sample_kernel(Sampling s)
         return;
     }
     const Scale scale{top.score, unit};
-    float all;
-    if (top.score < INFINITY && unit > 0.f && unit < INFINITY) all = block_sum(own_max == -INFINITY ? 0.f : sum * scale.weight(most), sh);
-    else {                                    // infinite logits or temperatures: the weights are 0 and 1
-        all = 0.f;
-        each<THREADS>(row, vocab, [&](float x, uint32_t) { all += x > -INFINITY ? scale.weight(x) : 0.f; });
-        all = block_sum(all, sh);
-    }
 
     uint32_t token = top.index;
     if (!greedy) {
         const bool cut = top_k > 0 && top_k < vocab;
         token = kNone;
-        if (cut && top_k <= min(kMostTopK, THREADS / 2)) token = from_list(row, noise, vocab, own_max, (uint32_t)top_k, top_p, min_p, scale, sh);
+        if (cut && top_k <= min(kMostTopK, 2 * THREADS)) token = from_list(row, noise, vocab, part_max, (uint32_t)top_k, top_p, min_p, scale, sh);
         if (token == kNone) {
             Front last{-INFINITY, kNone};
             float mass = all;
             if (cut) {
                 last = front_of(row, vocab, (uint32_t)top_k, sh);
                 mass = 0.f;
-                each<THREADS>(row, vocab, [&](float x, uint32_t i) { mass += last.holds(x, i) && x > -INFINITY ? scale.weight(x) : 0.f; });
+                each<THREADS>(row, vocab, [&](float x, uint32_t i) { mass += (last.holds(x, i) & (x > -INFINITY)) ? scale.weight(x) : 0.f; });
                 mass = block_sum(mass, sh);
             }
             if (top_p < 1.f) {
