@@ -81,10 +81,12 @@ __device__ __forceinline__ Span span_of(const KvAttention& a, int r, int group, 
     return s;
 }
 
-// Where 16-byte chunk c of row r of a V tile lies: rows of DH channels, chunks in an order that spreads both the writes (sixteen rows of
+// Where 16-byte chunk c of row r of a V tile lies: chunks in an order that spreads both the writes (sixteen rows of
 // one chunk) and the transposing reads (four rows of four chunks) over all LDS banks.
-template <int DH> __device__ __forceinline__ uint32_t v_slot(int r, int c)
+template <int D> constexpr int kRow = D <= 64 ? 64 : 128;     // channels that a row of D channels takes in LDS
+template <int D> __device__ __forceinline__ uint32_t v_slot(int r, int c)
 {
+    constexpr int DH = kRow<D>;
     const int f = DH == 128 ? (r & 3) * 4 + ((r >> 2) & 3) : ((r >> 1) & 1) * 4 + ((r >> 2) & 3);
     return (uint32_t)(r * DH * 2 + ((c ^ f) & (DH / 8 - 1)) * 16);
 }
@@ -92,13 +94,13 @@ template <int DH> __device__ __forceinline__ uint32_t v_slot(int r, int c)
 // acc += V^T P^T for 16 keys of a tile.  at: this lane's addresses of the transposing reads of keys 0..7 and 8..15, per 32 channels.
 // careful: a key may be hidden from some rows, and 0 * inf would reach them through the matrix core: values that are not finite are
 // then taken out of the operand and added one by one to the rows that see them (`sees(key of the 16)` says for this lane's row).
-template <int DH, class Sees>
-__device__ __forceinline__ void add_values(f32x16 (&acc)[DH / 32], const char* const (&at)[DH / 32][2], int offset, bf16x8 pf, bool careful, Sees sees)
+template <int D, class Sees>
+__device__ __forceinline__ void add_values(f32x16 (&acc)[D / 32], const char* const (&at)[D / 32][2], int offset, bf16x8 pf, bool careful, Sees sees)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int lane = threadIdx.x & 63, half = lane >> 5;
 #pragma unroll
-    for (int db = 0; db < DH / 32; ++db) {
+    for (int db = 0; db < D / 32; ++db) {
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at[db][0] + offset));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at[db][1] + offset));
         u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -144,17 +146,17 @@ struct FewHeader {                        // at the workspace's start, for the j
     unsigned long long base[1];           // [n_requests + 1] tiles before request r, of one cache head
 };
 __host__ __device__ constexpr int64_t few_header_bytes(int n_requests) { return (16 + 8 * (int64_t)(n_requests + 1) + 255) / 256 * 256; }
-// a part: maxima and sums [2][32], then the output [32][DH]
-template <int DH> constexpr int kPartFloats = 2 * kFewRows + kFewRows * DH;
+// a part: maxima and sums [2][32], then the output [32][D]
+template <int D> constexpr int kPartFloats = 2 * kFewRows + kFewRows * D;
 
-template <int DH> constexpr int kMergeRow = DH + 4;          // floats between the rows of a wavefront's output in LDS
-template <int DH> constexpr size_t kFewLds = (size_t)kFewWaves * kFewRows * kMergeRow<DH> * 4;
+template <int D> constexpr int kMergeRow = D + 4;          // floats between the rows of a wavefront's output in LDS
+template <int D> constexpr size_t kFewLds = (size_t)kFewWaves * kFewRows * kMergeRow<D> * 4;
 
-template <int DH, bool PAD>
+template <int D, bool PAD>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvCache c, KvAttention a, char* workspace)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kSteps = DH / 16, kBlocks = DH / 32;
+    constexpr int kSteps = D / 16, kBlocks = D / 32;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     __shared__ float stat[2][kFewWaves][kFewRows];
     __shared__ unsigned long long part_sum[kFewWaves];
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
         unsigned long long v = 0;
         if (r0 + tid < n) {
             const Span s = span_of(a, r0 + tid, group, table_tokens);
-            v = s.rows <= kFewRows ? (unsigned long long)s.tiles() : 0;
+            v = (unsigned long long)s.tiles();
         }
         unsigned long long sum = v;
         for (int d = 1; d < 64; d <<= 1) {
@@ -207,20 +209,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
     unsigned long long into = now - base[r] * (unsigned)c.kv_heads;       // tiles of this request that others did
     __syncthreads();
 
-    const int chunks = c.head_dim >> 3;
+    const int chunks = c.head_dim >> 3, last_step = (chunks - 1 - half) >> 1;       // this lane's last 16 bytes of a row; -1: none (8 channels)
     const float scale2 = a.scale * 1.44269504088896340736f;
-    char* const v_lds = lds + wid * (kKeys * DH * 2);
+    char* const v_lds = lds + wid * (kKeys * kRow<D> * 2);
     const char* v_at[kBlocks][2];
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            v_at[db][i] = v_lds + v_slot<DH>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+            v_at[db][i] = v_lds + v_slot<D>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
     const unsigned long long start = now;
 
     while (now < stop && r < n) {
         Span s = span_of(a, r, group, table_tokens);
-        int tiles = s.rows <= kFewRows ? s.tiles() : 0;
+        const int tiles = s.tiles();
         if (into >= (unsigned long long)tiles * (unsigned)c.kv_heads) {
             into = 0;
             ++r;
@@ -252,7 +254,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
             for (int x = 0; x < 16; ++x) o[db][x] = 0.f;
 
         const int32_t* const ids = a.table + (size_t)r * a.max_blocks;
-        const uint16_t *const k_base = c.k + kvh * c.head_stride + half * 8, *const v_base = c.v + kvh * c.head_stride + half * 8;
+        const int64_t lane_at = kvh * c.head_stride + (PAD && last_step < 0 ? 0 : half * 8);
+        const uint16_t *const k_base = c.k + lane_at, *const v_base = c.v + lane_at;
         auto id_of = [&](int tile) {      // block of this lane's key of a tile; -1: reads as zeros
             const int key = tile * kKeys + l32;
             int id = -1;
@@ -265,13 +268,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
         };
         auto fetch = [&](const uint16_t* p, u32x4 (&w)[kSteps]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) {
-                if (PAD) {
-                    w[ks] = u32x4{0, 0, 0, 0};
-                    if (2 * ks + half < chunks) w[ks] = *(const u32x4*)(p + ks * 16);
-                } else
-                    w[ks] = *(const u32x4*)(p + ks * 16);
-            }
+            for (int ks = 0; ks < kSteps; ++ks) w[ks] = *(const u32x4*)(p + (PAD ? max(0, min(ks, last_step)) : ks) * 16);
         };
         u32x4 kw[kSteps], vw[kSteps];
         int tile = first + t_begin + wid;
@@ -293,13 +290,16 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
                     vw[ks] = id < 0 ? u32x4{0, 0, 0, 0} : vw[ks];
                 }
             }
+            if (PAD)                      // what was read in the place of channels that are not there; the values' have results of their own
+#pragma unroll
+                for (int ks = 0; ks < kSteps; ++ks) kw[ks] = ks <= last_step ? kw[ks] : u32x4{0, 0, 0, 0};
             f32x16 sc;
 #pragma unroll
             for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < kSteps; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw[ks]), qf[ks], sc, 0, 0, 0);
 #pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) *(u32x4*)(v_lds + v_slot<DH>(l32, 2 * ks + half)) = vw[ks];
+            for (int ks = 0; ks < kSteps; ++ks) *(u32x4*)(v_lds + v_slot<D>(l32, 2 * ks + half)) = vw[ks];
             if (more) {
                 id = id_next;
                 const int64_t at = offset_of(tile + kFewWaves, id);
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
                 u32x4 pw;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) pw[e] = pack_bf16(sc[8 * t2 + 2 * e], sc[8 * t2 + 2 * e + 1]);
-                add_values<DH>(o, v_at, t2 * 16 * DH * 2, __builtin_bit_cast(bf16x8, pw), careful, [&](int j) {
+                add_values<D>(o, v_at, t2 * 16 * kRow<D> * 2, __builtin_bit_cast(bf16x8, pw), careful, [&](int j) {
                     const int key = key0 + 16 * t2 + j;
                     return row_ok && key <= pos && key > from;
                 });
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
 
         // the four wavefronts' results
         __syncthreads();
-        float* const mine = (float*)lds + wid * kFewRows * kMergeRow<DH> + l32 * kMergeRow<DH>;
+        float* const mine = (float*)lds + wid * kFewRows * kMergeRow<D> + l32 * kMergeRow<D>;
         if (row_ok) {
 #pragma unroll
             for (int db = 0; db < kBlocks; ++db)
@@ -364,9 +364,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
         }
         __syncthreads();
         const bool whole = t_begin == 0 && t_end == tiles;
-        float* const part = (float*)(workspace + few_header_bytes(n)) + ((size_t)blockIdx.x * 2 + (now != start)) * kPartFloats<DH>;
-        for (int i = tid; i < s.rows * (DH / 4); i += 64 * kFewWaves) {
-            const int rw = i / (DH / 4), ch = (i - rw * (DH / 4)) * 4;
+        float* const part = (float*)(workspace + few_header_bytes(n)) + ((size_t)blockIdx.x * 2 + (now != start)) * kPartFloats<D>;
+        for (int i = tid; i < s.rows * (D / 4); i += 64 * kFewWaves) {
+            const int rw = i / (D / 4), ch = (i - rw * (D / 4)) * 4;
             float mx = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kFewWaves; ++w) mx = fmaxf(mx, stat[0][w][rw]);
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
                 const float mw = stat[0][w][rw];
                 if (mw == -INFINITY) continue;
                 const float f = mw == mx ? 1.f : exp2_fast(mw - mx);
-                const float4 v = *(const float4*)((const float*)lds + (w * kFewRows + rw) * kMergeRow<DH> + ch);
+                const float4 v = *(const float4*)((const float*)lds + (w * kFewRows + rw) * kMergeRow<D> + ch);
                 sum += f * stat[1][w][rw];
                 acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
             }
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
                         make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
                 if (a.lse && ch == 0) a.lse[(int64_t)(q0 + tk) * a.heads + hd] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
             } else {
-                *(float4*)(part + 2 * kFewRows + rw * DH + ch) = acc;
+                *(float4*)(part + 2 * kFewRows + rw * D + ch) = acc;
                 if (ch == 0) {
                     part[rw] = mx;
                     part[kFewRows + rw] = sum;
@@ -403,46 +403,68 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
 #endif
 }
 
-// Adds up the parts of a history that several workgroups shared; a workgroup per request and cache head.
-template <int DH>
+// Adds up the parts of a history that several workgroups shared: a workgroup per request, cache head and kJoinRows query rows
+// (blockIdx.y).  Several threads share the parts of a row's four channels, since a long history has many; each leaves its sum
+// relative to its own maximum, and the first adds those up in their order.
+constexpr int kJoinRows = 1;
+template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAttention a, const char* workspace)
 {
+    constexpr int kColumns = kJoinRows * D / 4, kSplit = 256 / kColumns;
+    __shared__ float4 sums[256];
+    __shared__ float2 stats[256];
     const FewHeader* const h = (const FewHeader*)workspace;
     const int r = blockIdx.x / c.kv_heads, kvh = blockIdx.x - r * c.kv_heads, group = a.heads / c.kv_heads;
-    const unsigned long long tiles = h->base[r + 1] - h->base[r], per = h->per;
+    const unsigned long long first = h->base[r], tiles = h->base[r + 1] - first, per = h->per;
     if (tiles == 0) return;
-    const unsigned long long begin = h->base[r] * (unsigned)c.kv_heads + (unsigned)kvh * tiles, end = begin + tiles;
+    const unsigned long long begin = first * (unsigned)c.kv_heads + (unsigned)kvh * tiles, end = begin + tiles;
     const unsigned long long w0 = begin / per, w1 = (end - 1) / per;
     if (w0 == w1) return;
     const Span s = span_of(a, r, group, a.max_blocks << c.block_shift);
-    const int q0 = max(0, min(a.q_off[r], a.n_tokens));
-    const float* const parts = (const float*)(workspace + few_header_bytes(a.n_requests));
+    const int column = threadIdx.x % kColumns, share = threadIdx.x / kColumns;
+    const int rw = blockIdx.y * kJoinRows + column / (D / 4), ch = column % (D / 4) * 4;
+    if (blockIdx.y * kJoinRows >= s.rows) return;
     // a stretch's first history leaves the first part, its last one the second
-    auto part_of = [&](unsigned long long w) { return parts + (w * 2 + (begin > w * per)) * kPartFloats<DH>; };
-    for (int i = threadIdx.x; i < s.rows * (DH / 4); i += 256) {
-        const int rw = i / (DH / 4), ch = (i - rw * (DH / 4)) * 4;
-        float mx = -INFINITY, sum = 0.f;
-        for (unsigned long long w = w0; w <= w1; ++w) mx = fmaxf(mx, part_of(w)[rw]);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (unsigned long long w = w0; w <= w1; ++w) {
+    const float* const parts = (const float*)(workspace + few_header_bytes(a.n_requests));
+    auto part_of = [&](unsigned long long w) { return parts + (w * 2 + (begin > w * per)) * kPartFloats<D>; };
+    float mx = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (rw < s.rows && share < kSplit)
+#pragma unroll 2
+        for (unsigned long long w = w0 + share; w <= w1; w += kSplit) {
             const float* const p = part_of(w);
-            const float mw = p[rw];
+            const float mw = p[rw], lw = p[kFewRows + rw];
+            const float4 v = *(const float4*)(p + 2 * kFewRows + rw * D + ch);
             if (mw == -INFINITY) continue;
-            const float f = mw == mx ? 1.f : exp2f(mw - mx);
-            const float4 v = *(const float4*)(p + 2 * kFewRows + rw * DH + ch);
-            sum += f * p[kFewRows + rw];
-            acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
+            const float m_new = fmaxf(mx, mw), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mw - m_new);
+            sum = sum * keep + f * lw;
+            acc.x = acc.x * keep + f * v.x, acc.y = acc.y * keep + f * v.y, acc.z = acc.z * keep + f * v.z, acc.w = acc.w * keep + f * v.w;
+            mx = m_new;
         }
-        const int tk = rw / group, hd = kvh * group + (rw - tk * group);
-        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
-        if (ch < c.head_dim)
-            *(uint2*)(a.out + (int64_t)(q0 + tk) * a.out_token_stride + (int64_t)hd * a.out_head_stride + ch) =
-                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-        if (a.lse && ch == 0) a.lse[(int64_t)(q0 + tk) * a.heads + hd] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+    sums[threadIdx.x] = acc;
+    stats[threadIdx.x] = make_float2(mx, sum);
+    __syncthreads();
+    if (share > 0 || rw >= s.rows) return;
+    for (int i = 1; i < kSplit; ++i) mx = fmaxf(mx, stats[i * kColumns + column].x);
+    sum = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < kSplit; ++i) {
+        const float2 st = stats[i * kColumns + column];
+        if (st.x == -INFINITY) continue;
+        const float f = exp2f(st.x - mx);
+        const float4 v = sums[i * kColumns + column];
+        sum += f * st.y;
+        acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
     }
+    const int q0 = max(0, min(a.q_off[r], a.n_tokens)), tk = rw / group, hd = kvh * group + (rw - tk * group);
+    const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+    if (ch < c.head_dim)
+        *(uint2*)(a.out + (int64_t)(q0 + tk) * a.out_token_stride + (int64_t)hd * a.out_head_stride + ch) =
+            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    if (a.lse && ch == 0) a.lse[(int64_t)(q0 + tk) * a.heads + hd] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
 }
 
-// ---- many query rows (chunks of prompts): more than 32 per request and cache head --------------------------------------------
+// ---- many query rows (chunks of prompts, single tokens among them): steps with more than 32 per request and cache head ------------
 // Units of work are tiles of 128 query rows (32 to a wavefront) of a request and cache head, with all the 64-key tiles that one of
 // them sees.  A scheduling launch lists them, longest first, so that the last workgroups to start are short ones; where there are too
 // few units to fill the chip it cuts long ones into parts over the keys, which kv_attention_join_units_kernel adds up.  Block b
@@ -461,21 +483,21 @@ struct Joined { int32_t request, first_row, part, parts; };
 struct ManyHeader { int32_t units, joined, pad[62]; };
 
 __host__ __device__ constexpr int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
-// sizes of the workspace's pieces behind the few-row kernel's
+// where the workspace's pieces begin
 struct ManyLayout {
     int64_t most_units, most_joined, header, units, joined, parts, end;
 };
-__host__ __device__ inline ManyLayout many_layout(int64_t begin, int32_t n_requests, int32_t n_tokens, int32_t heads, int32_t kv_heads, int32_t dh)
+__host__ __device__ inline ManyLayout many_layout(int32_t n_requests, int32_t n_tokens, int32_t heads, int32_t kv_heads, int32_t dim)
 {
     ManyLayout l;
     const int64_t rows = (int64_t)n_tokens * (heads / kv_heads), cuts = (kManyGroups + kv_heads - 1) / kv_heads;
     l.most_units = rows / kManyRows + n_requests + cuts;
     l.most_joined = cuts;
-    l.header = begin;
-    l.units = begin + sizeof(ManyHeader);
+    l.header = 0;
+    l.units = sizeof(ManyHeader);
     l.joined = l.units + round256(l.most_units * (int64_t)sizeof(Unit));
     l.parts = l.joined + round256(l.most_joined * (int64_t)sizeof(Joined));
-    l.end = l.parts + 2 * cuts * kv_heads * (int64_t)(2 * kManyRows + kManyRows * dh) * 4;
+    l.end = l.parts + 2 * cuts * kv_heads * (int64_t)(2 * kManyRows + kManyRows * dim) * 4;
     return l;
 }
 
@@ -519,7 +541,7 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
         int v = 0;
         if (r0 + tid < n) {
             const Span s = span_of(a, r0 + tid, group, table_tokens);
-            v = s.rows > kFewRows ? (s.rows + kManyRows - 1) / kManyRows : 0;
+            v = (s.rows + kManyRows - 1) / kManyRows;
         }
         unsigned long long all;
         const unsigned long long before = segments + sum_before((unsigned)v, all);
@@ -604,13 +626,13 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(4))) int32_t constant_int;
 [[maybe_unused]] constexpr uint32_t kOutOfRange = 0x80000000u;   // buffer offset beyond any block: loads return zeros
 
-template <int DH> constexpr int kManyTile = kManyKeys * DH * 2;  // bytes of a K (or V) tile
+template <int D> constexpr int kManyTile = kManyKeys * kRow<D> * 2;  // bytes of a K (or V) tile
 
-template <int DH>
+template <int D>
 __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(KvCache c, KvAttention a, char* workspace, ManyLayout layout)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kSteps = DH / 16, kBlocks = DH / 32, kTile = kManyTile<DH>;
+    constexpr int DH = kRow<D>, kSteps = D / 16, kBlocks = D / 32, kTile = kManyTile<D>;
     constexpr int kRowsPerLoad = 1024 / (DH * 2), kLoads = kManyKeys / kRowsPerLoad / kManyWaves;     // of K, and the same of V
     extern __shared__ __attribute__((aligned(1024))) char lds[];          // two buffers of a K and a V tile
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
@@ -655,7 +677,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int in_tile = (wid * kLoads + j) * kRowsPerLoad, key = __builtin_amdgcn_readfirstlane(tile * kManyKeys + in_tile);
-            const int chunk = (int)(v_slot<DH>(in_tile + ld_row, ld_slot) / 16) & (DH / 8 - 1);       // the order is its own inverse
+            const int chunk = (int)(v_slot<D>(in_tile + ld_row, ld_slot) / 16) & (DH / 8 - 1);       // the order is its own inverse
             const bool ok = chunk < chunks && key + ld_row < s.end && key + ld_row >= s.begin;
             const uint32_t at = ok ? (uint32_t)ld_row * row_bytes + (uint32_t)chunk * 16u : kOutOfRange;
             const int id = key < s.end ? ids[key >> c.block_shift] : -1;
@@ -671,12 +693,12 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     // operand addresses inside a buffer
     uint32_t k_at[kSteps], v_at[kBlocks][2];
 #pragma unroll
-    for (int ks = 0; ks < kSteps; ++ks) k_at[ks] = v_slot<DH>(l32, 2 * ks + half);
+    for (int ks = 0; ks < kSteps; ++ks) k_at[ks] = v_slot<D>(l32, 2 * ks + half);
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            v_at[db][i] = kTile + v_slot<DH>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+            v_at[db][i] = kTile + v_slot<D>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
 
     float m = -INFINITY, l = 0.f;
     f32x16 o[kBlocks];
@@ -756,7 +778,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
                 for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) at[db][i] = kv + v_at[db][i];
-                add_values<DH>(o, at, (kb * 32 + t2 * 16) * DH * 2, __builtin_bit_cast(bf16x8, pw), masked, [&](int j) {
+                add_values<D>(o, at, (kb * 32 + t2 * 16) * DH * 2, __builtin_bit_cast(bf16x8, pw), masked, [&](int j) {
                     const int key = key0 + kb * 32 + t2 * 16 + j;
                     return row_ok && key <= pos && key > from;
                 });
@@ -775,13 +797,13 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
                     *(uint2*)(to + db * 32 + g * 8) = make_uint2(pack_bf16(o[db][4 * g] * inv, o[db][4 * g + 1] * inv), pack_bf16(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv));
         if (a.lse && half == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
     } else {
-        float* const to = (float*)(workspace + layout.parts) + ((size_t)part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * DH);
+        float* const to = (float*)(workspace + layout.parts) + ((size_t)part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * D);
         const int rw = wid * 32 + l32;
 #pragma unroll
         for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *(float4*)(to + 2 * kManyRows + rw * DH + db * 32 + g * 8 + half * 4) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+                *(float4*)(to + 2 * kManyRows + rw * D + db * 32 + g * 8 + half * 4) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
         if (half == 0) {
             to[rw] = m;
             to[kManyRows + rw] = l;
@@ -791,7 +813,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 }
 
 // Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.
-template <int DH>
+template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c, KvAttention a, const char* workspace, ManyLayout layout)
 {
     const int kvh = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
@@ -800,22 +822,23 @@ __global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c,
     const int group = a.heads / c.kv_heads;
     const Span s = span_of(a, u.request, group, a.max_blocks << c.block_shift);
     const int q0 = max(0, min(a.q_off[u.request], a.n_tokens));
-    const size_t stride = (size_t)c.kv_heads * (2 * kManyRows + kManyRows * DH);
-    const float* const parts = (const float*)(workspace + layout.parts) + ((size_t)u.part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * DH);
-    for (int i = threadIdx.x; i < 16 * (DH / 4); i += 256) {
-        const int rw = blockIdx.y * 16 + i / (DH / 4), ch = i % (DH / 4) * 4, row = u.first_row + rw;
+    const size_t stride = (size_t)c.kv_heads * (2 * kManyRows + kManyRows * D);
+    const float* const parts = (const float*)(workspace + layout.parts) + ((size_t)u.part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * D);
+    for (int i = threadIdx.x; i < 16 * (D / 4); i += 256) {
+        const int rw = blockIdx.y * 16 + i / (D / 4), ch = i % (D / 4) * 4, row = u.first_row + rw;
         if (row >= s.rows) continue;
         float mx = -INFINITY, sum = 0.f;
-        for (int p = 0; p < u.parts; ++p) mx = fmaxf(mx, parts[p * stride + rw]);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
         for (int p = 0; p < u.parts; ++p) {
             const float* const from = parts + p * stride;
-            const float mw = from[rw];
-            if (mw == -INFINITY) continue;
-            const float f = mw == mx ? 1.f : exp2f(mw - mx);
-            const float4 v = *(const float4*)(from + 2 * kManyRows + rw * DH + ch);
-            sum += f * from[kManyRows + rw];
-            acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
+            const float mp = from[rw], lp = from[kManyRows + rw];
+            const float4 v = *(const float4*)(from + 2 * kManyRows + rw * D + ch);
+            if (mp == -INFINITY) continue;
+            const float m_new = fmaxf(mx, mp), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mp - m_new);
+            sum = sum * keep + f * lp;
+            acc.x = acc.x * keep + f * v.x, acc.y = acc.y * keep + f * v.y, acc.z = acc.z * keep + f * v.z, acc.w = acc.w * keep + f * v.w;
+            mx = m_new;
         }
         const int token = row / group, head = kvh * group + (row - token * group);
         const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
@@ -826,60 +849,67 @@ __global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c,
     }
 }
 
-template <int DH> int64_t few_bytes(int32_t n_requests)
+// channels that the kernels compute with: the next multiple of 32
+int padded_dim(int32_t head_dim) { return (head_dim + 31) / 32 * 32; }
+int64_t few_bytes(int32_t n_requests, int dim)
 {
-    return few_header_bytes(n_requests) + (int64_t)kFewGroups * 2 * kPartFloats<DH> * 4;
+    return few_header_bytes(n_requests) + (int64_t)kFewGroups * 2 * (2 * kFewRows + kFewRows * dim) * 4;
 }
+bool is_few(int32_t max_new, int32_t heads, int32_t kv_heads) { return (int64_t)max_new * (heads / kv_heads) <= kFewRows; }
 
-template <int DH> hipError_t launch_few(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
+template <int D, bool PAD> hipError_t launch_few(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
 {
-    const size_t lds = std::max(kFewLds<DH>, ((size_t)a.n_requests + 1) * 8);
-    constexpr int kMost = 144 * 1024;
-    static const hipError_t configured[2] = {
-        hipFuncSetAttribute((const void*)kv_attention_few_kernel<DH, false>, hipFuncAttributeMaxDynamicSharedMemorySize, kMost),
-        hipFuncSetAttribute((const void*)kv_attention_few_kernel<DH, true>, hipFuncAttributeMaxDynamicSharedMemorySize, kMost)};
-    if (configured[0] != hipSuccess || configured[1] != hipSuccess) return configured[0] != hipSuccess ? configured[0] : configured[1];
-    if (c.head_dim == DH) hipLaunchKernelGGL((kv_attention_few_kernel<DH, false>), dim3(kFewGroups), dim3(64 * kFewWaves), lds, stream, c, a, workspace);
-    else hipLaunchKernelGGL((kv_attention_few_kernel<DH, true>), dim3(kFewGroups), dim3(64 * kFewWaves), lds, stream, c, a, workspace);
+    const size_t lds = std::max(kFewLds<D>, ((size_t)a.n_requests + 1) * 8);
+    static const hipError_t configured =
+        hipFuncSetAttribute((const void*)kv_attention_few_kernel<D, PAD>, hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024);
+    if (configured != hipSuccess) return configured;
+    hipLaunchKernelGGL((kv_attention_few_kernel<D, PAD>), dim3(kFewGroups), dim3(64 * kFewWaves), lds, stream, c, a, workspace);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kv_attention_join_kernel<DH>, dim3((unsigned)a.n_requests * c.kv_heads), dim3(256), 0, stream, c, a, workspace);
+    const int most_rows = a.max_new * (a.heads / c.kv_heads);
+    hipLaunchKernelGGL(kv_attention_join_kernel<D>, dim3((unsigned)a.n_requests * c.kv_heads, (most_rows + kJoinRows - 1) / kJoinRows), dim3(256), 0,
+                       stream, c, a, workspace);
     return hipGetLastError();
 }
 
-template <int DH> hipError_t launch_many(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
+template <int D> hipError_t launch_many(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
 {
-    constexpr int kLds = 4 * kManyTile<DH>;
+    constexpr int kLds = 4 * kManyTile<D>;
     static const hipError_t configured[2] = {
-        hipFuncSetAttribute((const void*)kv_attention_many_kernel<DH>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds),
+        hipFuncSetAttribute((const void*)kv_attention_many_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds),
         hipFuncSetAttribute((const void*)kv_attention_schedule_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (kPlanMaxRequests + 1) * 4)};
     if (configured[0] != hipSuccess || configured[1] != hipSuccess) return configured[0] != hipSuccess ? configured[0] : configured[1];
-    const ManyLayout at = many_layout(few_bytes<DH>(a.n_requests), a.n_requests, a.n_tokens, a.heads, c.kv_heads, DH);
+    const ManyLayout at = many_layout(a.n_requests, a.n_tokens, a.heads, c.kv_heads, D);
     if (at.most_units * c.kv_heads > 0x7FFFFFFFll) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kv_attention_schedule_kernel, dim3(1), dim3(kSchedThreads), (a.n_requests + 1) * 4, stream, c, a, workspace, at);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kv_attention_many_kernel<DH>, dim3((unsigned)(at.most_units * c.kv_heads)), dim3(64 * kManyWaves), kLds, stream, c, a, workspace, at);
+    hipLaunchKernelGGL(kv_attention_many_kernel<D>, dim3((unsigned)(at.most_units * c.kv_heads)), dim3(64 * kManyWaves), kLds, stream, c, a, workspace, at);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kv_attention_join_units_kernel<DH>, dim3((unsigned)(at.most_joined * c.kv_heads), kManyRows / 16), dim3(256), 0, stream, c, a, workspace, at);
+    hipLaunchKernelGGL(kv_attention_join_units_kernel<D>, dim3((unsigned)(at.most_joined * c.kv_heads), kManyRows / 16), dim3(256), 0, stream, c, a, workspace, at);
     return hipGetLastError();
+}
+
+template <int D> hipError_t launch(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
+{
+    if (!is_few(a.max_new, a.heads, c.kv_heads)) return launch_many<D>(c, a, workspace, stream);
+    return c.head_dim == D ? launch_few<D, false>(c, a, workspace, stream) : launch_few<D, true>(c, a, workspace, stream);
 }
 
 }  // namespace
 
 int64_t kv_attention_workspace(int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads, int32_t kv_heads, int32_t head_dim)
 {
-    const int64_t few = head_dim <= 64 ? few_bytes<64>(n_requests) : few_bytes<128>(n_requests);
-    if ((int64_t)std::min(max_new, n_tokens) * (heads / kv_heads) <= kFewRows) return few;
-    return many_layout(few, n_requests, n_tokens, heads, kv_heads, head_dim <= 64 ? 64 : 128).end;
+    if (is_few(std::min(max_new, n_tokens), heads, kv_heads)) return few_bytes(n_requests, padded_dim(head_dim));
+    return many_layout(n_requests, n_tokens, heads, kv_heads, padded_dim(head_dim)).end;
 }
 
 hipError_t kv_attention(const KvCache& c, const KvAttention& a, void* workspace, hipStream_t stream)
 {
-    const bool narrow = c.head_dim <= 64;
-    if ((int64_t)a.max_new * (a.heads / c.kv_heads) > kFewRows) {
-        const hipError_t e = narrow ? launch_many<64>(c, a, (char*)workspace, stream) : launch_many<128>(c, a, (char*)workspace, stream);
-        if (e != hipSuccess) return e;
+    switch (padded_dim(c.head_dim)) {
+    case 32: return launch<32>(c, a, (char*)workspace, stream);
+    case 64: return launch<64>(c, a, (char*)workspace, stream);
+    case 96: return launch<96>(c, a, (char*)workspace, stream);
+    default: return launch<128>(c, a, (char*)workspace, stream);
     }
-    return narrow ? launch_few<64>(c, a, (char*)workspace, stream) : launch_few<128>(c, a, (char*)workspace, stream);
 }
 
 }  // namespace k
