@@ -91,47 +91,87 @@ template <int D> __device__ __forceinline__ uint32_t v_slot(int r, int c)
     return (uint32_t)(r * DH * 2 + ((c ^ f) & (DH / 8 - 1)) * 16);
 }
 
-// acc += V^T P^T for 16 keys of a tile.  at: this lane's addresses of the transposing reads of keys 0..7 and 8..15, per 32 channels.
-// careful: a key may be hidden from some rows, and 0 * inf would reach them through the matrix core: values that are not finite are
-// then taken out of the operand and added one by one to the rows that see them (`sees(key of the 16)` says for this lane's row).
-template <int D, class Sees>
-__device__ __forceinline__ void add_values(f32x16 (&acc)[D / 32], const char* const (&at)[D / 32][2], int offset, bf16x8 pf, bool careful, Sees sees)
-{
 #if defined(__HIP_DEVICE_COMPILE__)
-    const int lane = threadIdx.x & 63, half = lane >> 5;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at[db][0] + offset));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at[db][1] + offset));
-        u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        if (careful) {
-            uint32_t odd = 0;                 // bit e: element e is inf or NaN
-#pragma unroll
-            for (int e = 0; e < 8; ++e) odd |= ((w[e >> 1] >> (16 * (e & 1))) & 0x7F80u) == 0x7F80u ? 1u << e : 0u;
-            const u32x4 all = w;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (odd >> e & 1) w[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-            const u32x4 p = __builtin_bit_cast(u32x4, pf);
-            for (unsigned long long left = __ballot(odd != 0); left; left &= left - 1) {
-                const int src = __builtin_ctzll(left), row = src & 31, kh = src >> 5;
-                const uint32_t which = __builtin_amdgcn_readlane(odd, src);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (!(which >> e & 1)) continue;
-                    const uint32_t bits = __builtin_amdgcn_readlane(all[e >> 1], src), word = __shfl(p[e >> 1], (lane & 31) + 32 * kh, 64);
-                    const float v = __uint_as_float(e & 1 ? bits & 0xFFFF0000u : bits << 16), q = __uint_as_float(e & 1 ? word & 0xFFFF0000u : word << 16);
-                    const bool mine = half == ((row >> 2) & 1) && sees(8 * (e >> 2) + 4 * kh + (e & 3));
-#pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        if (x == 4 * (row >> 3) + (row & 3) && mine) acc[db][x] += q * v;
-                }
-            }
-        }
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, acc[db], 0, 0, 0);
-    }
-#endif
+// The addresses of a V tile's reads differ from one lane's base by bits that the order of the chunks flips: 32 channels further, and eight
+// rows further.  The tile begins at a multiple of 4 KiB.
+template <int D> __device__ __forceinline__ uint32_t value_base(int lane)
+{
+    return v_slot<D>(4 * (lane >> 5) + ((lane >> 2) & 3), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
 }
+// V^T of 16 keys for channels 32 db .. : `base` is the LDS address of the tile's 32 (or 16) rows + value_base
+template <int D> __device__ __forceinline__ u32x4 values(uint32_t base, int db, int t2)
+{
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((base ^ (db * 64)) + t2 * 32 * kRow<D>));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((base ^ (db * 64 + 32 + 16 * kRow<D>)) + t2 * 32 * kRow<D>));
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// V^T of 16 keys, all channels
+template <int D> __device__ __forceinline__ void read_values(u32x4 (&v)[D / 32], uint32_t base, int t2)
+{
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) v[db] = values<D>(base, db, t2);
+}
+// acc += V^T P^T for 16 keys
+template <int D> __device__ __forceinline__ void add_values(f32x16 (&acc)[D / 32], const u32x4 (&v)[D / 32], u32x4 p)
+{
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[db]), __builtin_bit_cast(bf16x8, p), acc[db], 0, 0, 0);
+}
+// Where a key may be hidden from some rows, 0 * inf would reach them through the matrix core.  Which of the 32 keys of a tile at LDS
+// address `tile` have a value that is not finite:
+template <int D> __device__ __forceinline__ uint32_t odd_keys(uint32_t tile)
+{
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));            // rarely needed: its addresses are not worth registers outside
+    uint32_t odd = 0;
+#pragma unroll
+    for (int ch = 0; ch < D / 16; ++ch) {
+        const u32x4 w = *(const __attribute__((address_space(3))) u32x4*)(tile + v_slot<D>(lane & 31, 2 * ch + (lane >> 5)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= ((w[e] & 0x7F80u) == 0x7F80u) | ((w[e] & 0x7F800000u) == 0x7F800000u);
+    }
+    const unsigned long long b = __ballot(odd);
+    return (uint32_t)b | (uint32_t)(b >> 32);
+}
+// Their rows are added to the query rows that see them (`sees(key)` says for this lane's row) by themselves,
+template <int D, class Sees>
+__device__ __forceinline__ void add_odd_values(f32x16 (&acc)[D / 32], uint32_t tile, uint32_t odd, const u32x4 (&p)[2], Sees sees)
+{
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int half = lane >> 5;
+#pragma nounroll
+    for (; odd; odd &= odd - 1) {
+        const int key = __builtin_ctz(odd), d = (key >> 3 & 1) * 2 + (key >> 1 & 1);         // dword of p[key / 16] that holds it, in lanes of half key / 4 % 2
+        const uint32_t lo = d == 0 ? p[0][0] : d == 1 ? p[0][1] : d == 2 ? p[0][2] : p[0][3], hi = d == 0 ? p[1][0] : d == 1 ? p[1][1] : d == 2 ? p[1][2] : p[1][3];
+        const uint32_t word = __shfl(key < 16 ? lo : hi, (lane & 31) + 32 * (key >> 2 & 1), 64);
+        const float q = __uint_as_float(key & 1 ? word & 0xFFFF0000u : word << 16);
+        const bool mine = sees(key);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {     // four channels of this lane's
+                const uint2 w = *(const __attribute__((address_space(3))) uint2*)(tile + v_slot<D>(key, 4 * db + g) + 8 * half);
+                const float v[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u)};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[db][4 * g + e] = mine ? acc[db][4 * g + e] + q * v[e] : acc[db][4 * g + e];
+            }
+    }
+}
+// and taken out of the operands: what is left of 16 keys' pairs of values (dwords)
+__device__ __forceinline__ u32x4 even_only(uint32_t odd, int t2, int half)
+{
+    u32x4 keep;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const uint32_t at = odd >> (16 * t2 + 8 * (e >> 2) + 4 * half + (e & 3));
+        keep[e >> 1] = (at & 1 ? 0u : 0x0000FFFFu) | (at & 2 ? 0u : 0xFFFF0000u);
+    }
+    return keep;
+}
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
+#endif
 
 // ---- few query rows (single tokens): at most 32 per request and cache head ------------------------------------------------
 // The work is the list of all 32-key tiles, (request, cache head, tile) in that order; every workgroup takes an equal stretch of
@@ -157,7 +197,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int kSteps = D / 16, kBlocks = D / 32;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    extern __shared__ __attribute__((aligned(4096))) char lds[];
     __shared__ float stat[2][kFewWaves][kFewRows];
     __shared__ unsigned long long part_sum[kFewWaves];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
@@ -212,12 +252,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
     const int chunks = c.head_dim >> 3, last_step = (chunks - 1 - half) >> 1;       // this lane's last 16 bytes of a row; -1: none (8 channels)
     const float scale2 = a.scale * 1.44269504088896340736f;
     char* const v_lds = lds + wid * (kKeys * kRow<D> * 2);
-    const char* v_at[kBlocks][2];
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            v_at[db][i] = v_lds + v_slot<D>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+    const uint32_t v_tile = lds_address(v_lds), v_read = v_tile + value_base<D>(lane);
     const unsigned long long start = now;
 
     while (now < stop && r < n) {
@@ -334,16 +369,22 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
                 sc[x] = exp2_fast(sc[x] - m_use);
                 l += sc[x];
             }
-            const bool careful = masked && s.m > 1;
+            u32x4 pw[2];
+#pragma unroll
+            for (int x = 0; x < 16; x += 2) pw[x >> 3][(x >> 1) & 3] = pack_bf16(sc[x], sc[x + 1]);
+            if (masked && s.m > 1) {
+                const uint32_t odd = odd_keys<D>(v_tile);
+                if (odd) {                    // the tile is this wavefront's own: their rows are made zeros
+                    add_odd_values<D>(o, v_tile, odd, pw, [&](int j) { return row_ok && key0 + j <= pos && key0 + j > from; });
+                    if (odd >> l32 & 1)
+                        for (int ch = half; ch < kRow<D> / 8; ch += 2) *(__attribute__((address_space(3))) u32x4*)(v_tile + v_slot<D>(l32, ch)) = u32x4{0, 0, 0, 0};
+                }
+            }
 #pragma unroll
             for (int t2 = 0; t2 < 2; ++t2) {
-                u32x4 pw;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16(sc[8 * t2 + 2 * e], sc[8 * t2 + 2 * e + 1]);
-                add_values<D>(o, v_at, t2 * 16 * kRow<D> * 2, __builtin_bit_cast(bf16x8, pw), careful, [&](int j) {
-                    const int key = key0 + 16 * t2 + j;
-                    return row_ok && key <= pos && key > from;
-                });
+                u32x4 v[kBlocks];
+                read_values<D>(v, v_read, t2);
+                add_values<D>(o, v, pw[t2]);
             }
         }
         l = sum_halves(l);
@@ -634,7 +675,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int DH = kRow<D>, kSteps = D / 16, kBlocks = D / 32, kTile = kManyTile<D>;
     constexpr int kRowsPerLoad = 1024 / (DH * 2), kLoads = kManyKeys / kRowsPerLoad / kManyWaves;     // of K, and the same of V
-    extern __shared__ __attribute__((aligned(1024))) char lds[];          // two buffers of a K and a V tile
+    extern __shared__ __attribute__((aligned(4096))) char lds[];          // two buffers of K tiles, three of V
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     const int kvh = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
     if (index >= ((const ManyHeader*)(workspace + layout.header))->units) return;
@@ -665,7 +706,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             qf[ks] = __builtin_bit_cast(bf16x8, w);
         }
     }
-    const float scale2 = fabsf(a.scale) * 1.44269504088896340736f;
+    const float scale2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.4e-45f);          // a mask of -inf stays one with a scale of 0
 
     // Lane i of a load fills slot i % (DH / 8) of row i / (DH / 8) of its rows, and fetches the chunk that belongs there.
     const int ld_row = lane / (DH / 8), ld_slot = lane % (DH / 8);
@@ -673,80 +714,82 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     constant_int* const ids = (constant_int*)(uint64_t)(a.table + (size_t)r * a.max_blocks);
     const uint64_t head_bytes = (uint64_t)kvh * (uint64_t)c.head_stride * 2u;
     const int block_mask = (1 << c.block_shift) - 1;
-    auto load_tile = [&](int tile, int buf) __attribute__((always_inline)) {
+    uint32_t lane_at[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+        const int chunk = (int)(v_slot<D>((wid * kLoads + j) * kRowsPerLoad + ld_row, ld_slot) / 16) & (DH / 8 - 1);        // the order is its own inverse
+        lane_at[j] = chunk < chunks ? (uint32_t)ld_row * row_bytes + (uint32_t)chunk * 16u : kOutOfRange;
+    }
+    // block ids of this wavefront's rows of a tile, on their way before the tile's turn
+    int id[kLoads];
+    auto fetch_ids = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            id[j] = ids[max(0, min((tile0 + t) * kManyKeys + (wid * kLoads + j) * kRowsPerLoad, s.end - 1)) >> c.block_shift];
+    };
+    // K of tile t goes to buffer t % 2, V to buffer t % 3: while tile t is worked on, K and V of t + 1 are there or on their way
+    auto load = [&](int t) __attribute__((always_inline)) {
+        char *const k_to = lds + t % 2 * kTile, *const v_to = lds + (2 + t % 3) * kTile;
+        const int key0 = (tile0 + t) * kManyKeys;
+        const bool inside = key0 >= s.begin && key0 + kManyKeys <= s.end;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int in_tile = (wid * kLoads + j) * kRowsPerLoad, key = __builtin_amdgcn_readfirstlane(tile * kManyKeys + in_tile);
-            const int chunk = (int)(v_slot<D>(in_tile + ld_row, ld_slot) / 16) & (DH / 8 - 1);       // the order is its own inverse
-            const bool ok = chunk < chunks && key + ld_row < s.end && key + ld_row >= s.begin;
-            const uint32_t at = ok ? (uint32_t)ld_row * row_bytes + (uint32_t)chunk * 16u : kOutOfRange;
-            const int id = key < s.end ? ids[key >> c.block_shift] : -1;
-            const bool known = (uint32_t)id < (uint32_t)c.n_blocks;
-            const uint64_t block = (uint64_t)(known ? id : 0) * (uint64_t)c.block_stride * 2u + head_bytes + (uint64_t)(key & block_mask) * row_bytes;
-            const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.k + block, 0, known ? 0x7FFFFFFF : 0, 0x00020000);
-            const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.v + block, 0, known ? 0x7FFFFFFF : 0, 0x00020000);
-            char* const to = lds + buf * (2 * kTile) + in_tile * (DH * 2);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)to, 16, at, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(to + kTile), 16, at, 0, 0, 0);
+            const int in_tile = (wid * kLoads + j) * kRowsPerLoad, key = key0 + in_tile;
+            uint32_t at = lane_at[j];
+            if (!inside) at = (key + ld_row < s.end) & (key + ld_row >= s.begin) ? at : kOutOfRange;
+            const bool known = (uint32_t)id[j] < (uint32_t)c.n_blocks;
+            const uint64_t block = (uint64_t)(known ? id[j] : 0) * (uint64_t)c.block_stride * 2u + head_bytes + (uint64_t)(key & block_mask) * row_bytes;
+            const int size = known ? 0x7FFFFFFF : 0;
+            const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.k + block, 0, size, 0x00020000);
+            const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.v + block, 0, size, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)(k_to + in_tile * (DH * 2)), 16, at, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(v_to + in_tile * (DH * 2)), 16, at, 0, 0, 0);
         }
     };
-    // operand addresses inside a buffer
-    uint32_t k_at[kSteps], v_at[kBlocks][2];
-#pragma unroll
-    for (int ks = 0; ks < kSteps; ++ks) k_at[ks] = v_slot<D>(l32, 2 * ks + half);
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            v_at[db][i] = kTile + v_slot<D>(8 * i + 4 * half + ((lane >> 2) & 3), db * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+    // operand addresses inside a tile; 16 channels further is a bit of the chunks' order
+    const uint32_t lds0 = lds_address(lds), k_base = v_slot<D>(l32, half), v_base = value_base<D>(lane);
 
     float m = -INFINITY, l = 0.f;
-    f32x16 o[kBlocks];
+    f32x16 o[kBlocks], sc, next;
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
         for (int x = 0; x < 16; ++x) o[db][x] = 0.f;
 
-    int buf = 0;
-    if (tiles > 0) load_tile(tile0, 0);
-    for (int t = 0; t < tiles; ++t, buf ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));              // this tile's loads have landed, the last one's reads are done
-        __builtin_amdgcn_s_barrier();
-        if (t + 1 < tiles) load_tile(tile0 + t + 1, buf ^ 1);
-        const int key0 = (tile0 + t) * kManyKeys;
-        if (!works || key0 > high || (a.window > 0 && key0 + kManyKeys - 1 <= low - a.window)) continue;      // nothing here for these rows
-        const char* const kv = lds + buf * (2 * kTile);
-        f32x16 sc[2];
+    // Half a tile at a time: scores of the next half (matrix cores) are computed beside the exponentials of this one (vector unit), and the
+    // next half's maximum beside this one's values.
+    auto read_keys = [&](u32x4 (&k)[kSteps], int t, int kb) __attribute__((always_inline)) {
+        const uint32_t kt = lds0 + t % 2 * kTile + kb * 32 * DH * 2 + k_base;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int ks = 0; ks < kSteps; ++ks) k[ks] = *(const __attribute__((address_space(3))) u32x4*)(kt ^ (ks * 32));
+    };
+    auto scores = [&](f32x16& to, const u32x4 (&k)[kSteps]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int x = 0; x < 16; ++x) sc[kb][x] = 0.f;
+        for (int x = 0; x < 16; ++x) to[x] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) {
-                const bf16x8 kf = *(const bf16x8*)(kv + k_at[ks] + kb * 32 * DH * 2);
-                sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sc[kb], 0, 0, 0);
-            }
+        for (int ks = 0; ks < kSteps; ++ks) to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[ks]), qf[ks], to, 0, 0, 0);
+    };
+    auto is_masked = [&](int t, int kb) {
+        const int key0 = (tile0 + t) * kManyKeys + kb * 32;
+        return key0 + 31 > low || (a.window > 0 && key0 <= high - a.window);
+    };
+    auto mask = [&](f32x16& v, int t, int kb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const int key = (tile0 + t) * kManyKeys + kb * 32 + 8 * (x >> 2) + 4 * half + (x & 3);
+            if (!(row_ok && key <= pos && key > from)) v[x] = -INFINITY;
         }
-        const bool masked = key0 + kManyKeys - 1 > low || (a.window > 0 && key0 <= high - a.window);
-        if (masked) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const int key = key0 + kb * 32 + 8 * (x >> 2) + 4 * half + (x & 3);
-                    if (!(row_ok && key <= pos && key > from)) sc[kb][x] = -INFINITY;
-                }
-        }
+    };
+    auto highest = [&](const f32x16& v) __attribute__((always_inline)) {
         float top = -INFINITY;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[kb][x]);
+        for (int x = 0; x < 16; ++x) top = fmaxf(top, v[x]);
         top = max_halves(top);
-        // scale2 >= 0 keeps the order; 0 times -inf would not be a mask any more
-        top = top == -INFINITY ? top : top * scale2;
-        // The reference moves only when a score exceeds it by 2^8: exponentials up to 2^8 are as exact as up to 1, and moving it costs a
-        // multiplication of the whole output.
+        return top == -INFINITY ? top : top * scale2;         // scale2 >= 0 keeps the order; 0 times -inf would not be a mask any more
+    };
+    // The reference moves only when a score exceeds it by 2^8: exponentials up to 2^8 are as exact as up to 1, and moving it costs a
+    // multiplication of the whole output.
+    auto raise = [&](float top) __attribute__((always_inline)) {
         if (__any(top > m + 8.f)) {
             const float m_new = fmaxf(m, top), shrink = m_new == m ? 1.f : exp2_fast(m - m_new);
             l *= shrink;
@@ -756,33 +799,72 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
                 for (int x = 0; x < 16; ++x) o[db][x] *= shrink;
             m = m_new;
         }
+    };
+    // the half (t, kb), whose scores are in `cur`; the next half's, (tn, kn), go to `to` (of no use behind the last one, and not used)
+    auto half_step = [&](f32x16& cur, f32x16& to, int t, int kb, int tn, int kn, bool more) __attribute__((always_inline)) {
+        const bool masked = is_masked(t, kb);
         const float m_use = m == -INFINITY ? 0.f : m;
+        // Reads run ahead of their use by a phase: keys come while the exponentials are taken, values while scores are multiplied.
+        const uint32_t vt = lds0 + (2 + t % 3) * kTile + kb * 32 * DH * 2;
+        u32x4 k[kSteps], v0[kBlocks], v1[kBlocks], pw[2];
+        read_keys(k, tn, kn);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int x = 0; x < 16; x += 2) {
+            const float p0 = exp2_fast(__builtin_fmaf(cur[x], scale2, -m_use)), p1 = exp2_fast(__builtin_fmaf(cur[x + 1], scale2, -m_use));
+            l += p0 + p1;
+            pw[x >> 3][(x >> 1) & 3] = pack_bf16(p0, p1);
+        }
+        read_values<D>(v0, vt + v_base, 0);
+        asm volatile("" : "+v"(pw[0]), "+v"(pw[1]), "+v"(l));             // here, and not where they are used
+        __builtin_amdgcn_sched_barrier(0);
+        scores(to, k);
+        read_values<D>(v1, vt + v_base, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (masked) {
+            const uint32_t odd = odd_keys<D>(vt);
+            if (odd) {
+                const int key0 = (tile0 + t) * kManyKeys + kb * 32;
+                add_odd_values<D>(o, vt, odd, pw, [&](int j) { return row_ok && key0 + j <= pos && key0 + j > from; });
+                const u32x4 keep0 = even_only(odd, 0, half), keep1 = even_only(odd, 1, half);
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                float p = exp2_fast(__builtin_fmaf(sc[kb][x], scale2, -m_use));
-                if (masked && sc[kb][x] == -INFINITY) p = 0.f;            // scale2 = 0
-                sc[kb][x] = p;
-                l += p;
+                for (int db = 0; db < kBlocks; ++db) {
+                    v0[db] &= keep0;
+                    v1[db] &= keep1;
+                }
             }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int t2 = 0; t2 < 2; ++t2) {
-                u32x4 pw;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pw[e] = pack_bf16(sc[kb][8 * t2 + 2 * e], sc[kb][8 * t2 + 2 * e + 1]);
-                const char* at[kBlocks][2];
-#pragma unroll
-                for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) at[db][i] = kv + v_at[db][i];
-                add_values<D>(o, at, (kb * 32 + t2 * 16) * DH * 2, __builtin_bit_cast(bf16x8, pw), masked, [&](int j) {
-                    const int key = key0 + kb * 32 + t2 * 16 + j;
-                    return row_ok && key <= pos && key > from;
-                });
-            }
+        }
+        add_values<D>(o, v0, pw[0]);
+        add_values<D>(o, v1, pw[1]);
+        if (is_masked(tn, kn)) mask(to, tn, kn);
+        const float top = highest(to);
+        raise(more ? top : -INFINITY);
+    };
+
+    if (tiles > 0) {
+        fetch_ids(0);
+        load(0);
+        fetch_ids(1);
+        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
+        __builtin_amdgcn_s_barrier();
+        if (tiles > 1) load(1);
+        fetch_ids(2);
+        if (works) {
+            u32x4 k[kSteps];
+            read_keys(k, 0, 0);
+            scores(sc, k);
+            if (is_masked(0, 0)) mask(sc, 0, 0);
+            raise(highest(sc));
+        }
+    }
+    for (int t = 0; t < tiles; ++t) {
+        if (works) half_step(sc, next, t, 0, t, 1, true);
+        // the next tile has landed, and everybody is through with this one's K and the last one's V
+        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
+        __builtin_amdgcn_s_barrier();
+        if (t + 2 < tiles) load(t + 2);
+        fetch_ids(t + 3);
+        if (works) half_step(next, sc, t, 1, t + 1, 0, t + 1 < tiles);
     }
     l = sum_halves(l);
     if (!row_ok) return;
@@ -873,7 +955,7 @@ template <int D, bool PAD> hipError_t launch_few(const KvCache& c, const KvAtten
 
 template <int D> hipError_t launch_many(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
 {
-    constexpr int kLds = 4 * kManyTile<D>;
+    constexpr int kLds = 5 * kManyTile<D>;
     static const hipError_t configured[2] = {
         hipFuncSetAttribute((const void*)kv_attention_many_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds),
         hipFuncSetAttribute((const void*)kv_attention_schedule_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (kPlanMaxRequests + 1) * 4)};
