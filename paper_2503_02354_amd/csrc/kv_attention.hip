@@ -714,40 +714,58 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     constant_int* const ids = (constant_int*)(uint64_t)(a.table + (size_t)r * a.max_blocks);
     const uint64_t head_bytes = (uint64_t)kvh * (uint64_t)c.head_stride * 2u;
     const int block_mask = (1 << c.block_shift) - 1;
-    uint32_t lane_at[kLoads];
+    uint32_t lane_at[kLoads];                 // offset from this wavefront's first row of a tile, all of them in one block
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
         const int chunk = (int)(v_slot<D>((wid * kLoads + j) * kRowsPerLoad + ld_row, ld_slot) / 16) & (DH / 8 - 1);        // the order is its own inverse
-        lane_at[j] = chunk < chunks ? (uint32_t)ld_row * row_bytes + (uint32_t)chunk * 16u : kOutOfRange;
+        lane_at[j] = chunk < chunks ? (uint32_t)(j * kRowsPerLoad + ld_row) * row_bytes + (uint32_t)chunk * 16u : kOutOfRange;
     }
-    // block ids of this wavefront's rows of a tile, on their way before the tile's turn
-    int id[kLoads];
-    auto fetch_ids = [&](int t) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-            id[j] = ids[max(0, min((tile0 + t) * kManyKeys + (wid * kLoads + j) * kRowsPerLoad, s.end - 1)) >> c.block_shift];
+    const int wave_row = wid * kLoads * kRowsPerLoad;
+    auto id_at = [&](int key) { return ids[max(0, min(key, s.end - 1)) >> c.block_shift]; };
+    auto block_of = [&](int id, int key) {    // byte offset of a row in the cache
+        return (uint64_t)id * (uint64_t)c.block_stride * 2u + head_bytes + (uint64_t)(key & block_mask) * row_bytes;
     };
-    // K of tile t goes to buffer t % 2, V to buffer t % 3: while tile t is worked on, K and V of t + 1 are there or on their way
+    // K of tile t goes to buffer t % 2, V to buffer t % 3: while tile t is worked on, K and V of t + 1 are there or on their way.  The block id
+    // of this wavefront's sixteen rows is on its way before the tile's turn.
+    int next_id = 0;
+    auto fetch_id = [&](int t) __attribute__((always_inline)) { next_id = id_at((tile0 + t) * kManyKeys + wave_row); };
     auto load = [&](int t) __attribute__((always_inline)) {
-        char *const k_to = lds + t % 2 * kTile, *const v_to = lds + (2 + t % 3) * kTile;
-        const int key0 = (tile0 + t) * kManyKeys;
-        const bool inside = key0 >= s.begin && key0 + kManyKeys <= s.end;
+        char *const k_to = lds + t % 2 * kTile + wave_row * (DH * 2), *const v_to = lds + (2 + t % 3) * kTile + wave_row * (DH * 2);
+        const int key0 = (tile0 + t) * kManyKeys, first = key0 + wave_row;
+        if (key0 >= s.begin && key0 + kManyKeys <= s.end && block_mask >= 15 && (uint32_t)next_id < (uint32_t)c.n_blocks) {
+            const uint64_t block = block_of(next_id, first);
+            const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.k + block, 0, 0x7FFFFFFF, 0x00020000);
+            const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.v + block, 0, 0x7FFFFFFF, 0x00020000);
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)(k_to + j * 1024), 16, lane_at[j], 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(v_to + j * 1024), 16, lane_at[j], 0, 0, 0);
+            }
+            return;
+        }
+        // the history's first or last tile, blocks of eight rows, blocks outside the cache
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int in_tile = (wid * kLoads + j) * kRowsPerLoad, key = key0 + in_tile;
-            uint32_t at = lane_at[j];
-            if (!inside) at = (key + ld_row < s.end) & (key + ld_row >= s.begin) ? at : kOutOfRange;
-            const bool known = (uint32_t)id[j] < (uint32_t)c.n_blocks;
-            const uint64_t block = (uint64_t)(known ? id[j] : 0) * (uint64_t)c.block_stride * 2u + head_bytes + (uint64_t)(key & block_mask) * row_bytes;
+            const int key = first + j * kRowsPerLoad, id = id_at(key);
+            const bool known = (uint32_t)id < (uint32_t)c.n_blocks, inside = (key + ld_row < s.end) & (key + ld_row >= s.begin);
+            const uint32_t at = inside & (lane_at[j] != kOutOfRange) ? lane_at[j] - (uint32_t)(j * kRowsPerLoad) * row_bytes : kOutOfRange;
+            const uint64_t block = block_of(known ? id : 0, key);
             const int size = known ? 0x7FFFFFFF : 0;
             const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.k + block, 0, size, 0x00020000);
             const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.v + block, 0, size, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)(k_to + in_tile * (DH * 2)), 16, at, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(v_to + in_tile * (DH * 2)), 16, at, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)(k_to + j * 1024), 16, at, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(v_to + j * 1024), 16, at, 0, 0, 0);
         }
     };
     // operand addresses inside a tile; 16 channels further is a bit of the chunks' order
     const uint32_t lds0 = lds_address(lds), k_base = v_slot<D>(l32, half), v_base = value_base<D>(lane);
+    uint32_t k_read[kSteps], v_read[kBlocks][2];                          // of the tile that is read next
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks) k_read[ks] = lds0 + (k_base ^ (ks * 32));
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v_read[db][i] = lds0 + 2 * kTile + (v_base ^ (db * 64 + i * (32 + 16 * DH)));
 
     float m = -INFINITY, l = 0.f;
     f32x16 o[kBlocks], sc, next;
@@ -758,10 +776,17 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 
     // Half a tile at a time: scores of the next half (matrix cores) are computed beside the exponentials of this one (vector unit), and the
     // next half's maximum beside this one's values.
-    auto read_keys = [&](u32x4 (&k)[kSteps], int t, int kb) __attribute__((always_inline)) {
-        const uint32_t kt = lds0 + t % 2 * kTile + kb * 32 * DH * 2 + k_base;
+    auto read_keys = [&](u32x4 (&k)[kSteps], int kb) __attribute__((always_inline)) {
 #pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) k[ks] = *(const __attribute__((address_space(3))) u32x4*)(kt ^ (ks * 32));
+        for (int ks = 0; ks < kSteps; ++ks) k[ks] = *(const __attribute__((address_space(3))) u32x4*)(k_read[ks] + kb * 32 * DH * 2);
+    };
+    auto read_half = [&](u32x4 (&v)[kBlocks], int kb, int t2) __attribute__((always_inline)) {
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db) {
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v_read[db][0] + (kb * 32 + t2 * 16) * DH * 2));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v_read[db][1] + (kb * 32 + t2 * 16) * DH * 2));
+            v[db] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
     };
     auto scores = [&](f32x16& to, const u32x4 (&k)[kSteps]) __attribute__((always_inline)) {
 #pragma unroll
@@ -805,9 +830,13 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
         const bool masked = is_masked(t, kb);
         const float m_use = m == -INFINITY ? 0.f : m;
         // Reads run ahead of their use by a phase: keys come while the exponentials are taken, values while scores are multiplied.
-        const uint32_t vt = lds0 + (2 + t % 3) * kTile + kb * 32 * DH * 2;
         u32x4 k[kSteps], v0[kBlocks], v1[kBlocks], pw[2];
-        read_keys(k, tn, kn);
+        read_keys(k, kn);
+        if (kn == 1) {
+            const uint32_t on = t % 2 ? -kTile : kTile;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) k_read[ks] += on;
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int x = 0; x < 16; x += 2) {
@@ -815,14 +844,20 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             l += p0 + p1;
             pw[x >> 3][(x >> 1) & 3] = pack_bf16(p0, p1);
         }
-        read_values<D>(v0, vt + v_base, 0);
+        read_half(v0, kb, 0);
         asm volatile("" : "+v"(pw[0]), "+v"(pw[1]), "+v"(l));             // here, and not where they are used
         __builtin_amdgcn_sched_barrier(0);
         scores(to, k);
-        read_values<D>(v1, vt + v_base, 1);
+        read_half(v1, kb, 1);
+        if (kb == 1) {
+            const uint32_t on = t % 3 == 2 ? -2 * kTile : kTile;
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db) v_read[db][0] += on, v_read[db][1] += on;
+        }
         __builtin_amdgcn_sched_barrier(0);
+        if (kb == 1 && t + 2 < tiles) load(t + 2);        // behind the values' reads: those wait for every load that is on its way
         if (masked) {
-            const uint32_t odd = odd_keys<D>(vt);
+            const uint32_t vt = lds0 + (2 + t % 3) * kTile + kb * 32 * DH * 2, odd = odd_keys<D>(vt);
             if (odd) {
                 const int key0 = (tile0 + t) * kManyKeys + kb * 32;
                 add_odd_values<D>(o, vt, odd, pw, [&](int j) { return row_ok && key0 + j <= pos && key0 + j > from; });
@@ -842,16 +877,16 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     };
 
     if (tiles > 0) {
-        fetch_ids(0);
+        fetch_id(0);
         load(0);
-        fetch_ids(1);
+        fetch_id(1);
         __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
         __builtin_amdgcn_s_barrier();
         if (tiles > 1) load(1);
-        fetch_ids(2);
+        fetch_id(2);
         if (works) {
             u32x4 k[kSteps];
-            read_keys(k, 0, 0);
+            read_keys(k, 0);
             scores(sc, k);
             if (is_masked(0, 0)) mask(sc, 0, 0);
             raise(highest(sc));
@@ -862,9 +897,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
         // the next tile has landed, and everybody is through with this one's K and the last one's V
         __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
         __builtin_amdgcn_s_barrier();
-        if (t + 2 < tiles) load(t + 2);
-        fetch_ids(t + 3);
         if (works) half_step(next, sc, t, 1, t + 1, 0, t + 1 < tiles);
+        else if (t + 2 < tiles) load(t + 2);
+        fetch_id(t + 3);
     }
     l = sum_halves(l);
     if (!row_ok) return;
