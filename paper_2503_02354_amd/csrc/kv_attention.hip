@@ -747,8 +747,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int key = first + j * kRowsPerLoad, id = id_at(key);
-            const bool known = (uint32_t)id < (uint32_t)c.n_blocks, inside = (key + ld_row < s.end) & (key + ld_row >= s.begin);
-            const uint32_t at = inside & (lane_at[j] != kOutOfRange) ? lane_at[j] - (uint32_t)(j * kRowsPerLoad) * row_bytes : kOutOfRange;
+            const bool known = (uint32_t)id < (uint32_t)c.n_blocks, inside = key + ld_row < s.end && key + ld_row >= s.begin;
+            const uint32_t at = inside && lane_at[j] != kOutOfRange ? lane_at[j] - (uint32_t)(j * kRowsPerLoad) * row_bytes : kOutOfRange;
             const uint64_t block = block_of(known ? id : 0, key);
             const int size = known ? 0x7FFFFFFF : 0;
             const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.k + block, 0, size, 0x00020000);

@@ -19,20 +19,31 @@ namespace {
 // from the table that some other workgroup writes.
 // What bounds it: latency (lengths in, one scan, slots out).
 constexpr int kPlanThreads = 256;
+constexpr int kPlanInLds = 8192;              // requests whose lengths stay in LDS beside the sums
 constexpr uint32_t kFreed = 0x80000000u;      // the entry counts blocks that a finished request gives back
 constexpr uint32_t kTooLong = 0x40000000u;    // the request would outgrow its row of the table
+
+// place `i` behind `head` in a ring of n entries; head < n
+__device__ __forceinline__ uint32_t in_ring(uint32_t head, uint32_t i, uint32_t n)
+{
+    if (i >= n) i %= n;                       // only where more is given back than there is room for
+    const uint32_t at = head + i;
+    return at >= n ? at - n : at;
+}
 
 // inclusive sums over the workgroup of three values per thread; `part`: [3][kPlanThreads / 64]
 __device__ __forceinline__ void scan3(uint32_t (&v)[3], uint32_t* part)
 {
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
-        for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
             const uint32_t u = __shfl_up(v[i], d, 64);
             if (lane >= d) v[i] += u;
         }
     if (lane == 63)
+#pragma unroll
         for (int i = 0; i < 3; ++i) part[i * (kPlanThreads / 64) + wid] = v[i];
     __syncthreads();
     for (int i = 0; i < 3; ++i)
@@ -49,6 +60,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
     extern __shared__ uint32_t sums[];
     uint32_t* const tok = sums;               // [n + 1] new tokens of a request, then the sum over those before it
     uint32_t* const blk = sums + n + 1;       // [n] blocks taken (or kFreed | given back), then the sum over those before it
+    uint32_t* const len = sums + 2 * n + 1;   // [n] cached tokens, where they fit
+    const bool in_lds = n <= kPlanInLds;
     __shared__ uint32_t part[3 * (kPlanThreads / 64)];
     __shared__ int closed;
     const int tid = threadIdx.x;
@@ -61,6 +74,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
         const uint32_t h = min((uint32_t)max(have[r], 0), longest);
         const int32_t a = add[r];
         const uint32_t old_blocks = (h + bs - 1) >> shift;
+        if (in_lds) len[r] = h;
         if (a < 0) {
             tok[r] = 0;
             blk[r] = kFreed | old_blocks;
@@ -114,24 +128,25 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
     __syncthreads();
 
     if (blockIdx.x == 0 && tid == 0) {
-        next_state[0] = (int32_t)(((unsigned long long)head + taken_open) % (uint32_t)n_blocks);
+        next_state[0] = (int32_t)in_ring(head, taken_open, (uint32_t)n_blocks);
         next_state[1] = (int32_t)(count - taken_open + freed_total);
         next_state[2] = f;
         next_state[3] = (int32_t)tokens;
         q_off[n] = (int32_t)tokens;
     }
+    auto cached = [&](int r) { return in_lds ? len[r] : min((uint32_t)max(have[r], 0), longest); };
     const int wave = (blockIdx.x * kPlanThreads + tid) >> 6, waves = gridDim.x * (kPlanThreads / 64), lane = tid & 63;
     for (int r = blockIdx.x * kPlanThreads + tid; r < n; r += gridDim.x * kPlanThreads) {
-        const uint32_t h = min((uint32_t)max(have[r], 0), longest);
-        const int32_t a = add[r];
-        seq_len[r] = a < 0 ? 0 : (int32_t)(r < f ? h + (uint32_t)a : h);
+        // sums from f on may have wrapped into the flag: ask again
+        const bool freed = r < f ? (blk[r] & kFreed) != 0 : add[r] < 0;
+        seq_len[r] = freed ? 0 : (int32_t)(cached(r) + (r < f ? tok[r + 1] - tok[r] : 0u));
         q_off[r] = (int32_t)(r < f ? tok[r] : tokens);
     }
     for (int r = wave; r < n; r += waves) {   // blocks of finished requests to the ring's end
-        if (add[r] >= 0) continue;
-        const uint32_t h = min((uint32_t)max(have[r], 0), longest), blocks = (h + bs - 1) >> shift;
-        const unsigned long long to = (unsigned long long)head + count + (blk[r] & ~kFreed);
-        for (uint32_t j = lane; j < blocks; j += 64) ring[(to + j) % (uint32_t)n_blocks] = table[(size_t)r * max_blocks + j];
+        if (!(blk[r] & kFreed) || add[r] >= 0) continue;
+        const uint32_t blocks = (cached(r) + bs - 1) >> shift;
+        const uint32_t to = count + (blk[r] & ~kFreed);
+        for (uint32_t j = lane; j < blocks; j += 64) ring[in_ring(head, to + j, (uint32_t)n_blocks)] = table[(size_t)r * max_blocks + j];
     }
     for (int t = blockIdx.x * kPlanThreads + tid; t < token_cap; t += gridDim.x * kPlanThreads) {
         if ((uint32_t)t >= tokens) {
@@ -145,13 +160,13 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
             if (tok[mid] <= (uint32_t)t) lo = mid;
             else hi = mid;
         }
-        const uint32_t h = min((uint32_t)max(have[lo], 0), longest), old_blocks = (h + bs - 1) >> shift;
+        const uint32_t h = cached(lo), old_blocks = (h + bs - 1) >> shift;
         const uint32_t pos = h + (uint32_t)t - tok[lo], page = pos >> shift;
         int32_t* const row = table + (size_t)lo * max_blocks;
         int32_t id;
         if (page < old_blocks) id = row[page];
         else {
-            id = ring[((unsigned long long)head + blk[lo] + (page - old_blocks)) % (uint32_t)n_blocks];
+            id = ring[in_ring(head, blk[lo] + (page - old_blocks), (uint32_t)n_blocks)];
             if ((pos & (bs - 1)) == 0) row[page] = id;        // a new block's first token
         }
         slot[t] = (int32_t)(((uint32_t)id << shift) + (pos & (bs - 1)));
@@ -188,7 +203,7 @@ hipError_t kv_plan(int32_t n, int32_t block_shift, int32_t n_blocks, int32_t max
                    const int32_t* add, int32_t* ring, const int32_t* ring_state, int32_t* table, int32_t* seq_len, int32_t* q_off,
                    int32_t* slot, int32_t* position, int32_t* next_state, hipStream_t stream)
 {
-    const size_t lds = (2 * (size_t)n + 1) * 4;
+    const size_t lds = ((n <= kPlanInLds ? 3 : 2) * (size_t)n + 1) * 4;
     static const hipError_t configured = hipFuncSetAttribute((const void*)kv_plan_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                              (int)((2 * (size_t)kPlanMaxRequests + 1) * 4));
     if (configured != hipSuccess) return configured;
