@@ -56,40 +56,58 @@ constexpr uint32_t kNone = 0xFFFFFFFFu;
 __device__ __forceinline__ bool better_than(float score, uint32_t index, Best a) { return (score > a.score) | ((score == a.score) & (index < a.index)); }
 __device__ __forceinline__ Best better(Best a, Best b) { return better_than(b.score, b.index, a) ? b : a; }
 
-// A row and the workgroup's shared memory; every method is called by all threads.
-constexpr int kMostCandidates = 3072, kMostTopK = 1536;
+constexpr int kMostCandidates = 4096, kMostTopK = 1536, kBins = 512, kPairs = 640;       // the list is sorted in powers of two
 template <int THREADS> struct Shared {
     static constexpr int kWaves = THREADS / 64;
-    Best best[kWaves];
-    float sums[kWaves];
-    float sum_pair[kWaves];
-    uint32_t hist[256];
-    uint32_t pick[2];
+    // a wavefront's part of a reduction; two sets in turn, so that one barrier is enough
+    Best best[2][kWaves];
+    float4 sums[2][kWaves];
+    uint32_t hist[kBins];
+    uint32_t pick;
     uint32_t n_candidates;
     alignas(16) unsigned long long candidate[kMostCandidates + 4];
-    float weight[kMostTopK];
+    float weight[kMostTopK], score[kMostTopK];
     uint32_t index[kMostTopK];
 };
 
-template <int THREADS> __device__ __forceinline__ Best block_best(Best v, Shared<THREADS>& sh)
+__device__ __forceinline__ Best wave_best(Best v)
 {
+#pragma unroll
     for (int d = 32; d > 0; d >>= 1) v = better(v, Best{__shfl_xor(v.score, d, 64), (uint32_t)__shfl_xor((int)v.index, d, 64)});
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.best[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = sh.best[0];
-    for (int w = 1; w < Shared<THREADS>::kWaves; ++w) v = better(v, sh.best[w]);
     return v;
 }
-template <int THREADS> __device__ __forceinline__ float block_sum(float v, Shared<THREADS>& sh)
+__device__ __forceinline__ float wave_sum(float v)
 {
+#pragma unroll
     for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.sums[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int w = 0; w < Shared<THREADS>::kWaves; ++w) v += sh.sums[w];
     return v;
+}
+// `set` counts a thread's reductions.
+template <int THREADS> __device__ __forceinline__ Best block_best(Best v, Shared<THREADS>& sh, int& set)
+{
+    Best* const part = sh.best[set++ & 1];
+    v = wave_best(v);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < Shared<THREADS>::kWaves; ++w) v = better(v, part[w]);
+    return v;
+}
+template <int THREADS> __device__ __forceinline__ float2 block_sums(float2 v, Shared<THREADS>& sh, int& set)
+{
+    float4* const part = sh.sums[set++ & 1];
+    v = make_float2(wave_sum(v.x), wave_sum(v.y));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float4(v.x, v.y, 0.f, 0.f);
+    __syncthreads();
+    v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < Shared<THREADS>::kWaves; ++w) v.x += part[w].x, v.y += part[w].y;
+    return v;
+}
+template <int THREADS> __device__ __forceinline__ float block_sum(float v, Shared<THREADS>& sh, int& set)
+{
+    return block_sums(make_float2(v, 0.f), sh, set).x;
 }
 
 // The row in batches, this thread's share: f(x[], n, first index) for n logits as they are (NaN too), W at a time from 16 bytes (in_batch
@@ -164,10 +182,9 @@ struct Scale {
     __device__ __forceinline__ float weight(float x) const { return exp2_fast(rel2(x)); }
 };
 
-// The winner of the race among the tokens of a front: the largest log2(w) - log2 E.
+// This thread's winner of the race among the tokens of a front: the largest log2(w) - log2 E.
 template <int THREADS, typename T>
-__device__ __attribute__((noinline)) Best winner_by_logs(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float least, Scale scale,
-                                                         Shared<THREADS>& sh)
+__device__ __attribute__((noinline)) Best winner_by_logs(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float least, Scale scale)
 {
     Best win{-INFINITY, kNone};
     each<THREADS>(row, vocab, [&](float x, uint32_t i) {
@@ -175,20 +192,20 @@ __device__ __attribute__((noinline)) Best winner_by_logs(const T* row, const flo
         const float z = scale.rel2(x), score = z - log2f(noise[i]);
         if (((z >= least) | (i == top_index)) & (score > -INFINITY)) win = better(win, Best{score, i});
     });
-    return block_best(win, sh);
+    return win;
 }
 
 // The race decided by what the filters say.  It needs no sorted row: its winner among a front that holds all kept tokens is the drawn
 // token if it is kept itself, and whether it is takes one sum over the tokens before it.  If it is not, no token from its place on
-// is kept either, and the race is for the others.  The sums of the four best threads' winners are taken in one pass, since a row
+// is kept either, and the race is for the others.  The sums of the two best threads' winners are taken in one pass, since a row
 // whose winner falls to the nucleus would keep the launch waiting for another two.
 // w / E is compared by cross products; logarithms are taken of every thread's winner only.  Where fp32 may not hold the products
 // (random numbers below 2^-60, a winner below 2^-40, infinite logits), by logarithms after all.
 template <int THREADS, typename T>
 __device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float top_p, float mass, float min_p, Scale scale,
-                         Shared<THREADS>& sh)
+                         Shared<THREADS>& sh, int& set)
 {
-    constexpr int W = Vec<T>::kWidth, kFew = 4;
+    constexpr int W = Vec<T>::kWidth, kFew = 2;
     const float least = min_p > 0.f ? log2f(min_p) : -INFINITY;
     bool by_logs = !(scale.top < INFINITY);
     for (;;) {                                // the front shrinks with every round that goes on
@@ -225,17 +242,17 @@ __device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t t
             });
             by_logs = __syncthreads_or(smallest < 0x1p-60f);
             Best mine{index == kNone ? -INFINITY : log2f(win_w) - log2f(win_q), index};
-            c[0] = block_best(mine, sh);
+            c[0] = block_best(mine, sh, set);
             by_logs |= !(c[0].score > -40.f);
             if (!by_logs && top_p < 1.f && c[0].index != top_index) {
 #pragma unroll
                 for (int j = 1; j < kFew; ++j) {
                     if (mine.index == c[j - 1].index) mine = Best{-INFINITY, kNone};
-                    c[j] = block_best(mine, sh);
+                    c[j] = block_best(mine, sh, set);
                 }
             }
         }
-        if (by_logs) c[0] = winner_by_logs<THREADS>(row, noise, vocab, top_index, front, least, scale, sh);
+        if (by_logs) c[0] = block_best(winner_by_logs<THREADS>(row, noise, vocab, top_index, front, least, scale), sh, set);
         if (c[0].index == kNone) return top_index;
         if (!(top_p < 1.f) || c[0].index == top_index) return c[0].index;
 
@@ -251,11 +268,12 @@ __device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t t
 #pragma unroll
             for (int j = 0; j < kFew; ++j) before[j] += ahead[j].holds(x, i) ? w : 0.f;
         });
+        const float2 masses = block_sums(make_float2(before[0], before[1]), sh, set);
+        before[0] = masses.x, before[1] = masses.y;
         int kept = kFew;
         Front out{-INFINITY, kNone};          // in front of every token that turned out not to be kept
 #pragma unroll
         for (int j = 0; j < kFew; ++j) {
-            before[j] = block_sum(before[j], sh);
             if (kept < kFew || c[j].index == kNone) continue;
             if (c[j].index == top_index || before[j] < top_p * mass) kept = j;
             else if (!ahead[j].holds(out.x, out.end) || out.end == kNone) out = ahead[j];
@@ -265,7 +283,7 @@ __device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t t
             // A thread whose winner is not kept may hide another that is, and that beats the kept one: its share is looked through.
             bool hidden = false;
             const int lead = min(vocab, (int)((-(uintptr_t)row & 15) / sizeof(T))), vecs = (vocab - lead) / W, tail = lead + vecs * W;
-            const Best best = kept == 1 ? c[1] : kept == 2 ? c[2] : c[3];
+            const Best best = c[1];
 #pragma unroll
             for (int j = 0; j < kFew - 1; ++j) {
                 if (j >= kept) continue;
@@ -301,12 +319,12 @@ template <int THREADS, typename T> __device__ Front front_of(const T* row, int v
             int b = 255;
             uint32_t above = 0;
             while (above + sh.hist[b] < left) above += sh.hist[b--];
-            sh.pick[0] = (uint32_t)b;
-            sh.pick[1] = left - above;
+            sh.pick = (uint32_t)b;
+            sh.hist[b] = left - above;
         }
         __syncthreads();
-        last |= (unsigned long long)sh.pick[0] << shift;
-        left = sh.pick[1];
+        last |= (unsigned long long)sh.pick << shift;
+        left = sh.hist[sh.pick];
         __syncthreads();
     }
     return {logit_of((uint32_t)(last >> 32)), ~(uint32_t)last + 1};
@@ -314,48 +332,48 @@ template <int THREADS, typename T> __device__ Front front_of(const T* row, int v
 
 // A small top_k from a short list.  Every thread has met the largest logits of four parts of its share; with at least top_k of all these
 // at or above a bound, so are the first top_k tokens.  One pass collects what reaches the bound (little more than top_k tokens),
-// which then is ranked by comparing all pairs, and the filters are decided on it.  Returns kNone where the list does not hold (more
-// tokens reach the bound, because many are equal).
+// which then is ranked by comparing all pairs, and the filters are decided on it.  The bound is the edge of a bin of the distances
+// from the largest logit, 64 bins to an octave of 1 + distance.  Returns kNone where the list does not hold (more tokens reach the
+// bound, because many are equal or because the bins do not reach as far); else wavefront 0 has the token.
 template <int THREADS, typename T>
-__device__ uint32_t from_list(const T* row, const float* noise, int vocab, const float (&own_max)[4], uint32_t top_k, float top_p, float min_p, Scale scale, Shared<THREADS>& sh)
+__device__ uint32_t from_list(const T* row, const float* noise, int vocab, const float (&own_max)[4], uint32_t top_k, float top_p, float min_p, Scale scale,
+                              Shared<THREADS>& sh)
 {
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-    // the bound: two bytes of the top_k-th largest of the threads' maxima
-    uint32_t own_key[4];
+    constexpr uint32_t kOne = 0x3F800000u, kBinShift = 17;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) own_key[j] = key_of(own_max[j]);
-    uint32_t bound = 0, left = top_k;
-    for (int shift = 24; shift >= 16; shift -= 8) {
-        for (int b = tid; b < 256; b += THREADS) sh.hist[b] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (shift == 24 || own_key[j] >> 24 == bound >> 24) atomicAdd(&sh.hist[(own_key[j] >> shift) & 255], 1u);
-        __syncthreads();
-        if (wid == 0) {                       // lane l holds bins 255 - 4 l .. 252 - 4 l
-            uint32_t h[4], sum = 0;
-            for (int j = 0; j < 4; ++j) sum += h[j] = sh.hist[255 - 4 * lane - j];
-            uint32_t before = sum;
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t u = __shfl_up(before, d, 64);
-                if (lane >= d) before += u;
-            }
-            before -= sum;
-            for (int j = 0; j < 4; ++j) {
-                if (before < left && before + h[j] >= left) {
-                    sh.pick[0] = (uint32_t)(255 - 4 * lane - j);
-                    sh.pick[1] = left - before;
-                }
-                before += h[j];
-            }
-        }
-        __syncthreads();
-        bound |= sh.pick[0] << shift;
-        left = sh.pick[1];
+    for (int j = 0; j < 4; ++j) {
+        const float v = 1.f - scale.rel2(own_max[j]);
+        if (own_max[j] > -INFINITY) atomicAdd(&sh.hist[min(kBins - 1u, (__float_as_uint(v) - kOne) >> kBinShift)], 1u);
     }
-    if (tid == 0) sh.n_candidates = 0;
+    if (tid == 0) {
+        sh.n_candidates = 0;
+        sh.pick = kBins - 1;
+    }
     __syncthreads();
-    const float edge = logit_of(bound), least = edge == edge ? edge : -INFINITY;      // bits below those of -inf are no number's
+    if (wid == 0) {                           // lane l holds bins 8 l .. 8 l + 7
+        constexpr int kPer = kBins / 64;
+        uint32_t h[kPer], sum = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) sum += h[j] = sh.hist[kPer * lane + j];
+        uint32_t before = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t u = __shfl_up(before, d, 64);
+            if (lane >= d) before += u;
+        }
+        before -= sum;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if (before < top_k && before + h[j] >= top_k) sh.pick = (uint32_t)(kPer * lane + j);
+            before += h[j];
+        }
+    }
+    __syncthreads();
+    // the bin's far edge as a logit, a little further out than any rounding of the distances reaches
+    const uint32_t bin = sh.pick;
+    const float far = (__uint_as_float(kOne + ((bin + 1) << kBinShift)) * 1.00001f - 1.f) / scale.per2;
+    const float least = bin == kBins - 1 || !(scale.top < INFINITY) ? -INFINITY : scale.top - far * 1.00001f - fabsf(scale.top) * 1e-6f;
     batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
         float high = x[0];
 #pragma unroll
@@ -371,70 +389,84 @@ __device__ uint32_t from_list(const T* row, const float* noise, int vocab, const
     __syncthreads();
     const uint32_t n = sh.n_candidates;
     if (n > kMostCandidates) return kNone;
-    if (tid < 3) sh.candidate[n + tid] = 0;
-    __syncthreads();
-    // rank of every candidate; the list's own order, which atomics made, has no say in anything below
-    for (uint32_t c = tid; c < n; c += THREADS) {
-        const unsigned long long o = sh.candidate[c];
-        uint32_t rank = 0;
-        for (uint32_t j = 0; j < n; j += 4) {             // the places up to the next multiple of four hold zeros
-            const ulonglong2 a = *(const ulonglong2*)&sh.candidate[j], b = *(const ulonglong2*)&sh.candidate[j + 2];
-            rank += (a.x > o) + (a.y > o) + (b.x > o) + (b.y > o);
+    // The list in order; the order that atomics gave it has no say in anything below.  Few are ranked by comparing all pairs, more are
+    // sorted: one row of 50,001, us by pairs / sorted: 24.0 / 27.3 with a list of 450, 50.9 / 41.6 with one of 1400.
+    auto keep = [&](uint32_t rank, unsigned long long o) {
+        const float z = scale.rel2(logit_of((uint32_t)(o >> 32)));
+        sh.weight[rank] = exp2_fast(z);
+        sh.score[rank] = z - log2f(noise[~(uint32_t)o]);
+        sh.index[rank] = ~(uint32_t)o;
+    };
+    if (n <= kPairs) {
+        if (tid < 3) sh.candidate[n + tid] = 0;
+        __syncthreads();
+        for (uint32_t c = tid; c < n; c += THREADS) {
+            const unsigned long long o = sh.candidate[c];
+            uint32_t rank = 0;
+            for (uint32_t j = 0; j < n; j += 4) {         // the places up to the next multiple of four hold zeros
+                const ulonglong2 a = *(const ulonglong2*)&sh.candidate[j], b = *(const ulonglong2*)&sh.candidate[j + 2];
+                rank += (a.x > o) + (a.y > o) + (b.x > o) + (b.y > o);
+            }
+            if (rank < top_k) keep(rank, o);
         }
-        if (rank < top_k) {
-            sh.weight[rank] = scale.rel2(logit_of((uint32_t)(o >> 32)));
-            sh.index[rank] = ~(uint32_t)o;
-        }
+    } else {
+        const uint32_t size = 1u << (32 - __builtin_clz(n - 1));
+        for (uint32_t i = n + tid; i < size; i += THREADS) sh.candidate[i] = 0;
+        for (uint32_t run = 2; run <= size; run <<= 1)
+            for (uint32_t step = run >> 1; step > 0; step >>= 1) {
+                __syncthreads();
+                for (uint32_t i = tid; i < size / 2; i += THREADS) {
+                    const uint32_t lo = 2 * i - (i & (step - 1)), hi = lo + step;
+                    const unsigned long long a = sh.candidate[lo], b = sh.candidate[hi];
+                    if ((a < b) == ((lo & run) == 0)) {
+                        sh.candidate[lo] = b;
+                        sh.candidate[hi] = a;
+                    }
+                }
+            }
+        __syncthreads();
+        for (uint32_t c = tid; c < min(n, top_k); c += THREADS) keep(c, sh.candidate[c]);
     }
     __syncthreads();
     const uint32_t kept = min(n, top_k);
-    float before = 0.f, mass = 0.f, z[(kMostTopK + THREADS - 1) / THREADS], w[(kMostTopK + THREADS - 1) / THREADS];
+    // wavefront 0: the sums in the order of the ranks, 64 of them at a time; the whole sum first
+    if (wid > 0) return 0;
+    float mass = 0.f;
+    if (top_p < 1.f) {
+        for (uint32_t rank = lane; rank < kept; rank += 64) mass += sh.weight[rank];
+        mass = wave_sum(mass);
+    }
     Best win{-INFINITY, kNone};
-    // one token per thread and round; sums in the order of the ranks
-    constexpr int kRounds = (kMostTopK + THREADS - 1) / THREADS;
-    float at[kRounds];
+    float ahead = 0.f;
+    for (uint32_t base = 0; base < kept; base += 64) {
+        const uint32_t rank = base + lane;
+        const float w = rank < kept ? sh.weight[rank] : 0.f;
+        float sum = w;
 #pragma unroll
-    for (int round = 0; round < kRounds; ++round) {
-        const uint32_t rank = round * THREADS + tid;
-        z[round] = rank < kept ? sh.weight[rank] : -INFINITY;
-        w[round] = exp2_fast(z[round]);
-        float sum = w[round];
         for (int d = 1; d < 64; d <<= 1) {
             const float u = __shfl_up(sum, d, 64);
             if (lane >= d) sum += u;
         }
-        float* const part = round & 1 ? sh.sum_pair : sh.sums;
-        if (lane == 63) part[wid] = sum;
-        __syncthreads();
-        before = mass;
-        for (int v = 0; v < Shared<THREADS>::kWaves; ++v) {
-            if (v < wid) before += part[v];
-            mass += part[v];
+        const float shifted = __shfl_up(sum, 1, 64), before = ahead + (lane == 0 ? 0.f : shifted);
+        if (rank < kept && (rank == 0 || ((!(top_p < 1.f) || before < top_p * mass) && (!(min_p > 0.f) || w >= min_p)))) {
+            const float score = sh.score[rank];
+            if (score > -INFINITY) win = better(win, Best{score, sh.index[rank]});
         }
-        const float shifted = __shfl_up(sum, 1, 64);      // the sum before this lane, without taking its own off again
-        at[round] = before + (lane == 0 ? 0.f : shifted);
-        __syncthreads();
+        ahead += __shfl(sum, 63, 64);
     }
-#pragma unroll
-    for (int round = 0; round < kRounds; ++round) {
-        const uint32_t rank = round * THREADS + tid;
-        if (rank < kept && (rank == 0 || ((!(top_p < 1.f) || at[round] < top_p * mass) && (!(min_p > 0.f) || w[round] >= min_p)))) {
-            const uint32_t i = sh.index[rank];
-            const float score = z[round] - log2f(noise[i]);
-            if (score > -INFINITY) win = better(win, Best{score, i});
-        }
-    }
-    win = block_best(win, sh);
+    win = wave_best(win);
     return win.index == kNone ? sh.index[0] : win.index;
 }
 
 // A workgroup per row.
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel(Sampling s)
+__global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
 {
     __shared__ Shared<THREADS> sh;
-    const int tid = threadIdx.x, vocab = s.vocab;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, vocab = s.vocab;
+    int set = 0;
     const size_t r = blockIdx.x;
+    for (int b = tid; b < kBins; b += THREADS) sh.hist[b] = 0;
     const T* const row = (const T*)s.logits + r * s.logits_stride;
     const float* const noise = s.noise ? s.noise + r * s.noise_stride : nullptr;
     const float temperature = s.temperature ? s.temperature[r] : 1.f;
@@ -473,27 +505,48 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel
 #pragma unroll
         for (int e = 0; e < n; ++e) sum += exp2_fast(__builtin_fmaf(x[e], unit, -at));
     });
-    const float own_top = top.score;
-    const bool odd = __syncthreads_or(!(sum < INFINITY));
-    top = block_best(top, sh);
-    const float reference = top.score * unit;
+    // one barrier for the place of the largest, and for the sums, which are brought to a common reference on the way
     float all = 0.f;
-    if (!odd && fabsf(reference) < kFar) {
-        all = block_sum(own_top == -INFINITY ? 0.f : sum * exp2_fast(at - reference), sh);
+    {
+        float high = at;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) high = fmaxf(high, __shfl_xor(high, d, 64));
+        const bool odd = __any(!(sum < INFINITY));
+        sum = wave_sum(top.index == kNone ? 0.f : sum * exp2_fast(at - high));
+        top = wave_best(top);
+        if (lane == 0) {
+            sh.best[0][wid] = top;
+            sh.sums[0][wid] = make_float4(high, sum, odd ? 1.f : 0.f, 0.f);
+        }
+        set = 1;
+        __syncthreads();
+        bool any_odd = false;
+        top = sh.best[0][0];
+#pragma unroll
+        for (int w = 1; w < Shared<THREADS>::kWaves; ++w) top = better(top, sh.best[0][w]);
+        const float reference = top.score * unit;
+#pragma unroll
+        for (int w = 0; w < Shared<THREADS>::kWaves; ++w) {
+            const float4 v = sh.sums[0][w];
+            all += v.y * exp2_fast(v.x - reference);
+            any_odd |= v.z > 0.f;
+        }
         all *= exp2_fast(-__builtin_fmaf(top.score, unit, -reference));       // relative to the largest logit's weight
-    } else {
-        // NaN among the logits, infinite ones, or numbers too large for that
-        top = Best{-INFINITY, kNone};
-        each<THREADS>(row, vocab, [&](float raw, uint32_t i) {
-            const float x = number(raw);
-            if (x > top.score) top = Best{x, i};
-        });
-        part_max[0] = top.score;
-        part_max[1] = part_max[2] = part_max[3] = -INFINITY;
-        top = block_best(top, sh);
-        const Scale scale{top.score, unit};
-        each<THREADS>(row, vocab, [&](float raw, uint32_t) { all += number(raw) > -INFINITY ? scale.weight(raw) : 0.f; });
-        all = block_sum(all, sh);
+        if (any_odd || !(fabsf(reference) < kFar)) {
+            // NaN among the logits, infinite ones, numbers too large for that, or none at all
+            top = Best{-INFINITY, kNone};
+            each<THREADS>(row, vocab, [&](float raw, uint32_t i) {
+                const float x = number(raw);
+                if (x > top.score) top = Best{x, i};
+            });
+            part_max[0] = top.score;
+            part_max[1] = part_max[2] = part_max[3] = -INFINITY;
+            top = block_best(top, sh, set);
+            const Scale scale{top.score, unit};
+            all = 0.f;
+            each<THREADS>(row, vocab, [&](float raw, uint32_t) { all += number(raw) > -INFINITY ? scale.weight(raw) : 0.f; });
+            all = block_sum(all, sh, set);
+        }
     }
     if (top.index == kNone) {
         if (tid == 0) {
@@ -516,7 +569,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel
                 last = front_of(row, vocab, (uint32_t)top_k, sh);
                 mass = 0.f;
                 each<THREADS>(row, vocab, [&](float x, uint32_t i) { mass += (last.holds(x, i) & (x > -INFINITY)) ? scale.weight(x) : 0.f; });
-                mass = block_sum(mass, sh);
+                mass = block_sum(mass, sh, set);
             }
             if (top_p < 1.f) {
                 // Tokens lighter than (1 - top_p) mass / vocab weigh less than what the nucleus leaves out, all together: none of them is in
@@ -524,7 +577,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel
                 const float least = top.score + log2f(0.25f * (1.f - fmaxf(top_p, 0.f)) * mass / (float)vocab) / unit;
                 if (least > last.x) last = Front{least, kNone};
             }
-            token = race(row, noise, vocab, top.index, last, top_p, mass, min_p, scale, sh);
+            token = race(row, noise, vocab, top.index, last, top_p, mass, min_p, scale, sh, set);
         }
     }
     if (tid == 0) {
