@@ -483,7 +483,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
     // Weights relative to 2^at: x unit - at in one rounding, whatever number `at` is.  It follows the largest logit so far, but not below
     // -2^20: masks of the type's lowest value weigh nothing then, and what a rounding of `at` leaves of the largest weight stays near 1.
     constexpr float kFar = 1048576.f;
-    float at = 0.f, sum = 0.f;
+    float at = -kFar, sum = 0.f;              // a share with nothing in it does not raise its wavefront's reference
     batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
         float high[4];
 #pragma unroll
@@ -508,6 +508,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
     // one barrier for the place of the largest, and for the sums, which are brought to a common reference on the way
     float all = 0.f;
     {
+#pragma clang fp contract(off)                // the reference is the rounded product in every use
         float high = at;
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) high = fmaxf(high, __shfl_xor(high, d, 64));

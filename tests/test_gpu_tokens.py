@@ -527,6 +527,60 @@ def test_sample_exact_cuts(B):
     assert _sample_gpu(B, tiny, 1.0, 2, None, None, n)[0][0] == 200 and _sample_gpu(B, tiny, 1.0, 3, None, None, n)[0][0] == 100
 
 
+@pytest.mark.parametrize("vocab", [5, 300, 5000])
+@pytest.mark.parametrize("level", [-3000.0, -200.0, 0.0, 200.0, 3000.0])
+def test_sample_far_from_zero(B, vocab, level):
+    """Logits that all lie far on one side of 0: threads, wavefronts and masked stretches without a token do not set what weights are
+    relative to."""
+    rng = np.random.default_rng(vocab)
+    x = (level + np.round(64 * rng.standard_normal((6, vocab))) / 16).astype(np.float32)      # exact in fp32
+    x[1, vocab // 2:] = -np.inf
+    x[2, :vocab // 2] = -np.inf
+    for t, k, p in ((1.0, 0, 1.0), (0.5, 0, 0.8), (1.0, 20, 0.9), (3.0, 0, 0.5)):
+        _check_sample(B, x, t, k, p, 0.0, _noise(rng, x.shape))
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(300, 17003, "f32"), (300, 17003, "bf16"), (200, 20011, "bf16"), (3, 140001, "f32"), (3, 140001, "bf16"), (60, 70007, "bf16")])
+def test_sample_rows_by_number(B, rows, vocab, dtype):
+    """One row's tokens do not depend on how many others there are: every filter in turn, checked on some of the rows."""
+    rng = np.random.default_rng(rows)
+    settings = [(1.0, 0, 1.0, 0.0), (0.8, 0, 0.9, 0.0), (1.0, 0, 0.4, 0.0), (1.0, 60, 0.95, 0.0), (0.0, 0, 1.0, 0.0), (1.0, 900, 1.0, 0.001), (1.0, 5000, 0.9, 0.0),
+                (1.5, 0, 0.7, 0.01), (1.0, 0, 0.01, 0.0)]
+    x = (3 * rng.standard_normal((rows, vocab), dtype=np.float32)).astype(np.float32)
+    x[0, rng.random(vocab) < 0.99] = -np.inf
+    if dtype == "bf16":
+        x = _bf16(x)
+    t, k, p, m = (np.array([c[r % len(settings)] for r in range(rows)]) for c in zip(*settings))
+    noise = rng.standard_exponential((rows, vocab), dtype=np.float32)
+    some = sorted({0, 1, 2, rows - 1} | set(rng.integers(0, rows, 12).tolist()))
+    token, lp = _sample_gpu(B, x, t, k, p, m, noise)
+    wide = x if dtype == "f32" else None
+    for r in some:
+        x64 = (T.bf16_to_f64(x[r]) if wide is None else x[r].astype(np.float64))
+        near, ln = T.sample(x64, float(np.float32(t[r])), int(k[r]), float(np.float32(p[r])), float(np.float32(m[r])), noise[r], slack=1e-4)
+        assert int(token[r]) in near, (r, int(token[r]), near)
+        assert abs(lp[r] - ln[token[r]]) <= 1e-5 * (1 + abs(ln[token[r]])), r
+
+
+@pytest.mark.parametrize("vocab", [66000])
+def test_sample_hidden_winners(B, vocab):
+    """The best of the race fall to the nucleus one after the other, and the token that is drawn shares a thread's stretch with them."""
+    rng = np.random.default_rng(8)
+    rows = 24
+    x = np.full((rows, vocab), -4.0, np.float32) + rng.random((rows, vocab), dtype=np.float32)
+    noise = np.full((rows, vocab), 1.0, np.float32) + rng.random((rows, vocab), dtype=np.float32)
+    for r in range(rows):
+        at = rng.integers(0, vocab - 40)
+        x[r, at:at + 3] = 9.0, 8.9, 8.8               # the nucleus
+        x[r, rng.integers(0, vocab)] += 0.5
+        noise[r, at], noise[r, at + 1], noise[r, at + 2] = 3.0, 2.0, 1.5
+        for j in range(1, 1 + r % 7):                 # numbers so small that they win, of tokens that are not kept, next to it and far off
+            noise[r, (at + 3 + j) if j % 2 else rng.integers(0, vocab)] = 1e-12 * j
+    for p in (0.3, 0.6, 0.9):
+        _check_sample(B, x, 1.0, 0, p, 0.0, noise)
+        _check_sample(B, x[:, :9000], 1.0, 0, p, 0.0, noise[:, :9000])
+
+
 def test_sample_values_that_are_no_numbers(B):
     rng = np.random.default_rng(3)
     vocab = 2500
