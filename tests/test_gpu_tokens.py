@@ -685,3 +685,50 @@ def test_a_step_on_another_stream_and_in_a_graph(B):
             if a is out or a is lse:
                 a, b = a[:used], b[:used]
             assert torch.equal(a, b)
+
+
+# ---- the example that serves them together ------------------------------------------------------------------------
+def _dense_logits(e, expert, ids):
+    """The expert's logits at every place of ids: whole rows of scores, fp32 on the CPU, nothing cached."""
+    import torch
+    f = lambda w: w[expert].float().cpu()
+    norm = lambda x: x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-5)
+    n = len(ids)
+    x = f(e.embedding)[ids] + f(e.position)[:n]
+    mask = torch.full((n, n), -np.inf).triu(1)
+    for layer in range(e.layers):
+        q, k, v = (norm(x) @ f(e.qkv[layer])).view(n, -1, e.head_dim).split([e.heads, e.kv_heads, e.kv_heads], 1)
+        k, v = (a.repeat_interleave(e.heads // e.kv_heads, 1) for a in (k, v))
+        s = torch.einsum("qhd,khd->hqk", q, k) * e.head_dim ** -0.5 + mask
+        x = x + torch.einsum("hqk,khd->qhd", s.softmax(-1), v).reshape(n, -1) @ f(e.o[layer])
+        x = x + torch.nn.functional.gelu(norm(x) @ f(e.up[layer])) @ f(e.down[layer])
+    return norm(x) @ f(e.head)
+
+
+def test_example_generates_what_the_dense_model_says(B):
+    """Greedy tokens and log-probabilities of several experts in shared steps, prompts cut into chunks and a cache so small that
+    requests wait for blocks, against whole forwards without a cache."""
+    import importlib.util
+    import pathlib
+    spec = importlib.util.spec_from_file_location("generate", pathlib.Path(__file__).parent.parent / "examples" / "generate.py")
+    generate = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(generate)
+    experts = generate.Experts(3, max_len=200)
+    rng = np.random.default_rng(0)
+    prompts = [rng.integers(0, experts.vocab, m).tolist() for m in (1, 130, 17, 64, 3, 90, 33)]
+    route = [2, 0, 1, 0, 2, 0, 2]
+    server = generate.Server(experts, n_blocks=24, block_size=16, token_cap=96)
+    tokens, logprobs, steps = server.generate(prompts, route, 6)
+    assert steps > 10
+    # a bf16 rounding is at most 2^-9 of a value; some ten of them on the way through each of two layers add up to 2^-9 sqrt(20) = 0.9 % of
+    # the state, the logits are of deviation 1 (weights: variance 1 / fan-in): 0.01 each, and 0.06 is six deviations
+    for prompt, e, drawn, lp in zip(prompts, route, tokens, logprobs):
+        assert len(drawn) == 6
+        logits = _dense_logits(experts, e, prompt + drawn)[len(prompt) - 1:-1]
+        for row, token, value in zip(logits, drawn, lp):
+            assert row[token] >= row.max() - 0.12
+            assert abs(float(row.log_softmax(-1)[token]) - value) <= 0.12
+    # the same with room for everything at once draws the same way at any temperature
+    wide = generate.Server(experts, n_blocks=200, block_size=8, token_cap=512)
+    again = wide.generate(prompts, route, 6, temperature=0.9, top_p=0.8, seed=3)
+    assert wide.generate(prompts, route, 6, temperature=0.9, top_p=0.8, seed=3) == again and all(np.isfinite(v).all() for v in again[1])
