@@ -77,7 +77,7 @@ __device__ __forceinline__ Span span_of(const KvAttention& a, int r, int group, 
     s.rows = s.m * group;
     s.first_pos = len - m_all;
     s.end = max(0, min(len, s.first_pos + s.m));
-    s.begin = a.window > 0 ? min(s.end, max(0, s.first_pos - a.window + 1)) : 0;
+    s.begin = a.window > 0 ? min(s.end, max(0, max(0, s.first_pos) - a.window + 1)) : 0;      // of the largest window too
     return s;
 }
 
@@ -546,7 +546,7 @@ __host__ __device__ inline ManyLayout many_layout(int32_t n_requests, int32_t n_
 __device__ __forceinline__ void tiles_of(const Span& s, int window, int group, int row, int& first, int& count)
 {
     const int last = min(s.rows, row + kManyRows) - 1;
-    const int end = max(0, s.first_pos + last / group + 1), begin = window > 0 ? min(end, max(0, s.first_pos + row / group - window + 1)) : 0;
+    const int end = max(0, s.first_pos + last / group + 1), begin = window > 0 ? min(end, max(0, max(0, s.first_pos + row / group) - window + 1)) : 0;
     first = begin / kManyKeys;
     count = max(1, (end + kManyKeys - 1) / kManyKeys - first);
 }

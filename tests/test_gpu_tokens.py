@@ -373,6 +373,68 @@ def test_attention_fewer_new_tokens_than_announced_and_padding_rows(B):
     assert np.array_equal(a.run(lse=False)[0], base[0])
 
 
+def test_attention_of_many_requests(B):
+    """More requests than a workgroup has threads, single tokens only and in a mixed step; most histories are short."""
+    rng = np.random.default_rng(12)
+    ones = [(int(h), int(rng.random() < 0.9)) for h in rng.integers(0, 60, 700)]
+    a = Attend(B, ones, 4, 2, 64, seed=1)
+    a.check(*a.run())
+    mixed = [(int(h), int(m)) for h, m in zip(rng.integers(0, 40, 1500), rng.integers(0, 4, 1500))]
+    mixed[3], mixed[1400] = (200, 70), (0, 129)
+    a = Attend(B, mixed, 4, 2, 64, seed=2)
+    a.check(*a.run())
+
+
+@pytest.mark.parametrize("dim", [16, 24, 32, 56, 72, 112, 120])
+def test_attention_head_widths(B, dim):
+    for lengths in ([(100, 1), (0, 1), (37, 2)], [(60, 100), (33, 1)]):
+        a = Attend(B, lengths, 6, 2, dim, seed=dim)
+        a.check(*a.run())
+
+
+def test_attention_largest_window(B):
+    """A window beyond every history is none, also for rows that stand before the first cached token."""
+    for lengths in ([(-3, 5), (40, 1), (-1, 2)], [(-3, 70), (50, 90), (-40, 60)]):
+        base = Attend(B, lengths, 8, 2, 64, seed=1).run()
+        for window in (2 ** 31 - 1, 2 ** 31 - 40, 10 ** 6):
+            got = Attend(B, lengths, 8, 2, 64, seed=1, window=window).run()
+            assert np.array_equal(got[0], base[0]) and np.array_equal(got[1], base[1])
+
+
+def test_attention_window_past_freed_blocks(B):
+    """Blocks that lie wholly before every row's window may be given back: their table entries are not followed."""
+    for lengths in ([(500, 1), (300, 2)], [(500, 70), (300, 1)]):
+        a = Attend(B, lengths, 8, 2, 64, window=100, seed=3)
+        base = a.run()
+        for r, (have, _) in enumerate(lengths):
+            a.table[r, :(have - 100) // 16] = -1
+        got = a.run()
+        assert np.array_equal(got[0], base[0]) and np.array_equal(got[1], base[1])
+
+
+def test_attention_offsets_that_are_no_offsets(B):
+    """Row ranges that run backwards or past the tokens take what lies inside; no other row is written, and sound requests are served."""
+    for new in (1, 40):
+        a = Attend(B, [(60, new), (40, new), (80, new)], 4, 2, 64, seed=4)
+        base = a.run()[0]
+        import torch
+        k, v, cache = _make_cache(B, a.bits, "token")
+        q, out = _dev(a.q), _dev(np.full(a.q.shape, 0xFFC0, np.uint16))
+        need = B.coe_kv_attention_workspace(3, 3 * new, new, 4, 2, 64)
+        work = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+        off, total, table = _dev(np.array([0, new, new, 10 ** 9], np.int32)), _dev(a.total), _dev(a.table)
+        B.coe_kv_attention(cache, 3, 3 * new, new, 4, 0, a.scale, q.data_ptr(), q.stride(0), q.stride(1), off.data_ptr(), total.data_ptr(), table.data_ptr(),
+                           a.max_blocks, out.data_ptr(), out.stride(0), out.stride(1), 0, work.data_ptr(), need, _stream())
+        got = out.cpu().numpy().view(np.uint16)
+        assert np.array_equal(got[:new], base[:new]) and (got[2 * new:] == 0xFFC0).all()     # the third has more rows than were announced
+        off = _dev(np.array([0, new, -7, -9], np.int32))
+        out.copy_(_dev(np.full(a.q.shape, 0xFFC0, np.uint16)))
+        B.coe_kv_attention(cache, 3, 3 * new, new, 4, 0, a.scale, q.data_ptr(), q.stride(0), q.stride(1), off.data_ptr(), total.data_ptr(), table.data_ptr(),
+                           a.max_blocks, out.data_ptr(), out.stride(0), out.stride(1), 0, work.data_ptr(), need, _stream())
+        got = out.cpu().numpy().view(np.uint16)
+        assert np.array_equal(got[:new], base[:new]) and (got[new:] == 0xFFC0).all()
+
+
 def test_attention_cache_beyond_4_gib(B):
     """Blocks whose bytes begin past 2^32: the same bits as in a small cache."""
     import torch
