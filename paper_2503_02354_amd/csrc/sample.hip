@@ -56,12 +56,21 @@ constexpr uint32_t kNone = 0xFFFFFFFFu;
 __device__ __forceinline__ bool better_than(float score, uint32_t index, Best a) { return (score > a.score) | ((score == a.score) & (index < a.index)); }
 __device__ __forceinline__ Best better(Best a, Best b) { return better_than(b.score, b.index, a) ? b : a; }
 
+// Of a wavefront's part of a row: the largest logit and where, the winner of the race (score relative to 2^at), the sum of the weights
+// relative to 2^at.  odd: the sum is no number; tiny: a random number below 2^-40.
+struct Record {
+    Best top, won;
+    float at, sum;
+    uint32_t odd, tiny;
+};
+
 constexpr int kMostCandidates = 4096, kMostTopK = 1536, kBins = 512, kPairs = 640;       // the list is sorted in powers of two
 template <int THREADS> struct Shared {
     static constexpr int kWaves = THREADS / 64;
     // a wavefront's part of a reduction; two sets in turn, so that one barrier is enough
     Best best[2][kWaves];
     float4 sums[2][kWaves];
+    Record record[kWaves];
     uint32_t hist[kBins];
     uint32_t pick;
     uint32_t n_candidates;
@@ -177,11 +186,16 @@ struct Front {
 // What a row's weights are relative to, and in which unit.
 struct Scale {
     float top, per2;                          // largest logit; 1 / T in units of ln 2
+    float reference;                          // top per2, rounded
+    bool far;                                 // the row is no common one: near_weight may not be asked
     // log2 of the weight: 0 for the largest itself, be it infinite, and -inf for others then
     __device__ __forceinline__ float rel2(float x) const { return (x == top ? 0.f : x - top) * per2; }
     __device__ __forceinline__ float weight(float x) const { return exp2_fast(rel2(x)); }
+    // the same but for a factor near 1 that all tokens of the row share
+    __device__ __forceinline__ float near_weight(float x) const { return exp2_fast(__builtin_fmaf(x, per2, -reference)); }
 };
 
+constexpr float kTiny = 0x1p-40f;
 // This thread's winner of the race among the tokens of a front: the largest log2(w) - log2 E.
 template <int THREADS, typename T>
 __device__ __attribute__((noinline)) Best winner_by_logs(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float least, Scale scale)
@@ -195,110 +209,142 @@ __device__ __attribute__((noinline)) Best winner_by_logs(const T* row, const flo
     return win;
 }
 
+// The same by cross products of w and E; the logarithms are taken of a thread's winner only.  near: fp32 holds the products (no random
+// number is below 2^-40; a winner below 2^-40 says that it may not).
+template <int THREADS, typename T>
+__device__ __forceinline__ Best winner(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float least, Scale scale, bool& near)
+{
+    uint32_t index = kNone;
+    float win_w = 0.f, win_q = 1.f, smallest = 1.f;
+    batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
+        float high = x[0];
+#pragma unroll
+        for (int e = 1; e < n; ++e) high = fmaxf(high, x[e]);
+        if (!(high >= front.x)) return;
+        float q[16];
+        if constexpr (n == 1) q[0] = noise[i];
+        else {
+#pragma unroll
+            for (int e = 0; e < n; e += 4) {
+                const f32x4 v = *(const f32x4*)(noise + in_batch<THREADS, T>(i, e));
+                q[e] = v[0], q[e + 1] = v[1], q[e + 2] = v[2], q[e + 3] = v[3];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+            const uint32_t at = in_batch<THREADS, T>(i, e);
+            const float z = (x[e] - scale.top) * scale.per2, w = exp2_fast(z);
+            smallest = fminf(smallest, q[e]);
+            const bool wins = front.holds(x[e], at) & ((z >= least) | (at == top_index)) & (q[e] >= 0.f) & (w * win_q > win_w * q[e]);
+            win_w = wins ? w : win_w;
+            win_q = wins ? q[e] : win_q;
+            index = wins ? at : index;
+        }
+    });
+    near = !(smallest < kTiny);
+    return Best{index == kNone ? -INFINITY : log2f(win_w) - log2f(win_q), index};
+}
+
+// Whether a thread whose winner `at` is not kept hides another token of the front that beats `best`: its share of the row is looked
+// through.  Every thread takes a part of the share.
+template <int THREADS, typename T>
+__device__ __forceinline__ bool hides(const T* row, const float* noise, int vocab, int at, uint32_t top_index, Front front, float least, Scale scale, Best best)
+{
+    constexpr int W = Vec<T>::kWidth;
+    const int lead = min(vocab, (int)((-(uintptr_t)row & 15) / sizeof(T))), vecs = (vocab - lead) / W, tail = lead + vecs * W;
+    const int owner = at < lead ? at : at >= tail ? at - tail : (at - lead) / W % THREADS;
+    const int own_vecs = vecs > owner ? (vecs - owner + THREADS - 1) / THREADS : 0;
+    bool hidden = false;
+    for (int k = threadIdx.x; k < own_vecs * W + 2; k += blockDim.x) {
+        const int i = k < own_vecs * W ? lead + (owner + k / W * THREADS) * W + k % W : k == own_vecs * W ? (owner < lead ? owner : vocab) : tail + owner;
+        if (i >= vocab) continue;
+        const float x = logit(row, i), z = scale.rel2(x), score = z - log2f(noise[i]);
+        hidden = hidden || (front.holds(x, (uint32_t)i) && (z >= least || i == (int)top_index) && better_than(score, (uint32_t)i, best));
+    }
+    return hidden;
+}
+
+__device__ __forceinline__ float least_of(float min_p) { return min_p > 0.f ? log2f(min_p) : -INFINITY; }
+
+// The weights of the tokens before two tokens of the order.  For a batch that lies before (behind) a token by index, the bound itself counts
+// equal logits in (out).
+template <int THREADS, typename T, class Weight>
+__device__ __forceinline__ float2 masses_before(const T* row, int vocab, const Front (&ahead)[2], Weight weight)
+{
+    constexpr uint32_t kReach = (16 / Vec<T>::kWidth - 1) * THREADS * Vec<T>::kWidth + Vec<T>::kWidth;      // of a batch
+    // the next lower number: to be above it is to reach the bound
+    const float with[2] = {nextafterf(ahead[0].x, -INFINITY), nextafterf(ahead[1].x, -INFINITY)};
+    float before[2] = {0.f, 0.f};
+    batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
+        float above[2];
+        bool clear = true;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            above[j] = i + kReach <= ahead[j].end ? with[j] : ahead[j].x;
+            clear &= (i + kReach <= ahead[j].end) | (i >= ahead[j].end);
+        }
+        if (clear) {
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                const float w = weight(x[e]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) before[j] += x[e] > above[j] ? w : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                const float w = weight(x[e]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) before[j] += ahead[j].holds(x[e], in_batch<THREADS, T>(i, e)) ? w : 0.f;
+            }
+        }
+    });
+    return make_float2(before[0], before[1]);
+}
+
 // The race decided by what the filters say.  It needs no sorted row: its winner among a front that holds all kept tokens is the drawn
 // token if it is kept itself, and whether it is takes one sum over the tokens before it.  If it is not, no token from its place on
 // is kept either, and the race is for the others.  The sums of the two best threads' winners are taken in one pass, since a row
 // whose winner falls to the nucleus would keep the launch waiting for another two.
-// w / E is compared by cross products; logarithms are taken of every thread's winner only.  Where fp32 may not hold the products
-// (random numbers below 2^-60, a winner below 2^-40, infinite logits), by logarithms after all.
+// `first` and `mine` (this thread's) are the winners of a race that has been run; without an index: none has.  mass: near_weights' of
+// a row that is not far, else weights'.
 template <int THREADS, typename T>
-__device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float top_p, float mass, float min_p, Scale scale,
-                         Shared<THREADS>& sh, int& set)
+__device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float top_p, float mass, float min_p, Scale scale, Best first,
+                         Best mine, Shared<THREADS>& sh, int& set)
 {
-    constexpr int W = Vec<T>::kWidth, kFew = 2;
-    const float least = min_p > 0.f ? log2f(min_p) : -INFINITY;
+    const float least = least_of(min_p);
     bool by_logs = !(scale.top < INFINITY);
     for (;;) {                                // the front shrinks with every round that goes on
-        Best c[kFew];
-#pragma unroll
-        for (int j = 0; j < kFew; ++j) c[j] = Best{-INFINITY, kNone};
+        Best c[2] = {first, Best{-INFINITY, kNone}};
         if (!by_logs) {
-            uint32_t index = kNone;
-            float win_w = 0.f, win_q = 1.f, smallest = 1.f;
-            batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
-                float high = x[0];
-#pragma unroll
-                for (int e = 1; e < n; ++e) high = fmaxf(high, x[e]);
-                if (!(high >= front.x)) return;
-                float q[16];
-                if constexpr (n == 1) q[0] = noise[i];
-                else {
-#pragma unroll
-                    for (int e = 0; e < n; e += 4) {
-                        const f32x4 v = *(const f32x4*)(noise + in_batch<THREADS, T>(i, e));
-                        q[e] = v[0], q[e + 1] = v[1], q[e + 2] = v[2], q[e + 3] = v[3];
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < n; ++e) {
-                    const uint32_t at = in_batch<THREADS, T>(i, e);
-                    const float z = (x[e] - scale.top) * scale.per2, w = exp2_fast(z);
-                    smallest = fminf(smallest, q[e]);
-                    const bool wins = front.holds(x[e], at) & ((z >= least) | (at == top_index)) & (q[e] >= 0.f) & (w * win_q > win_w * q[e]);
-                    win_w = wins ? w : win_w;
-                    win_q = wins ? q[e] : win_q;
-                    index = wins ? at : index;
-                }
-            });
-            by_logs = __syncthreads_or(smallest < 0x1p-60f);
-            Best mine{index == kNone ? -INFINITY : log2f(win_w) - log2f(win_q), index};
-            c[0] = block_best(mine, sh, set);
-            by_logs |= !(c[0].score > -40.f);
+            if (first.index == kNone) {
+                bool near;
+                mine = winner<THREADS>(row, noise, vocab, top_index, front, least, scale, near);
+                by_logs = __syncthreads_or(!near);
+                c[0] = block_best(mine, sh, set);
+                by_logs |= !(c[0].score > -40.f);
+            }
             if (!by_logs && top_p < 1.f && c[0].index != top_index) {
-#pragma unroll
-                for (int j = 1; j < kFew; ++j) {
-                    if (mine.index == c[j - 1].index) mine = Best{-INFINITY, kNone};
-                    c[j] = block_best(mine, sh, set);
-                }
+                if (mine.index == c[0].index) mine = Best{-INFINITY, kNone};
+                c[1] = block_best(mine, sh, set);
             }
         }
+        first.index = kNone;
         if (by_logs) c[0] = block_best(winner_by_logs<THREADS>(row, noise, vocab, top_index, front, least, scale), sh, set);
         if (c[0].index == kNone) return top_index;
         if (!(top_p < 1.f) || c[0].index == top_index) return c[0].index;
 
-        Front ahead[kFew];
-        float before[kFew];
-#pragma unroll
-        for (int j = 0; j < kFew; ++j) {
-            ahead[j] = c[j].index == kNone ? Front{INFINITY, 0} : Front{logit(row, c[j].index), c[j].index};
-            before[j] = 0.f;
-        }
-        each<THREADS>(row, vocab, [&](float x, uint32_t i) {
-            const float w = scale.weight(x);
-#pragma unroll
-            for (int j = 0; j < kFew; ++j) before[j] += ahead[j].holds(x, i) ? w : 0.f;
-        });
-        const float2 masses = block_sums(make_float2(before[0], before[1]), sh, set);
-        before[0] = masses.x, before[1] = masses.y;
-        int kept = kFew;
-        Front out{-INFINITY, kNone};          // in front of every token that turned out not to be kept
-#pragma unroll
-        for (int j = 0; j < kFew; ++j) {
-            if (kept < kFew || c[j].index == kNone) continue;
-            if (c[j].index == top_index || before[j] < top_p * mass) kept = j;
-            else if (!ahead[j].holds(out.x, out.end) || out.end == kNone) out = ahead[j];
-        }
-        if (kept == 0) return c[0].index;
-        if (kept < kFew) {
-            // A thread whose winner is not kept may hide another that is, and that beats the kept one: its share is looked through.
-            bool hidden = false;
-            const int lead = min(vocab, (int)((-(uintptr_t)row & 15) / sizeof(T))), vecs = (vocab - lead) / W, tail = lead + vecs * W;
-            const Best best = c[1];
-#pragma unroll
-            for (int j = 0; j < kFew - 1; ++j) {
-                if (j >= kept) continue;
-                const int at = (int)c[j].index, owner = at < lead ? at : at >= tail ? at - tail : (at - lead) / W % THREADS;
-                const int own_vecs = vecs > owner ? (vecs - owner + THREADS - 1) / THREADS : 0;
-                for (int k = threadIdx.x; k < own_vecs * W + 2; k += THREADS) {
-                    const int i = k < own_vecs * W ? lead + (owner + k / W * THREADS) * W + k % W : k == own_vecs * W ? (owner < lead ? owner : vocab) : tail + owner;
-                    if (i >= vocab) continue;
-                    const float x = logit(row, i), z = scale.rel2(x), score = z - log2f(noise[i]);
-                    if (out.holds(x, (uint32_t)i) && (z >= least || i == (int)top_index) && better_than(score, (uint32_t)i, best)) hidden = true;
-                }
-            }
-            if (!__syncthreads_or(hidden)) return best.index;
-        }
-        front = out;
+        const Front ahead[2] = {Front{logit(row, c[0].index), c[0].index}, c[1].index == kNone ? Front{INFINITY, 0} : Front{logit(row, c[1].index), c[1].index}};
+        const float2 before = scale.far ? masses_before<THREADS>(row, vocab, ahead, [&](float x) { return scale.weight(x); })
+                                        : masses_before<THREADS>(row, vocab, ahead, [&](float x) { return scale.near_weight(x); });
+        const float2 masses = block_sums(before, sh, set);
+        if (masses.x < top_p * mass) return c[0].index;
+        front = ahead[0];
+        if (c[1].index == kNone) continue;
+        if (c[1].index == top_index || masses.y < top_p * mass) {
+            if (!__syncthreads_or(hides<THREADS>(row, noise, vocab, (int)c[0].index, top_index, front, least, scale, c[1]))) return c[1].index;
+        } else if (front.holds(ahead[1].x, ahead[1].end))
+            front = ahead[1];
     }
 }
 
@@ -330,28 +376,26 @@ template <int THREADS, typename T> __device__ Front front_of(const T* row, int v
     return {logit_of((uint32_t)(last >> 32)), ~(uint32_t)last + 1};
 }
 
-// A small top_k from a short list.  Every thread has met the largest logits of four parts of its share; with at least top_k of all these
+// A small top_k from a short list.  Every thread has met the largest logits of parts of its share; with at least top_k of all these
 // at or above a bound, so are the first top_k tokens.  One pass collects what reaches the bound (little more than top_k tokens),
-// which then is ranked by comparing all pairs, and the filters are decided on it.  The bound is the edge of a bin of the distances
-// from the largest logit, 64 bins to an octave of 1 + distance.  Returns kNone where the list does not hold (more tokens reach the
-// bound, because many are equal or because the bins do not reach as far); else wavefront 0 has the token.
-template <int THREADS, typename T>
-__device__ uint32_t from_list(const T* row, const float* noise, int vocab, const float (&own_max)[4], uint32_t top_k, float top_p, float min_p, Scale scale,
-                              Shared<THREADS>& sh)
+// which then is put in order, and the filters are decided on it.  The bound is the edge of a bin of the distances from the largest
+// logit, 64 bins to an octave of 1 + distance.
+constexpr uint32_t kOne = 0x3F800000u, kBinShift = 17;
+template <int THREADS> __device__ __forceinline__ void count_part(float part_max, Scale scale, Shared<THREADS>& sh)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-    constexpr uint32_t kOne = 0x3F800000u, kBinShift = 17;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float v = 1.f - scale.rel2(own_max[j]);
-        if (own_max[j] > -INFINITY) atomicAdd(&sh.hist[min(kBins - 1u, (__float_as_uint(v) - kOne) >> kBinShift)], 1u);
-    }
+    const float v = 1.f - scale.rel2(part_max);
+    if (part_max > -INFINITY) atomicAdd(&sh.hist[min(kBins - 1u, (__float_as_uint(v) - kOne) >> kBinShift)], 1u);
+}
+// the bound, from the counted parts
+template <int THREADS> __device__ __forceinline__ float bound_of(uint32_t top_k, Scale scale, Shared<THREADS>& sh)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
     if (tid == 0) {
         sh.n_candidates = 0;
         sh.pick = kBins - 1;
     }
     __syncthreads();
-    if (wid == 0) {                           // lane l holds bins 8 l .. 8 l + 7
+    if (tid < 64) {                           // lane l holds bins 8 l .. 8 l + 7
         constexpr int kPer = kBins / 64;
         uint32_t h[kPer], sum = 0;
 #pragma unroll
@@ -373,7 +417,11 @@ __device__ uint32_t from_list(const T* row, const float* noise, int vocab, const
     // the bin's far edge as a logit, a little further out than any rounding of the distances reaches
     const uint32_t bin = sh.pick;
     const float far = (__uint_as_float(kOne + ((bin + 1) << kBinShift)) * 1.00001f - 1.f) / scale.per2;
-    const float least = bin == kBins - 1 || !(scale.top < INFINITY) ? -INFINITY : scale.top - far * 1.00001f - fabsf(scale.top) * 1e-6f;
+    return bin == kBins - 1 || !(scale.top < INFINITY) ? -INFINITY : scale.top - far * 1.00001f - fabsf(scale.top) * 1e-6f;
+}
+template <int THREADS, typename T>
+__device__ __forceinline__ void collect(const T* row, int vocab, float least, uint32_t* count, unsigned long long* list)
+{
     batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
         float high = x[0];
 #pragma unroll
@@ -382,13 +430,16 @@ __device__ uint32_t from_list(const T* row, const float* noise, int vocab, const
 #pragma unroll
         for (int e = 0; e < n; ++e)
             if (x[e] >= least && x[e] > -INFINITY) {
-                const uint32_t at = atomicAdd(&sh.n_candidates, 1u);
-                if (at < kMostCandidates) sh.candidate[at] = order_of(x[e], in_batch<THREADS, T>(i, e));
+                const uint32_t at = atomicAdd(count, 1u);
+                if (at < kMostCandidates) list[at] = order_of(x[e], in_batch<THREADS, T>(i, e));
             }
     });
-    __syncthreads();
-    const uint32_t n = sh.n_candidates;
-    if (n > kMostCandidates) return kNone;
+}
+// The token of a list of n tokens that holds the first top_k; wavefront 0 has it.
+template <int THREADS>
+__device__ uint32_t from_list(uint32_t n, const float* noise, uint32_t top_k, float top_p, float min_p, Scale scale, Shared<THREADS>& sh)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     // The list in order; the order that atomics gave it has no say in anything below.  Few are ranked by comparing all pairs, more are
     // sorted: one row of 50,001, us by pairs / sorted: 24.0 / 27.3 with a list of 450, 50.9 / 41.6 with one of 1400.
     auto keep = [&](uint32_t rank, unsigned long long o) {
@@ -458,6 +509,70 @@ __device__ uint32_t from_list(const T* row, const float* noise, int vocab, const
     return win.index == kNone ? sh.index[0] : win.index;
 }
 
+// A thread's share of a row: its largest logit and where, the sum of its weights relative to 2^at, the largest logits of four parts of
+// it, and with RACE the winner among all its tokens (score relative to 2^at) and its smallest random number.
+// Weights are x unit - at in one rounding, whatever number `at` is.  It follows the largest logit so far, but not below -2^20: masks of
+// the type's lowest value weigh nothing then, and what a rounding of `at` leaves of the largest weight stays near 1.
+constexpr float kFar = 1048576.f;
+struct Share {
+    Best top, won;
+    float at, sum, smallest, part_max[4];
+};
+template <int THREADS, bool RACE, typename T> __device__ __forceinline__ Share first_pass(const T* row, const float* noise, int vocab, float unit)
+{
+    Best top{-INFINITY, kNone};
+    float part_max[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    float at = -kFar, sum = 0.f;              // a share with nothing in it does not raise its wavefront's reference
+    uint32_t index = kNone;
+    float win_w = 0.f, win_q = 1.f, smallest = 1.f;
+    batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
+        float q[16];
+        if constexpr (RACE) {
+            if constexpr (n == 1) q[0] = noise[i];
+            else {
+#pragma unroll
+                for (int e = 0; e < n; e += 4) {
+                    const f32x4 v = *(const f32x4*)(noise + in_batch<THREADS, T>(i, e));
+                    q[e] = v[0], q[e + 1] = v[1], q[e + 2] = v[2], q[e + 3] = v[3];
+                }
+            }
+        }
+        float high[4];
+#pragma unroll
+        for (int e = 0; e < n; ++e) high[e / 4] = e % 4 ? fmaxf(high[e / 4], x[e]) : x[e];
+        constexpr int kParts = (n + 3) / 4;
+        if constexpr (!RACE) {
+#pragma unroll
+            for (int j = 0; j < kParts; ++j) part_max[j] = fmaxf(part_max[j], high[j]);
+        }
+#pragma unroll
+        for (int j = 1; j < kParts; ++j) high[0] = fmaxf(high[0], high[j]);
+        if (high[0] > top.score) {
+            uint32_t where = 0;
+#pragma unroll
+            for (int e = n - 1; e >= 0; --e) where = x[e] == high[0] ? in_batch<THREADS, T>(i, e) : where;
+            const float now = fmaxf(high[0] * unit, -kFar), keep = exp2_fast(at - now);
+            sum = top.index == kNone ? 0.f : sum * keep;
+            if constexpr (RACE) win_w = top.index == kNone ? 0.f : win_w * keep;
+            at = now;
+            top = Best{high[0], where};
+        }
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+            const float w = exp2_fast(__builtin_fmaf(x[e], unit, -at));
+            sum += w;
+            if constexpr (RACE) {
+                smallest = fminf(smallest, q[e]);
+                const bool wins = (q[e] >= 0.f) & (w * win_q > win_w * q[e]);
+                win_w = wins ? w : win_w;
+                win_q = wins ? q[e] : win_q;
+                index = wins ? in_batch<THREADS, T>(i, e) : index;
+            }
+        }
+    });
+    return Share{top, Best{index == kNone ? -INFINITY : log2f(win_w) - log2f(win_q), index}, at, sum, smallest, {part_max[0], part_max[1], part_max[2], part_max[3]}};
+}
+
 // A workgroup per row.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
@@ -471,83 +586,63 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
     const float* const noise = s.noise ? s.noise + r * s.noise_stride : nullptr;
     const float temperature = s.temperature ? s.temperature[r] : 1.f;
     const bool greedy = !(temperature > 0.f) || !noise;
-    const float div = temperature > 0.f ? temperature : 1.f;
+    const float unit = fminf(fmaxf(1.44269504088896340736f / (temperature > 0.f ? temperature : 1.f), 1.4e-45f), 3.402823466e38f);      // neither 0 nor inf for any temperature
     const int32_t top_k = s.top_k ? s.top_k[r] : 0;
     const float top_p = s.top_p ? s.top_p[r] : 1.f, min_p = s.min_p ? s.min_p[r] : 0.f;
+    const bool cut = top_k > 0 && top_k < vocab;
 
     // One pass: the largest logit and where it is, and the sum of the weights relative to it, which is scaled down whenever a thread
-    // meets a larger one.
-    const float unit = fminf(fmaxf(1.44269504088896340736f / div, 1.4e-45f), 3.402823466e38f);      // neither 0 nor inf for any temperature
-    Best top{-INFINITY, kNone};
-    float part_max[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    // Weights relative to 2^at: x unit - at in one rounding, whatever number `at` is.  It follows the largest logit so far, but not below
-    // -2^20: masks of the type's lowest value weigh nothing then, and what a rounding of `at` leaves of the largest weight stays near 1.
-    constexpr float kFar = 1048576.f;
-    float at = -kFar, sum = 0.f;              // a share with nothing in it does not raise its wavefront's reference
-    batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
-        float high[4];
-#pragma unroll
-        for (int e = 0; e < n; ++e) high[e / 4] = e % 4 ? fmaxf(high[e / 4], x[e]) : x[e];
-        constexpr int kParts = (n + 3) / 4;
-#pragma unroll
-        for (int j = 0; j < kParts; ++j) part_max[j] = fmaxf(part_max[j], high[j]);
-#pragma unroll
-        for (int j = 1; j < kParts; ++j) high[0] = fmaxf(high[0], high[j]);
-        if (high[0] > top.score) {
-            uint32_t where = 0;
-#pragma unroll
-            for (int e = n - 1; e >= 0; --e) where = x[e] == high[0] ? in_batch<THREADS, T>(i, e) : where;
-            const float now = fmaxf(high[0] * unit, -kFar);
-            sum = top.index == kNone ? 0.f : sum * exp2_fast(at - now);
-            at = now;
-            top = Best{high[0], where};
-        }
-#pragma unroll
-        for (int e = 0; e < n; ++e) sum += exp2_fast(__builtin_fmaf(x[e], unit, -at));
-    });
-    // one barrier for the place of the largest, and for the sums, which are brought to a common reference on the way
-    float all = 0.f;
+    // meets a larger one.  Where all tokens are in the race, for all that is known yet, it is run beside that on the same weights.
+    const bool at_once = !greedy && !cut && !(min_p > 0.f);
+    Share own = at_once ? first_pass<THREADS, true>(row, noise, vocab, unit) : first_pass<THREADS, false>(row, noise, vocab, unit);
+    Best top, first{-INFINITY, kNone};
+    float all, mass = 0.f, reference;         // sums of weights and of near_weights
+    bool far, near = true;
     {
 #pragma clang fp contract(off)                // the reference is the rounded product in every use
-        float high = at;
+        // one barrier for all of it; what is relative to something is brought to a common reference on the way
+        Record part{wave_best(own.top), first, own.at, 0.f, (uint32_t)__any(!(own.sum < INFINITY)), (uint32_t)__any(own.smallest < kTiny)};
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) high = fmaxf(high, __shfl_xor(high, d, 64));
-        const bool odd = __any(!(sum < INFINITY));
-        sum = wave_sum(top.index == kNone ? 0.f : sum * exp2_fast(at - high));
-        top = wave_best(top);
-        if (lane == 0) {
-            sh.best[0][wid] = top;
-            sh.sums[0][wid] = make_float4(high, sum, odd ? 1.f : 0.f, 0.f);
+        for (int d = 32; d > 0; d >>= 1) part.at = fmaxf(part.at, __shfl_xor(part.at, d, 64));
+        part.sum = wave_sum(own.top.index == kNone ? 0.f : own.sum * exp2_fast(own.at - part.at));
+        if (at_once) {
+            own.won.score += own.at - part.at;
+            part.won = wave_best(own.won);
         }
-        set = 1;
+        if (lane == 0) sh.record[wid] = part;
         __syncthreads();
-        bool any_odd = false;
-        top = sh.best[0][0];
+        top = sh.record[0].top;
 #pragma unroll
-        for (int w = 1; w < Shared<THREADS>::kWaves; ++w) top = better(top, sh.best[0][w]);
-        const float reference = top.score * unit;
+        for (int w = 1; w < Shared<THREADS>::kWaves; ++w) top = better(top, sh.record[w].top);
+        reference = top.score * unit;
+        const float factor = __builtin_fmaf(top.score, unit, -reference);     // log2 of the largest logit's near_weight
+        far = !(fabsf(reference) < kFar);
 #pragma unroll
         for (int w = 0; w < Shared<THREADS>::kWaves; ++w) {
-            const float4 v = sh.sums[0][w];
-            all += v.y * exp2_fast(v.x - reference);
-            any_odd |= v.z > 0.f;
+            const Record v = sh.record[w];
+            mass += v.sum * exp2_fast(v.at - reference);
+            far |= v.odd != 0;
+            near &= v.tiny == 0;
+            if (at_once) first = better(first, Best{v.won.score + (v.at - reference) - factor, v.won.index});
         }
-        all *= exp2_fast(-__builtin_fmaf(top.score, unit, -reference));       // relative to the largest logit's weight
-        if (any_odd || !(fabsf(reference) < kFar)) {
-            // NaN among the logits, infinite ones, numbers too large for that, or none at all
-            top = Best{-INFINITY, kNone};
-            each<THREADS>(row, vocab, [&](float raw, uint32_t i) {
-                const float x = number(raw);
-                if (x > top.score) top = Best{x, i};
-            });
-            part_max[0] = top.score;
-            part_max[1] = part_max[2] = part_max[3] = -INFINITY;
-            top = block_best(top, sh, set);
-            const Scale scale{top.score, unit};
-            all = 0.f;
-            each<THREADS>(row, vocab, [&](float raw, uint32_t) { all += number(raw) > -INFINITY ? scale.weight(raw) : 0.f; });
-            all = block_sum(all, sh, set);
-        }
+        own.won.score += part.at - reference - factor;
+        all = mass * exp2_fast(-factor);
+    }
+    if (far || !near || !(first.score > -40.f)) first.index = kNone;
+    if (far) {
+        // NaN among the logits, infinite ones, numbers too large for that, or none at all
+        top = Best{-INFINITY, kNone};
+        each<THREADS>(row, vocab, [&](float raw, uint32_t i) {
+            const float x = number(raw);
+            if (x > top.score) top = Best{x, i};
+        });
+        own.part_max[0] = top.score;
+        own.part_max[1] = own.part_max[2] = own.part_max[3] = -INFINITY;
+        top = block_best(top, sh, set);
+        const Scale scale{top.score, unit, 0.f, true};
+        all = 0.f;
+        each<THREADS>(row, vocab, [&](float raw, uint32_t) { all += number(raw) > -INFINITY ? scale.weight(raw) : 0.f; });
+        all = mass = block_sum(all, sh, set);
     }
     if (top.index == kNone) {
         if (tid == 0) {
@@ -556,20 +651,30 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
         }
         return;
     }
-    const Scale scale{top.score, unit};
+    const Scale scale{top.score, unit, reference, far};
 
     uint32_t token = top.index;
     if (!greedy) {
-        const bool cut = top_k > 0 && top_k < vocab;
         token = kNone;
-        if (cut && top_k <= min(kMostTopK, 2 * THREADS)) token = from_list(row, noise, vocab, part_max, (uint32_t)top_k, top_p, min_p, scale, sh);
+        if (cut && top_k <= min(kMostTopK, 2 * THREADS)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) count_part(own.part_max[j], scale, sh);
+            const float least = bound_of((uint32_t)top_k, scale, sh);
+            collect<THREADS>(row, vocab, least, &sh.n_candidates, sh.candidate);
+            __syncthreads();
+            const uint32_t n = sh.n_candidates;
+            // more tokens may reach the bound, because many are equal or because the bins do not reach as far
+            if (n <= kMostCandidates) token = from_list(n, noise, (uint32_t)top_k, top_p, min_p, scale, sh);
+        }
         if (token == kNone) {
             Front last{-INFINITY, kNone};
-            float mass = all;
             if (cut) {
                 last = front_of(row, vocab, (uint32_t)top_k, sh);
                 mass = 0.f;
-                each<THREADS>(row, vocab, [&](float x, uint32_t i) { mass += (last.holds(x, i) & (x > -INFINITY)) ? scale.weight(x) : 0.f; });
+                each<THREADS>(row, vocab, [&](float x, uint32_t i) {
+                    const float w = far ? scale.weight(x) : scale.near_weight(x);
+                    mass += (last.holds(x, i) & (x > -INFINITY)) ? w : 0.f;
+                });
                 mass = block_sum(mass, sh, set);
             }
             if (top_p < 1.f) {
@@ -578,7 +683,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
                 const float least = top.score + log2f(0.25f * (1.f - fmaxf(top_p, 0.f)) * mass / (float)vocab) / unit;
                 if (least > last.x) last = Front{least, kNone};
             }
-            token = race(row, noise, vocab, top.index, last, top_p, mass, min_p, scale, sh, set);
+            token = race(row, noise, vocab, top.index, last, top_p, mass, min_p, scale, first, own.won, sh, set);
         }
     }
     if (tid == 0) {
