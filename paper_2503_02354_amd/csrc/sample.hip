@@ -64,19 +64,20 @@ struct Record {
     uint32_t odd, tiny;
 };
 
-constexpr int kMostCandidates = 4096, kMostTopK = 1536, kBins = 512, kPairs = 640;       // the list is sorted in powers of two
+constexpr int kMostCandidates = 4096, kMostBorder = 1024, kPairs = 256, kBins = 512;
 template <int THREADS> struct Shared {
     static constexpr int kWaves = THREADS / 64;
     // a wavefront's part of a reduction; two sets in turn, so that one barrier is enough
     Best best[2][kWaves];
-    float4 sums[2][kWaves];
+    float2 sums[2][kWaves];
     Record record[kWaves];
     uint32_t hist[kBins];
-    uint32_t pick;
-    uint32_t n_candidates;
-    alignas(16) unsigned long long candidate[kMostCandidates + 4];
-    float weight[kMostTopK], score[kMostTopK];
-    uint32_t index[kMostTopK];
+    uint32_t pick, before_pick;
+    uint32_t n_candidates, n_border;
+    alignas(16) unsigned long long candidate[kMostCandidates];
+    alignas(16) unsigned long long border[kMostBorder + 4];
+    float weight[kPairs], score[kPairs];      // of a short list, in order
+    uint32_t index[kPairs];
 };
 
 __device__ __forceinline__ Best wave_best(Best v)
@@ -105,9 +106,9 @@ template <int THREADS> __device__ __forceinline__ Best block_best(Best v, Shared
 }
 template <int THREADS> __device__ __forceinline__ float2 block_sums(float2 v, Shared<THREADS>& sh, int& set)
 {
-    float4* const part = sh.sums[set++ & 1];
+    float2* const part = sh.sums[set++ & 1];
     v = make_float2(wave_sum(v.x), wave_sum(v.y));
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float4(v.x, v.y, 0.f, 0.f);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     v = make_float2(0.f, 0.f);
 #pragma unroll
@@ -117,6 +118,20 @@ template <int THREADS> __device__ __forceinline__ float2 block_sums(float2 v, Sh
 template <int THREADS> __device__ __forceinline__ float block_sum(float v, Shared<THREADS>& sh, int& set)
 {
     return block_sums(make_float2(v, 0.f), sh, set).x;
+}
+
+// Sums whose terms are whole numbers do not depend on their order.
+template <int THREADS> __device__ __forceinline__ unsigned long long block_count(unsigned long long v, Shared<THREADS>& sh, int& set)
+{
+    unsigned long long* const part = (unsigned long long*)sh.sums[set++ & 1];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < Shared<THREADS>::kWaves; ++w) v += part[w];
+    return v;
 }
 
 // The row in batches, this thread's share: f(x[], n, first index) for n logits as they are (NaN too), W at a time from 16 bytes (in_batch
@@ -378,22 +393,15 @@ template <int THREADS, typename T> __device__ Front front_of(const T* row, int v
 
 // A small top_k from a short list.  Every thread has met the largest logits of parts of its share; with at least top_k of all these
 // at or above a bound, so are the first top_k tokens.  One pass collects what reaches the bound (little more than top_k tokens),
-// which then is put in order, and the filters are decided on it.  The bound is the edge of a bin of the distances from the largest
-// logit, 64 bins to an octave of 1 + distance.
+// and the filters are decided on that.  The bound is the edge of a bin of the distances from the largest logit, 64 bins to an octave
+// of 1 + distance.
 constexpr uint32_t kOne = 0x3F800000u, kBinShift = 17;
-template <int THREADS> __device__ __forceinline__ void count_part(float part_max, Scale scale, Shared<THREADS>& sh)
-{
-    const float v = 1.f - scale.rel2(part_max);
-    if (part_max > -INFINITY) atomicAdd(&sh.hist[min(kBins - 1u, (__float_as_uint(v) - kOne) >> kBinShift)], 1u);
-}
-// the bound, from the counted parts
-template <int THREADS> __device__ __forceinline__ float bound_of(uint32_t top_k, Scale scale, Shared<THREADS>& sh)
+__device__ __forceinline__ uint32_t bin_of(float x, Scale scale) { return min(kBins - 1u, (__float_as_uint(1.f - scale.rel2(x)) - kOne) >> kBinShift); }
+// the bin that holds the top_k-th of those counted (the last one if there are fewer), and how many lie in those before it
+template <int THREADS> __device__ __forceinline__ void pick_bin(uint32_t top_k, Shared<THREADS>& sh)
 {
     const int tid = threadIdx.x, lane = tid & 63;
-    if (tid == 0) {
-        sh.n_candidates = 0;
-        sh.pick = kBins - 1;
-    }
+    if (tid == 0) sh.pick = kBins - 1;
     __syncthreads();
     if (tid < 64) {                           // lane l holds bins 8 l .. 8 l + 7
         constexpr int kPer = kBins / 64;
@@ -409,19 +417,29 @@ template <int THREADS> __device__ __forceinline__ float bound_of(uint32_t top_k,
         before -= sum;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            if (before < top_k && before + h[j] >= top_k) sh.pick = (uint32_t)(kPer * lane + j);
+            if (before < top_k && before + h[j] >= top_k) {
+                sh.pick = (uint32_t)(kPer * lane + j);
+                sh.before_pick = before;
+            }
             before += h[j];
         }
     }
     __syncthreads();
+}
+template <int THREADS, typename T>
+__device__ __forceinline__ uint32_t collect(const T* row, int vocab, const float (&own_max)[4], uint32_t top_k, Scale scale, Shared<THREADS>& sh)
+{
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (own_max[j] > -INFINITY) atomicAdd(&sh.hist[bin_of(own_max[j], scale)], 1u);
+    if (tid == 0) sh.n_candidates = sh.n_border = 0;
+    pick_bin(top_k, sh);
     // the bin's far edge as a logit, a little further out than any rounding of the distances reaches
     const uint32_t bin = sh.pick;
     const float far = (__uint_as_float(kOne + ((bin + 1) << kBinShift)) * 1.00001f - 1.f) / scale.per2;
-    return bin == kBins - 1 || !(scale.top < INFINITY) ? -INFINITY : scale.top - far * 1.00001f - fabsf(scale.top) * 1e-6f;
-}
-template <int THREADS, typename T>
-__device__ __forceinline__ void collect(const T* row, int vocab, float least, uint32_t* count, unsigned long long* list)
-{
+    const float least = bin == kBins - 1 || !(scale.top < INFINITY) ? -INFINITY : scale.top - far * 1.00001f - fabsf(scale.top) * 1e-6f;
+    for (int b = tid; b < kBins; b += THREADS) sh.hist[b] = 0;          // for the list's own bins
     batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
         float high = x[0];
 #pragma unroll
@@ -430,57 +448,38 @@ __device__ __forceinline__ void collect(const T* row, int vocab, float least, ui
 #pragma unroll
         for (int e = 0; e < n; ++e)
             if (x[e] >= least && x[e] > -INFINITY) {
-                const uint32_t at = atomicAdd(count, 1u);
-                if (at < kMostCandidates) list[at] = order_of(x[e], in_batch<THREADS, T>(i, e));
+                const uint32_t at = atomicAdd(&sh.n_candidates, 1u);
+                if (at < kMostCandidates) sh.candidate[at] = order_of(x[e], in_batch<THREADS, T>(i, e));
             }
     });
+    __syncthreads();
+    return sh.n_candidates;
 }
-// The token of a list of n tokens that holds the first top_k; wavefront 0 has it.
+// The token of a list of n tokens that holds the first top_k, n <= kPairs; wavefront 0 has it.  The list is put in order by comparing
+// all pairs, so that the order which atomics gave it has no say in anything, and one wavefront goes through it.
 template <int THREADS>
-__device__ uint32_t from_list(uint32_t n, const float* noise, uint32_t top_k, float top_p, float min_p, Scale scale, Shared<THREADS>& sh)
+__device__ uint32_t from_short_list(uint32_t n, const float* noise, uint32_t top_k, float top_p, float min_p, Scale scale, Shared<THREADS>& sh)
 {
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-    // The list in order; the order that atomics gave it has no say in anything below.  Few are ranked by comparing all pairs, more are
-    // sorted: one row of 50,001, us by pairs / sorted: 24.0 / 27.3 with a list of 450, 50.9 / 41.6 with one of 1400.
-    auto keep = [&](uint32_t rank, unsigned long long o) {
-        const float z = scale.rel2(logit_of((uint32_t)(o >> 32)));
-        sh.weight[rank] = exp2_fast(z);
-        sh.score[rank] = z - log2f(noise[~(uint32_t)o]);
-        sh.index[rank] = ~(uint32_t)o;
-    };
-    if (n <= kPairs) {
-        if (tid < 3) sh.candidate[n + tid] = 0;
-        __syncthreads();
-        for (uint32_t c = tid; c < n; c += THREADS) {
-            const unsigned long long o = sh.candidate[c];
-            uint32_t rank = 0;
-            for (uint32_t j = 0; j < n; j += 4) {         // the places up to the next multiple of four hold zeros
-                const ulonglong2 a = *(const ulonglong2*)&sh.candidate[j], b = *(const ulonglong2*)&sh.candidate[j + 2];
-                rank += (a.x > o) + (a.y > o) + (b.x > o) + (b.y > o);
-            }
-            if (rank < top_k) keep(rank, o);
+    if (tid < 3) sh.candidate[n + tid] = 0;
+    __syncthreads();
+    if (tid < n) {
+        const unsigned long long o = sh.candidate[tid];
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < n; j += 4) {             // the places up to the next multiple of four hold zeros
+            const ulonglong2 a = *(const ulonglong2*)&sh.candidate[j], b = *(const ulonglong2*)&sh.candidate[j + 2];
+            rank += (a.x > o) + (a.y > o) + (b.x > o) + (b.y > o);
         }
-    } else {
-        const uint32_t size = 1u << (32 - __builtin_clz(n - 1));
-        for (uint32_t i = n + tid; i < size; i += THREADS) sh.candidate[i] = 0;
-        for (uint32_t run = 2; run <= size; run <<= 1)
-            for (uint32_t step = run >> 1; step > 0; step >>= 1) {
-                __syncthreads();
-                for (uint32_t i = tid; i < size / 2; i += THREADS) {
-                    const uint32_t lo = 2 * i - (i & (step - 1)), hi = lo + step;
-                    const unsigned long long a = sh.candidate[lo], b = sh.candidate[hi];
-                    if ((a < b) == ((lo & run) == 0)) {
-                        sh.candidate[lo] = b;
-                        sh.candidate[hi] = a;
-                    }
-                }
-            }
-        __syncthreads();
-        for (uint32_t c = tid; c < min(n, top_k); c += THREADS) keep(c, sh.candidate[c]);
+        if (rank < top_k) {
+            const float z = scale.rel2(logit_of((uint32_t)(o >> 32)));
+            sh.weight[rank] = exp2_fast(z);
+            sh.score[rank] = z - log2f(noise[~(uint32_t)o]);
+            sh.index[rank] = ~(uint32_t)o;
+        }
     }
     __syncthreads();
     const uint32_t kept = min(n, top_k);
-    // wavefront 0: the sums in the order of the ranks, 64 of them at a time; the whole sum first
+    // the sums in the order of the ranks, 64 of them at a time; the whole sum first
     if (wid > 0) return 0;
     float mass = 0.f;
     if (top_p < 1.f) {
@@ -507,6 +506,94 @@ __device__ uint32_t from_list(uint32_t n, const float* noise, uint32_t top_k, fl
     }
     win = wave_best(win);
     return win.index == kNone ? sh.index[0] : win.index;
+}
+// The same of a longer one, all wavefronts; kNone where too many equal tokens lie across the cut.  Nothing depends on the list's order:
+// tokens are compared as (logit, index), and masses are sums of whole numbers, weights in units of 2^-40.  The race goes as for whole
+// rows, but a round costs two reductions only.  96 rows of 128,000 fp32, us by pairs / in rounds: 27.4 / 32.8 with a top_k of 50 and a
+// nucleus (lists of 80), 37 / 32 with one of 400 (450); 58.7 sorted / 38.8 with one of 1000.
+template <int THREADS>
+__device__ uint32_t from_list(uint32_t n, const float* noise, uint32_t top_index, uint32_t top_k, float top_p, float min_p, Scale scale, Shared<THREADS>& sh, int& set)
+{
+    const int tid = threadIdx.x;
+    constexpr int kEach = kMostCandidates / THREADS;
+    unsigned long long o[kEach];              // 0: none
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) o[j] = tid + j * THREADS < n ? sh.candidate[tid + j * THREADS] : 0;
+    auto logit_in = [](unsigned long long v) { return logit_of((uint32_t)(v >> 32)); };
+    if (n > top_k) {                          // the cut: all before one bin, and of that bin the first
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (o[j]) atomicAdd(&sh.hist[bin_of(logit_in(o[j]), scale)], 1u);
+        __syncthreads();
+        pick_bin(top_k, sh);
+        const uint32_t pick = sh.pick, need = top_k - sh.before_pick;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (!o[j]) continue;
+            const uint32_t bin = bin_of(logit_in(o[j]), scale);
+            if (bin == pick) {
+                const uint32_t at = atomicAdd(&sh.n_border, 1u);
+                if (at < kMostBorder) sh.border[at] = o[j];
+            } else if (bin > pick)
+                o[j] = 0;
+        }
+        __syncthreads();
+        const uint32_t border = sh.n_border;
+        if (border > kMostBorder) return kNone;
+        if (border > need) {
+            if (tid < 3) sh.border[border + tid] = 0;
+            __syncthreads();
+            const unsigned long long low = need;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (!o[j] || bin_of(logit_in(o[j]), scale) != pick) continue;
+                uint32_t rank = 0;
+                for (uint32_t i = 0; i < border; i += 4) {            // the places up to the next multiple of four hold zeros
+                    const ulonglong2 a = *(const ulonglong2*)&sh.border[i], b = *(const ulonglong2*)&sh.border[i + 2];
+                    rank += (a.x > o[j]) + (a.y > o[j]) + (b.x > o[j]) + (b.y > o[j]);
+                }
+                if (rank >= low) o[j] = 0;
+            }
+        }
+    }
+    float score[kEach];
+    unsigned long long weight[kEach], mass = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        score[j] = -INFINITY;
+        weight[j] = 0;
+        if (!o[j]) continue;
+        const uint32_t index = ~(uint32_t)o[j];
+        const float z = scale.rel2(logit_in(o[j])), w = exp2_fast(z);
+        weight[j] = (unsigned long long)(w * 0x1p40f);
+        if (!(min_p > 0.f) || w >= min_p || index == top_index) score[j] = z - log2f(noise[index]);
+        mass += weight[j];
+    }
+    const bool nucleus = top_p < 1.f;
+    const double limit = nucleus ? (double)top_p * (double)block_count(mass, sh, set) : 0.;
+    for (;;) {                                // every round takes the winner and what is behind it out
+        Best win{-INFINITY, kNone};
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (score[j] > -INFINITY) win = better(win, Best{score[j], ~(uint32_t)o[j]});
+        const Best mine = win;
+        win = block_best(win, sh, set);
+        if (win.index == kNone) return top_index;
+        if (!nucleus || win.index == top_index) return win.index;
+        if (mine.index == win.index)
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (~(uint32_t)o[j] == win.index && o[j]) sh.candidate[0] = o[j];
+        __syncthreads();
+        const unsigned long long at = sh.candidate[0];
+        unsigned long long before = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            before += o[j] > at ? weight[j] : 0;
+            if (o[j] <= at) score[j] = -INFINITY;
+        }
+        if ((double)block_count(before, sh, set) < limit) return win.index;
+    }
 }
 
 // A thread's share of a row: its largest logit and where, the sum of its weights relative to 2^at, the largest logits of four parts of
@@ -656,15 +743,11 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(Sampling s)
     uint32_t token = top.index;
     if (!greedy) {
         token = kNone;
-        if (cut && top_k <= min(kMostTopK, 2 * THREADS)) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) count_part(own.part_max[j], scale, sh);
-            const float least = bound_of((uint32_t)top_k, scale, sh);
-            collect<THREADS>(row, vocab, least, &sh.n_candidates, sh.candidate);
-            __syncthreads();
-            const uint32_t n = sh.n_candidates;
+        if (cut && top_k <= 2 * THREADS) {
             // more tokens may reach the bound, because many are equal or because the bins do not reach as far
-            if (n <= kMostCandidates) token = from_list(n, noise, (uint32_t)top_k, top_p, min_p, scale, sh);
+            const uint32_t n = collect(row, vocab, own.part_max, (uint32_t)top_k, scale, sh);
+            if (n <= kPairs) token = from_short_list(n, noise, (uint32_t)top_k, top_p, min_p, scale, sh);
+            else if (n <= kMostCandidates) token = from_list(n, noise, top.index, (uint32_t)top_k, top_p, min_p, scale, sh, set);
         }
         if (token == kNone) {
             Front last{-INFINITY, kNone};
