@@ -68,17 +68,21 @@ struct Span {
     __device__ __forceinline__ int first_tile() const { return begin / kKeys; }
     __device__ __forceinline__ int tiles() const { return rows == 0 ? 0 : max(1, (end + kKeys - 1) / kKeys - begin / kKeys); }
 };
+__device__ __forceinline__ Span make_span(int m, int first_pos, int group, int window)
+{
+    Span s;
+    s.m = m;
+    s.rows = m * group;
+    s.first_pos = first_pos;
+    s.end = max(0, first_pos + m);
+    s.begin = window > 0 ? min(s.end, max(0, max(0, first_pos) - window + 1)) : 0;      // of the largest window too
+    return s;
+}
 __device__ __forceinline__ Span span_of(const KvAttention& a, int r, int group, int table_tokens)
 {
     const int q0 = max(0, min(a.q_off[r], a.n_tokens)), q1 = max(q0, min(a.q_off[r + 1], a.n_tokens));
     const int len = max(0, min(a.seq_len[r], table_tokens)), m_all = q1 - q0;
-    Span s;
-    s.m = min(m_all, a.max_new);
-    s.rows = s.m * group;
-    s.first_pos = len - m_all;
-    s.end = max(0, min(len, s.first_pos + s.m));
-    s.begin = a.window > 0 ? min(s.end, max(0, max(0, s.first_pos) - a.window + 1)) : 0;      // of the largest window too
-    return s;
+    return make_span(min(m_all, a.max_new), len - m_all, group, a.window);
 }
 
 // Where 16-byte chunk c of row r of a V tile lies: chunks in an order that spreads both the writes (sixteen rows of
@@ -457,20 +461,20 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
     const FewHeader* const h = (const FewHeader*)workspace;
     const int r = blockIdx.x / c.kv_heads, kvh = blockIdx.x - r * c.kv_heads, group = a.heads / c.kv_heads;
     const unsigned long long first = h->base[r], tiles = h->base[r + 1] - first, per = h->per;
+    const int rows = span_of(a, r, group, a.max_blocks << c.block_shift).rows, q0 = max(0, min(a.q_off[r], a.n_tokens));      // on their way together
     if (tiles == 0) return;
     const unsigned long long begin = first * (unsigned)c.kv_heads + (unsigned)kvh * tiles, end = begin + tiles;
     const unsigned long long w0 = begin / per, w1 = (end - 1) / per;
     if (w0 == w1) return;
-    const Span s = span_of(a, r, group, a.max_blocks << c.block_shift);
     const int column = threadIdx.x % kColumns, share = threadIdx.x / kColumns;
     const int rw = blockIdx.y * kJoinRows + column / (D / 4), ch = column % (D / 4) * 4;
-    if (blockIdx.y * kJoinRows >= s.rows) return;
+    if (blockIdx.y * kJoinRows >= rows) return;
     // a stretch's first history leaves the first part, its last one the second
     const float* const parts = (const float*)(workspace + few_header_bytes(a.n_requests));
     auto part_of = [&](unsigned long long w) { return parts + (w * 2 + (begin > w * per)) * kPartFloats<D>; };
     float mx = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (rw < s.rows && share < kSplit)
+    if (rw < rows && share < kSplit)
 #pragma unroll 2
         for (unsigned long long w = w0 + share; w <= w1; w += kSplit) {
             const float* const p = part_of(w);
@@ -485,7 +489,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
     sums[threadIdx.x] = acc;
     stats[threadIdx.x] = make_float2(mx, sum);
     __syncthreads();
-    if (share > 0 || rw >= s.rows) return;
+    if (share > 0 || rw >= rows) return;
     for (int i = 1; i < kSplit; ++i) mx = fmaxf(mx, stats[i * kColumns + column].x);
     sum = 0.f;
     acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -497,7 +501,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
         sum += f * st.y;
         acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
     }
-    const int q0 = max(0, min(a.q_off[r], a.n_tokens)), tk = rw / group, hd = kvh * group + (rw - tk * group);
+    const int tk = rw / group, hd = kvh * group + (rw - tk * group);
     const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
     if (ch < c.head_dim)
         *(uint2*)(a.out + (int64_t)(q0 + tk) * a.out_token_stride + (int64_t)hd * a.out_head_stride + ch) =
@@ -518,9 +522,13 @@ constexpr int kManyGroups = 512;          // two workgroups per compute unit
 struct Unit {
     int32_t request, first_row;           // request; first query row of the tile
     int32_t tile, tiles;                  // 64-key tiles
-    int32_t part, pad[3];                 // -1, or the part of the workspace that takes the result (times kv_heads)
+    int32_t part;                         // -1, or the part of the workspace that takes the result (times kv_heads)
+    int32_t q0, m, first_pos;             // the request's first new token, how many, and its position
 };
-struct Joined { int32_t request, first_row, part, parts; };
+struct Joined {
+    int32_t first_row, part, parts, q0;
+    int32_t rows, pad[3];                 // of the request
+};
 struct ManyHeader { int32_t units, joined, pad[62]; };
 
 __host__ __device__ constexpr int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
@@ -594,22 +602,26 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
     for (int i = tid; i < kSchedBins; i += kSchedThreads) bins[i] = 0;
     if (tid == 0) n_parts = n_joined = 0;
     __syncthreads();
-    auto segment = [&](int i, int& r, int& row, int& first, int& tiles) {
-        r = 0;
+    struct Segment { int r, row, first, tiles; Span s; };
+    auto find = [&](int i) {
+        Segment g;
+        int r = 0;
         for (int hi = n; hi - r > 1;) {
             const int mid = (r + hi) >> 1;
             if (first_segment[mid] <= i) r = mid;
             else hi = mid;
         }
-        const Span s = span_of(a, r, group, table_tokens);
-        row = (i - first_segment[r]) * kManyRows;
-        tiles_of(s, a.window, group, row, first, tiles);
+        g.r = r;
+        g.s = span_of(a, r, group, table_tokens);
+        g.row = (i - first_segment[r]) * kManyRows;
+        tiles_of(g.s, a.window, group, g.row, g.first, g.tiles);
+        return g;
     };
+    const Segment own = tid < count ? find(tid) : Segment{};             // the only one in most steps
+    auto segment = [&](int i) { return i == tid ? own : find(i); };
     unsigned long long mine = 0, total;
     for (int i = tid; i < count; i += kSchedThreads) {
-        int r, row, first, tiles;
-        segment(i, r, row, first, tiles);
-        mine += (unsigned)tiles;
+        mine += (unsigned)segment(i).tiles;
     }
     (void)sum_before(mine, total);
     // no part is shorter than 8 tiles, or than what fills the chip once
@@ -619,9 +631,7 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
     while ((most >> scale) >= kSchedBins) ++scale;
     auto bin_of = [&](int tiles) { return kSchedBins - 1 - min(kSchedBins - 1, tiles >> scale); };
     for (int i = tid; i < count; i += kSchedThreads) {
-        int r, row, first, tiles;
-        segment(i, r, row, first, tiles);
-        const int parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts;
+        const int tiles = segment(i).tiles, parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts;
         atomicAdd(&bins[bin_of(each)], parts);
     }
     __syncthreads();
@@ -644,19 +654,18 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
     Unit* const units = (Unit*)(workspace + at.units);
     Joined* const joined = (Joined*)(workspace + at.joined);
     for (int i = tid; i < count; i += kSchedThreads) {
-        int r, row, first, tiles;
-        segment(i, r, row, first, tiles);
-        const int parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts;
+        const Segment g = segment(i);
+        const int tiles = g.tiles, parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts, q0 = max(0, min(a.q_off[g.r], a.n_tokens));
         const int to = atomicAdd(&bins[bin_of(each)], parts);
         int part = -1;
         if (parts > 1) {
             part = atomicAdd(&n_parts, parts);
             const int j = atomicAdd(&n_joined, 1);
-            if (j < at.most_joined) joined[j] = {r, row, part, parts};
+            if (j < at.most_joined) joined[j] = {g.row, part, parts, q0, g.s.rows, {0, 0, 0}};
         }
         for (int p = 0; p < parts; ++p) {
             const int t0 = p * each, t1 = min(tiles, t0 + each);
-            if (to + p < at.most_units) units[to + p] = {r, row, first + t0, max(0, t1 - t0), part < 0 ? -1 : part + p, {0, 0, 0}};
+            if (to + p < at.most_units) units[to + p] = {g.r, g.row, g.first + t0, max(0, t1 - t0), part < 0 ? -1 : part + p, q0, g.s.m, g.s.first_pos};
         }
     }
     __syncthreads();
@@ -678,13 +687,14 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     extern __shared__ __attribute__((aligned(4096))) char lds[];          // two buffers of K tiles, three of V
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     const int kvh = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
-    if (index >= ((const ManyHeader*)(workspace + layout.header))->units) return;
-    const Unit* const up = (const Unit*)(workspace + layout.units) + index;
-    const int r = __builtin_amdgcn_readfirstlane(up->request), row0 = __builtin_amdgcn_readfirstlane(up->first_row);
-    const int tile0 = __builtin_amdgcn_readfirstlane(up->tile), tiles = __builtin_amdgcn_readfirstlane(up->tiles), part = __builtin_amdgcn_readfirstlane(up->part);
-    const int group = a.heads / c.kv_heads, table_tokens = a.max_blocks << c.block_shift;
-    const Span s = span_of(a, r, group, table_tokens);
-    const int q0 = max(0, min(a.q_off[r], a.n_tokens));
+    // one round trip for the number of units and the unit, whose place is there in any case
+    const int units = ((const ManyHeader*)(workspace + layout.header))->units;
+    const int4 *const up = (const int4*)((const Unit*)(workspace + layout.units) + index), u0 = up[0], u1 = up[1];
+    if (index >= units) return;
+    const int r = __builtin_amdgcn_readfirstlane(u0.x), row0 = __builtin_amdgcn_readfirstlane(u0.y);
+    const int tile0 = __builtin_amdgcn_readfirstlane(u0.z), tiles = __builtin_amdgcn_readfirstlane(u0.w), part = __builtin_amdgcn_readfirstlane(u1.x);
+    const int group = a.heads / c.kv_heads, q0 = __builtin_amdgcn_readfirstlane(u1.y);
+    const Span s = make_span(__builtin_amdgcn_readfirstlane(u1.z), __builtin_amdgcn_readfirstlane(u1.w), group, a.window);
     const int chunks = c.head_dim >> 3;
 
     // this lane's query row; a negative scale moves to the queries
@@ -934,16 +944,15 @@ template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c, KvAttention a, const char* workspace, ManyLayout layout)
 {
     const int kvh = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
-    if (index >= ((const ManyHeader*)(workspace + layout.header))->joined) return;
-    const Joined u = ((const Joined*)(workspace + layout.joined))[index];
-    const int group = a.heads / c.kv_heads;
-    const Span s = span_of(a, u.request, group, a.max_blocks << c.block_shift);
-    const int q0 = max(0, min(a.q_off[u.request], a.n_tokens));
+    const int n_joined = ((const ManyHeader*)(workspace + layout.header))->joined;
+    const Joined u = ((const Joined*)(workspace + layout.joined))[index];         // its place is there in any case
+    if (index >= n_joined) return;
+    const int group = a.heads / c.kv_heads, q0 = u.q0;
     const size_t stride = (size_t)c.kv_heads * (2 * kManyRows + kManyRows * D);
     const float* const parts = (const float*)(workspace + layout.parts) + ((size_t)u.part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * D);
     for (int i = threadIdx.x; i < 16 * (D / 4); i += 256) {
         const int rw = blockIdx.y * 16 + i / (D / 4), ch = i % (D / 4) * 4, row = u.first_row + rw;
-        if (row >= s.rows) continue;
+        if (row >= u.rows) continue;
         float mx = -INFINITY, sum = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
