@@ -54,7 +54,7 @@ def attention(q, k, v, seq_len, q_off, table, block, window, scale):
         m = q_off[r + 1] - q_off[r]
         for i in range(m):
             t, pos = q_off[r] + i, seq_len[r] - m + i
-            first = max(0, pos - window + 1) if window > 0 else 0
+            first = max(0, int(pos) - window + 1) if window > 0 else 0
             if pos < 0:
                 continue
             j = np.arange(first, pos + 1)

@@ -85,6 +85,17 @@ __device__ __forceinline__ Span span_of(const KvAttention& a, int r, int group, 
     return make_span(min(m_all, a.max_new), len - m_all, group, a.window);
 }
 
+// Four channels of query row `row` of a request and cache head, from the unnormalised output relative to maximum mx.
+__device__ __forceinline__ void finish_row(const KvCache& c, const KvAttention& a, int q0, int kvh, int row, int ch, float mx, float sum, float4 acc)
+{
+    const int group = a.heads / c.kv_heads, token = row / group, head = kvh * group + (row - token * group);
+    const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+    if (ch < c.head_dim)
+        *(uint2*)(a.out + (int64_t)(q0 + token) * a.out_token_stride + (int64_t)head * a.out_head_stride + ch) =
+            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    if (a.lse && ch == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+}
+
 // Where 16-byte chunk c of row r of a V tile lies: chunks in an order that spreads both the writes (sixteen rows of
 // one chunk) and the transposing reads (four rows of four chunks) over all LDS banks.
 template <int D> constexpr int kRow = D <= 64 ? 64 : 128;     // channels that a row of D channels takes in LDS
@@ -194,17 +205,188 @@ __host__ __device__ constexpr int64_t few_header_bytes(int n_requests) { return 
 template <int D> constexpr int kPartFloats = 2 * kFewRows + kFewRows * D;
 
 template <int D> constexpr int kMergeRow = D + 4;          // floats between the rows of a wavefront's output in LDS
-template <int D> constexpr size_t kFewLds = (size_t)kFewWaves * kFewRows * kMergeRow<D> * 4;
+template <int D, int WAVES = kFewWaves> constexpr size_t kFewLds = (size_t)WAVES * kFewRows * kMergeRow<D> * 4;
+
+#if defined(__HIP_DEVICE_COMPILE__)
+// One stretch [tile, tile_stop) of 32-key tiles of a request and cache head, at most 32 query rows, by WAVES wavefronts:
+// write(row, channel, maximum, sum, four channels of the unnormalised output) gets the result, relative to the row's maximum.
+template <int D, bool PAD, int WAVES, class Write>
+__device__ __forceinline__ void few_rows(const KvCache& c, const KvAttention& a, const Span& s, int r, int kvh, int tile_begin, int tile_stop, char* lds,
+                                         float (*stat)[WAVES][kFewRows], Write write)
+{
+    constexpr int kSteps = D / 16, kBlocks = D / 32;
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int group = a.heads / c.kv_heads, q0 = max(0, min(a.q_off[r], a.n_tokens));
+    const int chunks = c.head_dim >> 3, last_step = (chunks - 1 - half) >> 1;       // this lane's last 16 bytes of a row; -1: none (8 channels)
+    const float scale2 = a.scale * 1.44269504088896340736f;
+    char* const v_lds = lds + wid * (kKeys * kRow<D> * 2);
+    const uint32_t v_tile = lds_address(v_lds), v_read = v_tile + value_base<D>(lane);
+
+    // this lane's query row
+    const int row = l32, token = row / group, head = kvh * group + (row - token * group);
+    const bool row_ok = row < s.rows;
+    const int pos = s.first_pos + token, from = a.window > 0 ? pos - a.window : -1;       // sees keys from < j <= pos
+    bf16x8 qf[kSteps];
+    {
+        const uint16_t* qp = a.q + (int64_t)(q0 + (row_ok ? token : 0)) * a.q_token_stride + (int64_t)(row_ok ? head : 0) * a.q_head_stride + half * 8;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) {
+            u32x4 w = {0, 0, 0, 0};
+            if (row_ok && (!PAD || 2 * ks + half < chunks)) w = *(const u32x4*)(qp + ks * 16);
+            qf[ks] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+    float m = -INFINITY, l = 0.f;
+    f32x16 o[kBlocks];
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[db][x] = 0.f;
+
+    const int32_t* const ids = a.table + (size_t)r * a.max_blocks;
+    const int64_t lane_at = kvh * c.head_stride + (PAD && last_step < 0 ? 0 : half * 8);
+    const uint16_t *const k_base = c.k + lane_at, *const v_base = c.v + lane_at;
+    auto id_of = [&](int tile) {      // block of this lane's key of a tile; -1: reads as zeros
+        const int key = tile * kKeys + l32;
+        int id = -1;
+        if (key >= s.begin && key < s.end) id = ids[key >> c.block_shift];
+        return (uint32_t)id < (uint32_t)c.n_blocks ? id : -1;
+    };
+    auto offset_of = [&](int tile, int id) {
+        const int key = tile * kKeys + l32;
+        return id < 0 ? (int64_t)0 : id * c.block_stride + (key & ((1 << c.block_shift) - 1)) * c.token_stride;
+    };
+    auto fetch = [&](const uint16_t* p, u32x4 (&w)[kSteps]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) w[ks] = *(const u32x4*)(p + (PAD ? max(0, min(ks, last_step)) : ks) * 16);
+    };
+    u32x4 kw[kSteps], vw[kSteps];
+    int tile = tile_begin + wid;
+    int id = -1, id_next = -1;
+    if (tile < tile_stop) {
+        id = id_of(tile);
+        const int64_t at = offset_of(tile, id);
+        fetch(k_base + at, kw);
+        fetch(v_base + at, vw);
+        if (tile + WAVES < tile_stop) id_next = id_of(tile + WAVES);
+    }
+    for (; tile < tile_stop; tile += WAVES) {
+        const bool more = tile + WAVES < tile_stop;
+        if (__any(id < 0)) {          // rows outside the history, blocks outside the cache
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) {
+                kw[ks] = id < 0 ? u32x4{0, 0, 0, 0} : kw[ks];
+                vw[ks] = id < 0 ? u32x4{0, 0, 0, 0} : vw[ks];
+            }
+        }
+        if (PAD)                      // what was read in the place of channels that are not there; the values' have results of their own
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) kw[ks] = ks <= last_step ? kw[ks] : u32x4{0, 0, 0, 0};
+        f32x16 sc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw[ks]), qf[ks], sc, 0, 0, 0);
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) *(u32x4*)(v_lds + v_slot<D>(l32, 2 * ks + half)) = vw[ks];
+        if (more) {
+            id = id_next;
+            const int64_t at = offset_of(tile + WAVES, id);
+            fetch(k_base + at, kw);
+            fetch(v_base + at, vw);
+            if (tile + 2 * WAVES < tile_stop) id_next = id_of(tile + 2 * WAVES);
+        }
+        const int key0 = tile * kKeys;
+        const bool masked = key0 + kKeys - 1 > s.first_pos || key0 < s.begin || (a.window > 0 && key0 <= s.first_pos + s.m - 1 - a.window);
+        float top = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            sc[x] *= scale2;
+            const int key = key0 + 8 * (x >> 2) + 4 * half + (x & 3);
+            if (masked) sc[x] = row_ok && key <= pos && key > from && key >= 0 ? sc[x] : -INFINITY;
+            top = fmaxf(top, sc[x]);
+        }
+        top = max_halves(top);
+        const float m_new = fmaxf(m, top);
+        if (__any(m_new > m)) {
+            const float shrink = m_new == m ? 1.f : exp2_fast(m - m_new);
+            l *= shrink;
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[db][x] *= shrink;
+            m = m_new;
+        }
+        const float m_use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            sc[x] = exp2_fast(sc[x] - m_use);
+            l += sc[x];
+        }
+        u32x4 pw[2];
+#pragma unroll
+        for (int x = 0; x < 16; x += 2) pw[x >> 3][(x >> 1) & 3] = pack_bf16(sc[x], sc[x + 1]);
+        if (masked && s.m > 1) {
+            const uint32_t odd = odd_keys<D>(v_tile);
+            if (odd) {                    // the tile is this wavefront's own: their rows are made zeros
+                add_odd_values<D>(o, v_tile, odd, pw, [&](int j) { return row_ok && key0 + j <= pos && key0 + j > from; });
+                if (odd >> l32 & 1)
+                    for (int ch = half; ch < kRow<D> / 8; ch += 2) *(__attribute__((address_space(3))) u32x4*)(v_tile + v_slot<D>(l32, ch)) = u32x4{0, 0, 0, 0};
+            }
+        }
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2) {
+            u32x4 v[kBlocks];
+            read_values<D>(v, v_read, t2);
+            add_values<D>(o, v, pw[t2]);
+        }
+    }
+    l = sum_halves(l);
+
+    // the wavefronts' results
+    __syncthreads();
+    float* const mine = (float*)lds + wid * kFewRows * kMergeRow<D> + l32 * kMergeRow<D>;
+    if (row_ok) {
+#pragma unroll
+        for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(float4*)(mine + db * 32 + g * 8 + half * 4) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+    }
+    if (half == 0) {
+        stat[0][wid][l32] = m;
+        stat[1][wid][l32] = l;
+    }
+    __syncthreads();
+    for (int i = tid; i < s.rows * (D / 4); i += 64 * WAVES) {
+        const int rw = i / (D / 4), ch = (i - rw * (D / 4)) * 4;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, stat[0][w][rw]);
+        float sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float mw = stat[0][w][rw];
+            if (mw == -INFINITY) continue;
+            const float f = mw == mx ? 1.f : exp2_fast(mw - mx);
+            const float4 v = *(const float4*)((const float*)lds + (w * kFewRows + rw) * kMergeRow<D> + ch);
+            sum += f * stat[1][w][rw];
+            acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
+        }
+        write(rw, ch, mx, sum, acc);
+    }
+}
+#endif
 
 template <int D, bool PAD>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvCache c, KvAttention a, char* workspace)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kSteps = D / 16, kBlocks = D / 32;
     extern __shared__ __attribute__((aligned(4096))) char lds[];
     __shared__ float stat[2][kFewWaves][kFewRows];
     __shared__ unsigned long long part_sum[kFewWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = a.heads / c.kv_heads, table_tokens = a.max_blocks << c.block_shift, n = a.n_requests;
 
     // tiles before every request
@@ -253,10 +435,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
     unsigned long long into = now - base[r] * (unsigned)c.kv_heads;       // tiles of this request that others did
     __syncthreads();
 
-    const int chunks = c.head_dim >> 3, last_step = (chunks - 1 - half) >> 1;       // this lane's last 16 bytes of a row; -1: none (8 channels)
-    const float scale2 = a.scale * 1.44269504088896340736f;
-    char* const v_lds = lds + wid * (kKeys * kRow<D> * 2);
-    const uint32_t v_tile = lds_address(v_lds), v_read = v_tile + value_base<D>(lane);
     const unsigned long long start = now;
 
     while (now < stop && r < n) {
@@ -271,180 +449,38 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
         const int t_end = (int)min((unsigned long long)tiles, t_begin + (stop - now)), first = s.first_tile();
         const int q0 = max(0, min(a.q_off[r], a.n_tokens));
 
-        // this lane's query row
-        const int row = l32, token = row / group, head = kvh * group + (row - token * group);
-        const bool row_ok = row < s.rows;
-        const int pos = s.first_pos + token, from = a.window > 0 ? pos - a.window : -1;       // sees keys from < j <= pos
-        bf16x8 qf[kSteps];
-        {
-            const uint16_t* qp = a.q + (int64_t)(q0 + (row_ok ? token : 0)) * a.q_token_stride + (int64_t)(row_ok ? head : 0) * a.q_head_stride + half * 8;
-#pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) {
-                u32x4 w = {0, 0, 0, 0};
-                if (row_ok && (!PAD || 2 * ks + half < chunks)) w = *(const u32x4*)(qp + ks * 16);
-                qf[ks] = __builtin_bit_cast(bf16x8, w);
-            }
-        }
-        float m = -INFINITY, l = 0.f;
-        f32x16 o[kBlocks];
-#pragma unroll
-        for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) o[db][x] = 0.f;
-
-        const int32_t* const ids = a.table + (size_t)r * a.max_blocks;
-        const int64_t lane_at = kvh * c.head_stride + (PAD && last_step < 0 ? 0 : half * 8);
-        const uint16_t *const k_base = c.k + lane_at, *const v_base = c.v + lane_at;
-        auto id_of = [&](int tile) {      // block of this lane's key of a tile; -1: reads as zeros
-            const int key = tile * kKeys + l32;
-            int id = -1;
-            if (key >= s.begin && key < s.end) id = ids[key >> c.block_shift];
-            return (uint32_t)id < (uint32_t)c.n_blocks ? id : -1;
-        };
-        auto offset_of = [&](int tile, int id) {
-            const int key = tile * kKeys + l32;
-            return id < 0 ? (int64_t)0 : id * c.block_stride + (key & ((1 << c.block_shift) - 1)) * c.token_stride;
-        };
-        auto fetch = [&](const uint16_t* p, u32x4 (&w)[kSteps]) __attribute__((always_inline)) {
-#pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) w[ks] = *(const u32x4*)(p + (PAD ? max(0, min(ks, last_step)) : ks) * 16);
-        };
-        u32x4 kw[kSteps], vw[kSteps];
-        int tile = first + t_begin + wid;
-        const int tile_stop = first + t_end;
-        int id = -1, id_next = -1;
-        if (tile < tile_stop) {
-            id = id_of(tile);
-            const int64_t at = offset_of(tile, id);
-            fetch(k_base + at, kw);
-            fetch(v_base + at, vw);
-            if (tile + kFewWaves < tile_stop) id_next = id_of(tile + kFewWaves);
-        }
-        for (; tile < tile_stop; tile += kFewWaves) {
-            const bool more = tile + kFewWaves < tile_stop;
-            if (__any(id < 0)) {          // rows outside the history, blocks outside the cache
-#pragma unroll
-                for (int ks = 0; ks < kSteps; ++ks) {
-                    kw[ks] = id < 0 ? u32x4{0, 0, 0, 0} : kw[ks];
-                    vw[ks] = id < 0 ? u32x4{0, 0, 0, 0} : vw[ks];
-                }
-            }
-            if (PAD)                      // what was read in the place of channels that are not there; the values' have results of their own
-#pragma unroll
-                for (int ks = 0; ks < kSteps; ++ks) kw[ks] = ks <= last_step ? kw[ks] : u32x4{0, 0, 0, 0};
-            f32x16 sc;
-#pragma unroll
-            for (int x = 0; x < 16; ++x) sc[x] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kw[ks]), qf[ks], sc, 0, 0, 0);
-#pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) *(u32x4*)(v_lds + v_slot<D>(l32, 2 * ks + half)) = vw[ks];
-            if (more) {
-                id = id_next;
-                const int64_t at = offset_of(tile + kFewWaves, id);
-                fetch(k_base + at, kw);
-                fetch(v_base + at, vw);
-                if (tile + 2 * kFewWaves < tile_stop) id_next = id_of(tile + 2 * kFewWaves);
-            }
-            const int key0 = tile * kKeys;
-            const bool masked = key0 + kKeys - 1 > s.first_pos || key0 < s.begin || (a.window > 0 && key0 <= s.first_pos + s.m - 1 - a.window);
-            float top = -INFINITY;
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                sc[x] *= scale2;
-                const int key = key0 + 8 * (x >> 2) + 4 * half + (x & 3);
-                if (masked) sc[x] = row_ok && key <= pos && key > from && key >= 0 ? sc[x] : -INFINITY;
-                top = fmaxf(top, sc[x]);
-            }
-            top = max_halves(top);
-            const float m_new = fmaxf(m, top);
-            if (__any(m_new > m)) {
-                const float shrink = m_new == m ? 1.f : exp2_fast(m - m_new);
-                l *= shrink;
-#pragma unroll
-                for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) o[db][x] *= shrink;
-                m = m_new;
-            }
-            const float m_use = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                sc[x] = exp2_fast(sc[x] - m_use);
-                l += sc[x];
-            }
-            u32x4 pw[2];
-#pragma unroll
-            for (int x = 0; x < 16; x += 2) pw[x >> 3][(x >> 1) & 3] = pack_bf16(sc[x], sc[x + 1]);
-            if (masked && s.m > 1) {
-                const uint32_t odd = odd_keys<D>(v_tile);
-                if (odd) {                    // the tile is this wavefront's own: their rows are made zeros
-                    add_odd_values<D>(o, v_tile, odd, pw, [&](int j) { return row_ok && key0 + j <= pos && key0 + j > from; });
-                    if (odd >> l32 & 1)
-                        for (int ch = half; ch < kRow<D> / 8; ch += 2) *(__attribute__((address_space(3))) u32x4*)(v_tile + v_slot<D>(l32, ch)) = u32x4{0, 0, 0, 0};
-                }
-            }
-#pragma unroll
-            for (int t2 = 0; t2 < 2; ++t2) {
-                u32x4 v[kBlocks];
-                read_values<D>(v, v_read, t2);
-                add_values<D>(o, v, pw[t2]);
-            }
-        }
-        l = sum_halves(l);
-
-        // the four wavefronts' results
-        __syncthreads();
-        float* const mine = (float*)lds + wid * kFewRows * kMergeRow<D> + l32 * kMergeRow<D>;
-        if (row_ok) {
-#pragma unroll
-            for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *(float4*)(mine + db * 32 + g * 8 + half * 4) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
-        }
-        if (half == 0) {
-            stat[0][wid][l32] = m;
-            stat[1][wid][l32] = l;
-        }
-        __syncthreads();
         const bool whole = t_begin == 0 && t_end == tiles;
         float* const part = (float*)(workspace + few_header_bytes(n)) + ((size_t)blockIdx.x * 2 + (now != start)) * kPartFloats<D>;
-        for (int i = tid; i < s.rows * (D / 4); i += 64 * kFewWaves) {
-            const int rw = i / (D / 4), ch = (i - rw * (D / 4)) * 4;
-            float mx = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kFewWaves; ++w) mx = fmaxf(mx, stat[0][w][rw]);
-            float sum = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < kFewWaves; ++w) {
-                const float mw = stat[0][w][rw];
-                if (mw == -INFINITY) continue;
-                const float f = mw == mx ? 1.f : exp2_fast(mw - mx);
-                const float4 v = *(const float4*)((const float*)lds + (w * kFewRows + rw) * kMergeRow<D> + ch);
-                sum += f * stat[1][w][rw];
-                acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
-            }
-            const int tk = rw / group, hd = kvh * group + (rw - tk * group);
-            if (whole) {
-                const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
-                if (!PAD || ch < c.head_dim)
-                    *(uint2*)(a.out + (int64_t)(q0 + tk) * a.out_token_stride + (int64_t)hd * a.out_head_stride + ch) =
-                        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                if (a.lse && ch == 0) a.lse[(int64_t)(q0 + tk) * a.heads + hd] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
-            } else {
+        few_rows<D, PAD, kFewWaves>(c, a, s, r, kvh, first + t_begin, first + t_end, lds, stat, [&](int rw, int ch, float mx, float sum, float4 acc) __attribute__((always_inline)) {
+            if (whole) finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc);
+            else {
                 *(float4*)(part + 2 * kFewRows + rw * D + ch) = acc;
                 if (ch == 0) {
                     part[rw] = mx;
                     part[kFewRows + rw] = sum;
                 }
             }
-        }
+        });
         __syncthreads();
         now += (unsigned)(t_end - t_begin);
         into += (unsigned)(t_end - t_begin);
     }
+#endif
+}
+
+// Where histories are short: a workgroup per request and cache head, and no parts to join.
+template <int D, bool PAD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void kv_attention_short_kernel(KvCache c, KvAttention a)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    extern __shared__ __attribute__((aligned(4096))) char lds[];
+    __shared__ float stat[2][WAVES][kFewRows];
+    const int r = blockIdx.x / c.kv_heads, kvh = blockIdx.x - r * c.kv_heads;
+    const Span s = span_of(a, r, a.heads / c.kv_heads, a.max_blocks << c.block_shift);
+    if (s.rows == 0) return;
+    const int q0 = max(0, min(a.q_off[r], a.n_tokens)), first = s.first_tile();
+    few_rows<D, PAD, WAVES>(c, a, s, r, kvh, first, first + s.tiles(), lds, stat,
+                     [&](int rw, int ch, float mx, float sum, float4 acc) __attribute__((always_inline)) { finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc); });
 #endif
 }
 
@@ -501,12 +537,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
         sum += f * st.y;
         acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
     }
-    const int tk = rw / group, hd = kvh * group + (rw - tk * group);
-    const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
-    if (ch < c.head_dim)
-        *(uint2*)(a.out + (int64_t)(q0 + tk) * a.out_token_stride + (int64_t)hd * a.out_head_stride + ch) =
-            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-    if (a.lse && ch == 0) a.lse[(int64_t)(q0 + tk) * a.heads + hd] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+    finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc);
 }
 
 // ---- many query rows (chunks of prompts, single tokens among them): steps with more than 32 per request and cache head ------------
@@ -947,7 +978,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c,
     const int n_joined = ((const ManyHeader*)(workspace + layout.header))->joined;
     const Joined u = ((const Joined*)(workspace + layout.joined))[index];         // its place is there in any case
     if (index >= n_joined) return;
-    const int group = a.heads / c.kv_heads, q0 = u.q0;
+    const int q0 = u.q0;
     const size_t stride = (size_t)c.kv_heads * (2 * kManyRows + kManyRows * D);
     const float* const parts = (const float*)(workspace + layout.parts) + ((size_t)u.part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * D);
     for (int i = threadIdx.x; i < 16 * (D / 4); i += 256) {
@@ -966,12 +997,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c,
             acc.x = acc.x * keep + f * v.x, acc.y = acc.y * keep + f * v.y, acc.z = acc.z * keep + f * v.z, acc.w = acc.w * keep + f * v.w;
             mx = m_new;
         }
-        const int token = row / group, head = kvh * group + (row - token * group);
-        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
-        if (ch < c.head_dim)
-            *(uint2*)(a.out + (int64_t)(q0 + token) * a.out_token_stride + (int64_t)head * a.out_head_stride + ch) =
-                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-        if (a.lse && ch == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+        finish_row(c, a, q0, kvh, row, ch, mx, sum, acc);
     }
 }
 
@@ -983,8 +1009,30 @@ int64_t few_bytes(int32_t n_requests, int dim)
 }
 bool is_few(int32_t max_new, int32_t heads, int32_t kv_heads) { return (int64_t)max_new * (heads / kv_heads) <= kFewRows; }
 
+// Whether a workgroup of its own for every history is faster than equal stretches and a join: where the block tables, all that is known
+// here of the lengths, hold few tokens.  Single tokens, us, stretches / whole histories, at the longest tables of either limit: one
+// request, 12 heads of 64 channels, 624 tokens 10.4 / 9.2, 8 cache heads of 128, 304 tokens 13.5 / 9.4; 16 requests, 12 x 64, 1504 tokens 26.6 / 17.7, 8 x 128,
+// 624 tokens 22.5 / 16.2; 200 requests, 12 x 64, 1504 tokens 184 / 182.  Past them one request, 8 x 128, 624 tokens 11.3 / 15.0;
+// 200 requests, 12 x 64, 2048 tokens 238 / 246.
+bool is_short(const KvAttention& a, const KvCache& c)
+{
+    return ((int64_t)a.max_blocks << c.block_shift) * padded_dim(c.head_dim) <= ((int64_t)a.n_requests * c.kv_heads >= 128 ? 98304 : 40960);
+}
+
+template <int D, bool PAD, int WAVES> hipError_t launch_short(const KvCache& c, const KvAttention& a, hipStream_t stream)
+{
+    constexpr size_t kLds = kFewLds<D, WAVES>;
+    static const hipError_t configured =
+        hipFuncSetAttribute((const void*)kv_attention_short_kernel<D, PAD, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+    if (configured != hipSuccess) return configured;
+    hipLaunchKernelGGL((kv_attention_short_kernel<D, PAD, WAVES>), dim3((unsigned)a.n_requests * c.kv_heads), dim3(64 * WAVES), kLds, stream, c, a);
+    return hipGetLastError();
+}
+
 template <int D, bool PAD> hipError_t launch_few(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
 {
+    if (is_short(a, c))                       // eight wavefronts while there is a compute unit for every history: one request, 624 tokens, 12 x 64: 11.6 -> 9.2 us
+        return (int64_t)a.n_requests * c.kv_heads <= kFewGroups / 2 ? launch_short<D, PAD, 8>(c, a, stream) : launch_short<D, PAD, kFewWaves>(c, a, stream);
     const size_t lds = std::max(kFewLds<D>, ((size_t)a.n_requests + 1) * 8);
     static const hipError_t configured =
         hipFuncSetAttribute((const void*)kv_attention_few_kernel<D, PAD>, hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024);

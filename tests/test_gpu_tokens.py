@@ -373,6 +373,55 @@ def test_attention_fewer_new_tokens_than_announced_and_padding_rows(B):
     assert np.array_equal(a.run(lse=False)[0], base[0])
 
 
+class Wide(Attend):
+    """The same with block tables that could hold 8192 tokens a request, as a server's would."""
+
+    def __init__(self, *args, **kwargs):
+        super().__init__(*args, **kwargs)
+        wide = np.random.default_rng(1).integers(-3, self.n_blocks + 3, (len(self.table), 8192 // self.block)).astype(np.int32)
+        wide[:, :self.max_blocks] = self.table
+        self.table, self.max_blocks = wide, wide.shape[1]
+
+
+@pytest.mark.parametrize("heads,kv,dim", SHAPES)
+def test_attention_single_tokens_wide_tables(B, heads, kv, dim):
+    lengths = [(h, 1) for h in (0, 1, 7, 8, 15, 16, 17, 30, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 300)]
+    a = Wide(B, lengths, heads, kv, dim, seed=heads + dim)
+    a.check(*a.run())
+    a = Wide(B, [(0, 0), (50, 1), (0, 0), (33, 1), (-3, 2), (0, 0), (-1, 1)], heads, kv, dim, block=64, layout="pair", seed=dim)
+    a.check(*a.run())
+
+
+def test_attention_wide_tables_masks_and_counts(B):
+    """Windows, values that are no numbers behind the mask, blocks outside the cache, and 700 requests, with stretches that cross requests."""
+    rng = np.random.default_rng(12)
+    a = Wide(B, [(int(h), int(rng.random() < 0.9)) for h in rng.integers(0, 60, 700)], 4, 2, 64, seed=1)
+    a.check(*a.run())
+    for window in (1, 31, 33, 100, 2 ** 31 - 1):
+        a = Wide(B, [(0, 1), (31, 2), (32, 1), (500, 3), (1000, 1), (-3, 5)], 8, 2, 128, window=window, seed=window & 0xFFFF)
+        a.check(*a.run())
+    for value in (0x7F80, 0xFF80, 0x7FC0, 0x7F7F, 0xFF7F):
+        a = Wide(B, [(300, 4), (40, 1), (63, 8)], 8, 2, 128, seed=9)
+        base, base_lse = a.run()
+        clean = a.bits.copy()
+        a.bits[(slice(None),) + a.at(0, 302)] = value                 # seen by the last two of the first request's rows
+        a.bits[clean == 0x7FC0] = value
+        got, lse = a.run()
+        seen = np.arange(len(got)) // 2 == 1
+        assert np.array_equal(got[~seen], base[~seen]) and np.array_equal(lse[~seen], base_lse[~seen])
+    a = Wide(B, [(200, 1), (90, 5)], 8, 2, 64, seed=4)
+    a.table[0, 3], a.table[0, 5], a.table[1, 0] = -1, a.n_blocks, 2 ** 31 - 1
+    a.check(*a.run())
+
+
+def test_attention_short_tables_many_histories(B):
+    """More histories than compute units, each of them short: a workgroup of its own for each."""
+    rng = np.random.default_rng(5)
+    for heads, kv, dim, window in ((8, 8, 64, 0), (16, 4, 128, 0), (16, 4, 128, 40), (12, 4, 24, 0)):
+        a = Attend(B, [(int(h), int(m)) for h, m in zip(rng.integers(0, 200, 90), rng.integers(0, 4, 90))], heads, kv, dim, window=window, seed=kv)
+        a.check(*a.run())
+
+
 def test_attention_of_many_requests(B):
     """More requests than a workgroup has threads, single tokens only and in a mixed step; most histories are short."""
     rng = np.random.default_rng(12)
