@@ -810,6 +810,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 
     float m = -INFINITY, l = 0.f;
     f32x16 o[kBlocks], sc, next;
+    u32x4 v0[kBlocks], v1[kBlocks];           // values of the half that is worked on
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
@@ -871,7 +872,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
         const bool masked = is_masked(t, kb);
         const float m_use = m == -INFINITY ? 0.f : m;
         // Reads run ahead of their use by a phase: keys come while the exponentials are taken, values while scores are multiplied.
-        u32x4 k[kSteps], v0[kBlocks], v1[kBlocks], pw[2];
+        u32x4 k[kSteps], pw[2];
         read_keys(k, kn);
         if (kn == 1) {
             const uint32_t on = t % 2 ? -kTile : kTile;
@@ -885,18 +886,17 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             l += p0 + p1;
             pw[x >> 3][(x >> 1) & 3] = pack_bf16(p0, p1);
         }
-        read_half(v0, kb, 0);
+        if (kb == 1) read_half(v0, kb, 0);
         asm volatile("" : "+v"(pw[0]), "+v"(pw[1]), "+v"(l));             // here, and not where they are used
         __builtin_amdgcn_sched_barrier(0);
         scores(to, k);
-        read_half(v1, kb, 1);
         if (kb == 1) {
+            read_half(v1, kb, 1);
             const uint32_t on = t % 3 == 2 ? -2 * kTile : kTile;
 #pragma unroll
             for (int db = 0; db < kBlocks; ++db) v_read[db][0] += on, v_read[db][1] += on;
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (kb == 1 && t + 2 < tiles) load(t + 2);        // behind the values' reads: those wait for every load that is on its way
         if (masked) {
             const uint32_t vt = lds0 + (2 + t % 3) * kTile + kb * 32 * DH * 2, odd = odd_keys<D>(vt);
             if (odd) {
@@ -912,6 +912,12 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
         }
         add_values<D>(o, v0, pw[0]);
         add_values<D>(o, v1, pw[1]);
+        if (kb == 1) {                        // the next tile's first values; then what would hold them up: they wait for every load that is on its way
+            read_half(v0, 0, 0);
+            read_half(v1, 0, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (t + 2 < tiles) load(t + 2);
+        }
         if (is_masked(tn, kn)) mask(to, tn, kn);
         const float top = highest(to);
         raise(more ? top : -INFINITY);
@@ -923,6 +929,10 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
         fetch_id(1);
         __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
         __builtin_amdgcn_s_barrier();
+        if (works) {
+            read_half(v0, 0, 0);
+            read_half(v1, 0, 1);
+        }
         if (tiles > 1) load(1);
         fetch_id(2);
         if (works) {
