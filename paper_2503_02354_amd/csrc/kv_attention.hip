@@ -854,23 +854,30 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
         top = max_halves(top);
         return top == -INFINITY ? top : top * scale2;         // scale2 >= 0 keeps the order; 0 times -inf would not be a mask any more
     };
-    // The reference moves only when a score exceeds it by 2^8: exponentials up to 2^8 are as exact as up to 1, and moving it costs a
-    // multiplication of the whole output.
     auto raise = [&](float top) __attribute__((always_inline)) {
-        if (__any(top > m + 8.f)) {
-            const float m_new = fmaxf(m, top), shrink = m_new == m ? 1.f : exp2_fast(m - m_new);
-            l *= shrink;
+        const float m_new = fmaxf(m, top), shrink = m_new == m ? 1.f : exp2_fast(m - m_new);
+        l *= shrink;
 #pragma unroll
-            for (int db = 0; db < kBlocks; ++db)
+        for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-                for (int x = 0; x < 16; ++x) o[db][x] *= shrink;
-            m = m_new;
+            for (int x = 0; x < 16; ++x) o[db][x] *= shrink;
+        m = m_new;
+    };
+    // The exponentials of a half, packed; returns this lane's sum.
+    auto weigh = [&](const f32x16& v, u32x4 (&pw)[2]) __attribute__((always_inline)) {
+        const float m_use = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < 16; x += 2) {
+            const float p0 = exp2_fast(__builtin_fmaf(v[x], scale2, -m_use)), p1 = exp2_fast(__builtin_fmaf(v[x + 1], scale2, -m_use));
+            sum += p0 + p1;
+            pw[x >> 3][(x >> 1) & 3] = pack_bf16(p0, p1);
         }
+        return sum;
     };
     // the half (t, kb), whose scores are in `cur`; the next half's, (tn, kn), go to `to` (of no use behind the last one, and not used)
-    auto half_step = [&](f32x16& cur, f32x16& to, int t, int kb, int tn, int kn, bool more) __attribute__((always_inline)) {
+    auto half_step = [&](f32x16& cur, f32x16& to, int t, int kb, int tn, int kn) __attribute__((always_inline)) {
         const bool masked = is_masked(t, kb);
-        const float m_use = m == -INFINITY ? 0.f : m;
         // Reads run ahead of their use by a phase: keys come while the exponentials are taken, values while scores are multiplied.
         u32x4 k[kSteps], pw[2];
         read_keys(k, kn);
@@ -880,12 +887,17 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             for (int ks = 0; ks < kSteps; ++ks) k_read[ks] += on;
         }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int x = 0; x < 16; x += 2) {
-            const float p0 = exp2_fast(__builtin_fmaf(cur[x], scale2, -m_use)), p1 = exp2_fast(__builtin_fmaf(cur[x + 1], scale2, -m_use));
-            l += p0 + p1;
-            pw[x >> 3][(x >> 1) & 3] = pack_bf16(p0, p1);
+        // The reference is a row's first maximum, and follows it only when a half exceeds it by some 2^16: floats of any size are equally exact (values up to 2^110 find room), and
+        // looking for the maximum of every half costs a quarter of the vector instructions.
+        float sum = weigh(cur, pw);
+        const bool left = !(sum <= 0x1p16f) || m == -INFINITY;
+        if (__any(left)) {                    // of this row, in either half of the wavefront: what other rows need does not change its bits
+            const bool moves = left | (__shfl_xor((int)left, 32, 64) != 0);
+            const float top = highest(cur);
+            raise(moves ? top : -INFINITY);
+            sum = weigh(cur, pw);
         }
+        l += sum;
         if (kb == 1) read_half(v0, kb, 0);
         asm volatile("" : "+v"(pw[0]), "+v"(pw[1]), "+v"(l));             // here, and not where they are used
         __builtin_amdgcn_sched_barrier(0);
@@ -919,8 +931,6 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             if (t + 2 < tiles) load(t + 2);
         }
         if (is_masked(tn, kn)) mask(to, tn, kn);
-        const float top = highest(to);
-        raise(more ? top : -INFINITY);
     };
 
     if (tiles > 0) {
@@ -940,15 +950,14 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             read_keys(k, 0);
             scores(sc, k);
             if (is_masked(0, 0)) mask(sc, 0, 0);
-            raise(highest(sc));
         }
     }
     for (int t = 0; t < tiles; ++t) {
-        if (works) half_step(sc, next, t, 0, t, 1, true);
+        if (works) half_step(sc, next, t, 0, t, 1);
         // the next tile has landed, and everybody is through with this one's K and the last one's V
         __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
         __builtin_amdgcn_s_barrier();
-        if (works) half_step(next, sc, t, 1, t + 1, 0, t + 1 < tiles);
+        if (works) half_step(next, sc, t, 1, t + 1, 0);
         else if (t + 2 < tiles) load(t + 2);
         fetch_id(t + 3);
     }
