@@ -333,12 +333,15 @@ int coe_kv_append(const coe_kv_cache* cache, int32_t n_tokens, const void* k, in
  * seq_len as coe_kv_plan writes them); with m of them, row i stands at position p = seq_len[r] - m + i and sees the cached
  * tokens j <= p, with window > 0 only those with j > p - window.  Query head h reads cache head h / (heads / kv_heads).
  *   out = softmax_j(scale * q . k_j) v_j      lse = ln sum_j exp(scale * q . k_j)
- * A row that sees nothing (p < 0) gets out = 0 and lse = -inf.  What a row does not see does not reach it, whatever its bits.
+ * A row that sees nothing (p < 0), or whose scores are all -inf, gets out = 0 and lse = -inf.  What a row does not see does not
+ * reach it, whatever its bits.  Of a request with more than max_new new tokens the first max_new are served; rows of q that
+ * belong to no request are not read, and theirs of out and lse not written.
  * q and out: row t, head h at t * token_stride + h * head_stride elements of the cache's dtype, 16-byte aligned, strides
  * multiples of 8.  lse: [n_tokens][heads] fp32, or NULL.  table: [n_requests][max_blocks] block ids; a cached token whose
  * block id is outside the cache reads as zeros; seq_len is limited to max_blocks * block_size.
- * Numerics: products and sums in fp32, exponentials relative to a running maximum, the probabilities rounded to bf16 before
- * they meet the values, one rounding of the result to bf16.  The same inputs give the same bits.
+ * Numerics: products and sums in fp32, exponentials relative to a running reference (the maximum so far, which may be behind by
+ * up to 2^16; values up to 2^110 in magnitude find room), the probabilities rounded to bf16 before they meet the values, one
+ * rounding of the result to bf16.  The same inputs give the same bits.
  * heads: a multiple of kv_heads.  workspace: coe_kv_attention_workspace bytes for the same sizes, 16-byte aligned. */
 int64_t coe_kv_attention_workspace(int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads, int32_t kv_heads,
                                    int32_t head_dim);

@@ -195,7 +195,9 @@ __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_
 // finished here.  Inside a stretch the four wavefronts take tiles in turn, each for itself: keys go from memory straight into
 // registers (they are the first operand as they lie), values through registers into LDS of the wavefront's own, and the next tile's
 // are on their way while this one is multiplied.
-// What bounds it: HBM, keys and values once.
+// What bounds it: HBM, keys and values once.  96 requests of 50 to 5000 tokens, 32 heads on 8 of 128 channels: 1.006 GB in 214 to 220 us, 4.6 TB/s
+// (a copy of 2 GiB: 4.9); 3 of 90,000 to 131,000 tokens, 32 heads on 4: 0.72 GB in 140 us, 5.2 TB/s.  Joining the parts takes 7 to 9 us.
+// Two workgroups per compute unit are all that 250 registers a lane allow, and they suffice: LDS and matrix cores stand idle.
 struct FewHeader {                        // at the workspace's start, for the joining kernel
     unsigned long long per;               // tiles of a stretch
     unsigned long long base[1];           // [n_requests + 1] tiles before request r, of one cache head
@@ -486,7 +488,8 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void kv_attention_short_kern
 
 // Adds up the parts of a history that several workgroups shared: a workgroup per request, cache head and kJoinRows query rows
 // (blockIdx.y).  Several threads share the parts of a row's four channels, since a long history has many; each leaves its sum
-// relative to its own maximum, and the first adds those up in their order.
+// relative to its own maximum, and the first adds those up in their order.  What bounds it: round trips to memory.  96 requests: 7.2 us with a
+// row to a workgroup of 256 threads, 18.5 with 1024 (three requests of 131,000 tokens, hundreds of parts to a history: 9.3 and 8.3).
 constexpr int kJoinRows = 1;
 template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAttention a, const char* workspace)
@@ -545,8 +548,11 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
 // them sees.  A scheduling launch lists them, longest first, so that the last workgroups to start are short ones; where there are too
 // few units to fill the chip it cuts long ones into parts over the keys, which kv_attention_join_units_kernel adds up.  Block b
 // takes cache head b % kv_heads, so that with eight of them (or four, or two) the units of one head meet in the same second-level caches.
-// K and V tiles go from memory into LDS by DMA, two of them in turn; a wavefront reads every key and value of a tile for its 32
-// rows.  What bounds it: the matrix cores, with the softmax's vector instructions and 1 KiB of LDS reads per matrix instruction close by.
+// K tiles go from memory into two LDS buffers by DMA, V tiles into three, in turn; a wavefront reads every key and value of a tile for
+// its 32 rows.  What bounds it: matrix and vector instructions, at the clock that the power leaves (1.85 GHz): two prompts of some 8,000
+// tokens behind 1000 and 2000, 32 heads on 8 of 128 channels, 1.28 TFLOP in 1.24 to 1.39 ms, 0.92 to 1.03 PFLOP/s from card to card, where a matrix product of
+// 8192 x 8192 x 8192 reaches 1.16 to 1.19; a matrix instruction takes 1 KiB of LDS reads, without bank conflicts.  Wavefronts of 64 rows would halve
+// those and do not fit the registers (4.8 ms).
 constexpr int kManyRows = 128, kManyKeys = 64, kManyWaves = 4;
 constexpr int kManyGroups = 512;          // two workgroups per compute unit
 
@@ -590,6 +596,7 @@ __device__ __forceinline__ void tiles_of(const Span& s, int window, int group, i
     count = max(1, (end + kManyKeys - 1) / kManyKeys - first);
 }
 
+// One workgroup: latency.  7.5 us for 40 requests, five round trips to memory and a few scans.
 constexpr int kSchedThreads = 1024, kSchedBins = 2048;
 __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(KvCache c, KvAttention a, char* workspace, ManyLayout at)
 {
@@ -773,6 +780,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     auto load = [&](int t) __attribute__((always_inline)) {
         char *const k_to = lds + t % 2 * kTile + wave_row * (DH * 2), *const v_to = lds + (2 + t % 3) * kTile + wave_row * (DH * 2);
         const int key0 = (tile0 + t) * kManyKeys, first = key0 + wave_row;
+        // two prompts of 4000 tokens: blocks of 16 and 64 rows, which are loaded here, 494 us, blocks of 8 rows 556
         if (key0 >= s.begin && key0 + kManyKeys <= s.end && block_mask >= 15 && (uint32_t)next_id < (uint32_t)c.n_blocks) {
             const uint64_t block = block_of(next_id, first);
             const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc((char*)c.k + block, 0, 0x7FFFFFFF, 0x00020000);
@@ -989,7 +997,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 #endif
 }
 
-// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.
+// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.  Latency: 8.4 us with 25 cut units of 8 heads, 4.7 without any.  The last
+// workgroup of a unit doing it instead costs more: what makes parts visible on all of the chip, a release of the second-level cache, slowed
+// the units down from 88 to 183 us.
 template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c, KvAttention a, const char* workspace, ManyLayout layout)
 {
@@ -1026,6 +1036,8 @@ int64_t few_bytes(int32_t n_requests, int dim)
 {
     return few_header_bytes(n_requests) + (int64_t)kFewGroups * 2 * (2 * kFewRows + kFewRows * dim) * 4;
 }
+// Rows that one wavefront's tile holds go to the kernel that reads every key once.  8 cache heads of 128, us, few / many: 4 requests of 3000 tokens with 8 rows
+// 25 / 30, with 32 rows 29 / 35; 32 requests 94 / 99 and 108 / 104; 64 of 1500 tokens 97 / 89 to 98 and 121 / 94.
 bool is_few(int32_t max_new, int32_t heads, int32_t kv_heads) { return (int64_t)max_new * (heads / kv_heads) <= kFewRows; }
 
 // Whether a workgroup of its own for every history is faster than equal stretches and a join: where the block tables, all that is known

@@ -17,9 +17,10 @@ namespace {
 // workgroup computes the sums of all requests for itself in LDS, where a token finds its request by bisection; the workgroups
 // then share the tokens and the requests.  None waits for another: a token of a new block takes the block's id from the ring, not
 // from the table that some other workgroup writes.
-// What bounds it: latency (lengths in, one scan, slots out).
+// What bounds it: latency (lengths in, one scan, slots out): 7.3 us for 192 requests with a token each, 12.0 us for 1500 requests and 86,000
+// tokens, of which a launch with one load and one store takes 2.8.
 constexpr int kPlanThreads = 256;
-constexpr int kPlanInLds = 8192;              // requests whose lengths stay in LDS beside the sums
+constexpr int kPlanInLds = 8192;              // requests whose lengths stay in LDS beside the sums (96 KiB); more ask memory again, per token
 constexpr uint32_t kFreed = 0x80000000u;      // the entry counts blocks that a finished request gives back
 constexpr uint32_t kTooLong = 0x40000000u;    // the request would outgrow its row of the table
 
@@ -176,7 +177,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
 
 // ---- append -------------------------------------------------------------------------------------------------------
 // A copy of rows to scattered places; a thread moves 16 bytes of a key and the same of a value.  What bounds it: HBM, or the
-// launch itself where there are few tokens.
+// launch itself where there are few tokens: 8000 tokens of 8 heads of 128 (65.6 MB) 11.4 us, 5.7 TB/s, which is what a copy of that size
+// reaches; 48 tokens 2.8 us.
 __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, int n_tokens, const uint16_t* __restrict__ k, int64_t k_ts, int64_t k_hs,
                                                         const uint16_t* __restrict__ v, int64_t v_ts, int64_t v_hs,
                                                         const int32_t* __restrict__ slot)
