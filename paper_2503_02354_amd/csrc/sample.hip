@@ -290,7 +290,12 @@ __device__ __forceinline__ float2 masses_before(const T* row, int vocab, const F
     // the next lower number: to be above it is to reach the bound
     const float with[2] = {nextafterf(ahead[0].x, -INFINITY), nextafterf(ahead[1].x, -INFINITY)};
     float before[2] = {0.f, 0.f};
+    const float lowest = fminf(ahead[0].x, ahead[1].x);
     batches<THREADS>(row, vocab, [&](const float (&x)[16], auto n, uint32_t i) {
+        float high = x[0];
+#pragma unroll
+        for (int e = 1; e < n; ++e) high = fmaxf(high, x[e]);
+        if (!(high >= lowest)) return;
         float above[2];
         bool clear = true;
 #pragma unroll
@@ -327,6 +332,8 @@ template <int THREADS, typename T>
 __device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t top_index, Front front, float top_p, float mass, float min_p, Scale scale, Best first,
                          Best mine, Shared<THREADS>& sh, int& set)
 {
+    // what lies before the second token is the first one's weight: a nucleus of one
+    if (top_p < 1.f && !((scale.far ? 1.f : scale.near_weight(scale.top)) < top_p * mass)) return top_index;
     const float least = least_of(min_p);
     bool by_logs = !(scale.top < INFINITY);
     for (;;) {                                // the front shrinks with every round that goes on
@@ -354,7 +361,7 @@ __device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t t
                                         : masses_before<THREADS>(row, vocab, ahead, [&](float x) { return scale.near_weight(x); });
         const float2 masses = block_sums(before, sh, set);
         if (masses.x < top_p * mass) return c[0].index;
-        front = ahead[0];
+        if (front.holds(ahead[0].x, ahead[0].end)) front = ahead[0];
         if (c[1].index == kNone) continue;
         if (c[1].index == top_index || masses.y < top_p * mass) {
             if (!__syncthreads_or(hides<THREADS>(row, noise, vocab, (int)c[0].index, top_index, front, least, scale, c[1]))) return c[1].index;
