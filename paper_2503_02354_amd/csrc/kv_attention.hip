@@ -210,10 +210,10 @@ template <int D> constexpr int kMergeRow = D + 4;          // floats between the
 template <int D, int WAVES = kFewWaves> constexpr size_t kFewLds = (size_t)WAVES * kFewRows * kMergeRow<D> * 4;
 
 #if defined(__HIP_DEVICE_COMPILE__)
-// One stretch [tile, tile_stop) of 32-key tiles of a request and cache head, at most 32 query rows, by WAVES wavefronts:
-// write(row, channel, maximum, sum, four channels of the unnormalised output) gets the result, relative to the row's maximum.
+// Query rows [row0, row0 + rows), at most 32, at positions low to high, of a request and cache head over the 32-key tiles [tile_begin, tile_stop), by WAVES wavefronts:
+// write(row - row0, channel, maximum, sum, four channels of the unnormalised output) gets the result, relative to the row's maximum.
 template <int D, bool PAD, int WAVES, class Write>
-__device__ __forceinline__ void few_rows(const KvCache& c, const KvAttention& a, const Span& s, int r, int kvh, int tile_begin, int tile_stop, char* lds,
+__device__ __forceinline__ void few_rows(const KvCache& c, const KvAttention& a, const Span& s, int r, int kvh, int row0, int rows, int low, int high, int tile_begin, int tile_stop, char* lds,
                                          float (*stat)[WAVES][kFewRows], Write write)
 {
     constexpr int kSteps = D / 16, kBlocks = D / 32;
@@ -225,8 +225,8 @@ __device__ __forceinline__ void few_rows(const KvCache& c, const KvAttention& a,
     const uint32_t v_tile = lds_address(v_lds), v_read = v_tile + value_base<D>(lane);
 
     // this lane's query row
-    const int row = l32, token = row / group, head = kvh * group + (row - token * group);
-    const bool row_ok = row < s.rows;
+    const int row = row0 + l32, token = row / group, head = kvh * group + (row - token * group);
+    const bool row_ok = l32 < rows;
     const int pos = s.first_pos + token, from = a.window > 0 ? pos - a.window : -1;       // sees keys from < j <= pos
     bf16x8 qf[kSteps];
     {
@@ -299,7 +299,7 @@ __device__ __forceinline__ void few_rows(const KvCache& c, const KvAttention& a,
             if (tile + 2 * WAVES < tile_stop) id_next = id_of(tile + 2 * WAVES);
         }
         const int key0 = tile * kKeys;
-        const bool masked = key0 + kKeys - 1 > s.first_pos || key0 < s.begin || (a.window > 0 && key0 <= s.first_pos + s.m - 1 - a.window);
+        const bool masked = key0 + kKeys - 1 > low || key0 < s.begin || (a.window > 0 && key0 <= high - a.window);
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
@@ -360,7 +360,7 @@ __device__ __forceinline__ void few_rows(const KvCache& c, const KvAttention& a,
         stat[1][wid][l32] = l;
     }
     __syncthreads();
-    for (int i = tid; i < s.rows * (D / 4); i += 64 * WAVES) {
+    for (int i = tid; i < rows * (D / 4); i += 64 * WAVES) {
         const int rw = i / (D / 4), ch = (i - rw * (D / 4)) * 4;
         float mx = -INFINITY;
 #pragma unroll
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
 
         const bool whole = t_begin == 0 && t_end == tiles;
         float* const part = (float*)(workspace + few_header_bytes(n)) + ((size_t)blockIdx.x * 2 + (now != start)) * kPartFloats<D>;
-        few_rows<D, PAD, kFewWaves>(c, a, s, r, kvh, first + t_begin, first + t_end, lds, stat, [&](int rw, int ch, float mx, float sum, float4 acc) __attribute__((always_inline)) {
+        few_rows<D, PAD, kFewWaves>(c, a, s, r, kvh, 0, s.rows, s.first_pos, s.first_pos + s.m - 1, first + t_begin, first + t_end, lds, stat, [&](int rw, int ch, float mx, float sum, float4 acc) __attribute__((always_inline)) {
             if (whole) finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc);
             else {
                 *(float4*)(part + 2 * kFewRows + rw * D + ch) = acc;
@@ -470,19 +470,22 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void kv_attention_few_kernel(KvC
 #endif
 }
 
-// Where histories are short: a workgroup per request and cache head, and no parts to join.
+// Where histories are short and rows are few: a workgroup per request, cache head and 32 query rows (those that see most first), one launch,
+// and no parts to join.  What bounds it: latency, tiles in turn; one token behind 612, 12 heads of 64 channels, 9.3 us.
 template <int D, bool PAD, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void kv_attention_short_kernel(KvCache c, KvAttention a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     extern __shared__ __attribute__((aligned(4096))) char lds[];
     __shared__ float stat[2][WAVES][kFewRows];
-    const int r = blockIdx.x / c.kv_heads, kvh = blockIdx.x - r * c.kv_heads;
-    const Span s = span_of(a, r, a.heads / c.kv_heads, a.max_blocks << c.block_shift);
-    if (s.rows == 0) return;
-    const int q0 = max(0, min(a.q_off[r], a.n_tokens)), first = s.first_tile();
-    few_rows<D, PAD, WAVES>(c, a, s, r, kvh, first, first + s.tiles(), lds, stat,
-                     [&](int rw, int ch, float mx, float sum, float4 acc) __attribute__((always_inline)) { finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc); });
+    const int r = blockIdx.x / c.kv_heads, kvh = blockIdx.x - r * c.kv_heads, row0 = (int)(gridDim.y - 1 - blockIdx.y) * kFewRows, group = a.heads / c.kv_heads;
+    const Span s = span_of(a, r, group, a.max_blocks << c.block_shift);
+    if (row0 >= s.rows) return;
+    const int q0 = max(0, min(a.q_off[r], a.n_tokens)), rows = min(kFewRows, s.rows - row0);
+    const int low = s.first_pos + (row0 == 0 ? 0 : row0 / group), high = s.first_pos + (row0 + rows == s.rows ? s.m : (row0 + rows - 1) / group + 1) - 1;
+    const int begin = a.window > 0 ? max(0, max(0, low) - a.window + 1) : 0, end = max(0, high + 1);
+    few_rows<D, PAD, WAVES>(c, a, s, r, kvh, row0, rows, low, high, begin / kKeys, (end + kKeys - 1) / kKeys, lds, stat,
+                            [&](int rw, int ch, float mx, float sum, float4 acc) __attribute__((always_inline)) { finish_row(c, a, q0, kvh, row0 + rw, ch, mx, sum, acc); });
 #endif
 }
 
@@ -543,7 +546,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
     finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc);
 }
 
-// ---- many query rows (chunks of prompts, single tokens among them): steps with more than 32 per request and cache head ------------
+// ---- many query rows (chunks of prompts, single tokens among them): steps with more than 32 per request and cache head that are not short ----
 // Units of work are tiles of 128 query rows (32 to a wavefront) of a request and cache head, with all the 64-key tiles that one of
 // them sees.  A scheduling launch lists them, longest first, so that the last workgroups to start are short ones; where there are too
 // few units to fill the chip it cuts long ones into parts over the keys, which kv_attention_join_units_kernel adds up.  Block b
@@ -743,17 +746,13 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     const int low = __builtin_amdgcn_readfirstlane(s.first_pos + (row0 + wid * 32) / group);
     const int high = __builtin_amdgcn_readfirstlane(s.first_pos + (min(s.rows, row0 + wid * 32 + 32) - 1) / group);
     const bool works = row0 + wid * 32 < s.rows;
-    bf16x8 qf[kSteps];
-    {
-        const uint16_t* qp = a.q + (int64_t)(q0 + (row_ok ? token : 0)) * a.q_token_stride + (int64_t)(row_ok ? head : 0) * a.q_head_stride + half * 8;
-        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    u32x4 q_raw[kSteps];
+    {                                         // all on their way before one is looked at; what is no row or channel becomes zeros then
+        const uint16_t* const qp = a.q + (int64_t)(q0 + (row_ok ? token : 0)) * a.q_token_stride + (int64_t)(row_ok ? head : 0) * a.q_head_stride;
 #pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) {
-            u32x4 w = {0, 0, 0, 0};
-            if (row_ok && 2 * ks + half < chunks) w = *(const u32x4*)(qp + ks * 16) ^ flip;
-            qf[ks] = __builtin_bit_cast(bf16x8, w);
-        }
+        for (int ks = 0; ks < kSteps; ++ks) q_raw[ks] = *(const u32x4*)(qp + (2 * ks + half < chunks ? ks * 16 + half * 8 : 0));
     }
+    bf16x8 qf[kSteps];
     const float scale2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.4e-45f);          // a mask of -inf stays one with a scale of 0
 
     // Lane i of a load fills slot i % (DH / 8) of row i / (DH / 8) of its rows, and fetches the chunk that belongs there.
@@ -945,6 +944,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
         fetch_id(0);
         load(0);
         fetch_id(1);
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, row_ok && 2 * ks + half < chunks ? q_raw[ks] ^ flip : u32x4{0, 0, 0, 0});
         __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8));
         __builtin_amdgcn_s_barrier();
         if (works) {
@@ -1045,9 +1047,15 @@ bool is_few(int32_t max_new, int32_t heads, int32_t kv_heads) { return (int64_t)
 // request, 12 heads of 64 channels, 624 tokens 10.4 / 9.2, 8 cache heads of 128, 304 tokens 13.5 / 9.4; 16 requests, 12 x 64, 1504 tokens 26.6 / 17.7, 8 x 128,
 // 624 tokens 22.5 / 16.2; 200 requests, 12 x 64, 1504 tokens 184 / 182.  Past them one request, 8 x 128, 624 tokens 11.3 / 15.0;
 // 200 requests, 12 x 64, 2048 tokens 238 / 246.
+// Chunks, us, units and a join / a workgroup for 32 rows of each: one prompt of 500 tokens, 12 heads of 64, 25.5 / 12.6, 32 on 8 of 128 29.5 / 21.2, of 1000 tokens
+// 28 / 20 and 40 / 52; 8 prompts of 128, 32 on 8 of 128 23.3 / 21.1, of 256 30.7 / 45.9; 64 tokens behind 900, 32 on 8 of 128, 34 / 24;
+// 40 prompts of 64, 32 on 8 of 128 (2560 workgroups) 35 / 42.
+int64_t row_blocks(const KvAttention& a, const KvCache& c) { return ((int64_t)a.max_new * (a.heads / c.kv_heads) + kFewRows - 1) / kFewRows; }
 bool is_short(const KvAttention& a, const KvCache& c)
 {
-    return ((int64_t)a.max_blocks << c.block_shift) * padded_dim(c.head_dim) <= ((int64_t)a.n_requests * c.kv_heads >= 128 ? 98304 : 40960);
+    const int64_t blocks = row_blocks(a, c), groups = (int64_t)a.n_requests * c.kv_heads * blocks, longest = ((int64_t)a.max_blocks << c.block_shift) * padded_dim(c.head_dim);
+    if (blocks == 1) return longest <= (groups >= 128 ? 98304 : 40960);
+    return groups <= 2048 && longest <= 131072 && groups * longest <= 52ll << 20;
 }
 
 template <int D, bool PAD, int WAVES> hipError_t launch_short(const KvCache& c, const KvAttention& a, hipStream_t stream)
@@ -1056,14 +1064,12 @@ template <int D, bool PAD, int WAVES> hipError_t launch_short(const KvCache& c, 
     static const hipError_t configured =
         hipFuncSetAttribute((const void*)kv_attention_short_kernel<D, PAD, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
     if (configured != hipSuccess) return configured;
-    hipLaunchKernelGGL((kv_attention_short_kernel<D, PAD, WAVES>), dim3((unsigned)a.n_requests * c.kv_heads), dim3(64 * WAVES), kLds, stream, c, a);
+    hipLaunchKernelGGL((kv_attention_short_kernel<D, PAD, WAVES>), dim3((unsigned)a.n_requests * c.kv_heads, (unsigned)row_blocks(a, c)), dim3(64 * WAVES), kLds, stream, c, a);
     return hipGetLastError();
 }
 
 template <int D, bool PAD> hipError_t launch_few(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
 {
-    if (is_short(a, c))                       // eight wavefronts while there is a compute unit for every history: one request, 624 tokens, 12 x 64: 11.6 -> 9.2 us
-        return (int64_t)a.n_requests * c.kv_heads <= kFewGroups / 2 ? launch_short<D, PAD, 8>(c, a, stream) : launch_short<D, PAD, kFewWaves>(c, a, stream);
     const size_t lds = std::max(kFewLds<D>, ((size_t)a.n_requests + 1) * 8);
     static const hipError_t configured =
         hipFuncSetAttribute((const void*)kv_attention_few_kernel<D, PAD>, hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024);
@@ -1095,6 +1101,11 @@ template <int D> hipError_t launch_many(const KvCache& c, const KvAttention& a, 
 
 template <int D> hipError_t launch(const KvCache& c, const KvAttention& a, char* workspace, hipStream_t stream)
 {
+    if (is_short(a, c)) {                     // eight wavefronts while there is a compute unit for every workgroup: one request, 624 tokens, 12 x 64: 11.6 -> 9.2 us
+        const bool wide = (int64_t)a.n_requests * c.kv_heads * row_blocks(a, c) <= kFewGroups / 2;
+        if (c.head_dim == D) return wide ? launch_short<D, false, 8>(c, a, stream) : launch_short<D, false, kFewWaves>(c, a, stream);
+        return wide ? launch_short<D, true, 8>(c, a, stream) : launch_short<D, true, kFewWaves>(c, a, stream);
+    }
     if (!is_few(a.max_new, a.heads, c.kv_heads)) return launch_many<D>(c, a, workspace, stream);
     return c.head_dim == D ? launch_few<D, false>(c, a, workspace, stream) : launch_few<D, true>(c, a, workspace, stream);
 }

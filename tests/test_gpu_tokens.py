@@ -843,3 +843,97 @@ def test_example_generates_what_the_dense_model_says(B):
     wide = generate.Server(experts, n_blocks=200, block_size=8, token_cap=512)
     again = wide.generate(prompts, route, 6, temperature=0.9, top_p=0.8, seed=3)
     assert wide.generate(prompts, route, 6, temperature=0.9, top_p=0.8, seed=3) == again and all(np.isfinite(v).all() for v in again[1])
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(4, 4, 64), (8, 2, 128), (12, 4, 96), (16, 1, 80), (7, 1, 8)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_attention_chunks_by_table_width(B, heads, kv, dim, wide):
+    """Chunks of every length around 32 query rows, with histories, windows and empty requests, where tables are narrow (a workgroup
+    for 32 rows) and wide."""
+    kind = Wide if wide else Attend
+    for lengths, window in (([(0, 9), (5, 33), (0, 0), (100, 20), (-4, 11), (31, 1)], 0), ([(0, 40), (64, 17), (90, 50)], 21), ([(200, 64)], 0), ([(0, 65), (0, 1)], 32)):
+        a = kind(B, lengths, heads, kv, dim, window=window, seed=dim)
+        a.check(*a.run())
+
+
+def test_attention_chunks_of_narrow_tables_mask(B):
+    """Values behind the mask do not reach a row, row by row, in chunks that narrow tables serve."""
+    for value in (0x7F80, 0x7FC0, 0x7F7F, 0xFF7F):
+        a = Attend(B, [(10, 70), (40, 3)], 8, 2, 64, seed=9)
+        base, base_lse = a.run()
+        clean = a.bits.copy()
+        a.bits[(slice(None),) + a.at(0, 50)] = value                  # seen by the last thirty of the first request's rows
+        a.bits[clean == 0x7FC0] = value
+        got, lse = a.run()
+        seen = np.arange(len(got)) - 40
+        seen = (seen >= 0) & (seen < 30)
+        assert np.array_equal(got[~seen], base[~seen]) and np.array_equal(lse[~seen], base_lse[~seen])
+        assert len(got) == 73
+
+
+CHUNKS = [
+    [(0, 33)], [(0, 64), (0, 65)], [(0, 127), (0, 128), (0, 129)], [(100, 257)], [(64, 3), (200, 35), (3, 8), (0, 9)],
+    [(0, 0), (50, 1), (0, 0), (33, 40), (0, 0)], [(-3, 5), (-5, 5), (-40, 60), (10, 2)], [(0, 300), (700, 1), (700, 20), (31, 1), (1000, 64)],
+]
+
+
+@pytest.mark.parametrize("lengths", CHUNKS)
+@pytest.mark.parametrize("heads,kv,dim", [(4, 4, 64), (8, 2, 128), (12, 4, 96), (5, 1, 80), (2, 2, 8)])
+def test_attention_chunks_wide_tables(B, lengths, heads, kv, dim):
+    a = Wide(B, lengths, heads, kv, dim, seed=len(lengths) + dim)
+    a.check(*a.run())
+
+
+@pytest.mark.parametrize("block,layout", [(8, "token"), (16, "head"), (32, "pair"), (64, "inner"), (128, "token"), (1024, "head")])
+def test_attention_chunks_wide_tables_blocks_and_windows(B, block, layout):
+    for window in (0, 1, 31, 33, 64, 129):
+        for heads, kv, dim in ((8, 2, 128), (6, 6, 64)):
+            a = Wide(B, [(300, 40), (0, 90), (129, 1), (5, 130)], heads, kv, dim, block=block, layout=layout, window=window, seed=block)
+            a.check(*a.run())
+
+
+@pytest.mark.parametrize("value", [0x7F80, 0xFF80, 0x7FC0, 0x7F7F, 0xFF7F])
+@pytest.mark.parametrize("window", [0, 50])
+def test_attention_chunks_wide_tables_keep_what_is_masked_out(B, value, window):
+    for heads, kv, dim in ((8, 2, 128), (4, 4, 64), (6, 2, 96)):
+        a = Wide(B, [(60, 150), (0, 70), (90, 1)], heads, kv, dim, window=window, seed=9)
+        base, base_lse = a.run()
+        clean = a.bits.copy()
+        bad = [(0, 130), (0, 209), (1, 33), (1, 69)] + [(0, 5)] * (window > 0)
+        for r, j in bad:
+            a.bits[(slice(None),) + a.at(r, j)] = value
+        a.bits[clean == 0x7FC0] = value
+        got, lse = a.run()
+        seen = np.zeros(len(got), bool)
+        for r, j in bad:
+            for i in range(a.new[r]):
+                pos = a.total[r] - a.new[r] + i
+                seen[a.off[r] + i] |= j <= pos and (window == 0 or j > pos - window)
+        assert np.array_equal(got[~seen], base[~seen]) and np.array_equal(lse[~seen], base_lse[~seen])
+
+
+def test_attention_chunks_wide_tables_odd_inputs(B):
+    """Unknown blocks, flat, negative and steep scales, a reference that has to move often, and bits that repeat."""
+    a = Wide(B, [(200, 40), (90, 64)], 8, 2, 64, seed=4)
+    a.table[0, 3], a.table[0, 5], a.table[1, 0] = -1, a.n_blocks, 2 ** 31 - 1
+    a.check(*a.run())
+    for scale in (0.0, -0.1, 1e-30):
+        a = Wide(B, [(300, 70), (40, 1)], 4, 2, 64, seed=2, scale=scale)
+        a.check(*a.run())
+    for sign in (1.0, -1.0):                          # scores that rise (fall) by 2 with every key, from -500 on
+        a = Wide(B, [(700, 40), (200, 80)], 4, 2, 64, seed=3)
+        a.q[:] = _bf16(np.ones_like(a.q, np.float64))
+        for r, t in enumerate(a.total):
+            for j in range(t):
+                a.bits[0][a.at(r, j)] = _bf16(np.full((2, 64), sign * (j - 250) / 4.0))
+        got, logs = a.run()
+        out, lse, size = T.attention(T.bf16_to_f64(a.q), T.bf16_to_f64(a.bits[0]), T.bf16_to_f64(a.bits[1]), a.total, a.off, a.table, 16, 0, a.scale)
+        # keys beyond 64 are rounded alike on both sides; scores are sums of 64 equal numbers, exact but for the scale's rounding and the product's,
+        # 2^-23 of at most 1500 together: 2e-4, on a probability twice that
+        assert (np.abs(T.bf16_to_f64(got) - out) <= 2.0 ** -8 * np.abs(out) + (2.0 ** -8 + 2e-3) * size + 1e-30).all()
+        assert (np.abs(logs - lse) <= 1e-3 + 1e-6 * np.abs(lse)).all()
+    a = Wide(B, [(3000, 1), (100, 1), (900, 90), (0, 300)], 8, 2, 128, seed=6)
+    base = a.run()
+    for _ in range(3):
+        got = a.run()
+        assert np.array_equal(got[0], base[0]) and np.array_equal(got[1], base[1])
