@@ -493,7 +493,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void kv_attention_short_kern
 // (blockIdx.y).  Several threads share the parts of a row's four channels, since a long history has many; each leaves its sum
 // relative to its own maximum, and the first adds those up in their order.  What bounds it: round trips to memory.  96 requests: 7.2 us with a
 // row to a workgroup of 256 threads, 18.5 with 1024 (three requests of 131,000 tokens, hundreds of parts to a history: 9.3 and 8.3).
-constexpr int kJoinRows = 1;
+constexpr int kJoinRows = 1, kAhead = 4;
 template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAttention a, const char* workspace)
 {
@@ -517,16 +517,24 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
     float mx = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (rw < rows && share < kSplit)
-#pragma unroll 2
-        for (unsigned long long w = w0 + share; w <= w1; w += kSplit) {
-            const float* const p = part_of(w);
-            const float mw = p[rw], lw = p[kFewRows + rw];
-            const float4 v = *(const float4*)(p + 2 * kFewRows + rw * D + ch);
-            if (mw == -INFINITY) continue;
-            const float m_new = fmaxf(mx, mw), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mw - m_new);
-            sum = sum * keep + f * lw;
-            acc.x = acc.x * keep + f * v.x, acc.y = acc.y * keep + f * v.y, acc.z = acc.z * keep + f * v.z, acc.w = acc.w * keep + f * v.w;
-            mx = m_new;
+        for (unsigned long long w = w0 + share; w <= w1; w += kAhead * kSplit) {
+            float mw[kAhead], lw[kAhead];
+            float4 v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {            // on their way together
+                const float* const p = part_of(min(w + i * kSplit, w1));
+                mw[i] = w + i * kSplit <= w1 ? p[rw] : -INFINITY;
+                lw[i] = p[kFewRows + rw];
+                v[i] = *(const float4*)(p + 2 * kFewRows + rw * D + ch);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (mw[i] == -INFINITY) continue;
+                const float m_new = fmaxf(mx, mw[i]), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mw[i] - m_new);
+                sum = sum * keep + f * lw[i];
+                acc.x = acc.x * keep + f * v[i].x, acc.y = acc.y * keep + f * v[i].y, acc.z = acc.z * keep + f * v[i].z, acc.w = acc.w * keep + f * v[i].w;
+                mx = m_new;
+            }
         }
     sums[threadIdx.x] = acc;
     stats[threadIdx.x] = make_float2(mx, sum);
