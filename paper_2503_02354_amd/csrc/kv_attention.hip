@@ -1010,34 +1010,41 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 // Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.  Latency: 8.4 us with 25 cut units of 8 heads, 4.7 without any.  The last
 // workgroup of a unit doing it instead costs more: what makes parts visible on all of the chip, a release of the second-level cache, slowed
 // the units down from 88 to 183 us.
+constexpr int kUnitRows = 16;
+template <int D> constexpr int kUnitThreads = kUnitRows * D / 4;          // four channels of a row each
 template <int D>
-__global__ __launch_bounds__(256) void kv_attention_join_units_kernel(KvCache c, KvAttention a, const char* workspace, ManyLayout layout)
+__global__ __launch_bounds__(kUnitThreads<D>) void kv_attention_join_units_kernel(KvCache c, KvAttention a, const char* workspace, ManyLayout layout)
 {
     const int kvh = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
     const int n_joined = ((const ManyHeader*)(workspace + layout.header))->joined;
     const Joined u = ((const Joined*)(workspace + layout.joined))[index];         // its place is there in any case
     if (index >= n_joined) return;
-    const int q0 = u.q0;
     const size_t stride = (size_t)c.kv_heads * (2 * kManyRows + kManyRows * D);
     const float* const parts = (const float*)(workspace + layout.parts) + ((size_t)u.part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * D);
-    for (int i = threadIdx.x; i < 16 * (D / 4); i += 256) {
-        const int rw = blockIdx.y * 16 + i / (D / 4), ch = i % (D / 4) * 4, row = u.first_row + rw;
-        if (row >= u.rows) continue;
-        float mx = -INFINITY, sum = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-        for (int p = 0; p < u.parts; ++p) {
-            const float* const from = parts + p * stride;
-            const float mp = from[rw], lp = from[kManyRows + rw];
-            const float4 v = *(const float4*)(from + 2 * kManyRows + rw * D + ch);
-            if (mp == -INFINITY) continue;
-            const float m_new = fmaxf(mx, mp), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mp - m_new);
-            sum = sum * keep + f * lp;
-            acc.x = acc.x * keep + f * v.x, acc.y = acc.y * keep + f * v.y, acc.z = acc.z * keep + f * v.z, acc.w = acc.w * keep + f * v.w;
+    const int rw = blockIdx.y * kUnitRows + (int)threadIdx.x / (D / 4), ch = (int)threadIdx.x % (D / 4) * 4, row = u.first_row + rw;
+    if (row >= u.rows) return;
+    float mx = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < u.parts; p += kAhead) {
+        float mp[kAhead], lp[kAhead];
+        float4 v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {                // on their way together
+            const float* const from = parts + min(p + i, u.parts - 1) * stride;
+            mp[i] = p + i < u.parts ? from[rw] : -INFINITY;
+            lp[i] = from[kManyRows + rw];
+            v[i] = *(const float4*)(from + 2 * kManyRows + rw * D + ch);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (mp[i] == -INFINITY) continue;
+            const float m_new = fmaxf(mx, mp[i]), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mp[i] - m_new);
+            sum = sum * keep + f * lp[i];
+            acc.x = acc.x * keep + f * v[i].x, acc.y = acc.y * keep + f * v[i].y, acc.z = acc.z * keep + f * v[i].z, acc.w = acc.w * keep + f * v[i].w;
             mx = m_new;
         }
-        finish_row(c, a, q0, kvh, row, ch, mx, sum, acc);
     }
+    finish_row(c, a, u.q0, kvh, row, ch, mx, sum, acc);
 }
 
 // channels that the kernels compute with: the next multiple of 32
@@ -1103,7 +1110,7 @@ template <int D> hipError_t launch_many(const KvCache& c, const KvAttention& a, 
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(kv_attention_many_kernel<D>, dim3((unsigned)(at.most_units * c.kv_heads)), dim3(64 * kManyWaves), kLds, stream, c, a, workspace, at);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kv_attention_join_units_kernel<D>, dim3((unsigned)(at.most_joined * c.kv_heads), kManyRows / 16), dim3(256), 0, stream, c, a, workspace, at);
+    hipLaunchKernelGGL(kv_attention_join_units_kernel<D>, dim3((unsigned)(at.most_joined * c.kv_heads), kManyRows / kUnitRows), dim3(kUnitThreads<D>), 0, stream, c, a, workspace, at);
     return hipGetLastError();
 }
 
