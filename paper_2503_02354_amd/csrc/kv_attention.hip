@@ -608,7 +608,7 @@ __device__ __forceinline__ void tiles_of(const Span& s, int window, int group, i
 }
 
 // One workgroup: latency.  7.5 us for 40 requests, five round trips to memory and a few scans.
-constexpr int kSchedThreads = 1024, kSchedBins = 2048;
+constexpr int kSchedThreads = 1024, kSchedBins = 2048, kSchedInLds = 4096;
 __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(KvCache c, KvAttention a, char* workspace, ManyLayout at)
 {
     extern __shared__ int32_t first_segment[];            // [n_requests + 1] row tiles before request r
@@ -617,10 +617,12 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
     __shared__ int32_t n_parts, n_joined;
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n = a.n_requests;
     const int group = a.heads / c.kv_heads, table_tokens = a.max_blocks << c.block_shift;
-    auto sum_before = [&](unsigned long long v, unsigned long long& all) {
-        unsigned long long sum = v;
+    int32_t *const news = first_segment + n + 1, *const firsts = news + n, *const q0s = firsts + n;        // of the requests, where they fit
+    const bool in_lds = n <= kSchedInLds;
+    auto sum_before = [&](uint32_t v, unsigned long long& all) {          // 64 of them are below 2^32
+        uint32_t sum = v;
         for (int d = 1; d < 64; d <<= 1) {
-            const unsigned long long u = __shfl_up(sum, d, 64);
+            const uint32_t u = __shfl_up(sum, d, 64);
             if (lane >= d) sum += u;
         }
         __syncthreads();
@@ -628,9 +630,11 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
         __syncthreads();
         unsigned long long before = sum - v;
         all = 0;
+#pragma unroll
         for (int w = 0; w < kSchedThreads / 64; ++w) {
-            if (w < wid) before += wave_sum[w];
-            all += wave_sum[w];
+            const unsigned long long u = wave_sum[w];
+            before += w < wid ? u : 0;
+            all += u;
         }
         return before;
     };
@@ -639,10 +643,15 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
         int v = 0;
         if (r0 + tid < n) {
             const Span s = span_of(a, r0 + tid, group, table_tokens);
-            v = (s.rows + kManyRows - 1) / kManyRows;
+            v = (s.rows + kManyRows - 1) / kManyRows;     // below 2^24
+            if (in_lds) {
+                news[r0 + tid] = s.m;
+                firsts[r0 + tid] = s.first_pos;
+                q0s[r0 + tid] = max(0, min(a.q_off[r0 + tid], a.n_tokens));
+            }
         }
         unsigned long long all;
-        const unsigned long long before = segments + sum_before((unsigned)v, all);
+        const unsigned long long before = segments + sum_before((uint32_t)v, all);
         if (r0 + tid < n) first_segment[r0 + tid] = (int32_t)min(before, (unsigned long long)at.most_units);
         segments += all;
     }
@@ -651,7 +660,7 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
     for (int i = tid; i < kSchedBins; i += kSchedThreads) bins[i] = 0;
     if (tid == 0) n_parts = n_joined = 0;
     __syncthreads();
-    struct Segment { int r, row, first, tiles; Span s; };
+    struct Segment { int r, row, first, tiles, q0; Span s; };
     auto find = [&](int i) {
         Segment g;
         int r = 0;
@@ -661,18 +670,23 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
             else hi = mid;
         }
         g.r = r;
-        g.s = span_of(a, r, group, table_tokens);
+        g.s = in_lds ? make_span(news[r], firsts[r], group, a.window) : span_of(a, r, group, table_tokens);
+        g.q0 = in_lds ? q0s[r] : max(0, min(a.q_off[r], a.n_tokens));
         g.row = (i - first_segment[r]) * kManyRows;
         tiles_of(g.s, a.window, group, g.row, g.first, g.tiles);
         return g;
     };
     const Segment own = tid < count ? find(tid) : Segment{};             // the only one in most steps
     auto segment = [&](int i) { return i == tid ? own : find(i); };
-    unsigned long long mine = 0, total;
-    for (int i = tid; i < count; i += kSchedThreads) {
-        mine += (unsigned)segment(i).tiles;
-    }
-    (void)sum_before(mine, total);
+    unsigned long long mine = 0;
+    for (int i = tid; i < count; i += kSchedThreads) mine += (unsigned)segment(i).tiles;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d, 64);
+    if (lane == 0) wave_sum[wid] = mine;      // read by all before the barrier that ends the segments' sums
+    __syncthreads();
+    unsigned long long total = 0;
+#pragma unroll
+    for (int w = 0; w < kSchedThreads / 64; ++w) total += wave_sum[w];
     // no part is shorter than 8 tiles, or than what fills the chip once
     const int most = (int)max(8ull, (total * (unsigned)c.kv_heads + kManyGroups - 1) / kManyGroups);
     // longest first: by length, the longer halves of the range in coarser steps
@@ -692,7 +706,7 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
             sum += own[j];
         }
         unsigned long long all;
-        int before = (int)sum_before((unsigned)sum, all);
+        int before = (int)sum_before((uint32_t)sum, all);
         for (int j = 0; j < kPer; ++j) {
             bins[tid * kPer + j] = before;
             before += own[j];
@@ -704,7 +718,7 @@ __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(Kv
     Joined* const joined = (Joined*)(workspace + at.joined);
     for (int i = tid; i < count; i += kSchedThreads) {
         const Segment g = segment(i);
-        const int tiles = g.tiles, parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts, q0 = max(0, min(a.q_off[g.r], a.n_tokens));
+        const int tiles = g.tiles, parts = (tiles + most - 1) / most, each = (tiles + parts - 1) / parts, q0 = g.q0;
         const int to = atomicAdd(&bins[bin_of(each)], parts);
         int part = -1;
         if (parts > 1) {
@@ -1103,10 +1117,12 @@ template <int D> hipError_t launch_many(const KvCache& c, const KvAttention& a, 
     static const hipError_t configured[2] = {
         hipFuncSetAttribute((const void*)kv_attention_many_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds),
         hipFuncSetAttribute((const void*)kv_attention_schedule_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (kPlanMaxRequests + 1) * 4)};
+    static_assert(4 * kSchedInLds <= kPlanMaxRequests, "lengths beside the sums");
     if (configured[0] != hipSuccess || configured[1] != hipSuccess) return configured[0] != hipSuccess ? configured[0] : configured[1];
     const ManyLayout at = many_layout(a.n_requests, a.n_tokens, a.heads, c.kv_heads, D);
     if (at.most_units * c.kv_heads > 0x7FFFFFFFll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kv_attention_schedule_kernel, dim3(1), dim3(kSchedThreads), (a.n_requests + 1) * 4, stream, c, a, workspace, at);
+    const size_t sched_lds = ((a.n_requests <= kSchedInLds ? 4 : 1) * (size_t)a.n_requests + 1) * 4;
+    hipLaunchKernelGGL(kv_attention_schedule_kernel, dim3(1), dim3(kSchedThreads), sched_lds, stream, c, a, workspace, at);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(kv_attention_many_kernel<D>, dim3((unsigned)(at.most_units * c.kv_heads)), dim3(64 * kManyWaves), kLds, stream, c, a, workspace, at);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
