@@ -17,7 +17,7 @@ namespace {
 // workgroup computes the sums of all requests for itself in LDS, where a token finds its request by bisection; the workgroups
 // then share the tokens and the requests.  None waits for another: a token of a new block takes the block's id from the ring, not
 // from the table that some other workgroup writes.
-// What bounds it: latency (lengths in, one scan, slots out): 7.3 us for 192 requests with a token each, 12.0 us for 1500 requests and 86,000
+// What bounds it: latency (lengths in, one scan, slots out): 7.4 us for 192 requests with a token each, 8.5 us for 1500 requests and 86,000
 // tokens, of which a launch with one load and one store takes 2.8.
 constexpr int kPlanThreads = 256;
 constexpr int kPlanInLds = 8192;              // requests whose lengths stay in LDS beside the sums (96 KiB); more ask memory again, per token
@@ -88,8 +88,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
     __syncthreads();
     // Sums past the request that closes the step may wrap and are not used; up to it they are exact (each term is below 2^31 and the
     // sum before it within the limits).
-    const int per = (n + kPlanThreads - 1) / kPlanThreads, begin = min(n, tid * per), end = min(n, begin + per);
-    uint32_t own[3] = {0, 0, 0};
+    const int per = (n + kPlanThreads - 1) / kPlanThreads | 1, begin = min(n, tid * per), end = min(n, begin + per);
+    uint32_t own[3] = {0, 0, 0};              // an odd number of requests to a thread: LDS banks apart
     for (int r = begin; r < end; ++r) {
         const uint32_t b = blk[r];
         own[0] += b & kFreed ? 0u : b & ~kTooLong;
@@ -209,8 +209,10 @@ hipError_t kv_plan(int32_t n, int32_t block_shift, int32_t n_blocks, int32_t max
     static const hipError_t configured = hipFuncSetAttribute((const void*)kv_plan_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                              (int)((2 * (size_t)kPlanMaxRequests + 1) * 4));
     if (configured != hipSuccess) return configured;
-    const int by_tokens = (int)(((long long)token_cap + 1023) / 1024), by_requests = (n + 1023) / 1024;
-    const int grid = std::max(1, std::min(256, std::max(by_tokens, by_requests)));
+    // A thread for every token while scans are short: 1500 requests with 86,000 tokens 8.4 us, 11.9 with four tokens to a thread; many requests one
+    // workgroup per compute unit: 8000 with 240,000 tokens 23.5 us, 38 with two; 4000 with 200,000 15.1 and 13.8.
+    const int by_tokens = (int)(((long long)token_cap + kPlanThreads - 1) / kPlanThreads), by_requests = (n + kPlanThreads - 1) / kPlanThreads;
+    const int grid = std::max(1, std::min(n <= 4096 ? 512 : 256, std::max(by_tokens, by_requests)));
     hipLaunchKernelGGL(kv_plan_kernel, dim3(grid), dim3(kPlanThreads), lds, stream, n, block_shift, n_blocks, max_blocks, token_cap, have, add, ring,
                        ring_state, table, seq_len, q_off, slot, position, next_state);
     return hipGetLastError();
