@@ -195,8 +195,8 @@ __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_
 // finished here.  Inside a stretch the four wavefronts take tiles in turn, each for itself: keys go from memory straight into
 // registers (they are the first operand as they lie), values through registers into LDS of the wavefront's own, and the next tile's
 // are on their way while this one is multiplied.
-// What bounds it: HBM, keys and values once.  96 requests of 50 to 5000 tokens, 32 heads on 8 of 128 channels: 1.006 GB in 214 to 220 us, 4.6 TB/s
-// (a copy of 2 GiB: 4.9); 3 of 90,000 to 131,000 tokens, 32 heads on 4: 0.72 GB in 140 us, 5.2 TB/s.  Joining the parts takes 7 to 9 us.
+// What bounds it: HBM, keys and values once.  96 requests of 50 to 5000 tokens, 32 heads on 8 of 128 channels: 1.006 GB in 213 to 220 us, 4.7 TB/s
+// (a copy of 2 GiB: 4.9); 3 of 90,000 to 131,000 tokens, 32 heads on 4: 0.72 GB in 136 to 141 us, 5.2 TB/s.  Joining the parts takes 6 to 7 us.
 // Two workgroups per compute unit are all that 250 registers a lane allow, and they suffice: LDS and matrix cores stand idle.
 struct FewHeader {                        // at the workspace's start, for the joining kernel
     unsigned long long per;               // tiles of a stretch
@@ -491,8 +491,9 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void kv_attention_short_kern
 
 // Adds up the parts of a history that several workgroups shared: a workgroup per request, cache head and kJoinRows query rows
 // (blockIdx.y).  Several threads share the parts of a row's four channels, since a long history has many; each leaves its sum
-// relative to its own maximum, and the first adds those up in their order.  What bounds it: round trips to memory.  96 requests: 7.2 us with a
-// row to a workgroup of 256 threads, 18.5 with 1024 (three requests of 131,000 tokens, hundreds of parts to a history: 9.3 and 8.3).
+// relative to its own maximum, and the first adds those up in their order.  What bounds it: round trips to memory, so every thread fetches
+// four parts at a time: three histories of 131,000 tokens, a hundred parts and more to each, 6.1 us (9.2 with two at a time, 8.3 with 1024
+// threads, which cost 96 requests 18.5 instead of 6.7).
 constexpr int kJoinRows = 1, kAhead = 4;
 template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAttention a, const char* workspace)
@@ -607,7 +608,7 @@ __device__ __forceinline__ void tiles_of(const Span& s, int window, int group, i
     count = max(1, (end + kManyKeys - 1) / kManyKeys - first);
 }
 
-// One workgroup: latency.  7.5 us for 40 requests, five round trips to memory and a few scans.
+// One workgroup: latency.  6.7 us for 40 requests.
 constexpr int kSchedThreads = 1024, kSchedBins = 2048, kSchedInLds = 4096;
 __global__ __launch_bounds__(kSchedThreads) void kv_attention_schedule_kernel(KvCache c, KvAttention a, char* workspace, ManyLayout at)
 {
@@ -1021,7 +1022,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 #endif
 }
 
-// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.  Latency: 8.4 us with 25 cut units of 8 heads, 4.7 without any.  The last
+// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.  Latency: 7.8 us with 25 cut units of 8 heads, 4.7 without any.  The last
 // workgroup of a unit doing it instead costs more: what makes parts visible on all of the chip, a release of the second-level cache, slowed
 // the units down from 88 to 183 us.
 constexpr int kUnitRows = 16;
