@@ -908,7 +908,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     // the half (t, kb), whose scores are in `cur`; the next half's, (tn, kn), go to `to` (of no use behind the last one, and not used)
     auto half_step = [&](f32x16& cur, f32x16& to, int t, int kb, int tn, int kn) __attribute__((always_inline)) {
         const bool masked = is_masked(t, kb);
-        // Reads run ahead of their use by a phase: keys come while the exponentials are taken, values while scores are multiplied.
+        // Scores are multiplied between the exponentials of the half before; operands come while the first of those are taken, or earlier.
         u32x4 k[kSteps], pw[2];
         read_keys(k, kn);
         if (kn == 1) {
@@ -916,10 +916,26 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 #pragma unroll
             for (int ks = 0; ks < kSteps; ++ks) k_read[ks] += on;
         }
+        if (kb == 1) {
+            read_half(v0, kb, 0);
+            read_half(v1, kb, 1);
+            const uint32_t on = t % 3 == 2 ? -2 * kTile : kTile;
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db) v_read[db][0] += on, v_read[db][1] += on;
+        }
         __builtin_amdgcn_sched_barrier(0);
         // The reference is a row's first maximum, and follows it only when a half exceeds it by some 2^16: floats of any size are equally exact (values up to 2^110 find room), and
         // looking for the maximum of every half costs a quarter of the vector instructions.
         float sum = weigh(cur, pw);
+        scores(to, k);
+        asm volatile("" : "+v"(pw[0]), "+v"(pw[1]));
+        __builtin_amdgcn_sched_group_barrier(0x402, 20, 0);
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         const bool left = !(sum <= 0x1p16f) || m == -INFINITY;
         if (__any(left)) {                    // of this row, in either half of the wavefront: what other rows need does not change its bits
             const bool moves = left | (__shfl_xor((int)left, 32, 64) != 0);
@@ -928,17 +944,6 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             sum = weigh(cur, pw);
         }
         l += sum;
-        if (kb == 1) read_half(v0, kb, 0);
-        asm volatile("" : "+v"(pw[0]), "+v"(pw[1]), "+v"(l));             // here, and not where they are used
-        __builtin_amdgcn_sched_barrier(0);
-        scores(to, k);
-        if (kb == 1) {
-            read_half(v1, kb, 1);
-            const uint32_t on = t % 3 == 2 ? -2 * kTile : kTile;
-#pragma unroll
-            for (int db = 0; db < kBlocks; ++db) v_read[db][0] += on, v_read[db][1] += on;
-        }
-        __builtin_amdgcn_sched_barrier(0);
         if (masked) {
             const uint32_t vt = lds0 + (2 + t % 3) * kTile + kb * 32 * DH * 2, odd = odd_keys<D>(vt);
             if (odd) {
