@@ -338,7 +338,8 @@ int coe_kv_append(const coe_kv_cache* cache, int32_t n_tokens, const void* k, in
  * belong to no request are not read, and theirs of out and lse not written.
  * q and out: row t, head h at t * token_stride + h * head_stride elements of the cache's dtype, 16-byte aligned, strides
  * multiples of 8.  lse: [n_tokens][heads] fp32, or NULL.  table: [n_requests][max_blocks] block ids; a cached token whose
- * block id is outside the cache reads as zeros; seq_len is limited to max_blocks * block_size.
+ * block id is outside the cache reads as zeros; seq_len is limited to max_blocks * block_size.  max_blocks and max_new are all that
+ * the host knows of the lengths: steps whose tables and chunks can only be small take fewer launches.
  * Numerics: products and sums in fp32, exponentials relative to a running reference (the maximum so far, which may be behind by
  * up to 2^16; values up to 2^110 in magnitude find room), the probabilities rounded to bf16 before they meet the values, one
  * rounding of the result to bf16.  The same inputs give the same bits.
