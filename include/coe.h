@@ -333,8 +333,8 @@ int coe_kv_append(const coe_kv_cache* cache, int32_t n_tokens, const void* k, in
  * seq_len as coe_kv_plan writes them); with m of them, row i stands at position p = seq_len[r] - m + i and sees the cached
  * tokens j <= p, with window > 0 only those with j > p - window.  Query head h reads cache head h / (heads / kv_heads).
  *   out = softmax_j(scale * q . k_j) v_j      lse = ln sum_j exp(scale * q . k_j)
- * A row that sees nothing (p < 0), or whose scores are all -inf, gets out = 0 and lse = -inf.  What a row does not see does not
- * reach it, whatever its bits.  Of a request with more than max_new new tokens the first max_new are served; rows of q that
+ * A row that sees nothing (p < 0), or whose scores are all -inf, gets out = 0 and lse = -inf; one with a score that is NaN gets NaN
+ * for both.  What a row does not see does not reach it, whatever its bits.  Of a request with more than max_new new tokens the first max_new are served; rows of q that
  * belong to no request are not read, and theirs of out and lse not written.
  * q and out: row t, head h at t * token_stride + h * head_stride elements of the cache's dtype, 16-byte aligned, strides
  * multiples of 8.  lse: [n_tokens][heads] fp32, or NULL.  table: [n_requests][max_blocks] block ids; a cached token whose

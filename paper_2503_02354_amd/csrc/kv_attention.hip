@@ -85,15 +85,24 @@ __device__ __forceinline__ Span span_of(const KvAttention& a, int r, int group, 
     return make_span(min(m_all, a.max_new), len - m_all, group, a.window);
 }
 
+// Nothing above -inf among a row's scores.  A maximum passes NaN by, a sum does not: where the scores are NaN and none is above -inf, the
+// maximum is -inf too, but the sum is NaN.
+__device__ __forceinline__ bool is_empty(float mx, float sum) { return mx == -INFINITY && sum == 0.f; }
+
+// What a part relative to 2^from weighs relative to 2^to, the larger: 1 where both are -inf (or inf), so that a NaN in a part stays.
+[[maybe_unused]] __device__ __forceinline__ float weight_of_part(float from, float to) { return from == to ? 1.f : exp2f(from - to); }
+
 // Four channels of query row `row` of a request and cache head, from the unnormalised output relative to maximum mx.
 __device__ __forceinline__ void finish_row(const KvCache& c, const KvAttention& a, int q0, int kvh, int row, int ch, float mx, float sum, float4 acc)
 {
     const int group = a.heads / c.kv_heads, token = row / group, head = kvh * group + (row - token * group);
-    const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+    const bool empty = is_empty(mx, sum);
+    if (empty) acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float inv = empty ? 0.f : 1.f / sum;
     if (ch < c.head_dim)
         *(uint2*)(a.out + (int64_t)(q0 + token) * a.out_token_stride + (int64_t)head * a.out_head_stride + ch) =
             make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-    if (a.lse && ch == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+    if (a.lse && ch == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = empty ? -INFINITY : (mx + log2f(sum)) * kLn2;
 }
 
 // Where 16-byte chunk c of row r of a V tile lies: chunks in an order that spreads both the writes (sixteen rows of
@@ -370,7 +379,6 @@ __device__ __forceinline__ void few_rows(const KvCache& c, const KvAttention& a,
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const float mw = stat[0][w][rw];
-            if (mw == -INFINITY) continue;
             const float f = mw == mx ? 1.f : exp2_fast(mw - mx);
             const float4 v = *(const float4*)((const float*)lds + (w * kFewRows + rw) * kMergeRow<D> + ch);
             sum += f * stat[1][w][rw];
@@ -524,14 +532,14 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {            // on their way together
                 const float* const p = part_of(min(w + i * kSplit, w1));
-                mw[i] = w + i * kSplit <= w1 ? p[rw] : -INFINITY;
+                mw[i] = p[rw];
                 lw[i] = p[kFewRows + rw];
                 v[i] = *(const float4*)(p + 2 * kFewRows + rw * D + ch);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (mw[i] == -INFINITY) continue;
-                const float m_new = fmaxf(mx, mw[i]), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mw[i] - m_new);
+                if (w + i * kSplit > w1) continue;
+                const float m_new = fmaxf(mx, mw[i]), keep = weight_of_part(mx, m_new), f = weight_of_part(mw[i], m_new);
                 sum = sum * keep + f * lw[i];
                 acc.x = acc.x * keep + f * v[i].x, acc.y = acc.y * keep + f * v[i].y, acc.z = acc.z * keep + f * v[i].z, acc.w = acc.w * keep + f * v[i].w;
                 mx = m_new;
@@ -546,8 +554,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
     acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = 0; i < kSplit; ++i) {
         const float2 st = stats[i * kColumns + column];
-        if (st.x == -INFINITY) continue;
-        const float f = exp2f(st.x - mx);
+        const float f = weight_of_part(st.x, mx);
         const float4 v = sums[i * kColumns + column];
         sum += f * st.y;
         acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
@@ -1002,7 +1009,13 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
     l = sum_halves(l);
     if (!row_ok) return;
     if (part < 0) {
-        const float inv = m == -INFINITY ? 0.f : 1.f / l;
+        const bool empty = is_empty(m, l);
+        const float inv = empty ? 0.f : 1.f / l;
+        if (empty)
+#pragma unroll
+            for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[db][x] = 0.f;
         uint16_t* const to = a.out + (int64_t)(q0 + token) * a.out_token_stride + (int64_t)head * a.out_head_stride + half * 4;
 #pragma unroll
         for (int db = 0; db < kBlocks; ++db)
@@ -1010,7 +1023,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             for (int g = 0; g < 4; ++g)
                 if (db * 32 + g * 8 < c.head_dim)
                     *(uint2*)(to + db * 32 + g * 8) = make_uint2(pack_bf16(o[db][4 * g] * inv, o[db][4 * g + 1] * inv), pack_bf16(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv));
-        if (a.lse && half == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+        if (a.lse && half == 0) a.lse[(int64_t)(q0 + token) * a.heads + head] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
     } else {
         float* const to = (float*)(workspace + layout.parts) + ((size_t)part * c.kv_heads + kvh) * (2 * kManyRows + kManyRows * D);
         const int rw = wid * 32 + l32;
@@ -1051,14 +1064,14 @@ __global__ __launch_bounds__(kUnitThreads<D>) void kv_attention_join_units_kerne
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {                // on their way together
             const float* const from = parts + min(p + i, u.parts - 1) * stride;
-            mp[i] = p + i < u.parts ? from[rw] : -INFINITY;
+            mp[i] = from[rw];
             lp[i] = from[kManyRows + rw];
             v[i] = *(const float4*)(from + 2 * kManyRows + rw * D + ch);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (mp[i] == -INFINITY) continue;
-            const float m_new = fmaxf(mx, mp[i]), keep = mx == -INFINITY ? 0.f : exp2f(mx - m_new), f = exp2f(mp[i] - m_new);
+            if (p + i >= u.parts) continue;
+            const float m_new = fmaxf(mx, mp[i]), keep = weight_of_part(mx, m_new), f = weight_of_part(mp[i], m_new);
             sum = sum * keep + f * lp[i];
             acc.x = acc.x * keep + f * v[i].x, acc.y = acc.y * keep + f * v[i].y, acc.z = acc.z * keep + f * v[i].z, acc.w = acc.w * keep + f * v[i].w;
             mx = m_new;

@@ -937,3 +937,60 @@ def test_attention_chunks_wide_tables_odd_inputs(B):
     for _ in range(3):
         got = a.run()
         assert np.array_equal(got[0], base[0]) and np.array_equal(got[1], base[1])
+
+
+# ---- scores that are no numbers -----------------------------------------------------------------------------------
+# lengths that each kernel serves: (kind of tables, requests, the tokens of request 0 whose keys become NaN)
+NAN_PATHS = {
+    "narrow tables, single tokens": (Attend, [(100, 1), (40, 1), (0, 1)], range(32, 64)),
+    "narrow tables, chunks": (Attend, [(100, 20), (10, 30)], range(32, 64)),
+    "wide tables, single tokens": (Wide, [(100, 1), (40, 1), (0, 1)], range(32, 64)),
+    "stretches that are joined": (Attend, [(9000, 1), (40, 1), (0, 2)], range(256, 384)),
+    "units": (Wide, [(100, 60), (0, 90), (3, 1)], range(64, 128)),
+    "units that are cut": (Wide, [(5000, 40), (0, 33), (7, 1)], range(512, 1024)),
+}
+
+
+@pytest.mark.parametrize("path", NAN_PATHS)
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 64), (4, 4, 80)])
+def test_attention_scores_that_are_no_numbers(B, path, heads, kv, dim):
+    """A NaN score makes its row NaN, output and logarithm, whichever wavefront, part or unit meets it; no other row's bits change."""
+    kind, lengths, keys = NAN_PATHS[path]
+    a = kind(B, lengths, heads, kv, dim, seed=dim)
+    base, base_lse = a.run()
+    q, bits = a.q.copy(), a.bits.copy()
+
+    def expect(bad):                                  # [token][head]
+        got, lse = a.run()
+        numbers = int(np.count_nonzero(~np.isnan(T.bf16_to_f64(got[bad])))), int(np.count_nonzero(~np.isnan(lse[bad])))
+        changed = int(np.count_nonzero(got[~bad] != base[~bad])), int(np.count_nonzero(lse[~bad] != base_lse[~bad]))
+        assert numbers == (0, 0) and changed == (0, 0)
+        a.q[:], a.bits[:] = q, bits
+    for place in (0, len(base) - 1, int(a.off[1])):   # a query with a NaN: all of a row's scores
+        bad = np.zeros(base.shape[:2], bool)
+        bad[place, 1] = True
+        a.q[place, 1, 3] = 0x7FC0
+        expect(bad)
+    for some in (list(keys), [keys[5]], list(range(int(a.total[0])))):              # keys: of a stretch, one, of all a row's tokens
+        bad = np.zeros(base.shape[:2], bool)
+        for j in some:
+            a.bits[(0,) + a.at(0, j)] = 0x7FC0
+        for i in range(a.new[0]):
+            bad[i] = min(some) <= a.total[0] - a.new[0] + i
+        expect(bad)
+
+
+@pytest.mark.parametrize("path", NAN_PATHS)
+def test_attention_scores_that_are_all_minus_infinity(B, path):
+    """A row whose scores are all -inf gets zeros and -inf, whatever its values hold."""
+    kind, lengths, _ = NAN_PATHS[path]
+    a = kind(B, lengths, 8, 2, 64, seed=1)
+    base, base_lse = a.run()
+    a.q[:a.off[1]] = _bf16(np.ones_like(a.q[:a.off[1]], np.float64))
+    base[:a.off[1]], base_lse[:a.off[1]] = 0, -np.inf
+    for value in (0x3F80, 0x7F80, 0x7FC0):
+        for j in range(int(a.total[0])):
+            a.bits[(0,) + a.at(0, j)] = 0xFF80
+            a.bits[(1,) + a.at(0, j)] = value
+        got, lse = a.run()
+        assert not np.count_nonzero(got != base) and not np.count_nonzero(lse != base_lse)
