@@ -340,9 +340,10 @@ int coe_kv_append(const coe_kv_cache* cache, int32_t n_tokens, const void* k, in
  * multiples of 8.  lse: [n_tokens][heads] fp32, or NULL.  table: [n_requests][max_blocks] block ids; a cached token whose
  * block id is outside the cache reads as zeros; seq_len is limited to max_blocks * block_size.  max_blocks and max_new are all that
  * the host knows of the lengths: steps whose tables and chunks can only be small take fewer launches.
- * Numerics: products and sums in fp32, exponentials relative to a running reference (the maximum so far, which may be behind by
- * up to 2^16; values up to 2^110 in magnitude find room), the probabilities rounded to bf16 before they meet the values, one
- * rounding of the result to bf16.  The same inputs give the same bits.
+ * Numerics: products and sums in fp32, exponentials relative to a running reference (the maximum so far, or as far from it as
+ * keeps a row's sum below 2^17; values up to 2^110 in magnitude find room, whatever the length, in steps of fewer than 2^26 cached
+ * tokens x cache heads), the probabilities rounded to bf16 before they meet the values, one rounding of the result to bf16.  The
+ * same inputs give the same bits.
  * heads: a multiple of kv_heads.  workspace: coe_kv_attention_workspace bytes for the same sizes, 16-byte aligned. */
 int64_t coe_kv_attention_workspace(int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads, int32_t kv_heads,
                                    int32_t head_dim);

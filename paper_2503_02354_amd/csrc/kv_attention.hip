@@ -92,13 +92,18 @@ __device__ __forceinline__ bool is_empty(float mx, float sum) { return mx == -IN
 // What a part relative to 2^from weighs relative to 2^to, the larger: 1 where both are -inf (or inf), so that a NaN in a part stays.
 [[maybe_unused]] __device__ __forceinline__ float weight_of_part(float from, float to) { return from == to ? 1.f : exp2f(from - to); }
 
-// Four channels of query row `row` of a request and cache head, from the unnormalised output relative to maximum mx.
-__device__ __forceinline__ void finish_row(const KvCache& c, const KvAttention& a, int q0, int kvh, int row, int ch, float mx, float sum, float4 acc)
+// Room for values of 2^110: the weights that meet in a sum of fp32 add up to 2^17, so that they and the values stay below 2^128.  A part's
+// own do: the few-rows kernel's are 1 at most (and its stretches hold 2^17 keys of a history at most, unless a step has 2^26 cached tokens x cache heads), the
+// many-rows kernel moves its reference.  Joining adds up to some 512 parts: their outputs are taken times 2^-10 and the result back.
+[[maybe_unused]] constexpr float kJoinRoom = 0x1p-10f;
+
+// Four channels of query row `row` of a request and cache head, from the unnormalised output (divided by `grow`) relative to maximum mx.
+__device__ __forceinline__ void finish_row(const KvCache& c, const KvAttention& a, int q0, int kvh, int row, int ch, float mx, float sum, float4 acc, float grow = 1.f)
 {
     const int group = a.heads / c.kv_heads, token = row / group, head = kvh * group + (row - token * group);
     const bool empty = is_empty(mx, sum);
     if (empty) acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float inv = empty ? 0.f : 1.f / sum;
+    const float inv = empty ? 0.f : grow / sum;
     if (ch < c.head_dim)
         *(uint2*)(a.out + (int64_t)(q0 + token) * a.out_token_stride + (int64_t)head * a.out_head_stride + ch) =
             make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
@@ -541,7 +546,8 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
                 if (w + i * kSplit > w1) continue;
                 const float m_new = fmaxf(mx, mw[i]), keep = weight_of_part(mx, m_new), f = weight_of_part(mw[i], m_new);
                 sum = sum * keep + f * lw[i];
-                acc.x = acc.x * keep + f * v[i].x, acc.y = acc.y * keep + f * v[i].y, acc.z = acc.z * keep + f * v[i].z, acc.w = acc.w * keep + f * v[i].w;
+                const float g = f * kJoinRoom;
+                acc.x = acc.x * keep + g * v[i].x, acc.y = acc.y * keep + g * v[i].y, acc.z = acc.z * keep + g * v[i].z, acc.w = acc.w * keep + g * v[i].w;
                 mx = m_new;
             }
         }
@@ -559,7 +565,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAtt
         sum += f * st.y;
         acc.x += f * v.x, acc.y += f * v.y, acc.z += f * v.z, acc.w += f * v.w;
     }
-    finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc);
+    finish_row(c, a, q0, kvh, rw, ch, mx, sum, acc, 1.f / kJoinRoom);
 }
 
 // ---- many query rows (chunks of prompts, single tokens among them): steps with more than 32 per request and cache head that are not short ----
@@ -931,8 +937,10 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             for (int db = 0; db < kBlocks; ++db) v_read[db][0] += on, v_read[db][1] += on;
         }
         __builtin_amdgcn_sched_barrier(0);
-        // The reference is a row's first maximum, and follows it only when a half exceeds it by some 2^16: floats of any size are equally exact (values up to 2^110 find room), and
-        // looking for the maximum of every half costs a quarter of the vector instructions.
+        // The reference is a row's first maximum, and moves only when the row's sum so far, this half's with it, passes 2^16 in a lane (of two): floats of
+        // any size are equally exact, and looking for the maximum of every half costs a quarter of the vector instructions.  It moves to this half's maximum, or
+        // by 2^8 where many keys of little more than the reference's weight made the sum (beyond scores of 2^26, which are 8 and more apart, equal ones may
+        // grow to more).
         float sum = weigh(cur, pw);
         scores(to, k);
         asm volatile("" : "+v"(pw[0]), "+v"(pw[1]));
@@ -943,10 +951,10 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
             __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        const bool left = !(sum <= 0x1p16f) || m == -INFINITY;
+        const bool left = !(l + sum <= 0x1p16f) || m == -INFINITY;
         if (__any(left)) {                    // of this row, in either half of the wavefront: what other rows need does not change its bits
             const bool moves = left | (__shfl_xor((int)left, 32, 64) != 0);
-            const float top = highest(cur);
+            const float top = fmaxf(highest(cur), m + 8.f);
             raise(moves ? top : -INFINITY);
             sum = weigh(cur, pw);
         }
@@ -1073,11 +1081,12 @@ __global__ __launch_bounds__(kUnitThreads<D>) void kv_attention_join_units_kerne
             if (p + i >= u.parts) continue;
             const float m_new = fmaxf(mx, mp[i]), keep = weight_of_part(mx, m_new), f = weight_of_part(mp[i], m_new);
             sum = sum * keep + f * lp[i];
-            acc.x = acc.x * keep + f * v[i].x, acc.y = acc.y * keep + f * v[i].y, acc.z = acc.z * keep + f * v[i].z, acc.w = acc.w * keep + f * v[i].w;
+            const float g = f * kJoinRoom;
+            acc.x = acc.x * keep + g * v[i].x, acc.y = acc.y * keep + g * v[i].y, acc.z = acc.z * keep + g * v[i].z, acc.w = acc.w * keep + g * v[i].w;
             mx = m_new;
         }
     }
-    finish_row(c, a, u.q0, kvh, row, ch, mx, sum, acc);
+    finish_row(c, a, u.q0, kvh, row, ch, mx, sum, acc, 1.f / kJoinRoom);
 }
 
 // channels that the kernels compute with: the next multiple of 32

@@ -994,3 +994,42 @@ def test_attention_scores_that_are_all_minus_infinity(B, path):
             a.bits[(1,) + a.at(0, j)] = value
         got, lse = a.run()
         assert not np.count_nonzero(got != base) and not np.count_nonzero(lse != base_lse)
+
+
+# ---- large values -------------------------------------------------------------------------------------------------
+def _steps_of_scores(a, high):
+    """Scores of 0, and of 7.5 for the 32 keys of every half tile that high(number of the half) names; values of 2^110, every third negative."""
+    a.q[:] = _bf16(np.ones_like(a.q, np.float64))
+    a.scale = 1 / a.dim
+    for r, t in enumerate(a.total):
+        j = np.arange(int(t))
+        at = a.table[r, j // a.block], j % a.block
+        a.bits[(0,) + at] = _bf16(np.where(high(j // 32), 7.5, 0.0))[:, None, None]
+        a.bits[(1,) + at] = np.where(j % 3 == 2, 0xF680, 0x7680).astype(np.uint16)[:, None, None]
+    return a
+
+
+@pytest.mark.parametrize("kind", [Attend, Wide])
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 64), (4, 4, 128)])
+def test_attention_large_values_behind_a_low_start(B, kind, heads, kv, dim):
+    """A row's first keys weigh 2^-11 of the others: sums relative to the first maximum must not grow until values of 2^110 overflow."""
+    for lengths in ([(400, 40), (440, 9)], [(4056, 40), (10, 1)], [(400, 1), (4000, 1)]):
+        for high in (lambda h: h > 0, lambda h: h % 16 >= 8, lambda h: (h % 16 == 1) | (h % 16 == 3)):
+            a = _steps_of_scores(kind(B, lengths, heads, kv, dim, seed=1), high)
+            a.check(*a.run())
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_large_values_of_a_long_history(B, new):
+    """More than 2^18 keys of the same weight, values of 2^110: their sum has no room in fp32, their mean has."""
+    a = _steps_of_scores(Attend(B, [(270000, new)], 2, 1, 8, block=64), lambda h: h < 0)
+    a.bits[1][a.bits[1] == 0xF680] = 0x7680
+    a.check(*a.run())
+
+
+def test_attention_large_values_of_slowly_growing_sums(B):
+    """Weights that are each too small to move a row's reference, and whose sum is not: two parts of seventeen tiles that begin with a low half."""
+    a = _steps_of_scores(Wide(B, [(2060, 33)] * 40, 8, 8, 8, seed=1), lambda h: (h != 0) & (h != 34))
+    a.bits[0][a.bits[0] == 0x40F0] = _bf16(5.3125)
+    a.bits[1][a.bits[1] == 0xF680] = 0x7680
+    a.check(*a.run())
