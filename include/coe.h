@@ -299,7 +299,8 @@ int coe_regroup_static(int32_t n, const int32_t* cur, int32_t n_experts, int32_t
  * give their blocks to the ring's end, in request order; they can be taken from the next call on.
  * Written: seq_len[r] = tokens after the step (0 for a finished request); q_off[n_requests + 1] = first new token of every
  * request in the step's token order; for token t of them position[t] (its place in its request, from 0) and slot[t] =
- * block * block_size + position % block_size, both -1 from the last token up to token_cap; next_state = {head, count,
+ * block * block_size + position % block_size (-1 where the table or the ring holds an id outside 0..n_blocks - 1: such a row is not
+ * appended, and attention reads zeros there), both -1 from the last token up to token_cap; next_state = {head, count,
  * requests before the one that closed the step (n_requests if none did), new tokens}.  Nothing that the next call's inputs
  * need is written in place but the table and the ring: seq_len and next_state serve as have and ring_state then, and must
  * not alias them.  The same inputs give the same outputs, ids included; repeating a call is harmless.

@@ -33,7 +33,8 @@ def plan(block, n_blocks, max_blocks, token_cap, have, add, ring, state, table):
             taken += need
             for p in range(h, h + a):
                 position.append(p)
-                slot.append(int(table[r, p // block]) * block + p % block)
+                b = int(table[r, p // block])
+                slot.append(b * block + p % block if 0 <= b < n_blocks else -1)
             seq_len.append(h + a)
         q_off.append(len(slot))
     n = len(slot)

@@ -1033,3 +1033,24 @@ def test_attention_large_values_of_slowly_growing_sums(B):
     a.bits[0][a.bits[0] == 0x40F0] = _bf16(5.3125)
     a.bits[1][a.bits[1] == 0xF680] = 0x7680
     a.check(*a.run())
+
+
+# ---- block ids outside the cache ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("block", [8, 16, 1024])
+def test_plan_ids_outside_the_cache(B, block):
+    """Ids whose product with the block size would wrap round to a slot of another block give no slot, in the table and in the ring."""
+    n_blocks, width, wrap = 50, 8, 2 ** 32 // block
+    bad = [v - 2 ** 32 if v >= 2 ** 31 else v for v in (wrap + 1, 2 * wrap, 2 ** 32 - wrap, wrap * 3 + 7, n_blocks, 2 ** 31 - 1, 2 ** 32 - 1, 2 ** 31)]
+    bad = [v for v in bad if not 0 <= v < n_blocks and -2 ** 31 <= v < 2 ** 31]
+    n = len(bad)
+    table = np.zeros((n + 2, width), np.int32)
+    table[:n, 0] = bad
+    table[n:, 0] = 11, 12
+    ring = np.full(n_blocks, 13, np.int32)
+    ring[5:5 + n] = bad
+    have, add = [block - 3] * (n + 2), [4] * n + [2, 1]             # three tokens in the table's block, one in a block of the ring
+    args = (block, n_blocks, width, 4 * n + 5, have, add, ring, [5, 40], table)
+    want, got = T.plan(*args), _plan_gpu(B, *args)
+    assert (want["slot"][:4 * n] == -1).all() and want["slot"][4 * n:].tolist() == [11 * block + block - 3, 11 * block + block - 2, 12 * block + block - 3, -1, -1]
+    for k in want:
+        assert np.array_equal(got[k], want[k]), k

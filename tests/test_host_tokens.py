@@ -146,3 +146,11 @@ def test_statement_of_sampling_by_hand():
     assert T.sample(x, 1.0, 0, 0.5, 0.0, e)[0] == {1} and T.sample(x, 1.0, 0, 0.51, 0.0, e)[0] == {2} and T.sample(x, 1.0, 0, 1.0, 0.3, e)[0] == {2}
     assert T.sample(x, 0.0, 0, 1.0, 0.0, e)[0] == {1} and T.sample(np.full(4, -np.inf), 1.0, 0, 1.0, 0.0, e)[0] == {-1}
     assert np.allclose(T.sample(x, 1.0, 0, 1.0, 0.0, e)[1], np.log(np.array([1, 4, 2, 1]) / 8))
+
+
+def test_statement_of_plan_ids_outside_the_cache():
+    """Blocks of 16 of a cache of 8: an id from the table and one from the ring that would wrap round to other blocks' slots in 32 bits."""
+    table = np.array([[0x10000001, 0], [3, 0]], np.int32)
+    out = T.plan(16, 8, 2, 4, [15, 2], [2, 1], np.full(8, -2 ** 28, np.int32), [0, 8], table)
+    assert out["slot"].tolist() == [-1, -1, 3 * 16 + 2, -1] and out["position"].tolist() == [15, 16, 2, -1]
+    assert out["table"].tolist() == [[0x10000001, -2 ** 28], [3, 0]] and out["next_state"].tolist() == [1, 7, 2, 3]
