@@ -149,8 +149,8 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
         const uint32_t to = count + (blk[r] & ~kFreed);
         for (uint32_t j = lane; j < blocks; j += 64) ring[in_ring(head, to + j, (uint32_t)n_blocks)] = table[(size_t)r * max_blocks + j];
     }
-    for (int t = blockIdx.x * kPlanThreads + tid; t < token_cap; t += gridDim.x * kPlanThreads) {
-        if ((uint32_t)t >= tokens) {
+    for (uint32_t t = blockIdx.x * kPlanThreads + tid; t < (uint32_t)token_cap; t += gridDim.x * kPlanThreads) {      // a step past 2^31 stays above the cap
+        if (t >= tokens) {
             slot[t] = -1;
             position[t] = -1;
             continue;
@@ -158,11 +158,11 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(int n, int shift,
         int lo = 0, hi = f;                   // the last request below f that starts at or before t
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (tok[mid] <= (uint32_t)t) lo = mid;
+            if (tok[mid] <= t) lo = mid;
             else hi = mid;
         }
         const uint32_t h = cached(lo), old_blocks = (h + bs - 1) >> shift;
-        const uint32_t pos = h + (uint32_t)t - tok[lo], page = pos >> shift;
+        const uint32_t pos = h + t - tok[lo], page = pos >> shift;
         int32_t* const row = table + (size_t)lo * max_blocks;
         int32_t id;
         if (page < old_blocks) id = row[page];

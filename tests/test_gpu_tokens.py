@@ -1054,3 +1054,18 @@ def test_plan_ids_outside_the_cache(B, block):
     assert (want["slot"][:4 * n] == -1).all() and want["slot"][4 * n:].tolist() == [11 * block + block - 3, 11 * block + block - 2, 12 * block + block - 3, -1, -1]
     for k in want:
         assert np.array_equal(got[k], want[k]), k
+
+
+# ---- sizes at the end of 32 bits ----------------------------------------------------------------------------------
+def test_plan_of_the_largest_token_cap(B):
+    """Room for 2^31 - 1 tokens: the padding fills it, and nothing is written outside."""
+    import torch
+    cap = 2 ** 31 - 1
+    room = torch.full((2, cap + 1), 5, dtype=torch.int32, device="cuda")     # 17 GB
+    have, add, ring, state, table = (_dev(np.array(v, np.int32)) for v in ([3, 0], [2, 9], np.arange(8), [0, 8], [[7, 0], [0, 0]]))
+    out = [torch.zeros(size, dtype=torch.int32, device="cuda") for size in (2, 3, 4)]
+    B.coe_kv_plan(2, 16, 8, 2, cap, *(t.data_ptr() for t in (have, add, ring, state, table, *out[:2])), room[0].data_ptr(), room[1].data_ptr(), out[2].data_ptr(),
+                  _stream())
+    assert [t.tolist() for t in out] == [[5, 9], [0, 2, 11], [1, 7, 2, 11]]
+    assert room[:, :11].tolist() == [[7 * 16 + 3, 7 * 16 + 4, *range(9)], [3, 4, *range(9)]]
+    assert (room[:, 11:cap] == -1).all().item() and room[:, cap].tolist() == [5, 5]
