@@ -271,8 +271,9 @@ __device__ __forceinline__ bool hides(const T* row, const float* noise, int voca
     const int own_vecs = vecs > owner ? (vecs - owner + THREADS - 1) / THREADS : 0;
     bool hidden = false;
     for (int k = threadIdx.x; k < own_vecs * W + 2; k += blockDim.x) {
-        const int i = k < own_vecs * W ? lead + (owner + k / W * THREADS) * W + k % W : k == own_vecs * W ? (owner < lead ? owner : vocab) : tail + owner;
-        if (i >= vocab) continue;
+        const uint32_t place = k < own_vecs * W ? lead + (owner + k / W * THREADS) * W + k % W : k == own_vecs * W ? (owner < lead ? owner : vocab) : (uint32_t)tail + owner;
+        if (place >= (uint32_t)vocab) continue;
+        const int i = (int)place;
         const float x = logit(row, i), z = scale.rel2(x), score = z - log2f(noise[i]);
         hidden = hidden || (front.holds(x, (uint32_t)i) && (z >= least || i == (int)top_index) && better_than(score, (uint32_t)i, best));
     }

@@ -1069,3 +1069,20 @@ def test_plan_of_the_largest_token_cap(B):
     assert [t.tolist() for t in out] == [[5, 9], [0, 2, 11], [1, 7, 2, 11]]
     assert room[:, :11].tolist() == [[7 * 16 + 3, 7 * 16 + 4, *range(9)], [3, 4, *range(9)]]
     assert (room[:, 11:cap] == -1).all().item() and room[:, cap].tolist() == [5, 5]
+
+
+def test_sample_of_the_largest_vocabulary(B):
+    """2^31 - 1 logits: the race's winner falls to the nucleus, and the share of its thread is looked through up to the row's end."""
+    import torch
+    vocab = 2 ** 31 - 1
+    x = torch.full((vocab,), -9.0, dtype=torch.bfloat16, device="cuda")
+    noise = torch.ones(vocab, device="cuda")
+    first, drawn, lost = 77, vocab - 3000, vocab - 5000                      # the first two make the nucleus of 0.9; all but these three weigh 2^31 e^-69
+    x[first], x[drawn], x[lost] = 60.0, 59.0, 55.0
+    noise[drawn], noise[lost] = 0.01, 1e-6
+    one = lambda v, t: torch.full((1,), v, dtype=t, device="cuda")
+    temperature, top_p, token, logprob = one(1.0, torch.float32), one(0.9, torch.float32), one(-9, torch.int32), one(0.0, torch.float32)
+    B.coe_sample_tokens(1, vocab, B.COE_DT_BF16, x.data_ptr(), vocab, temperature.data_ptr(), 0, top_p.data_ptr(), 0, noise.data_ptr(), vocab, token.data_ptr(),
+                        logprob.data_ptr(), 0, 0, _stream())
+    want = -1 - math.log(1 + math.exp(-1) + math.exp(-5))
+    assert token.item() == drawn and abs(logprob.item() - want) <= 1e-5 * (1 - want)
