@@ -345,7 +345,7 @@ int coe_kv_append(const coe_kv_cache* cache, int32_t n_tokens, const void* k, in
  * keeps a row's sum below 2^17; values up to 2^110 in magnitude find room, whatever the length, in steps of fewer than 2^26 cached
  * tokens x cache heads), the probabilities rounded to bf16 before they meet the values, one rounding of the result to bf16.  The
  * same inputs give the same bits.
- * heads: a multiple of kv_heads.  workspace: coe_kv_attention_workspace bytes for the same sizes, 16-byte aligned. */
+ * heads: a multiple of kv_heads; n_tokens * heads and max_blocks * block_size at most 2^31 - 4096.  workspace: coe_kv_attention_workspace bytes for the same sizes, 16-byte aligned. */
 int64_t coe_kv_attention_workspace(int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads, int32_t kv_heads,
                                    int32_t head_dim);
 int coe_kv_attention(const coe_kv_cache* cache, int32_t n_requests, int32_t n_tokens, int32_t max_new, int32_t heads,

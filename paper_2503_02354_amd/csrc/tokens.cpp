@@ -119,10 +119,12 @@ int coe_kv_attention(const coe_kv_cache* cache, int32_t n_requests, int32_t n_to
     if (n_requests < 0 || n_requests > COE_KV_MAX_REQUESTS || n_tokens < 0 || max_new < 0 || window < 0)
         return fail(COE_EINVAL, "%s: a size is negative or n_requests exceeds %d", call, COE_KV_MAX_REQUESTS);
     if (heads <= 0 || heads > 65535 || heads % c.kv_heads) return fail(COE_EINVAL, "%s: heads %d is not a multiple of kv_heads %d", call, heads, c.kv_heads);
-    if (max_blocks <= 0 || (long long)max_blocks * cache->block_size > 0x7FFFFFFFll)
-        return fail(COE_EINVAL, "%s: max_blocks * block_size must be in 1..2^31 - 1", call);
-    if ((long long)n_tokens * heads > 0x7FFFFFFFll || (long long)n_requests * c.kv_heads > 0x7FFFFFFFll)
-        return fail(COE_EINVAL, "%s: n_tokens * heads must be below 2^31", call);
+    // the kernels round positions and rows up to whole tiles, and look a few tiles ahead, in 32 bits
+    constexpr long long kMost = (1ll << 31) - 4096;
+    if (max_blocks <= 0 || (long long)max_blocks * cache->block_size > kMost)
+        return fail(COE_EINVAL, "%s: max_blocks * block_size must be in 1..2^31 - 4096", call);
+    if ((long long)n_tokens * heads > kMost || (long long)n_requests * c.kv_heads > 0x7FFFFFFFll)
+        return fail(COE_EINVAL, "%s: n_tokens * heads must be at most 2^31 - 4096", call);
     if (!(scale == scale) || scale - scale != 0.f) return fail(COE_EINVAL, "%s: scale must be finite", call);
     if (n_requests == 0 || n_tokens == 0 || max_new == 0) return COE_OK;
     if (!q || !q_off || !seq_len || !table || !out) return fail(COE_EINVAL, "%s: null argument", call);

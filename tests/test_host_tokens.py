@@ -154,3 +154,15 @@ def test_statement_of_plan_ids_outside_the_cache():
     out = T.plan(16, 8, 2, 4, [15, 2], [2, 1], np.full(8, -2 ** 28, np.int32), [0, 8], table)
     assert out["slot"].tolist() == [-1, -1, 3 * 16 + 2, -1] and out["position"].tolist() == [15, 16, 2, -1]
     assert out["table"].tolist() == [[0x10000001, -2 ** 28], [3, 0]] and out["next_state"].tolist() == [1, 7, 2, 3]
+
+
+def test_attention_refuses_sizes_that_leave_no_room_for_whole_tiles(B):
+    """Lengths and query rows so near 2^31 that rounding them up to a tile of 32, 64 or 128 does not fit 32 bits."""
+    def call(heads, tokens, block, width):
+        B.coe_kv_attention(_cache(B, kv_heads=1, n_blocks=1, block_size=block, block_stride=64 * 1024), 1, tokens, tokens, heads, 0, 1.0, P, 64, 64, P, P, P, width,
+                           P, 64, 64, P, P, 0, 0)
+    for heads, tokens, block, width, text in ((1, 2 ** 31 - 1, 16, 4, "n_tokens * heads"), (3, (2 ** 31 - 1) // 3, 16, 4, "n_tokens * heads"), (1, 2 ** 31 - 4095, 16, 4, "n_tokens * heads"),
+                                              (1, 1, 8, 2 ** 28 - 1, "max_blocks"), (1, 1, 16, 2 ** 27 - 1, "max_blocks"), (1, 1, 1024, 2 ** 21 - 3, "max_blocks")):
+        _refused(B, B.COE_EINVAL, text, call, heads, tokens, block, width)
+    for sizes in ((1, 2 ** 31 - 4096, 16, 4), (1, 1, 8, 2 ** 28 - 512), (1, 1, 1024, 2 ** 21 - 4)):       # the largest get as far as the workspace
+        _refused(B, B.COE_ERANGE, "workspace", call, *sizes)
