@@ -1086,3 +1086,59 @@ def test_sample_of_the_largest_vocabulary(B):
                         logprob.data_ptr(), 0, 0, _stream())
     want = -1 - math.log(1 + math.exp(-1) + math.exp(-5))
     assert token.item() == drawn and abs(logprob.item() - want) <= 1e-5 * (1 - want)
+
+
+# ---- many requests, and requests longer than announced ------------------------------------------------------------
+def _check_some(a, got, lse, some):
+    """Compare the rows of some requests with the 64-bit statement; `a` is left as it is."""
+    import copy
+    rows = np.concatenate([np.arange(a.off[r], a.off[r + 1]) for r in some]).astype(int)
+    part = copy.copy(a)
+    part.q, part.total, part.new, part.table = a.q[rows], a.total[some], a.new[some], a.table[some]
+    part.off = np.concatenate([[0], np.cumsum(part.new)]).astype(np.int32)
+    part.check(got[rows], lse[rows])
+
+
+@pytest.mark.parametrize("n", [4097, 5000, 16384])
+@pytest.mark.parametrize("chunks", [False, True])
+def test_attention_of_thousands_of_requests(B, n, chunks):
+    """More requests than the schedule keeps lengths of, and prefix sums beyond the LDS that tiles take, up to the largest number there may be."""
+    rng = np.random.default_rng(n)
+    lengths = [(int(h), int(m)) for h, m in zip(rng.integers(0, 12, n), rng.integers(0, 3, n))]
+    odd = {0: (700, 1), 3: (40, 2), n // 2: (300, 2), n - 2: (0, 0), n - 1: (100, 1)}
+    if chunks:
+        odd.update({7: (20, 70), n // 3: (0, 129), n - 1: (3, 40)})
+    for r, v in odd.items():
+        lengths[r] = v
+    a = Wide(B, lengths, 2, 1, 32, block=32, seed=n)
+    got, lse = a.run()
+    _check_some(a, got, lse, sorted(set(odd) | set(range(0, n, 37)) | set(range(n - 40, n))))
+
+
+@pytest.mark.parametrize("kind,have,new,most", [(Attend, 100, 9, 5), (Attend, 60, 70, 40), (Wide, 100, 9, 5), (Attend, 5000, 7, 3), (Wide, 100, 150, 140), (Wide, 5000, 60, 35)])
+@pytest.mark.parametrize("window", [0, 45])
+def test_attention_of_requests_longer_than_announced(B, kind, have, new, most, window):
+    """The first max_new rows of a request with more new tokens stand where they stand without that limit; the others are not written."""
+    a = kind(B, [(30, 2), (have, new), (17, 1), (40, new)], 8, 2, 64, window=window, seed=have)
+    got, lse = a.run(max_new=most)
+    served = np.concatenate([np.arange(m) < most for m in a.new])
+    assert (got[~served] == 0xFFC0).all() and (lse[~served] == 7.5).all() and (~served).sum() == 2 * (new - most)
+    out, logs, size = T.attention(T.bf16_to_f64(a.q), T.bf16_to_f64(a.bits[0]), T.bf16_to_f64(a.bits[1]), a.total, a.off, a.table, a.block, window, a.scale)
+    # the bounds of Attend.check
+    assert (np.abs(T.bf16_to_f64(got) - out)[served] <= (2.0 ** -8 * np.abs(out) + (2.0 ** -8 + 1e-3) * size + 1e-30)[served]).all()
+    assert (np.abs(lse - logs)[served] <= (2e-4 + 2e-6 * np.abs(logs))[served]).all()
+
+
+def test_sample_rows_alone_and_among_others(B):
+    """A row's token and logarithm are the same bits alone and among up to 255 others, and within the bounds of the statement among more."""
+    rng = np.random.default_rng(4)
+    vocab = 9001
+    settings = [(1.0, 0, 1.0, 0.0), (0.8, 0, 0.9, 0.0), (1.0, 60, 0.95, 0.0), (0.0, 0, 1.0, 0.0), (1.0, 900, 1.0, 0.001), (1.0, 5000, 0.9, 0.0), (1.5, 0, 0.7, 0.01)]
+    x, noise = (3 * rng.standard_normal((300, vocab))).astype(np.float32), _noise(rng, (300, vocab))
+    t, k, p, m = (np.array([c[r % len(settings)] for r in range(300)]) for c in zip(*settings))
+    token, lp = _sample_gpu(B, x[:256], t[:256], k[:256], p[:256], m[:256], noise[:256])
+    for r in range(0, 256, 25):
+        one = slice(r, r + 1)
+        alone = _sample_gpu(B, x[one], t[one], k[one], p[one], m[one], noise[one])
+        assert alone[0][0] == token[r] and alone[1][0] == lp[r]
+    _check_sample(B, x, t, k, p, m, noise)
