@@ -505,8 +505,8 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void kv_attention_short_kern
 // Adds up the parts of a history that several workgroups shared: a workgroup per request, cache head and kJoinRows query rows
 // (blockIdx.y).  Several threads share the parts of a row's four channels, since a long history has many; each leaves its sum
 // relative to its own maximum, and the first adds those up in their order.  What bounds it: round trips to memory, so every thread fetches
-// four parts at a time: three histories of 131,000 tokens, a hundred parts and more to each, 6.1 us (9.2 with two at a time, 8.3 with 1024
-// threads, which cost 96 requests 18.5 instead of 6.7).
+// four parts at a time: three histories of 131,000 tokens, a hundred parts and more to each, 6.5 us (9.2 with two at a time, 8.3 with 1024
+// threads, which cost 96 requests 18.5 instead of 6.9).
 constexpr int kJoinRows = 1, kAhead = 4;
 template <int D>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(KvCache c, KvAttention a, const char* workspace)
@@ -1048,7 +1048,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void kv_attention_many_kernel(K
 #endif
 }
 
-// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.  Latency: 7.8 us with 25 cut units of 8 heads, 4.7 without any.  The last
+// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.  Latency: 8.3 us with 25 cut units of 8 heads, 4.7 without any.  The last
 // workgroup of a unit doing it instead costs more: what makes parts visible on all of the chip, a release of the second-level cache, slowed
 // the units down from 88 to 183 us.
 constexpr int kUnitRows = 16;
@@ -1100,10 +1100,11 @@ int64_t few_bytes(int32_t n_requests, int dim)
 bool is_few(int32_t max_new, int32_t heads, int32_t kv_heads) { return (int64_t)max_new * (heads / kv_heads) <= kFewRows; }
 
 // Whether a workgroup of its own for every history is faster than equal stretches and a join: where the block tables, all that is known
-// here of the lengths, hold few tokens.  Single tokens, us, stretches / whole histories, at the longest tables of either limit: one
-// request, 12 heads of 64 channels, 624 tokens 10.4 / 9.2, 8 cache heads of 128, 304 tokens 13.5 / 9.4; 16 requests, 12 x 64, 1504 tokens 26.6 / 17.7, 8 x 128,
-// 624 tokens 22.5 / 16.2; 200 requests, 12 x 64, 1504 tokens 184 / 182.  Past them one request, 8 x 128, 624 tokens 11.3 / 15.0;
-// 200 requests, 12 x 64, 2048 tokens 238 / 246.
+// here of the lengths, hold few tokens.  Single tokens in replayed graphs, us, stretches / whole histories, tables as long as their histories.  At
+// the limits: one request, 12 heads of 64 channels, 640 tokens 9.6 / 8.6, 8 cache heads of 128, 320 tokens 13.2 / 9.3; 16 requests, 12 x 64, 1536
+// tokens 25.1 / 17.5, 8 x 128, 768 tokens 20.3 / 19.4; 200 requests 188 / 186 and 137 / 138.  Past them the whole histories' gain shrinks, then turns: one
+// request, 12 x 64, 832 tokens 11.8 / 10.3, 1024 tokens 9.8 / 11.6, 8 x 128, 432 tokens 13.3 / 11.7, 528 tokens 10.9 / 12.6; 16 requests, 12 x 64, 2064 tokens
+// 28.9 / 21.2, 8 x 128, 1024 tokens 21.5 / 23.4; 200 requests, 12 x 64, 2064 tokens 236 / 244, 8 x 128, 1024 tokens 173 / 180.
 // Chunks, us, units and a join / a workgroup for 32 rows of each: one prompt of 500 tokens, 12 heads of 64, 25.5 / 12.6, 32 on 8 of 128 29.5 / 21.2, of 1000 tokens
 // 28 / 20 and 40 / 52; 8 prompts of 128, 32 on 8 of 128 23.3 / 21.1, of 256 30.7 / 45.9; 64 tokens behind 900, 32 on 8 of 128, 34 / 24;
 // 40 prompts of 64, 32 on 8 of 128 (2560 workgroups) 35 / 42.

@@ -371,7 +371,8 @@ __device__ uint32_t race(const T* row, const float* noise, int vocab, uint32_t t
     }
 }
 
-// The front of the first top_k tokens, byte by byte from the top of the order as one number, key first, then index.
+// The front of the first top_k tokens, byte by byte from the top of the order as one number, key first, then index.  What bounds it: eight passes
+// over the row, with LDS atomics.  96 rows of 128,000 fp32 with a top_k from 2049 on 242 to 273 us, where a list of 2000 takes 54.7.
 template <int THREADS, typename T> __device__ Front front_of(const T* row, int vocab, uint32_t left, Shared<THREADS>& sh)
 {
     const int tid = threadIdx.x;
