@@ -329,6 +329,23 @@ typedef struct {
 int coe_kv_append(const coe_kv_cache* cache, int32_t n_tokens, const void* k, int64_t k_token_stride, int64_t k_head_stride,
                   const void* v, int64_t v_token_stride, int64_t v_head_stride, const int32_t* slot, void* stream);
 
+/* coe_kv_append with a rotation by position on the way: the keys' copies in the cache and the queries' in q_out are turned, values are
+ * copied.  With p = position[t] and channels (a, b) of pair i < rotated / 2,
+ *   a' = a cos(p f_i) - b sin(p f_i)      b' = b cos(p f_i) + a sin(p f_i)      f_i = frequency[i]
+ * pairing COE_PAIR_HALVES: pair i is channels i and i + rotated / 2; COE_PAIR_NEIGHBOURS: channels 2 i and 2 i + 1.  Channels from
+ * `rotated` on stay as they are.  A token of negative position (the padding of coe_kv_plan) is left out: neither its queries are
+ * written nor is its row appended; one whose slot lies outside the cache has its queries turned only.
+ * q and q_out: row t, head h < heads at t * token_stride + h * head_stride elements of the cache's dtype, 16-byte aligned, strides multiples of 8;
+ * q_out is q with the same strides (in place) or overlaps none of the inputs.  heads = 0: keys and values only (q, q_out may be NULL).  k, v
+ * and slot as in coe_kv_append; position: [n_tokens].  frequency: [rotated / 2] fp32; rotated: even, in 2..head_dim.
+ * Numerics: angles are the products' exact values rounded in fp64 and reduced there, sine, cosine and the rotation are fp32, one rounding to
+ * bf16.  NaN or infinite frequencies give NaN. */
+enum { COE_PAIR_HALVES = 0, COE_PAIR_NEIGHBOURS = 1 };
+int coe_kv_append_rotated(const coe_kv_cache* cache, int32_t n_tokens, int32_t heads, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                          void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                          const void* v, int64_t v_token_stride, int64_t v_head_stride, const int32_t* slot, const int32_t* position,
+                          const float* frequency, int32_t rotated, int32_t pairing, void* stream);
+
 /* Attention of every request's new tokens over its cached ones, the new ones included (append first).
  * Request r's new tokens are rows q_off[r] .. q_off[r + 1] - 1 of q (at most max_new of them; n_tokens rows in all; q_off and
  * seq_len as coe_kv_plan writes them); with m of them, row i stands at position p = seq_len[r] - m + i and sees the cached
@@ -373,6 +390,91 @@ int coe_sample_tokens(int32_t n_rows, int32_t vocab, int32_t dtype, const void* 
                       const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                       const float* noise, int64_t noise_stride, int32_t* token, float* logprob, void* workspace,
                       int64_t workspace_bytes, void* stream);
+
+/* ---- decoders that look at an encoder's states, and search with beams ---------------------------------------------------------
+ * These calls stand beside the ones above and keep to the same rules (device pointers, `stream`, workspaces, checks, errors).  A request
+ * searched with W beams is W consecutive rows ("requests" to coe_kv_plan and coe_kv_attention); a step of it is coe_kv_plan; per layer
+ * coe_kv_append or coe_kv_append_rotated, coe_kv_attention and coe_cross_attention; then coe_beam_select on the logits, and coe_kv_fork and
+ * coe_kv_copy, after which row r's cache is its chosen parent's. */
+
+/* What an encoder left of its inputs ("sources"), for one layer of a decoder: the key (value) of row i and head h is head_dim contiguous
+ * channels at k + i * k_row_stride + h * k_head_stride (v likewise) elements of dtype (COE_DT_BF16).  head_dim: a multiple of 8 in 8..128; k
+ * and v 16-byte aligned, strides multiples of 8, not negative; 64 rows lie within 2^31 bytes, all of them may take any size.  seen: [n_rows]
+ * bytes, 0 hides a row from every query, or NULL (none is hidden). */
+typedef struct {
+    int32_t dtype, n_rows, kv_heads, head_dim;
+    const void *k, *v;
+    int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+    const uint8_t* seen;
+} coe_states;
+
+/* Attention of tokens over their source's states.  Source s is the rows first[s] .. first[s] + length[s] - 1 of the states, in any order and
+ * overlapping as the caller likes; its queries are rows q_off[s * beams] .. q_off[(s + 1) * beams] - 1 of q, at most max_new of them (q_off:
+ * [n_sources * beams + 1] as coe_kv_plan writes it; beams share their source's states, which are read once for all of them).  Every query sees
+ * every row of its source that is not hidden.  Query head h reads head h / (heads / kv_heads) of the states.
+ *   out = softmax_j(scale * q . k_j) v_j      lse = ln sum_j exp(scale * q . k_j)
+ * A query that sees nothing (length 0, every row hidden), or whose scores are all -inf, gets out = 0 and lse = -inf; one with a score that is
+ * NaN gets NaN for both.  Hidden rows do not reach it, whatever their bits.  Of a source with more than max_new queries the first max_new
+ * are served; rows of q that belong to no source are not read, and theirs of out and lse not written.  length is limited to max_rows and
+ * to the rows that there are behind first; a negative first or length counts as a source without rows.
+ * q, out and lse as in coe_kv_attention (lse may be NULL); scale, numerics and limits too.  heads: a multiple of kv_heads; n_tokens * heads and
+ * max_rows at most 2^31 - 4096; n_sources * beams at most COE_KV_MAX_REQUESTS.  The same inputs give the same bits.
+ * workspace: coe_cross_attention_workspace bytes for the same sizes (may be 0), 16-byte aligned. */
+int64_t coe_cross_attention_workspace(int32_t n_sources, int32_t n_tokens, int32_t max_new, int32_t max_rows, int32_t heads, int32_t kv_heads,
+                                      int32_t head_dim);
+int coe_cross_attention(const coe_states* states, int32_t n_sources, int32_t n_tokens, int32_t beams, int32_t max_new, int32_t max_rows, int32_t heads,
+                        float scale, const void* q, int64_t q_token_stride, int64_t q_head_stride, const int32_t* q_off, const int32_t* first,
+                        const int32_t* length, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/* The best `picks` continuations of every request's beams.  Beam b of request r is row r * beams + b of logits [n_requests * beams][vocab]
+ * (COE_DT_F32 or COE_DT_BF16, rows logits_stride elements apart) and has the score score[row] so far, a sum of log-probabilities; -inf or NaN: it
+ * is not there.  Its candidates are its tokens v with score[row] + x_v - ln sum exp x; where ended[row] != 0 (ended may be NULL: none has) it is a
+ * candidate itself instead, with token end_token and its score as it is, and its logits are not read.  A logit of -inf or NaN is no
+ * candidate and weighs nothing; where a row's largest is +inf, those share its probability.  Those with the largest scores are written in that
+ * order, candidates of one row in the order of their logits, equal ones by token, and equal scores of different rows by row: next_score, next_row
+ * (of logits: r * beams + b), next_token, and next_ended (may be NULL): 1 where the
+ * beam had ended or the token is end_token, else 0.  All are [n_requests][picks]; where fewer than picks candidates are there, the rest is -inf,
+ * -1, -1, 0.  With picks == beams, next_score and next_ended are the next step's score and ended, and next_row coe_kv_fork's parent; outputs
+ * must not alias inputs.
+ * beams in 1..COE_BEAM_MAX, picks in 1..COE_BEAM_PICKS_MAX.
+ * Numerics: exponentials and their sums over a few hundred tokens in fp32, sums over a row, logarithms and scores in fp64, in which candidates
+ * are compared; one rounding of next_score to fp32.  The same inputs give the same outputs, and rows of equal bits equal scores.
+ * workspace: coe_beam_workspace bytes (may be 0), 16-byte aligned. */
+#define COE_BEAM_MAX 32
+#define COE_BEAM_PICKS_MAX 64
+int64_t coe_beam_workspace(int32_t n_requests, int32_t beams, int32_t picks, int32_t vocab);
+int coe_beam_select(int32_t n_requests, int32_t beams, int32_t picks, int32_t vocab, int32_t dtype, const void* logits, int64_t logits_stride,
+                    const float* score, const int32_t* ended, int32_t end_token, float* next_score, int32_t* next_row, int32_t* next_token,
+                    int32_t* next_ended, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Reorders block tables after a selection: row i continues row parent[i], which is one of its own request's rows (r * beams ..
+ * r * beams + beams - 1), or becomes empty (any other value, -1 by custom).  n = n_requests * beams rows; table [n][max_blocks], seq_len [n], ring
+ * and ring_state as coe_kv_plan has them.
+ *   next_len[i] = seq_len[parent[i]] (0 for an empty row)      next_table[i][j] = table[parent[i]][j]  for the blocks of next_len[i] tokens
+ * so rows of a request share blocks.  Only a last block that is not full must not be shared: the first of a row's children (the lowest i) keeps
+ * it, every other gets a block of its own in its place, and copy[i] = {the old block, the new one} says what coe_kv_copy is to bring there;
+ * {-1, -1} for every other row.  An old block that no row holds any more is free.  A request's copies take the blocks that it frees itself, in order
+ * of their place in the table, then of the row, a block counted where it first is; then ids from the ring's front; what it frees beyond its copies goes
+ * to the ring's end, requests in order.  The first request that needs more ids than the ring has left closes the call: it and every later one keep
+ * their rows (next_table, next_len as they were, no copies).  Ids given back here can be taken from the ring from the next call on.
+ * next_state = {head, count, requests before the one that closed the call (n_requests if none did), copies}.
+ * Rows of a request may share a block at the same place of their tables only, as this call leaves them; rows of different requests share none.
+ * coe_kv_plan gives every block of a finished row back by itself: rows that share blocks are finished here instead (parent -1), and
+ * have no tokens then.  Entries of next_table behind a row's blocks are not written.  Ids outside the cache are passed on, never copied
+ * and never given back.  A negative seq_len counts as 0, one beyond max_blocks * block_size as that.  next_table, next_len and next_state must not alias
+ * table, seq_len and ring_state; repeating a call is harmless, and the same inputs give the same outputs.
+ * beams in 1..COE_BEAM_MAX, n at most COE_KV_MAX_REQUESTS; the rest as in coe_kv_plan.  workspace: coe_kv_fork_workspace bytes, 16-byte aligned. */
+int64_t coe_kv_fork_workspace(int32_t n_requests, int32_t beams);
+int coe_kv_fork(int32_t n_requests, int32_t beams, int32_t block_size, int32_t n_blocks, int32_t max_blocks, const int32_t* parent, const int32_t* seq_len,
+                const int32_t* table, int32_t* ring, const int32_t* ring_state, int32_t* next_table, int32_t* next_len, int32_t* copy,
+                int32_t* next_state, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Brings the rows of blocks that are not full to their copies, in every layer's cache at once: for every i < n with copy[i] = {from, to}, both in the
+ * cache, the first seq_len[i] % block_size rows of block `from` (all of them where that is 0) go to block `to`; other entries are skipped.
+ * caches: [n_caches] host values, read during the call; they may differ in heads, channels, layout and number of blocks, not in block_size.  No block may be the
+ * target of two entries, or the target of one and the source of another. */
+int coe_kv_copy(int32_t n_caches, const coe_kv_cache* caches, int32_t n, const int32_t* copy, const int32_t* seq_len, void* stream);
 
 /* Launch sequences of the last step in launch order: the first expert of each, its predicted cost and the executor it ran
  * on.  Writes at most cap entries (arrays nullable); *n_units receives the total. */

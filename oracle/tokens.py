@@ -1,4 +1,5 @@
-"""Plain 64-bit statement of the calls for token-generating experts (include/coe.h, "paged key/value cache").  numpy only."""
+"""Plain 64-bit statement of the calls for token-generating experts (include/coe.h, "paged key/value cache" and "decoders that look at an
+encoder's states, and search with beams").  numpy only."""
 import numpy as np
 
 
@@ -118,3 +119,123 @@ def sample(x, temperature, top_k, top_p, min_p, noise, slack=0.0):
             return {int(ids[score == best].min())}, ln
         near = {int(i) for i in ids[score >= best - slack]} if np.isfinite(best) else {int(ids[score == best].min())}
     return near, ln
+
+
+def rotate(x, position, frequency, rotated, neighbours):
+    """x [tokens][heads][dim] float64.  Returns the rotated rows and |a| + |b| of every channel's pair (0 where it is not rotated)."""
+    out, size, half = np.array(x), np.zeros_like(x), rotated // 2
+    angle = position.astype(np.float64)[:, None] * frequency.astype(np.float64)[None, :]
+    cos, sin = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    first = slice(0, rotated, 2) if neighbours else slice(0, half)
+    second = slice(1, rotated, 2) if neighbours else slice(half, rotated)
+    a, b = x[..., first], x[..., second]
+    out[..., first], out[..., second] = a * cos - b * sin, b * cos + a * sin
+    size[..., first] = size[..., second] = np.abs(a) + np.abs(b)
+    return out, size
+
+
+def cross(q, k, v, q_off, first, length, beams, scale, seen=None, max_new=None, max_rows=None):
+    """q [tokens][heads][dim]; k, v [rows][kv_heads][dim]: float64.  Returns out, lse, A = sum of p |v| (for error bounds) and which tokens are
+    served."""
+    tokens, heads, dim = q.shape
+    group = heads // k.shape[1]
+    out = np.zeros((tokens, heads, dim)); size = np.zeros((tokens, heads, dim)); lse = np.full((tokens, heads), -np.inf)
+    served = np.zeros(tokens, bool)
+    for s in range(len(first)):
+        begin, end = int(q_off[s * beams]), int(q_off[(s + 1) * beams])
+        end = end if max_new is None else min(end, begin + max_new)
+        served[begin:end] = True
+        f, n = int(first[s]), int(length[s])
+        n = 0 if f < 0 else max(0, min(n, len(k) - f, n if max_rows is None else max_rows))
+        rows = np.arange(f, f + n)
+        if seen is not None:
+            rows = rows[seen[rows] != 0]
+        if len(rows) == 0:
+            continue
+        for h in range(heads):
+            kk, vv = k[rows, h // group], v[rows, h // group]
+            x = scale * (q[begin:end, h] @ kk.T)
+            top = x.max(1, keepdims=True)
+            e = np.exp(x - top)
+            lse[begin:end, h] = (top + np.log(e.sum(1, keepdims=True)))[:, 0]
+            out[begin:end, h] = e @ vv / e.sum(1, keepdims=True)
+            size[begin:end, h] = e @ np.abs(vv) / e.sum(1, keepdims=True)
+    return out, lse, size, served
+
+
+def beam(x, score, ended, beams, picks, end_token):
+    """x [rows][vocab] float64 logits.  Returns (scores, rows, tokens, ended), each [requests][picks], scores float64."""
+    requests = len(x) // beams
+    out = []
+    for r in range(requests):
+        found = []
+        for row in range(r * beams, (r + 1) * beams):
+            s = float(score[row])
+            if not s > -np.inf:
+                continue
+            if ended is not None and ended[row]:
+                found.append((-s, row, 0, int(end_token), 1))
+                continue
+            z = np.where(np.isnan(x[row]), -np.inf, x[row])
+            top = z.max()
+            if top == -np.inf:
+                continue
+            with np.errstate(invalid="ignore"):
+                z = np.where(z == top, 0.0, np.where(np.isinf(z - top), -np.inf, z - top))
+            z = z - np.log(np.exp(z).sum())
+            likely = np.argsort(-z, kind="stable")[:picks]
+            found += [(-(s + z[t]), row, place, int(t), int(t == end_token)) for place, t in enumerate(likely) if z[t] > -np.inf]
+        found = sorted(found)[:picks]
+        out.append([(-c[0], c[1], c[3], c[4]) for c in found] + [(-np.inf, -1, -1, 0)] * (picks - len(found)))
+    out = np.array(out, np.float64).reshape(requests, picks, 4)
+    return out[..., 0], *(out[..., i].astype(np.int32) for i in (1, 2, 3))
+
+
+def fork(block, n_blocks, beams, parent, seq_len, ring, state, table, next_table):
+    """Rows that continue others, request by request.  Returns dict of the outputs; next_table and ring as they are afterwards."""
+    ring, next_table = ring.copy(), next_table.copy()
+    n, width = table.shape
+    head, count = int(state[0]) % n_blocks, min(max(int(state[1]), 0), n_blocks)
+    length = np.clip(seq_len, 0, width * block).astype(np.int32)
+    copy, next_len = np.full((n, 2), -1, np.int32), np.zeros(n, np.int32)
+    taken, given, forked = 0, [], None
+    for r in range(n // beams):
+        rows = list(range(r * beams, (r + 1) * beams))
+        child_of = {i: int(parent[i]) if int(parent[i]) in rows else None for i in rows}
+        continued = [p for p in rows if p in child_of.values()]
+        owned = {p: -(-int(length[p]) // block) for p in rows}
+        inside = lambda b: 0 <= b < n_blocks
+        free, seen_parents, copies = [], set(), []
+        for j in range(width):
+            held = {int(table[p, j]) for p in continued if j < owned[p]}
+            for p in rows:
+                b = int(table[p, j])
+                if p not in continued and j < owned[p] and b not in held and inside(b):
+                    held.add(b)
+                    free.append(b)
+        for i in rows:
+            p = child_of[i]
+            if p in seen_parents and length[p] % block and inside(int(table[p, owned[p] - 1])):
+                copies.append(i)
+            seen_parents.add(p if p is not None else -1)
+        if forked is None and taken + max(0, len(copies) - len(free)) > count:
+            forked = r
+        for i in rows:
+            p = child_of[i] if forked is None else i
+            if p is None:
+                continue
+            next_len[i] = length[p]
+            next_table[i, :owned[p]] = table[p, :owned[p]]
+            if forked is None and i in copies:
+                if free:
+                    to = free.pop(0)
+                else:
+                    to = ring[(head + taken) % n_blocks]
+                    taken += 1
+                copy[i] = table[p, owned[p] - 1], to
+                next_table[i, owned[p] - 1] = to
+        given += free if forked is None else []
+    for i, b in enumerate(given):
+        ring[(head + count + i) % n_blocks] = b
+    state = [(head + taken) % n_blocks, count - taken + len(given), n // beams if forked is None else forked, int((copy[:, 0] >= 0).sum())]
+    return dict(next_table=next_table, next_len=next_len, copy=copy, ring=ring, next_state=np.array(state, np.int32))

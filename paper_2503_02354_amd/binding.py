@@ -28,9 +28,12 @@ EXPORTS = [
     "coe_regroup_static", "coe_debug_last_chunks", "coe_set_host_tier", "coe_debug_host_log", "coe_profiler_memory_scores", "coe_profiler_expert_budget", "coe_profiler_executable_batch", "coe_profiler_usage_probabilities",
     "coe_profiler_fit_latency", "coe_profiler_max_batch", "coe_profiler_arranging_window", "coe_profiler_window_step",
     "coe_kv_plan", "coe_kv_append", "coe_kv_attention_workspace", "coe_kv_attention", "coe_sample_workspace", "coe_sample_tokens",
+    "coe_kv_append_rotated", "coe_cross_attention_workspace", "coe_cross_attention", "coe_beam_workspace", "coe_beam_select", "coe_kv_fork_workspace", "coe_kv_fork", "coe_kv_copy",
 ]
 COE_DT_F32, COE_DT_BF16 = 0, 1
 COE_KV_MAX_REQUESTS = 16384
+COE_PAIR_HALVES, COE_PAIR_NEIGHBOURS = 0, 1
+COE_BEAM_MAX, COE_BEAM_PICKS_MAX = 32, 64
 
 
 class coe_layer(C.Structure):
@@ -61,6 +64,12 @@ class coe_kv_cache(C.Structure):
     """One layer's paged cache; k and v are device addresses, strides in elements."""
     _fields_ = [("dtype", C.c_int32), ("n_blocks", C.c_int32), ("block_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("k", C.c_void_p), ("v", C.c_void_p), ("block_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class coe_states(C.Structure):
+    """What an encoder left for one layer of a decoder; k, v and seen are device addresses, strides in elements."""
+    _fields_ = [("dtype", C.c_int32), ("n_rows", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_row_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_row_stride", C.c_int64), ("v_head_stride", C.c_int64), ("seen", C.c_void_p)]
 
 
 class coe_window_state(C.Structure):
@@ -129,6 +138,14 @@ def _load():
     L.coe_kv_attention.argtypes = [C.POINTER(coe_kv_cache)] + [i32] * 5 + [C.c_float, vp, i64, i64, vp, vp, vp, i32, vp, i64, i64, vp, vp, i64, vp]
     L.coe_sample_workspace.argtypes = [i32, i32]; L.coe_sample_workspace.restype = i64
     L.coe_sample_tokens.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
+    L.coe_kv_append_rotated.argtypes = [C.POINTER(coe_kv_cache), i32, i32] + [vp, i64, i64] * 4 + [vp, vp, vp, i32, i32, vp]
+    L.coe_cross_attention_workspace.argtypes = [i32] * 7; L.coe_cross_attention_workspace.restype = i64
+    L.coe_cross_attention.argtypes = [C.POINTER(coe_states)] + [i32] * 6 + [C.c_float, vp, i64, i64, vp, vp, vp, vp, i64, i64, vp, vp, i64, vp]
+    L.coe_beam_workspace.argtypes = [i32] * 4; L.coe_beam_workspace.restype = i64
+    L.coe_beam_select.argtypes = [i32] * 5 + [vp, i64, vp, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+    L.coe_kv_fork_workspace.argtypes = [i32] * 2; L.coe_kv_fork_workspace.restype = i64
+    L.coe_kv_fork.argtypes = [i32] * 5 + [vp] * 10 + [i64, vp]
+    L.coe_kv_copy.argtypes = [i32, C.POINTER(coe_kv_cache), i32, vp, vp, vp]
     return L
 
 
@@ -201,6 +218,62 @@ def coe_sample_tokens(n_rows: int, vocab: int, dtype: int, logits: int, logits_s
     _static(lib.coe_sample_tokens(n_rows, vocab, dtype, logits or None, logits_stride, temperature or None, top_k or None, top_p or None,
                                   min_p or None, noise or None, noise_stride, token or None, logprob or None, workspace or None, workspace_bytes,
                                   stream or None))
+
+
+def coe_kv_append_rotated(cache: coe_kv_cache, n_tokens: int, heads: int, q: int, q_token_stride: int, q_head_stride: int, q_out: int,
+                          q_out_token_stride: int, q_out_head_stride: int, k: int, k_token_stride: int, k_head_stride: int, v: int, v_token_stride: int,
+                          v_head_stride: int, slot: int, position: int, frequency: int, rotated: int, pairing: int = COE_PAIR_HALVES, stream: int = 0) -> None:
+    """New keys and values into their cache slots, keys and queries rotated by their positions on the way; enqueued on `stream`."""
+    _static(lib.coe_kv_append_rotated(C.byref(cache), n_tokens, heads, q or None, q_token_stride, q_head_stride, q_out or None, q_out_token_stride,
+                                      q_out_head_stride, k or None, k_token_stride, k_head_stride, v or None, v_token_stride, v_head_stride, slot or None,
+                                      position or None, frequency or None, rotated, pairing, stream or None))
+
+
+def coe_cross_attention_workspace(n_sources: int, n_tokens: int, max_new: int, max_rows: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return _static(lib.coe_cross_attention_workspace(n_sources, n_tokens, max_new, max_rows, heads, kv_heads, head_dim))
+
+
+def coe_cross_attention(states: coe_states, n_sources: int, n_tokens: int, beams: int, max_new: int, max_rows: int, heads: int, scale: float, q: int,
+                        q_token_stride: int, q_head_stride: int, q_off: int, first: int, length: int, out: int, out_token_stride: int,
+                        out_head_stride: int, lse: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """Attention of tokens over their source's states; enqueued on `stream`."""
+    _static(lib.coe_cross_attention(C.byref(states), n_sources, n_tokens, beams, max_new, max_rows, heads, scale, q or None, q_token_stride, q_head_stride,
+                                    q_off or None, first or None, length or None, out or None, out_token_stride, out_head_stride, lse or None,
+                                    workspace or None, workspace_bytes, stream or None))
+
+
+def coe_beam_workspace(n_requests: int, beams: int, picks: int, vocab: int) -> int:
+    return _static(lib.coe_beam_workspace(n_requests, beams, picks, vocab))
+
+
+def coe_beam_select(n_requests: int, beams: int, picks: int, vocab: int, dtype: int, logits: int, logits_stride: int, score: int, ended: int,
+                    end_token: int, next_score: int, next_row: int, next_token: int, next_ended: int, workspace: int, workspace_bytes: int,
+                    stream: int = 0) -> None:
+    """The best continuations of every request's beams; enqueued on `stream`."""
+    _static(lib.coe_beam_select(n_requests, beams, picks, vocab, dtype, logits or None, logits_stride, score or None, ended or None, end_token,
+                                next_score or None, next_row or None, next_token or None, next_ended or None, workspace or None, workspace_bytes,
+                                stream or None))
+
+
+def coe_kv_fork_workspace(n_requests: int, beams: int) -> int:
+    return _static(lib.coe_kv_fork_workspace(n_requests, beams))
+
+
+def coe_kv_fork(n_requests: int, beams: int, block_size: int, n_blocks: int, max_blocks: int, parent: int, seq_len: int, table: int, ring: int,
+                ring_state: int, next_table: int, next_len: int, copy: int, next_state: int, workspace: int, workspace_bytes: int,
+                stream: int = 0) -> None:
+    """Block tables of rows that continue others; enqueued on `stream`."""
+    _static(lib.coe_kv_fork(n_requests, beams, block_size, n_blocks, max_blocks, parent or None, seq_len or None, table or None, ring or None,
+                            ring_state or None, next_table or None, next_len or None, copy or None, next_state or None, workspace or None,
+                            workspace_bytes, stream or None))
+
+
+def coe_kv_copy(caches, n: int, copy: int, seq_len: int, stream: int = 0) -> None:
+    """Rows of blocks that are not full to their copies, in every layer; caches: an array of coe_kv_cache, `(coe_kv_cache * layers)(...)`, or a
+    sequence of them; enqueued on `stream`."""
+    if not isinstance(caches, C.Array):
+        caches = (coe_kv_cache * len(caches))(*caches)
+    _static(lib.coe_kv_copy(len(caches), caches, n, copy or None, seq_len or None, stream or None))
 
 
 def coe_profiler_fit_latency(batch, latency_us) -> Tuple[float, float]:

@@ -227,5 +227,70 @@ struct Sampling {
 int64_t sample_workspace(int32_t n_rows, int32_t vocab);
 hipError_t sample_tokens(int dtype, int32_t n_rows, const Sampling& s, void* workspace, hipStream_t stream);
 
+// append with rotation; pairing: 0 halves, 1 neighbours
+struct Rotation {
+    const uint16_t* q;
+    int64_t q_token_stride, q_head_stride;
+    uint16_t* q_out;
+    int64_t q_out_token_stride, q_out_head_stride;
+    const uint16_t* k;
+    int64_t k_token_stride, k_head_stride;
+    const uint16_t* v;
+    int64_t v_token_stride, v_head_stride;
+    const int32_t *slot, *position;
+    const float* frequency;
+    int32_t n_tokens, heads, rotated, pairing;
+};
+hipError_t kv_append_rotated(const KvCache& cache, const Rotation& r, hipStream_t stream);
+
+// Strides in elements; seen: null or [n_rows].
+struct States {
+    const uint16_t *k, *v;
+    int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+    const uint8_t* seen;
+    int32_t n_rows, kv_heads, head_dim;
+};
+struct CrossAttention {
+    int32_t n_sources, n_tokens, beams, max_new, max_rows, heads;
+    float scale;
+    const uint16_t* q;
+    int64_t q_token_stride, q_head_stride;
+    const int32_t *q_off, *first, *length;
+    uint16_t* out;
+    int64_t out_token_stride, out_head_stride;
+    float* lse;
+};
+int64_t cross_attention_workspace(int32_t n_sources, int32_t n_tokens, int32_t max_new, int32_t max_rows, int32_t heads, int32_t kv_heads, int32_t head_dim);
+hipError_t cross_attention(const States& states, const CrossAttention& a, void* workspace, hipStream_t stream);
+
+constexpr int kBeamMax = 32, kBeamPicksMax = 64;
+struct BeamSelection {
+    const void* logits;
+    int64_t logits_stride;
+    const float* score;
+    const int32_t* ended;
+    float* next_score;
+    int32_t *next_row, *next_token, *next_ended;
+    int32_t n_requests, beams, picks, vocab, end_token;
+};
+int64_t beam_workspace(int32_t n_requests, int32_t beams, int32_t picks, int32_t vocab);
+hipError_t beam_select(int dtype, const BeamSelection& s, void* workspace, hipStream_t stream);
+
+struct KvFork {
+    int32_t n_requests, beams, block_shift, n_blocks, max_blocks;
+    const int32_t *parent, *seq_len, *table;
+    int32_t* ring;
+    const int32_t* ring_state;
+    int32_t *next_table, *next_len, *copy, *next_state;
+};
+int64_t kv_fork_workspace(int32_t n_requests, int32_t beams);
+hipError_t kv_fork(const KvFork& f, void* workspace, hipStream_t stream);
+// the caches of up to kCopyCaches layers, by value
+constexpr int kCopyCaches = 32;
+struct KvCaches {
+    KvCache c[kCopyCaches];
+};
+hipError_t kv_copy(int32_t n_caches, const KvCaches& caches, int32_t n, const int32_t* copy, const int32_t* seq_len, hipStream_t stream);
+
 }  // namespace k
 }  // namespace coe

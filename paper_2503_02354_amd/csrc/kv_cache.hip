@@ -1,5 +1,5 @@
 // gfx950 kernels that keep the paged key/value cache of token-generating experts: a step's block tables and slot map, and the
-// append of new rows.
+// append of new rows, as they come or rotated by their positions.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -200,6 +200,95 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, int n_tokens,
     }
 }
 
+// ---- append with rotation -----------------------------------------------------------------------------------------
+// Pair (a, b) of a token at position p turns by p f: (a + ib) e^{ipf}.  A workgroup's tokens have their sines and cosines computed once, in
+// LDS, for all heads; a thread then turns V pairs of a head, or copies what is not turned.  The angle in turns, p f / 2 pi, is an fp64 product whose
+// nearest integer is taken off there: what is left is exact to 2^-22 of a turn at positions of 2^31, and its sine and cosine are fp32.
+constexpr int kTurnThreads = 256, kTurnTokens = 4;
+
+template <int V> struct Packed;               // V bf16 values
+template <> struct Packed<8> { typedef uint4 type; };
+template <> struct Packed<4> { typedef uint2 type; };
+template <> struct Packed<1> { typedef uint16_t type; };
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ uint16_t to_bf16(float v)
+{
+    const __bf16 b = (__bf16)v;               // to nearest even
+    return __builtin_bit_cast(uint16_t, b);
+}
+
+template <int V, bool HALVES>
+__global__ __launch_bounds__(kTurnThreads) void kv_append_rotated_kernel(KvCache c, Rotation r)
+{
+    __shared__ float2 turn[kTurnTokens][64];  // (cosine, sine) of every pair
+    const int half = r.rotated >> 1, units = half / V;            // of a head
+    constexpr int kRest = V == 1 ? 2 : 8;     // channels behind the rotated ones that a thread copies
+    const int rest = (c.head_dim - r.rotated) / kRest, per_head = units + rest, chunks = c.head_dim >> 3;
+    const int turned = (r.heads + c.kv_heads) * per_head, per_token = turned + c.kv_heads * chunks;
+    for (long long t0 = (long long)blockIdx.x * kTurnTokens; t0 < r.n_tokens; t0 += (long long)gridDim.x * kTurnTokens) {
+        const int tokens = (int)min((long long)kTurnTokens, r.n_tokens - t0);
+        for (int i = threadIdx.x; i < tokens * half; i += kTurnThreads) {
+            const int t = i / half, pair = i - t * half;
+            const double turns = (double)r.position[t0 + t] * (double)r.frequency[pair] * 0.15915494309189533577;
+            float s, co;
+            sincospif(2.f * (float)(turns - rint(turns)), &s, &co);
+            turn[t][pair] = make_float2(co, s);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < tokens * per_token; i += kTurnThreads) {
+            const int sub = i / per_token;
+            int u = i - sub * per_token;
+            const long long t = t0 + sub;
+            if (r.position[t] < 0) continue;
+            const int32_t slot = r.slot[t], block = slot >> c.block_shift, row = slot & ((1 << c.block_shift) - 1);
+            const bool kept = slot >= 0 && block < c.n_blocks;
+            const int64_t to_cache = block * c.block_stride + row * c.token_stride;
+            if (u >= turned) {                // values
+                u -= turned;
+                const int head = u / chunks, ch = (u - head * chunks) * 8;
+                if (kept) *(uint4*)(c.v + to_cache + head * c.head_stride + ch) = *(const uint4*)(r.v + t * r.v_token_stride + head * r.v_head_stride + ch);
+                continue;
+            }
+            int head = u / per_head;
+            u -= head * per_head;
+            const uint16_t* from;
+            uint16_t* to;
+            if (head < r.heads) {
+                from = r.q + t * r.q_token_stride + head * r.q_head_stride;
+                to = r.q_out + t * r.q_out_token_stride + head * r.q_out_head_stride;
+            } else {
+                head -= r.heads;
+                if (!kept) continue;
+                from = r.k + t * r.k_token_stride + head * r.k_head_stride;
+                to = c.k + to_cache + head * c.head_stride;
+            }
+            if (u >= units) {                 // channels that are not turned
+                const int ch = r.rotated + (u - units) * kRest;
+                if (V == 1) *(uint32_t*)(to + ch) = *(const uint32_t*)(from + ch);
+                else *(uint4*)(to + ch) = *(const uint4*)(from + ch);
+                continue;
+            }
+            typedef typename Packed<V>::type Pack;
+            const int p0 = u * V, at0 = HALVES ? p0 : 2 * p0, at1 = HALVES ? half + p0 : 2 * p0 + V;
+            uint16_t x[2 * V];                // the unit's channels in the order of their addresses
+            *(Pack*)x = *(const Pack*)(from + at0);
+            *(Pack*)(x + V) = *(const Pack*)(from + at1);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int ia = HALVES ? j : 2 * j, ib = HALVES ? V + j : 2 * j + 1;
+                const float a = bf16_lo(x[ia]), b = bf16_lo(x[ib]);
+                const float2 cs = turn[sub][p0 + j];
+                x[ia] = to_bf16(a * cs.x - b * cs.y);
+                x[ib] = to_bf16(b * cs.x + a * cs.y);
+            }
+            *(Pack*)(to + at0) = *(const Pack*)x;
+            *(Pack*)(to + at1) = *(const Pack*)(x + V);
+        }
+        __syncthreads();
+    }
+}
+
 }  // namespace
 
 hipError_t kv_plan(int32_t n, int32_t block_shift, int32_t n_blocks, int32_t max_blocks, int32_t token_cap, const int32_t* have,
@@ -226,6 +315,18 @@ hipError_t kv_append(const KvCache& c, int32_t n_tokens, const uint16_t* k, int6
     const long long blocks = ((long long)n_tokens + tokens - 1) / tokens;
     hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)std::min<long long>(blocks, 1 << 20)), dim3(256), 0, stream, c, n_tokens, k, k_ts, k_hs, v,
                        v_ts, v_hs, slot);
+    return hipGetLastError();
+}
+
+hipError_t kv_append_rotated(const KvCache& c, const Rotation& r, hipStream_t stream)
+{
+    const long long blocks = ((long long)r.n_tokens + kTurnTokens - 1) / kTurnTokens;
+    const dim3 grid((unsigned)std::min<long long>(blocks, 1 << 20)), threads(kTurnThreads);
+    const bool halves = r.pairing == 0;
+    // as many pairs to a thread as come in aligned pieces of 16 or 8 bytes
+    if (r.rotated % 16 == 0) hipLaunchKernelGGL((halves ? kv_append_rotated_kernel<8, true> : kv_append_rotated_kernel<8, false>), grid, threads, 0, stream, c, r);
+    else if (r.rotated % 8 == 0) hipLaunchKernelGGL((halves ? kv_append_rotated_kernel<4, true> : kv_append_rotated_kernel<4, false>), grid, threads, 0, stream, c, r);
+    else hipLaunchKernelGGL((halves ? kv_append_rotated_kernel<1, true> : kv_append_rotated_kernel<1, false>), grid, threads, 0, stream, c, r);
     return hipGetLastError();
 }
 
