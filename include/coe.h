@@ -437,7 +437,7 @@ int coe_cross_attention(const coe_states* states, int32_t n_sources, int32_t n_t
  * beam had ended or the token is end_token, else 0.  All are [n_requests][picks]; where fewer than picks candidates are there, the rest is -inf,
  * -1, -1, 0.  With picks == beams, next_score and next_ended are the next step's score and ended, and next_row coe_kv_fork's parent; outputs
  * must not alias inputs.
- * beams in 1..COE_BEAM_MAX, picks in 1..COE_BEAM_PICKS_MAX.
+ * beams in 1..COE_BEAM_MAX, picks in 1..COE_BEAM_PICKS_MAX, n_requests * beams below 2^23.
  * Numerics: exponentials and their sums over a few hundred tokens in fp32, sums over a row, logarithms and scores in fp64, in which candidates
  * are compared; one rounding of next_score to fp32.  The same inputs give the same outputs, and rows of equal bits equal scores.
  * workspace: coe_beam_workspace bytes (may be 0), 16-byte aligned. */

@@ -1,4 +1,10 @@
 // gfx950 kernels for the selection of a beam search: the best continuations of a request's beams.
+//
+// A row's candidates come in the order of their logits, and what they are short of the score, ln sum exp x, is one number for all of them.  So
+// one pass over a row finds both that sum and its best logits, and the rows of a request meet afterwards with a few candidates each:
+//   score(row, v) = score[row] + ((x_v - m) - ln S)      m = max x,  S = sum exp(x - m)
+// Candidates of different rows may be as near to each other as their logits' last bits, so scores are fp64, and so are S (from fp32 sums of a lane's
+// terms relative to the lane's largest, whose errors are independent) and its logarithm.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -10,115 +16,421 @@ namespace k {
 
 namespace {
 
-constexpr int kThreads = 256;
-
-__device__ __forceinline__ float logit_at(const float* x, int64_t i) { return x[i]; }
-__device__ __forceinline__ float logit_at(const uint16_t* x, int64_t i) { return __uint_as_float((uint32_t)x[i] << 16); }
-__device__ __forceinline__ float known(float x) { return x == x ? x : -INFINITY; }     // NaN weighs nothing
-
-struct Candidate {
-    double score;
-    int row, token;                           // row < 0: none
-    float x;
+// 16 bytes of logits of any alignment: which lane sums which tokens goes by the index alone, so that equal rows have equal sums
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int kWidth = 4;
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
+    static __device__ __forceinline__ float one(const float* p) { return *p; }
+    static __device__ __forceinline__ float at(const type& w, int e) { return __uint_as_float(w[e]); }
 };
-__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b)         // a is taken before b
+template <> struct Vec<uint16_t> {
+    static constexpr int kWidth = 8;
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2)));
+    static __device__ __forceinline__ float one(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+    static __device__ __forceinline__ float at(const type& w, int e) { return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16); }
+};
+
+// A candidate of a row as an integer that grows in the row's order: the logit (-0 and +0 the same), then the complement of the index.  0: none.
+__device__ __forceinline__ uint32_t key_of(float x)
 {
-    if (b.row < 0 || a.row < 0) return a.row >= 0;
-    if (a.score != b.score && a.row != b.row) return a.score > b.score;
-    if (a.row != b.row) return a.row < b.row;
-    return a.x != b.x ? a.x > b.x : a.token < b.token;
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
+
+__device__ __forceinline__ float exp_fast(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f);
+#else
+    return v;
+#endif
+}
+// the largest of three; a signalling NaN among them makes it NaN (fmaxf would quiet every operand first, an instruction each)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+#else
+    return a + b + c;
+#endif
+}
+__device__ __forceinline__ int count_of(bool b) { return __popcll(__ballot(b)); }
+// LDS that the lanes of a wavefront write for each other
+__device__ __forceinline__ void wave_sync()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#endif
 }
 
-// A workgroup per request: the rows' maxima and sums, then the best candidate behind the last one, picks times.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void beam_plain_kernel(BeamSelection s)
+// ---- rows ---------------------------------------------------------------------------------------------------------
+// A workgroup takes a part of a row, its wavefronts steps of 1024 logits in turn.  A lane keeps its largest logit and its sum of weights
+// relative to it.  A wavefront keeps a list, in LDS, of at least the best `picks` of what it has seen: of the first step everything from the picks-th
+// best of the lanes' maxima on, then what lies above a threshold that never passes the picks-th best; a list that grows is cut back to at most kSlack more
+// than picks, and the threshold rises to its lowest logit.  Indices ascend from step to step, so an equal logit that comes later is never wanted.
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kPerLane = 16, kStep = 64 * kPerLane, kSlack = 32, kGrow = 64;
+constexpr int kList = kBeamPicksMax + kGrow + kStep;
+struct RowPart {                              // the workspace: [rows][parts] of these, then as many lists of `picks` keys
+    double sum;
+    float top;
+    int32_t pad;
+};
+
+// Cuts a list of n keys to the largest, at least `picks` and at most kSlack more: those from a threshold on, which is a logit where that does it, else a key.  `low`
+// is the least of its logits that may be there; returns the list's new length, and in `low` what the rest lies at or above.
+__device__ __forceinline__ int cut_list(unsigned long long* list, int n, int picks, uint32_t& low)
 {
-    __shared__ double part[kThreads];
-    __shared__ float top[kThreads];
-    __shared__ Candidate best[kThreads];
-    __shared__ float row_max[kBeamMax];
-    __shared__ double row_log[kBeamMax];
-    const int tid = threadIdx.x, r = blockIdx.x;
-    for (int b = 0; b < s.beams; ++b) {
-        const int64_t row = (int64_t)r * s.beams + b;
-        const float so_far = s.score[row];
-        if (!(so_far > -INFINITY) || (s.ended && s.ended[row])) continue;
-        const T* const x = (const T*)s.logits + row * s.logits_stride;
-        float m = -INFINITY;
-        for (int i = tid; i < s.vocab; i += kThreads) m = fmaxf(m, known(logit_at(x, i)));
-        top[tid] = m;
-        __syncthreads();
-        for (int d = kThreads / 2; d > 0; d >>= 1) {
-            if (tid < d) top[tid] = fmaxf(top[tid], top[tid + d]);
-            __syncthreads();
+    const int lane = threadIdx.x & 63;
+    wave_sync();
+    auto count = [&](auto holds) {
+        int c = 0;
+        for (int i = lane; i - lane < n; i += 64) c += count_of(i < n && holds(list[i]));
+        return c;
+    };
+    uint32_t lo = low, hi = 0;                // enough of them are at or above lo; above hi there are none
+    for (int i = lane; i < n; i += 64) hi = max(hi, (uint32_t)(list[i] >> 32));
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, d, 64));
+    int at_lo = n;
+    while (at_lo > picks + kSlack && lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        const int c = count([&](unsigned long long k) { return (uint32_t)(k >> 32) >= mid; });
+        if (c >= picks) lo = mid, at_lo = c;
+        else hi = mid - 1;
+    }
+    uint32_t index = 0;                       // of logits equal to lo, those from here on (complements of indices)
+    if (at_lo > picks + kSlack) {
+        const int above = count([&](unsigned long long k) { return (uint32_t)(k >> 32) > lo; });
+        uint32_t top = 0xFFFFFFFFu;
+        while (at_lo > picks + kSlack && index < top) {
+            const uint32_t mid = index + (top - index) / 2 + 1;
+            const int c = above + count([&](unsigned long long k) { return (uint32_t)(k >> 32) == lo && (uint32_t)k >= mid; });
+            if (c >= picks) index = mid, at_lo = c;
+            else top = mid - 1;
         }
-        m = top[0];
+    }
+    const unsigned long long from = (unsigned long long)lo << 32 | index;
+    int kept = 0;
+    for (int i = lane; i - lane < n; i += 64) {
+        const unsigned long long k = i < n ? list[i] : 0;
+        const bool keep = k >= from && i < n;
+        const unsigned long long b = __ballot(keep);
+        wave_sync();
+        if (keep) list[kept + __popcll(b & ((1ull << lane) - 1))] = k;
+        wave_sync();
+        kept += __popcll(b);
+    }
+    low = lo;
+    return kept;
+}
+
+// One wavefront's share of a part of a row, its 16-byte pieces [begin, end).  SAFE: NaN counts as -inf, and equal infinities weigh 1; without it they make
+// the sum NaN.
+template <typename T, bool SAFE>
+__device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int end, int picks, unsigned long long* list, int& n, float& top, double& sum)
+{
+    typedef typename Vec<T>::type Piece;
+    constexpr int W = Vec<T>::kWidth, kPieces = kPerLane / W;
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, whole = min(end, vocab / W);       // pieces without an end in them
+    float m = -INFINITY, s = 0.f;
+    Piece next[kPieces];
+    auto fetch = [&](long long at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const long long piece = at + j * 64 + lane;
+            if (piece < whole) next[j] = *(const Piece*)(row + piece * W);
+        }
+    };
+    constexpr int kStride = kWaves * kPieces * 64;
+    long long at = begin + (long long)wid * kPieces * 64;
+    fetch(at);
+    n = 0;
+    uint32_t low = 0;                         // key of the threshold
+    float threshold = -INFINITY;
+    bool first = true;
+    for (; at < end; at += kStride) {
+        float x[kPerLane];
+        if (at + kPieces * 64 > whole) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const long long piece = at + j * 64 + lane;
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const long long i = piece * W + e;
+                    x[j * W + e] = piece < whole ? Vec<T>::at(next[j], e) : piece < end && i < vocab ? Vec<T>::one(row + i) : -INFINITY;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+                for (int e = 0; e < W; ++e) x[j * W + e] = Vec<T>::at(next[j], e);
+        }
+        fetch(at + kStride);
+        if (SAFE)
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e) x[e] = x[e] == x[e] ? x[e] : -INFINITY;
+        float most = x[0];
+#pragma unroll
+        for (int e = 1; e + 1 < kPerLane; e += 2) most = max3(most, x[e], x[e + 1]);
+        most = max3(most, x[kPerLane - 1], x[0]);
+        const float m_new = max3(m, most, m), m_use = m_new == -INFINITY ? 0.f : m_new;
+        s = m == m_new ? s : s * exp_fast(m - m_new);
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < kPerLane; ++e) part[e & 3] += SAFE && x[e] == m_new && x[e] > -INFINITY ? 1.f : exp_fast(x[e] - m_use);
+        s += (part[0] + part[1]) + (part[2] + part[3]);
+        m = m_new;
+        bool strict = true;
+        if (first) {                          // the lanes' maxima: from the picks-th of them on, to 16 bits
+            first = false;
+            strict = false;
+            const uint32_t key = key_of(most) >> 16;
+            uint32_t t = 0;
+            for (uint32_t bit = 0x8000u; bit; bit >>= 1)
+                if (count_of(key >= (t | bit)) >= picks) t |= bit;
+            low = t << 16;
+            if (low <= key_of(-INFINITY)) low = key_of(-INFINITY) + 1;       // -inf is no candidate
+        }
+        if (__any(strict ? most > threshold : key_of(most) >= low)) {
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e) {
+                const uint32_t key = key_of(x[e]);
+                const bool take = strict ? x[e] > threshold : key >= low && x[e] == x[e];
+                const unsigned long long b = __ballot(take);
+                if (b) {
+                    const uint32_t i = (uint32_t)((at + e / W * 64 + lane) * W + e % W);
+                    if (take) list[n + __popcll(b & ((1ull << lane) - 1))] = (unsigned long long)key << 32 | (uint32_t)~i;
+                    n += __popcll(b);
+                }
+            }
+            if (n > picks + kGrow) n = cut_list(list, n, picks, low);
+        }
+        if (n >= picks) threshold = logit_of(low);
+    }
+    // the lanes' sums
+    float wave_top = m;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) wave_top = fmaxf(wave_top, __shfl_xor(wave_top, d, 64));
+    double v = m == wave_top ? (double)s : (double)s * exp((double)m - (double)wave_top);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    top = wave_top;
+    sum = __any(s != s) ? __longlong_as_double(0x7FF8000000000000ll) : v;
+    wave_sync();
+}
+
+__device__ __forceinline__ bool is_there(const BeamSelection& s, int64_t row) { return s.score[row] > -INFINITY; }
+
+template <typename T>
+__global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s, int parts, RowPart* stats, unsigned long long* lists)
+{
+    constexpr int W = Vec<T>::kWidth;
+    __shared__ unsigned long long list[kWaves][kList];
+    __shared__ int lengths[kWaves];
+    __shared__ float tops[kWaves];
+    __shared__ double sums[kWaves];
+    const int tid = threadIdx.x, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t row = blockIdx.x / parts;
+    const int part = blockIdx.x - (int)row * parts;
+    if (!is_there(s, row) || (s.ended && s.ended[row])) return;
+    const T* const x = (const T*)s.logits + row * s.logits_stride;
+    const int pieces = (int)(((long long)s.vocab + W - 1) / W), each = (int)(((long long)pieces + parts - 1) / parts);
+    const int begin = (int)min((long long)pieces, (long long)part * each), end = (int)min((long long)pieces, (long long)begin + each);
+    int n;
+    float top;
+    double sum;
+    scan_row<T, false>(x, s.vocab, begin, end, s.picks, list[wid], n, top, sum);
+    if (sum != sum) scan_row<T, true>(x, s.vocab, begin, end, s.picks, list[wid], n, top, sum);
+    if ((tid & 63) == 0) {
+        lengths[wid] = n;
+        tops[wid] = top;
+        sums[wid] = sum;
+    }
+    __syncthreads();
+    unsigned long long* const out = lists + (size_t)blockIdx.x * s.picks;
+    if (tid == 0) {
+        float t = tops[0];
+        for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
+        double v = 0;
+        for (int w = 0; w < kWaves; ++w) v += tops[w] == t ? sums[w] : sums[w] * exp((double)tops[w] - (double)t);
+        stats[blockIdx.x] = {v, t, 0};
+    }
+    // the wavefronts' lists, a key to a thread: its place is the number of larger ones
+    int all = 0;
+    for (int w = 0; w < kWaves; ++w) all += lengths[w];
+    for (int i = tid; i < all; i += kThreads) {
+        int w = 0, at = i;
+        while (at >= lengths[w]) at -= lengths[w++];
+        const unsigned long long mine = list[w][at];
+        int place = 0;
+        for (w = 0; w < kWaves; ++w)
+            for (int j = 0; j < lengths[w]; ++j) place += list[w][j] > mine;
+        if (place < s.picks) out[place] = mine;
+    }
+    for (int i = all + tid; i < s.picks; i += kThreads) out[i] = 0;
+}
+
+// ---- requests -----------------------------------------------------------------------------------------------------
+// A workgroup per request: the rows' sums, then the best of all lists.  From the picks-th best of the threads' best on, candidates are listed and
+// counted against each other; where that is too many (an order that no list of a row has by chance), they are found one after the other.
+constexpr int kMeet = 1024;
+struct Candidate {
+    unsigned long long score;                 // fp64 as an integer that grows with it; 0: none
+    unsigned long long key;                   // of the row
+    int32_t row;                              // of the request
+};
+__device__ __forceinline__ unsigned long long order_of(double v)
+{
+    const unsigned long long b = (unsigned long long)__double_as_longlong(v + 0.);
+    return b >> 63 ? ~b : b | 1ull << 63;
+}
+__device__ __forceinline__ double score_of(unsigned long long o) { return __longlong_as_double((long long)(o >> 63 ? o & ~(1ull << 63) : ~o)); }
+__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b)
+{
+    if (a.score != b.score) return a.score > b.score;
+    return a.row != b.row ? a.row < b.row : a.key > b.key;
+}
+__device__ __forceinline__ void write_pick(const BeamSelection& s, int r, int place, const Candidate& c)
+{
+    const int64_t at = (int64_t)r * s.picks + place, row = (int64_t)r * s.beams + c.row;
+    const bool done = c.score && s.ended && s.ended[row];
+    const int token = c.score == 0 ? -1 : done ? s.end_token : (int)~(uint32_t)c.key;
+    s.next_score[at] = c.score ? (float)score_of(c.score) : -INFINITY;
+    s.next_row[at] = c.score ? (int)row : -1;
+    s.next_token[at] = token;
+    if (s.next_ended) s.next_ended[at] = c.score && (done || token == s.end_token);
+}
+
+__global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, int parts, const RowPart* stats, const unsigned long long* lists)
+{
+    __shared__ float row_top[kBeamMax];
+    __shared__ double row_log[kBeamMax], row_score[kBeamMax];
+    __shared__ int row_state[kBeamMax];       // 0: not there, 1: candidates, 2: ended
+    __shared__ unsigned long long best[kThreads];
+    __shared__ Candidate met[kMeet];
+    __shared__ int n_met;
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
+    const size_t first = (size_t)r * s.beams;
+    for (int b = wid; b < s.beams; b += kWaves) {
+        const int state = !is_there(s, first + b) ? 0 : s.ended && s.ended[first + b] ? 2 : 1;
+        float top = -INFINITY;
         double sum = 0;
-        for (int i = tid; i < s.vocab; i += kThreads) {
-            const float v = known(logit_at(x, i));
-            if (v > -INFINITY) sum += v == m ? 1. : exp((double)v - m);
+        if (state == 1) {
+            for (int p = lane; p < parts; p += 64) {
+                const RowPart v = stats[(first + b) * parts + p];
+                const float t = fmaxf(top, v.top);
+                sum = (top == t ? sum : sum * exp((double)top - (double)t)) + (v.top == t ? v.sum : v.sum * exp((double)v.top - (double)t));
+                top = t;
+            }
+            float all = top;
+            for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
+            sum = top == all ? sum : sum * exp((double)top - (double)all);
+            for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+            top = all;
         }
-        part[tid] = sum;
-        __syncthreads();
-        for (int d = kThreads / 2; d > 0; d >>= 1) {
-            if (tid < d) part[tid] += part[tid + d];
-            __syncthreads();
+        if (lane == 0) {
+            row_top[b] = top;
+            row_log[b] = log(sum);
+            row_score[b] = s.score[first + b];
+            row_state[b] = state;
         }
-        if (tid == 0) {
-            row_max[b] = m;
-            row_log[b] = log(part[0]);
-        }
-        __syncthreads();
     }
-    Candidate last{INFINITY, -1, -1, 0.f};
-    bool any = true;
+    if (tid == 0) n_met = 0;
+    __syncthreads();
+    // candidate i: a row's lists one behind the other, then the row itself where it has ended
+    const int per_row = parts * s.picks, n = s.beams * (per_row + 1);
+    auto candidate = [&](int i) {
+        Candidate c{0, 0, i / (per_row + 1)};
+        const int at = i - c.row * (per_row + 1), state = row_state[c.row];
+        if (at == per_row) {
+            if (state == 2) c.score = order_of(row_score[c.row]);
+        } else if (state == 1) {
+            c.key = lists[(first + c.row) * per_row + at];
+            const float x = logit_of((uint32_t)(c.key >> 32)), top = row_top[c.row];
+            if (c.key != 0 && (x == top || top < INFINITY)) c.score = order_of(row_score[c.row] + ((x == top ? 0. : (double)x - (double)top) - row_log[c.row]));
+        }
+        return c;
+    };
+    unsigned long long mine = 0;
+    for (int i = tid; i < n; i += kThreads) mine = max(mine, candidate(i).score);
+    best[tid] = mine;
+    __syncthreads();
+    // the picks-th largest of the threads' best
+    int larger = 0;
+    for (int j = 0; j < kThreads; ++j) larger += best[j] > mine || (best[j] == mine && j < tid);
+    __shared__ unsigned long long from;
+    if (larger == s.picks - 1) from = mine;
+    __syncthreads();
+    const unsigned long long low = max(from, 1ull);
+    for (int i = tid; i < n; i += kThreads) {
+        const Candidate c = candidate(i);
+        if (c.score >= low) {
+            const int at = atomicAdd(&n_met, 1);
+            if (at < kMeet) met[at] = c;
+        }
+    }
+    __syncthreads();
+    const int all = n_met;
+    if (all <= kMeet) {
+        for (int i = tid; i < all; i += kThreads) {
+            const Candidate c = met[i];
+            int place = 0;
+            for (int j = 0; j < all; ++j) place += before(met[j], c);
+            if (place < s.picks) write_pick(s, r, place, c);
+        }
+        for (int i = all + tid; i < s.picks; i += kThreads) write_pick(s, r, i, Candidate{0, 0, 0});
+        return;
+    }
+    Candidate last{~0ull, ~0ull, -1};
     for (int p = 0; p < s.picks; ++p) {
-        Candidate mine{0, -1, -1, 0.f};
-        for (int b = 0; b < s.beams && any; ++b) {
-            const int64_t row = (int64_t)r * s.beams + b;
-            const float so_far = s.score[row];
-            if (!(so_far > -INFINITY)) continue;
-            auto offer = [&](double score, int token, float v) {
-                const Candidate c{score, (int)row, token, v};
-                if ((last.row < 0 || before(last, c)) && before(c, mine)) mine = c;
-            };
-            if (s.ended && s.ended[row]) {
-                if (tid == 0) offer(so_far, s.end_token, 0.f);
-                continue;
-            }
-            const T* const x = (const T*)s.logits + row * s.logits_stride;
-            for (int i = tid; i < s.vocab; i += kThreads) {
-                const float v = known(logit_at(x, i));
-                if (v > -INFINITY && (v == row_max[b] || row_max[b] < INFINITY)) offer(so_far + ((v == row_max[b] ? 0. : (double)v - row_max[b]) - row_log[b]), i, v);
-            }
+        Candidate c{0, 0, 0};
+        for (int i = tid; i < n; i += kThreads) {
+            const Candidate v = candidate(i);
+            if (before(last, v) && before(v, c)) c = v;
         }
-        best[tid] = mine;
+        __syncthreads();
+        met[tid] = c;
         __syncthreads();
         for (int d = kThreads / 2; d > 0; d >>= 1) {
-            if (tid < d && before(best[tid + d], best[tid])) best[tid] = best[tid + d];
+            if (tid < d && before(met[tid + d], met[tid])) met[tid] = met[tid + d];
             __syncthreads();
         }
-        last = best[0];
-        any = last.row >= 0;
-        __syncthreads();
-        if (tid == 0) {
-            const int64_t at = (int64_t)r * s.picks + p;
-            s.next_score[at] = any ? (float)last.score : -INFINITY;
-            s.next_row[at] = any ? last.row : -1;
-            s.next_token[at] = any ? last.token : -1;
-            if (s.next_ended) s.next_ended[at] = any && ((s.ended && s.ended[last.row]) || last.token == s.end_token);
-        }
+        last = met[0];
+        if (tid == 0) write_pick(s, r, p, last);
     }
+}
+
+// Parts of a row: as many as fill the chip (four workgroups to a compute unit), of 4096 logits or more.
+int row_parts(int64_t rows, int32_t vocab)
+{
+    return (int)std::max<int64_t>(1, std::min<int64_t>((1024 + rows - 1) / std::max<int64_t>(rows, 1), ((int64_t)vocab + 4095) / 4096));
 }
 
 }  // namespace
 
-int64_t beam_workspace(int32_t, int32_t, int32_t, int32_t) { return 0; }
-
-hipError_t beam_select(int dtype, const BeamSelection& s, void*, hipStream_t stream)
+int64_t beam_workspace(int32_t n_requests, int32_t beams, int32_t picks, int32_t vocab)
 {
-    if (dtype == 0) hipLaunchKernelGGL(beam_plain_kernel<float>, dim3((unsigned)s.n_requests), dim3(kThreads), 0, stream, s);
-    else hipLaunchKernelGGL(beam_plain_kernel<uint16_t>, dim3((unsigned)s.n_requests), dim3(kThreads), 0, stream, s);
+    const int64_t rows = (int64_t)n_requests * beams;
+    return rows * row_parts(rows, vocab) * (int64_t)(sizeof(RowPart) + 8 * picks);
+}
+
+hipError_t beam_select(int dtype, const BeamSelection& s, void* workspace, hipStream_t stream)
+{
+    const int64_t rows = (int64_t)s.n_requests * s.beams;
+    const int parts = row_parts(rows, s.vocab);
+    if (rows * parts > 0x7FFFFFFFll / kThreads) return hipErrorInvalidValue;
+    RowPart* const stats = (RowPart*)workspace;
+    unsigned long long* const lists = (unsigned long long*)(stats + rows * parts);
+    if (dtype == 0) hipLaunchKernelGGL(beam_rows_kernel<float>, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, s, parts, stats, lists);
+    else hipLaunchKernelGGL(beam_rows_kernel<uint16_t>, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, s, parts, stats, lists);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(beam_meet_kernel, dim3((unsigned)s.n_requests), dim3(kThreads), 0, stream, s, parts, stats, lists);
     return hipGetLastError();
 }
 

@@ -252,7 +252,7 @@ static_assert(COE_BEAM_MAX == coe::k::kBeamMax && COE_BEAM_PICKS_MAX == coe::k::
 
 int64_t coe_beam_workspace(int32_t n_requests, int32_t beams, int32_t picks, int32_t vocab)
 {
-    if (n_requests < 0 || beams <= 0 || beams > COE_BEAM_MAX || picks <= 0 || picks > COE_BEAM_PICKS_MAX || vocab <= 0 || (long long)n_requests * beams > 0x7FFFFFFFll)
+    if (n_requests < 0 || beams <= 0 || beams > COE_BEAM_MAX || picks <= 0 || picks > COE_BEAM_PICKS_MAX || vocab <= 0 || (long long)n_requests * beams >= 1 << 23)
         return fail(COE_EINVAL, "coe_beam_workspace: bad size");
     return coe::k::beam_workspace(n_requests, beams, picks, vocab);
 }
@@ -266,6 +266,7 @@ int coe_beam_select(int32_t n_requests, int32_t beams, int32_t picks, int32_t vo
     if (beams <= 0 || beams > COE_BEAM_MAX) return fail(COE_EINVAL, "%s: beams %d outside 1..%d", call, beams, COE_BEAM_MAX);
     if (picks <= 0 || picks > COE_BEAM_PICKS_MAX) return fail(COE_EINVAL, "%s: picks %d outside 1..%d", call, picks, COE_BEAM_PICKS_MAX);
     if ((long long)n_requests * beams > 0x7FFFFFFFll || (long long)n_requests * picks > 0x7FFFFFFFll) return fail(COE_EINVAL, "%s: n_requests * beams and n_requests * picks must be below 2^31", call);
+    if ((long long)n_requests * beams >= 1 << 23) return fail(COE_EINVAL, "%s: n_requests * beams must be below 2^23", call);
     if (dtype != COE_DT_F32 && dtype != COE_DT_BF16) return fail(COE_EINVAL, "%s: unknown dtype %d", call, dtype);
     if (n_requests == 0) return COE_OK;
     if (!logits || !score || !next_score || !next_row || !next_token) return fail(COE_EINVAL, "%s: null argument", call);
