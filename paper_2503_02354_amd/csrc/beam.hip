@@ -70,9 +70,10 @@ __device__ __forceinline__ void wave_sync()
 
 // ---- rows ---------------------------------------------------------------------------------------------------------
 // A workgroup takes a part of a row, its wavefronts steps of 1024 logits in turn.  A lane keeps its largest logit and its sum of weights
-// relative to it.  A wavefront keeps a list, in LDS, of at least the best `picks` of what it has seen: of the first step everything from the picks-th
-// best of the lanes' maxima on, then what lies above a threshold that never passes the picks-th best; a list that grows is cut back to at most kSlack more
-// than picks, and the threshold rises to its lowest logit.  Indices ascend from step to step, so an equal logit that comes later is never wanted.
+// relative to it.  A wavefront keeps a list, in LDS, of all that it has seen above a threshold, which `picks` logits of the part are known to reach: a
+// quarter of them in every wavefront (each says what its quarter reaches after its first step, its second, its fourth, ...; the lowest of the four holds), or
+// all of them in its own list.  A list that grows all the same is cut back to at most kSlack more than picks.  Indices ascend from step to step, so an
+// equal logit that comes later in the same wavefront is never wanted, but in another it may be.
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kPerLane = 16, kStep = 64 * kPerLane, kSlack = 32, kGrow = 64;
 constexpr int kList = kBeamPicksMax + kGrow + kStep;
 struct RowPart {                              // the workspace: [rows][parts] of these, then as many lists of `picks` keys
@@ -80,23 +81,50 @@ struct RowPart {                              // the workspace: [rows][parts] of
     float top;
     int32_t pad;
 };
+constexpr uint32_t kLeast = 0x00800000u;      // key of the lowest finite logit: -inf is no candidate
+// the largest logit below those of key `low` (> kLeast - 1)
+__device__ __forceinline__ float below(uint32_t low) { return logit_of(low - (low == 0x80000000u ? 2 : 1)); }
 
-// Cuts a list of n keys to the largest, at least `picks` and at most kSlack more: those from a threshold on, which is a logit where that does it, else a key.  `low`
-// is the least of its logits that may be there; returns the list's new length, and in `low` what the rest lies at or above.
-__device__ __forceinline__ int cut_list(unsigned long long* list, int n, int picks, uint32_t& low)
+// A key that at least `picks` of a wavefront's keys reach (n of them to a lane, 0: none), and not many more: their most significant bits as far as
+// fewer than `enough` more reach it; 0 where there are not that many.
+template <int N> __device__ __forceinline__ uint32_t reached(const uint32_t (&key)[N], int picks, int enough)
+{
+    uint32_t t = 0;
+    int c = 0;
+#pragma nounroll
+    for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+        int now = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) now += count_of(key[i] >= (t | bit));
+        if (now >= picks) {
+            t |= bit;
+            c = now;
+            if (c <= picks + enough) break;
+        }
+    }
+    return t;
+}
+
+// Cuts a list of n keys to the largest, at least `picks` and at most kSlack more: those from a threshold on, which is a logit where that does it, else a
+// key.  `low` is the least of its logits that may be there; returns the list's new length, and in `low` what the rest lies at or above.
+__device__ int cut_list(unsigned long long* list, int n, int picks, uint32_t& low)
 {
     const int lane = threadIdx.x & 63;
     wave_sync();
     auto count = [&](auto holds) {
         int c = 0;
-        for (int i = lane; i - lane < n; i += 64) c += count_of(i < n && holds(list[i]));
+#pragma nounroll
+        for (int i = 0; i < n; i += 64) c += count_of(i + lane < n && holds(list[i + lane]));
         return c;
     };
     uint32_t lo = low, hi = 0;                // enough of them are at or above lo; above hi there are none
+#pragma nounroll
     for (int i = lane; i < n; i += 64) hi = max(hi, (uint32_t)(list[i] >> 32));
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, d, 64));
+    hi = __builtin_amdgcn_readfirstlane(hi);
     int at_lo = n;
+#pragma nounroll
     while (at_lo > picks + kSlack && lo < hi) {
         const uint32_t mid = lo + (hi - lo) / 2 + 1;
         const int c = count([&](unsigned long long k) { return (uint32_t)(k >> 32) >= mid; });
@@ -107,6 +135,7 @@ __device__ __forceinline__ int cut_list(unsigned long long* list, int n, int pic
     if (at_lo > picks + kSlack) {
         const int above = count([&](unsigned long long k) { return (uint32_t)(k >> 32) > lo; });
         uint32_t top = 0xFFFFFFFFu;
+#pragma nounroll
         while (at_lo > picks + kSlack && index < top) {
             const uint32_t mid = index + (top - index) / 2 + 1;
             const int c = above + count([&](unsigned long long k) { return (uint32_t)(k >> 32) == lo && (uint32_t)k >= mid; });
@@ -116,9 +145,10 @@ __device__ __forceinline__ int cut_list(unsigned long long* list, int n, int pic
     }
     const unsigned long long from = (unsigned long long)lo << 32 | index;
     int kept = 0;
-    for (int i = lane; i - lane < n; i += 64) {
-        const unsigned long long k = i < n ? list[i] : 0;
-        const bool keep = k >= from && i < n;
+#pragma nounroll
+    for (int i = 0; i < n; i += 64) {
+        const unsigned long long k = i + lane < n ? list[i + lane] : 0;
+        const bool keep = i + lane < n && k >= from;
         const unsigned long long b = __ballot(keep);
         wave_sync();
         if (keep) list[kept + __popcll(b & ((1ull << lane) - 1))] = k;
@@ -130,13 +160,13 @@ __device__ __forceinline__ int cut_list(unsigned long long* list, int n, int pic
 }
 
 // One wavefront's share of a part of a row, its 16-byte pieces [begin, end).  SAFE: NaN counts as -inf, and equal infinities weigh 1; without it they make
-// the sum NaN.
+// the sum NaN.  quarter: [kWaves] what every wavefront's quarter of the picks reaches, 0 for not yet.
 template <typename T, bool SAFE>
-__device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int end, int picks, unsigned long long* list, int& n, float& top, double& sum)
+__device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int end, int wid, int picks, unsigned long long* list, volatile uint32_t* quarter, int& n, float& top, double& sum)
 {
     typedef typename Vec<T>::type Piece;
-    constexpr int W = Vec<T>::kWidth, kPieces = kPerLane / W;
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, whole = min(end, vocab / W);       // pieces without an end in them
+    constexpr int W = Vec<T>::kWidth, kPieces = kPerLane / W, kStride = kWaves * kPieces * 64;
+    const int lane = threadIdx.x & 63, whole = min(end, vocab / W);       // pieces without the row's end in them
     float m = -INFINITY, s = 0.f;
     Piece next[kPieces];
     auto fetch = [&](long long at) __attribute__((always_inline)) {
@@ -146,32 +176,12 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
             if (piece < whole) next[j] = *(const Piece*)(row + piece * W);
         }
     };
-    constexpr int kStride = kWaves * kPieces * 64;
-    long long at = begin + (long long)wid * kPieces * 64;
-    fetch(at);
     n = 0;
-    uint32_t low = 0;                         // key of the threshold
-    float threshold = -INFINITY;
-    bool first = true;
-    for (; at < end; at += kStride) {
-        float x[kPerLane];
-        if (at + kPieces * 64 > whole) {
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
-                const long long piece = at + j * 64 + lane;
-#pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    const long long i = piece * W + e;
-                    x[j * W + e] = piece < whole ? Vec<T>::at(next[j], e) : piece < end && i < vocab ? Vec<T>::one(row + i) : -INFINITY;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j)
-#pragma unroll
-                for (int e = 0; e < W; ++e) x[j * W + e] = Vec<T>::at(next[j], e);
-        }
-        fetch(at + kStride);
+    uint32_t low = kLeast;                    // what the list's logits lie at or above
+    float threshold = -INFINITY;              // what is wanted lies above
+    int step = 0;
+    auto work = [&](float (&x)[kPerLane], long long at) __attribute__((always_inline)) {
+        const uint32_t q = min(min(quarter[0], quarter[1]), min(quarter[2], quarter[3]));
         if (SAFE)
 #pragma unroll
             for (int e = 0; e < kPerLane; ++e) x[e] = x[e] == x[e] ? x[e] : -INFINITY;
@@ -186,32 +196,63 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
         for (int e = 0; e < kPerLane; ++e) part[e & 3] += SAFE && x[e] == m_new && x[e] > -INFINITY ? 1.f : exp_fast(x[e] - m_use);
         s += (part[0] + part[1]) + (part[2] + part[3]);
         m = m_new;
-        bool strict = true;
-        if (first) {                          // the lanes' maxima: from the picks-th of them on, to 16 bits
-            first = false;
-            strict = false;
-            const uint32_t key = key_of(most) >> 16;
-            uint32_t t = 0;
-            for (uint32_t bit = 0x8000u; bit; bit >>= 1)
-                if (count_of(key >= (t | bit)) >= picks) t |= bit;
-            low = t << 16;
-            if (low <= key_of(-INFINITY)) low = key_of(-INFINITY) + 1;       // -inf is no candidate
+        const int share = (picks + kWaves - 1) / kWaves;
+        if (step == 0) {                      // the lanes' maxima stand for the step
+            const uint32_t key[1] = {most > -INFINITY ? key_of(most) : 0u};
+            const uint32_t mine = reached(key, share, share);
+            if (lane == 0) quarter[wid] = mine;
+            const uint32_t all = max(reached(key, picks, picks), kLeast);
+            threshold = below(all);
         }
-        if (__any(strict ? most > threshold : key_of(most) >= low)) {
+        if (q > kLeast) threshold = fmaxf(threshold, below(q));
+        if (__any(most > threshold)) {
 #pragma unroll
             for (int e = 0; e < kPerLane; ++e) {
-                const uint32_t key = key_of(x[e]);
-                const bool take = strict ? x[e] > threshold : key >= low && x[e] == x[e];
+                const bool take = x[e] > threshold;
                 const unsigned long long b = __ballot(take);
                 if (b) {
                     const uint32_t i = (uint32_t)((at + e / W * 64 + lane) * W + e % W);
-                    if (take) list[n + __popcll(b & ((1ull << lane) - 1))] = (unsigned long long)key << 32 | (uint32_t)~i;
+                    if (take) list[n + __popcll(b & ((1ull << lane) - 1))] = (unsigned long long)key_of(x[e]) << 32 | (uint32_t)~i;
                     n += __popcll(b);
                 }
             }
-            if (n > picks + kGrow) n = cut_list(list, n, picks, low);
+            if (n > picks + kGrow) {
+                n = cut_list(list, n, picks, low);
+                threshold = fmaxf(threshold, logit_of(low));
+            }
         }
-        if (n >= picks) threshold = logit_of(low);
+        ++step;
+        if (step > 1 && (step & (step - 1)) == 0 && n >= share) {
+            wave_sync();
+            uint32_t key[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) key[i] = i * 64 + lane < n ? (uint32_t)(list[i * 64 + lane] >> 32) : 0u;
+            const uint32_t mine = reached(key, share, share / 2);
+            if (lane == 0 && mine > quarter[wid]) quarter[wid] = mine;
+        }
+    };
+    long long at = begin + (long long)wid * kPieces * 64;
+    fetch(at);
+#pragma nounroll
+    for (; at < end; at += kStride) {
+        float x[kPerLane];
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+            for (int e = 0; e < W; ++e) x[j * W + e] = Vec<T>::at(next[j], e);
+        if (at + kPieces * 64 > whole)        // the part's last step, in one wavefront or none
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const long long piece = at + j * 64 + lane;
+                if (piece < whole) continue;
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const long long i = piece * W + e;
+                    x[j * W + e] = piece < end && i < vocab ? Vec<T>::one(row + i) : -INFINITY;
+                }
+            }
+        fetch(at + kStride);
+        work(x, at);
     }
     // the lanes' sums
     float wave_top = m;
@@ -235,6 +276,7 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
     __shared__ int lengths[kWaves];
     __shared__ float tops[kWaves];
     __shared__ double sums[kWaves];
+    __shared__ uint32_t quarter[kWaves];
     const int tid = threadIdx.x, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = blockIdx.x / parts;
     const int part = blockIdx.x - (int)row * parts;
@@ -245,8 +287,14 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
     int n;
     float top;
     double sum;
-    scan_row<T, false>(x, s.vocab, begin, end, s.picks, list[wid], n, top, sum);
-    if (sum != sum) scan_row<T, true>(x, s.vocab, begin, end, s.picks, list[wid], n, top, sum);
+    if (tid < kWaves) quarter[tid] = 0;
+    __syncthreads();
+    scan_row<T, false>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
+    if (__syncthreads_or(sum != sum)) {       // a quarter that counted NaN or signs of them holds for nobody
+        if (tid < kWaves) quarter[tid] = 0;
+        __syncthreads();
+        scan_row<T, true>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
+    }
     if ((tid & 63) == 0) {
         lengths[wid] = n;
         tops[wid] = top;
@@ -277,9 +325,9 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
 }
 
 // ---- requests -----------------------------------------------------------------------------------------------------
-// A workgroup per request: the rows' sums, then the best of all lists.  From the picks-th best of the threads' best on, candidates are listed and
+// A workgroup per request: the rows' sums, then the best of all lists.  From a score on that enough of the threads' best reach, candidates are listed and
 // counted against each other; where that is too many (an order that no list of a row has by chance), they are found one after the other.
-constexpr int kMeet = 1024;
+constexpr int kMeet = 1024, kHeld = 4;        // candidates that are listed; keys that a thread holds, more are read again
 struct Candidate {
     unsigned long long score;                 // fp64 as an integer that grows with it; 0: none
     unsigned long long key;                   // of the row
@@ -293,7 +341,7 @@ __device__ __forceinline__ unsigned long long order_of(double v)
 __device__ __forceinline__ double score_of(unsigned long long o) { return __longlong_as_double((long long)(o >> 63 ? o & ~(1ull << 63) : ~o)); }
 __device__ __forceinline__ bool before(const Candidate& a, const Candidate& b)
 {
-    if (a.score != b.score) return a.score > b.score;
+    if (a.score != b.score) return a.score > b.score;     // equal ones are rare
     return a.row != b.row ? a.row < b.row : a.key > b.key;
 }
 __device__ __forceinline__ void write_pick(const BeamSelection& s, int r, int place, const Candidate& c)
@@ -307,74 +355,85 @@ __device__ __forceinline__ void write_pick(const BeamSelection& s, int r, int pl
     if (s.next_ended) s.next_ended[at] = c.score && (done || token == s.end_token);
 }
 
-__global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, int parts, const RowPart* stats, const unsigned long long* lists)
+__global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, int parts, const RowPart* __restrict__ stats, const unsigned long long* __restrict__ lists)
 {
+    constexpr int kLanes = kThreads / kBeamMax;           // that share a row's parts
     __shared__ float row_top[kBeamMax];
     __shared__ double row_log[kBeamMax], row_score[kBeamMax];
     __shared__ int row_state[kBeamMax];       // 0: not there, 1: candidates, 2: ended
-    __shared__ unsigned long long best[kThreads];
+    __shared__ __attribute__((aligned(16))) uint32_t best[kThreads];
     __shared__ Candidate met[kMeet];
     __shared__ int n_met;
-    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, r = blockIdx.x;
     const size_t first = (size_t)r * s.beams;
-    for (int b = wid; b < s.beams; b += kWaves) {
-        const int state = !is_there(s, first + b) ? 0 : s.ended && s.ended[first + b] ? 2 : 1;
+    const int per_row = parts * s.picks, n = s.beams * per_row;
+    const unsigned long long* const keys = lists + first * per_row;
+    unsigned long long held[kHeld];
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c) held[c] = tid + c * kThreads < n ? keys[tid + c * kThreads] : 0;
+    {
+        const int b = tid / kLanes, sub = tid % kLanes;
         float top = -INFINITY;
         double sum = 0;
-        if (state == 1) {
-            for (int p = lane; p < parts; p += 64) {
-                const RowPart v = stats[(first + b) * parts + p];
-                const float t = fmaxf(top, v.top);
-                sum = (top == t ? sum : sum * exp((double)top - (double)t)) + (v.top == t ? v.sum : v.sum * exp((double)v.top - (double)t));
-                top = t;
-            }
-            float all = top;
-            for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
-            sum = top == all ? sum : sum * exp((double)top - (double)all);
-            for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-            top = all;
+        int state = 0;
+        float so_far = 0.f;
+        if (b < s.beams) {
+            RowPart v = stats[(first + b) * parts + min(sub, parts - 1)];     // of any bits where the row has none; on its way with the row's state
+            so_far = s.score[first + b];
+            state = !(so_far > -INFINITY) ? 0 : s.ended && s.ended[first + b] ? 2 : 1;
+            if (state == 1)
+                for (int p = sub; p < parts; p += kLanes) {
+                    if (p != sub) v = stats[(first + b) * parts + p];
+                    const float t = fmaxf(top, v.top);
+                    sum = (top == t ? sum : sum * exp((double)top - (double)t)) + (v.top == t ? v.sum : v.sum * exp((double)v.top - (double)t));
+                    top = t;
+                }
         }
-        if (lane == 0) {
-            row_top[b] = top;
+        float all = top;
+#pragma unroll
+        for (int d = 1; d < kLanes; d <<= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
+        sum = top == all ? sum : sum * exp((double)top - (double)all);
+#pragma unroll
+        for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d, 64);
+        if (sub == 0 && b < s.beams) {
+            row_top[b] = all;
             row_log[b] = log(sum);
-            row_score[b] = s.score[first + b];
+            row_score[b] = so_far;
             row_state[b] = state;
         }
     }
     if (tid == 0) n_met = 0;
     __syncthreads();
-    // candidate i: a row's lists one behind the other, then the row itself where it has ended
-    const int per_row = parts * s.picks, n = s.beams * (per_row + 1);
-    auto candidate = [&](int i) {
-        Candidate c{0, 0, i / (per_row + 1)};
-        const int at = i - c.row * (per_row + 1), state = row_state[c.row];
-        if (at == per_row) {
-            if (state == 2) c.score = order_of(row_score[c.row]);
-        } else if (state == 1) {
-            c.key = lists[(first + c.row) * per_row + at];
-            const float x = logit_of((uint32_t)(c.key >> 32)), top = row_top[c.row];
-            if (c.key != 0 && (x == top || top < INFINITY)) c.score = order_of(row_score[c.row] + ((x == top ? 0. : (double)x - (double)top) - row_log[c.row]));
-        }
+    auto candidate = [&](int i, unsigned long long key) {
+        Candidate c{0, key, i / per_row};
+        const float x = logit_of((uint32_t)(key >> 32)), top = row_top[c.row];
+        if (row_state[c.row] == 1 && key != 0 && (x == top || top < INFINITY))
+            c.score = order_of(row_score[c.row] + ((x == top ? 0. : (double)x - (double)top) - row_log[c.row]));
         return c;
     };
+    // every candidate of this thread's: its keys, then a row that has ended
+    auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < kHeld; ++c)
+            if (tid + c * kThreads < n) f(candidate(tid + c * kThreads, held[c]));
+        for (int i = tid + kHeld * kThreads; i < n; i += kThreads) f(candidate(i, keys[i]));
+        if (tid < s.beams && row_state[tid] == 2) f(Candidate{order_of(row_score[tid]), 0, tid});
+    };
     unsigned long long mine = 0;
-    for (int i = tid; i < n; i += kThreads) mine = max(mine, candidate(i).score);
-    best[tid] = mine;
+    each([&](const Candidate& c) { mine = max(mine, c.score); });
+    best[tid] = (uint32_t)(mine >> 32);
     __syncthreads();
-    // the picks-th largest of the threads' best
-    int larger = 0;
-    for (int j = 0; j < kThreads; ++j) larger += best[j] > mine || (best[j] == mine && j < tid);
-    __shared__ unsigned long long from;
-    if (larger == s.picks - 1) from = mine;
-    __syncthreads();
-    const unsigned long long low = max(from, 1ull);
-    for (int i = tid; i < n; i += kThreads) {
-        const Candidate c = candidate(i);
-        if (c.score >= low) {
-            const int at = atomicAdd(&n_met, 1);
-            if (at < kMeet) met[at] = c;
-        }
+    uint32_t low;
+    {
+        const uint4 four = *(const uint4*)(best + 4 * lane);
+        const uint32_t key[4] = {four.x, four.y, four.z, four.w};
+        low = max(reached(key, s.picks, 16), 1u);             // no score's upper half is 0
     }
+    each([&](const Candidate& c) {
+        if ((uint32_t)(c.score >> 32) < low) return;
+        const int at = atomicAdd(&n_met, 1);
+        if (at < kMeet) met[at] = c;
+    });
     __syncthreads();
     const int all = n_met;
     if (all <= kMeet) {
@@ -390,10 +449,9 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
     Candidate last{~0ull, ~0ull, -1};
     for (int p = 0; p < s.picks; ++p) {
         Candidate c{0, 0, 0};
-        for (int i = tid; i < n; i += kThreads) {
-            const Candidate v = candidate(i);
-            if (before(last, v) && before(v, c)) c = v;
-        }
+        each([&](const Candidate& v) {
+            if (v.score != 0 && before(last, v) && before(v, c)) c = v;
+        });
         __syncthreads();
         met[tid] = c;
         __syncthreads();
