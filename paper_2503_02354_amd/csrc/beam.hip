@@ -68,6 +68,22 @@ __device__ __forceinline__ void wave_sync()
 #endif
 }
 
+// the largest of a wavefront's values, in every lane's hands; six register operations
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false));        // one lane up, two, four, eight in a row of 16
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false));        // a row's last lane to the next row, the second row's to the last two
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false));
+    v = (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+#endif
+    return v;
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) { return ~wave_max(~v); }
+
 // ---- rows ---------------------------------------------------------------------------------------------------------
 // A workgroup takes a part of a row, its wavefronts steps of 1024 logits in turn.  A lane keeps its largest logit and its sum of weights
 // relative to it.  A wavefront keeps a list, in LDS, of all that it has seen above a threshold, which `picks` logits of the part are known to reach: a
@@ -85,24 +101,25 @@ constexpr uint32_t kLeast = 0x00800000u;      // key of the lowest finite logit:
 // the largest logit below those of key `low` (> kLeast - 1)
 __device__ __forceinline__ float below(uint32_t low) { return logit_of(low - (low == 0x80000000u ? 2 : 1)); }
 
-// A key that at least `picks` of a wavefront's keys reach (n of them to a lane, 0: none), and not many more: their most significant bits as far as
-// fewer than `enough` more reach it; 0 where there are not that many.
-template <int N> __device__ __forceinline__ uint32_t reached(const uint32_t (&key)[N], int picks, int enough)
+// A key that at least `picks` of a wavefront's keys (N to a lane) reach, and at most `enough` more unless they are equal.  That many reach lo, and
+// none passes hi.
+template <int N> __device__ __forceinline__ uint32_t reached(const uint32_t (&key)[N], int picks, int enough, uint32_t lo, uint32_t hi)
 {
-    uint32_t t = 0;
-    int c = 0;
-#pragma nounroll
-    for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-        int now = 0;
+    auto count = [&](uint32_t t) {
+        int c = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) now += count_of(key[i] >= (t | bit));
-        if (now >= picks) {
-            t |= bit;
-            c = now;
-            if (c <= picks + enough) break;
-        }
+        for (int i = 0; i < N; ++i) c += count_of(key[i] >= t);
+        return c;
+    };
+    int c = count(lo);
+#pragma nounroll
+    while (c > picks + enough && lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        const int now = count(mid);
+        if (now >= picks) lo = mid, c = now;
+        else hi = mid - 1;
     }
-    return t;
+    return lo;
 }
 
 // Cuts a list of n keys to the largest, at least `picks` and at most kSlack more: those from a threshold on, which is a logit where that does it, else a
@@ -120,9 +137,7 @@ __device__ int cut_list(unsigned long long* list, int n, int picks, uint32_t& lo
     uint32_t lo = low, hi = 0;                // enough of them are at or above lo; above hi there are none
 #pragma nounroll
     for (int i = lane; i < n; i += 64) hi = max(hi, (uint32_t)(list[i] >> 32));
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, d, 64));
-    hi = __builtin_amdgcn_readfirstlane(hi);
+    hi = wave_max(hi);
     int at_lo = n;
 #pragma nounroll
     while (at_lo > picks + kSlack && lo < hi) {
@@ -159,87 +174,31 @@ __device__ int cut_list(unsigned long long* list, int n, int picks, uint32_t& lo
     return kept;
 }
 
-// One wavefront's share of a part of a row, its 16-byte pieces [begin, end).  SAFE: NaN counts as -inf, and equal infinities weigh 1; without it they make
-// the sum NaN.  quarter: [kWaves] what every wavefront's quarter of the picks reaches, 0 for not yet.
+// One wavefront's share of a part of a row, its 16-byte pieces [begin, end); all of the workgroup's wavefronts call this together.  SAFE: NaN counts as
+// -inf, and equal infinities weigh 1; without it they make the sum NaN.  quarter: [kWaves] what every wavefront's quarter of the picks reaches, 0 for
+// not yet.
 template <typename T, bool SAFE>
 __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int end, int wid, int picks, unsigned long long* list, volatile uint32_t* quarter, int& n, float& top, double& sum)
 {
     typedef typename Vec<T>::type Piece;
     constexpr int W = Vec<T>::kWidth, kPieces = kPerLane / W, kStride = kWaves * kPieces * 64;
     const int lane = threadIdx.x & 63, whole = min(end, vocab / W);       // pieces without the row's end in them
+    const int share = (picks + kWaves - 1) / kWaves;
     float m = -INFINITY, s = 0.f;
-    Piece next[kPieces];
-    auto fetch = [&](long long at) __attribute__((always_inline)) {
+    constexpr int kDepth = kPieces <= 2 ? 2 : 1;          // steps ahead: 64 bytes of a lane
+    Piece next[kDepth][kPieces];
+    auto fetch = [&](Piece (&to)[kPieces], long long at) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             const long long piece = at + j * 64 + lane;
-            if (piece < whole) next[j] = *(const Piece*)(row + piece * W);
+            if (piece < whole) to[j] = *(const Piece*)(row + piece * W);
         }
     };
-    n = 0;
-    uint32_t low = kLeast;                    // what the list's logits lie at or above
-    float threshold = -INFINITY;              // what is wanted lies above
-    int step = 0;
-    auto work = [&](float (&x)[kPerLane], long long at) __attribute__((always_inline)) {
-        const uint32_t q = min(min(quarter[0], quarter[1]), min(quarter[2], quarter[3]));
-        if (SAFE)
-#pragma unroll
-            for (int e = 0; e < kPerLane; ++e) x[e] = x[e] == x[e] ? x[e] : -INFINITY;
-        float most = x[0];
-#pragma unroll
-        for (int e = 1; e + 1 < kPerLane; e += 2) most = max3(most, x[e], x[e + 1]);
-        most = max3(most, x[kPerLane - 1], x[0]);
-        const float m_new = max3(m, most, m), m_use = m_new == -INFINITY ? 0.f : m_new;
-        s = m == m_new ? s : s * exp_fast(m - m_new);
-        float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < kPerLane; ++e) part[e & 3] += SAFE && x[e] == m_new && x[e] > -INFINITY ? 1.f : exp_fast(x[e] - m_use);
-        s += (part[0] + part[1]) + (part[2] + part[3]);
-        m = m_new;
-        const int share = (picks + kWaves - 1) / kWaves;
-        if (step == 0) {                      // the lanes' maxima stand for the step
-            const uint32_t key[1] = {most > -INFINITY ? key_of(most) : 0u};
-            const uint32_t mine = reached(key, share, share);
-            if (lane == 0) quarter[wid] = mine;
-            const uint32_t all = max(reached(key, picks, picks), kLeast);
-            threshold = below(all);
-        }
-        if (q > kLeast) threshold = fmaxf(threshold, below(q));
-        if (__any(most > threshold)) {
-#pragma unroll
-            for (int e = 0; e < kPerLane; ++e) {
-                const bool take = x[e] > threshold;
-                const unsigned long long b = __ballot(take);
-                if (b) {
-                    const uint32_t i = (uint32_t)((at + e / W * 64 + lane) * W + e % W);
-                    if (take) list[n + __popcll(b & ((1ull << lane) - 1))] = (unsigned long long)key_of(x[e]) << 32 | (uint32_t)~i;
-                    n += __popcll(b);
-                }
-            }
-            if (n > picks + kGrow) {
-                n = cut_list(list, n, picks, low);
-                threshold = fmaxf(threshold, logit_of(low));
-            }
-        }
-        ++step;
-        if (step > 1 && (step & (step - 1)) == 0 && n >= share) {
-            wave_sync();
-            uint32_t key[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) key[i] = i * 64 + lane < n ? (uint32_t)(list[i * 64 + lane] >> 32) : 0u;
-            const uint32_t mine = reached(key, share, share / 2);
-            if (lane == 0 && mine > quarter[wid]) quarter[wid] = mine;
-        }
-    };
-    long long at = begin + (long long)wid * kPieces * 64;
-    fetch(at);
-#pragma nounroll
-    for (; at < end; at += kStride) {
-        float x[kPerLane];
+    auto unpack = [&](float (&x)[kPerLane], const Piece (&from)[kPieces], long long at) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j)
 #pragma unroll
-            for (int e = 0; e < W; ++e) x[j * W + e] = Vec<T>::at(next[j], e);
+            for (int e = 0; e < W; ++e) x[j * W + e] = Vec<T>::at(from[j], e);
         if (at + kPieces * 64 > whole)        // the part's last step, in one wavefront or none
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
@@ -251,9 +210,97 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
                     x[j * W + e] = piece < end && i < vocab ? Vec<T>::one(row + i) : -INFINITY;
                 }
             }
-        fetch(at + kStride);
-        work(x, at);
+        if (SAFE)
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e) x[e] = x[e] == x[e] ? x[e] : -INFINITY;
+    };
+    auto most_of = [&](const float (&x)[kPerLane]) __attribute__((always_inline)) {
+        float most = x[0];
+#pragma unroll
+        for (int e = 1; e + 1 < kPerLane; e += 2) most = max3(most, x[e], x[e + 1]);
+        return max3(most, x[kPerLane - 1], x[0]);
+    };
+    auto weigh = [&](const float (&x)[kPerLane], float most) __attribute__((always_inline)) {
+        const float m_new = max3(m, most, m), m_use = m_new == -INFINITY ? 0.f : m_new;
+        s = m == m_new ? s : s * exp_fast(m - m_new);
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < kPerLane; ++e) part[e & 3] += SAFE && x[e] == m_new && x[e] > -INFINITY ? 1.f : exp_fast(x[e] - m_use);
+        s += (part[0] + part[1]) + (part[2] + part[3]);
+        m = m_new;
+    };
+    n = 0;
+    uint32_t low = kLeast;                    // what the list's logits lie at or above
+    float threshold = -INFINITY;              // what is wanted lies above
+    auto put = [&](const float (&x)[kPerLane], long long at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < kPerLane; ++e) {
+            const bool take = x[e] > threshold;
+            const unsigned long long b = __ballot(take);
+            if (b) {
+                const uint32_t i = (uint32_t)((at + e / W * 64 + lane) * W + e % W);
+                if (take) list[n + __popcll(b & ((1ull << lane) - 1))] = (unsigned long long)key_of(x[e]) << 32 | (uint32_t)~i;
+                n += __popcll(b);
+            }
+        }
+        if (n > picks + kGrow) {
+            n = cut_list(list, n, picks, low);
+            threshold = fmaxf(threshold, logit_of(low));
+        }
+    };
+    // what a quarter of the picks reaches in this wavefront's list
+    auto tell = [&]() __attribute__((always_inline)) {
+        wave_sync();
+        uint32_t key[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) key[i] = i * 64 + lane < n ? (uint32_t)(list[i * 64 + lane] >> 32) : 0u;
+        const uint32_t least = wave_min(min(key[0] - 1, key[1] - 1)) + 1;     // of those that are there
+        const uint32_t mine = reached(key, share, share / 2, least, wave_max(max(key[0], key[1])));
+        if (lane == 0 && mine > quarter[wid]) quarter[wid] = mine;
+    };
+    auto all_reach = [&]() { return min(min(quarter[0], quarter[1]), min(quarter[2], quarter[3])); };
+
+    long long at = begin + (long long)wid * kPieces * 64;
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) fetch(next[d], at + d * kStride);
+    {                                         // the first step: the lanes' maxima stand for it
+        float x[kPerLane], most = -INFINITY;
+        if (at < end) {
+            unpack(x, next[0], at);
+            fetch(next[0], at + kDepth * kStride);
+            most = most_of(x);
+            weigh(x, most);
+        }
+        const uint32_t key[1] = {most > -INFINITY ? key_of(most) : 0u};
+        const uint32_t least = wave_min(key[0]), high = wave_max(key[0]), mine = least ? reached(key, share, share / 2, least, high) : 0u;
+        if (lane == 0) quarter[wid] = mine;
+        __syncthreads();
+        const uint32_t q = all_reach();
+        if (q) threshold = below(q);
+        else if (least) threshold = below(reached(key, picks, picks, least, high));
+        if (at < end) put(x, at);
     }
+    int step = 1;
+    auto go = [&](Piece (&from)[kPieces]) __attribute__((always_inline)) {
+        const uint32_t q = all_reach();
+        float x[kPerLane];
+        unpack(x, from, at);
+        fetch(from, at + kDepth * kStride);
+        const float most = most_of(x);
+        weigh(x, most);
+        if (q) threshold = fmaxf(threshold, below(q));
+        if (__any(most > threshold)) put(x, at);
+        if ((step & (step + 1)) == 0 && n >= share) tell();
+        at += kStride;
+        ++step;
+    };
+    at += kStride;
+#pragma nounroll
+    while (at < end) {
+        go(next[kDepth - 1]);
+        if (kDepth > 1 && at < end) go(next[0]);
+    }
+    if (step > 2 && n >= share) tell();
     // the lanes' sums
     float wave_top = m;
 #pragma unroll
@@ -296,7 +343,6 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
         scan_row<T, true>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
     }
     if ((tid & 63) == 0) {
-        lengths[wid] = n;
         tops[wid] = top;
         sums[wid] = sum;
     }
@@ -309,17 +355,31 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
         for (int w = 0; w < kWaves; ++w) v += tops[w] == t ? sums[w] : sums[w] * exp((double)tops[w] - (double)t);
         stats[blockIdx.x] = {v, t, 0};
     }
-    // the wavefronts' lists, a key to a thread: its place is the number of larger ones
+    // the wavefronts' lists without what the quarters pass, then a key to a thread: its place is the number of larger ones
+    const int lane = tid & 63;
+    const uint32_t q = min(min(quarter[0], quarter[1]), min(quarter[2], quarter[3]));
+    int mine = 0;
+    for (int i = 0; i < n; i += 64) {
+        const unsigned long long k = i + lane < n ? list[wid][i + lane] : 0;
+        const bool keep = k != 0 && (uint32_t)(k >> 32) >= q;
+        const unsigned long long b = __ballot(keep);
+        wave_sync();
+        if (keep) list[wid][mine + __popcll(b & ((1ull << lane) - 1))] = k;
+        wave_sync();
+        mine += __popcll(b);
+    }
+    if (lane == 0) lengths[wid] = mine;
+    __syncthreads();
     int all = 0;
     for (int w = 0; w < kWaves; ++w) all += lengths[w];
     for (int i = tid; i < all; i += kThreads) {
         int w = 0, at = i;
         while (at >= lengths[w]) at -= lengths[w++];
-        const unsigned long long mine = list[w][at];
+        const unsigned long long key = list[w][at];
         int place = 0;
         for (w = 0; w < kWaves; ++w)
-            for (int j = 0; j < lengths[w]; ++j) place += list[w][j] > mine;
-        if (place < s.picks) out[place] = mine;
+            for (int j = 0; j < lengths[w]; ++j) place += list[w][j] > key;
+        if (place < s.picks) out[place] = key;
     }
     for (int i = all + tid; i < s.picks; i += kThreads) out[i] = 0;
 }
@@ -427,7 +487,8 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
     {
         const uint4 four = *(const uint4*)(best + 4 * lane);
         const uint32_t key[4] = {four.x, four.y, four.z, four.w};
-        low = max(reached(key, s.picks, 16), 1u);             // no score's upper half is 0
+        const uint32_t most = max(max(key[0], key[1]), max(key[2], key[3]));
+        low = max(reached(key, s.picks, 16, wave_min(most), wave_max(most)), 1u);             // no score's upper half is 0
     }
     each([&](const Candidate& c) {
         if ((uint32_t)(c.score >> 32) < low) return;
