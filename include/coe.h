@@ -464,7 +464,7 @@ int coe_beam_select(int32_t n_requests, int32_t beams, int32_t picks, int32_t vo
  * have no tokens then.  Entries of next_table behind a row's blocks are not written.  Ids outside the cache are passed on, never copied
  * and never given back.  A negative seq_len counts as 0, one beyond max_blocks * block_size as that.  next_table, next_len and next_state must not alias
  * table, seq_len and ring_state; repeating a call is harmless, and the same inputs give the same outputs.
- * beams in 1..COE_BEAM_MAX, n at most COE_KV_MAX_REQUESTS; the rest as in coe_kv_plan.  workspace: coe_kv_fork_workspace bytes, 16-byte aligned. */
+ * beams in 1..COE_BEAM_MAX, n at most COE_KV_MAX_REQUESTS, max_blocks * beams below 2^30, copy 8-byte aligned; the rest as in coe_kv_plan.  workspace: coe_kv_fork_workspace bytes, 16-byte aligned. */
 int64_t coe_kv_fork_workspace(int32_t n_requests, int32_t beams);
 int coe_kv_fork(int32_t n_requests, int32_t beams, int32_t block_size, int32_t n_blocks, int32_t max_blocks, const int32_t* parent, const int32_t* seq_len,
                 const int32_t* table, int32_t* ring, const int32_t* ring_state, int32_t* next_table, int32_t* next_len, int32_t* copy,

@@ -201,91 +201,126 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, int n_tokens,
 }
 
 // ---- append with rotation -----------------------------------------------------------------------------------------
-// Pair (a, b) of a token at position p turns by p f: (a + ib) e^{ipf}.  A workgroup's tokens have their sines and cosines computed once, in
-// LDS, for all heads; a thread then turns V pairs of a head, or copies what is not turned.  The angle in turns, p f / 2 pi, is an fp64 product whose
-// nearest integer is taken off there: what is left is exact to 2^-22 of a turn at positions of 2^31, and its sine and cosine are fp32.
-constexpr int kTurnThreads = 256, kTurnTokens = 4;
+// Pair (a, b) of a token at position p turns by p f: (a + ib) e^{ipf}.  A wavefront takes a token, or one of `split` shares of its heads; its lanes take a
+// pair's sine and cosine each and leave them in LDS for all heads, while the first channels are on their way; then a lane turns V pairs of a head
+// at a time, or copies what is not turned.  The angle in turns, p f / 2 pi, is an fp64 product whose nearest integer is taken off there: what is left is
+// exact to 2^-22 of a turn at positions of 2^31, and its sine and cosine are fp32.
+constexpr int kTurnWaves = 4, kTurnAhead = 4;             // pieces that a lane has on their way
 
 template <int V> struct Packed;               // V bf16 values
-template <> struct Packed<8> { typedef uint4 type; };
-template <> struct Packed<4> { typedef uint2 type; };
+template <> struct Packed<8> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Packed<4> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Packed<1> { typedef uint16_t type; };
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ uint16_t to_bf16(float v)
+template <int V> __device__ __forceinline__ float value_of(const typename Packed<V>::type& p, int i)
 {
-    const __bf16 b = (__bf16)v;               // to nearest even
-    return __builtin_bit_cast(uint16_t, b);
+    if constexpr (V == 1) return __uint_as_float((uint32_t)p << 16);
+    else return __uint_as_float(i & 1 ? p[i / 2] & 0xFFFF0000u : p[i / 2] << 16);
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <int V> __device__ __forceinline__ typename Packed<V>::type packed(const float (&v)[V])     // to nearest even
+{
+    typename Packed<V>::type p;
+    if constexpr (V == 1) p = __builtin_bit_cast(uint16_t, (__bf16)v[0]);
+    else
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            const f32x2 two = {v[i], v[i + 1]};
+            p[i / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+        }
+    return p;
 }
 
 template <int V, bool HALVES>
-__global__ __launch_bounds__(kTurnThreads) void kv_append_rotated_kernel(KvCache c, Rotation r)
+__global__ __launch_bounds__(64 * kTurnWaves) void kv_append_rotated_kernel(KvCache c, Rotation r, int split)
 {
-    __shared__ float2 turn[kTurnTokens][64];  // (cosine, sine) of every pair
+    typedef typename Packed<V>::type Pack;
+    __shared__ float2 turns[kTurnWaves][64];  // (cosine, sine) of every pair
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    float2* const turn = turns[wid];
     const int half = r.rotated >> 1, units = half / V;            // of a head
-    constexpr int kRest = V == 1 ? 2 : 8;     // channels behind the rotated ones that a thread copies
-    const int rest = (c.head_dim - r.rotated) / kRest, per_head = units + rest, chunks = c.head_dim >> 3;
-    const int turned = (r.heads + c.kv_heads) * per_head, per_token = turned + c.kv_heads * chunks;
-    for (long long t0 = (long long)blockIdx.x * kTurnTokens; t0 < r.n_tokens; t0 += (long long)gridDim.x * kTurnTokens) {
-        const int tokens = (int)min((long long)kTurnTokens, r.n_tokens - t0);
-        for (int i = threadIdx.x; i < tokens * half; i += kTurnThreads) {
-            const int t = i / half, pair = i - t * half;
-            const double turns = (double)r.position[t0 + t] * (double)r.frequency[pair] * 0.15915494309189533577;
-            float s, co;
-            sincospif(2.f * (float)(turns - rint(turns)), &s, &co);
-            turn[t][pair] = make_float2(co, s);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < tokens * per_token; i += kTurnThreads) {
-            const int sub = i / per_token;
-            int u = i - sub * per_token;
-            const long long t = t0 + sub;
-            if (r.position[t] < 0) continue;
-            const int32_t slot = r.slot[t], block = slot >> c.block_shift, row = slot & ((1 << c.block_shift) - 1);
-            const bool kept = slot >= 0 && block < c.n_blocks;
-            const int64_t to_cache = block * c.block_stride + row * c.token_stride;
-            if (u >= turned) {                // values
-                u -= turned;
-                const int head = u / chunks, ch = (u - head * chunks) * 8;
-                if (kept) *(uint4*)(c.v + to_cache + head * c.head_stride + ch) = *(const uint4*)(r.v + t * r.v_token_stride + head * r.v_head_stride + ch);
-                continue;
-            }
-            int head = u / per_head;
-            u -= head * per_head;
-            const uint16_t* from;
-            uint16_t* to;
-            if (head < r.heads) {
-                from = r.q + t * r.q_token_stride + head * r.q_head_stride;
-                to = r.q_out + t * r.q_out_token_stride + head * r.q_out_head_stride;
-            } else {
-                head -= r.heads;
-                if (!kept) continue;
-                from = r.k + t * r.k_token_stride + head * r.k_head_stride;
-                to = c.k + to_cache + head * c.head_stride;
-            }
-            if (u >= units) {                 // channels that are not turned
-                const int ch = r.rotated + (u - units) * kRest;
-                if (V == 1) *(uint32_t*)(to + ch) = *(const uint32_t*)(from + ch);
-                else *(uint4*)(to + ch) = *(const uint4*)(from + ch);
-                continue;
-            }
-            typedef typename Packed<V>::type Pack;
-            const int p0 = u * V, at0 = HALVES ? p0 : 2 * p0, at1 = HALVES ? half + p0 : 2 * p0 + V;
-            uint16_t x[2 * V];                // the unit's channels in the order of their addresses
-            *(Pack*)x = *(const Pack*)(from + at0);
-            *(Pack*)(x + V) = *(const Pack*)(from + at1);
+    constexpr int kRest = V == 1 ? 2 : 8;     // channels behind the rotated ones that a lane copies
+    const int per_head = units + (c.head_dim - r.rotated) / kRest, chunks = c.head_dim >> 3;
+    const float f = lane < half ? r.frequency[lane] : 0.f;
+    const long long waves = (long long)gridDim.x * kTurnWaves, wave = (long long)blockIdx.x * kTurnWaves + wid;
+    const int step = 64 * split, step_heads = step / per_head, step_units = step - step_heads * per_head, first = (int)(wave % split) * 64 + lane;
+    for (long long t = wave / split; t < r.n_tokens; t += waves / split) {
+        const int32_t position = r.position[t], slot = r.slot[t], block = slot >> c.block_shift, row = slot & ((1 << c.block_shift) - 1);
+        if (position < 0) continue;
+        const bool kept = slot >= 0 && block < c.n_blocks;
+        const int64_t to_cache = block * c.block_stride + row * c.token_stride;
+        const uint16_t *const q = r.q + t * r.q_token_stride, *const k = r.k + t * r.k_token_stride, *const v = r.v + t * r.v_token_stride;
+        uint16_t* const q_out = r.q_out + t * r.q_out_token_stride;
+        const int heads = r.heads + (kept ? c.kv_heads : 0);
+        int head = first / per_head, u = first - head * per_head;
+        bool turned = false;
+        while (__any(head < heads)) {
+            Pack a[kTurnAhead], b[kTurnAhead];
+            int at_head[kTurnAhead], at_unit[kTurnAhead];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int ia = HALVES ? j : 2 * j, ib = HALVES ? V + j : 2 * j + 1;
-                const float a = bf16_lo(x[ia]), b = bf16_lo(x[ib]);
-                const float2 cs = turn[sub][p0 + j];
-                x[ia] = to_bf16(a * cs.x - b * cs.y);
-                x[ib] = to_bf16(b * cs.x + a * cs.y);
+            for (int i = 0; i < kTurnAhead; ++i) {
+                at_head[i] = head, at_unit[i] = u;
+                const uint16_t* const from = head < r.heads ? q + head * r.q_head_stride : k + (head - r.heads) * r.k_head_stride;
+                if (head < heads && u < units) {
+                    a[i] = *(const Pack*)(from + (HALVES ? u * V : 2 * u * V));
+                    b[i] = *(const Pack*)(from + (HALVES ? half + u * V : 2 * u * V + V));
+                }
+                head += step_heads, u += step_units;
+                if (u >= per_head) u -= per_head, ++head;
             }
-            *(Pack*)(to + at0) = *(const Pack*)x;
-            *(Pack*)(to + at1) = *(const Pack*)(x + V);
+            if (!turned) {
+                turned = true;
+                const double all = (double)position * (double)f * 0.15915494309189533577;
+                float si, co;
+                sincospif(2.f * (float)(all - rint(all)), &si, &co);
+                __builtin_amdgcn_wave_barrier();          // the last token's are read
+                turn[lane] = make_float2(co, si);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+#pragma unroll
+            for (int i = 0; i < kTurnAhead; ++i) {
+                const int h = at_head[i], w = at_unit[i];
+                if (h >= heads) continue;
+                uint16_t* const to = h < r.heads ? q_out + h * r.q_out_head_stride : c.k + to_cache + (h - r.heads) * c.head_stride;
+                if (w >= units) {             // channels that are not turned
+                    const uint16_t* const from = h < r.heads ? q + h * r.q_head_stride : k + (h - r.heads) * r.k_head_stride;
+                    const int ch = r.rotated + (w - units) * kRest;
+                    if (V == 1) *(uint32_t*)(to + ch) = *(const uint32_t*)(from + ch);
+                    else *(uint4*)(to + ch) = *(const uint4*)(from + ch);
+                    continue;
+                }
+                float x[V], y[V];
+                if (HALVES) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float2 cs = turn[w * V + j];
+                        const float p = value_of<V>(a[i], j), m = value_of<V>(b[i], j);
+                        x[j] = p * cs.x - m * cs.y;
+                        y[j] = m * cs.x + p * cs.y;
+                    }
+                } else {                      // the unit's channels in the order of their addresses: x, then y
+                    float z[2 * V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float2 cs = turn[w * V + j];
+                        const float p = 2 * j < V ? value_of<V>(a[i], 2 * j) : value_of<V>(b[i], 2 * j - V);
+                        const float m = 2 * j + 1 < V ? value_of<V>(a[i], 2 * j + 1) : value_of<V>(b[i], 2 * j + 1 - V);
+                        z[2 * j] = p * cs.x - m * cs.y;
+                        z[2 * j + 1] = m * cs.x + p * cs.y;
+                    }
+#pragma unroll
+                    for (int j = 0; j < V; ++j) x[j] = z[j], y[j] = z[V + j];
+                }
+                *(Pack*)(to + (HALVES ? w * V : 2 * w * V)) = packed<V>(x);
+                *(Pack*)(to + (HALVES ? half + w * V : 2 * w * V + V)) = packed<V>(y);
+            }
         }
-        __syncthreads();
+        if (!kept) continue;
+        for (int i = first; i < c.kv_heads * chunks; i += step) {
+            const int h = i / chunks, ch = (i - h * chunks) * 8;
+            *(uint4*)(c.v + to_cache + h * c.head_stride + ch) = *(const uint4*)(v + h * r.v_head_stride + ch);
+        }
     }
 }
 
@@ -318,15 +353,23 @@ hipError_t kv_append(const KvCache& c, int32_t n_tokens, const uint16_t* k, int6
     return hipGetLastError();
 }
 
+template <int V> void launch_rotated(const KvCache& c, const Rotation& r, int split, unsigned grid, hipStream_t stream)
+{
+    if (r.pairing == 0) hipLaunchKernelGGL((kv_append_rotated_kernel<V, true>), dim3(grid), dim3(64 * kTurnWaves), 0, stream, c, r, split);
+    else hipLaunchKernelGGL((kv_append_rotated_kernel<V, false>), dim3(grid), dim3(64 * kTurnWaves), 0, stream, c, r, split);
+}
+
 hipError_t kv_append_rotated(const KvCache& c, const Rotation& r, hipStream_t stream)
 {
-    const long long blocks = ((long long)r.n_tokens + kTurnTokens - 1) / kTurnTokens;
-    const dim3 grid((unsigned)std::min<long long>(blocks, 1 << 20)), threads(kTurnThreads);
-    const bool halves = r.pairing == 0;
-    // as many pairs to a thread as come in aligned pieces of 16 or 8 bytes
-    if (r.rotated % 16 == 0) hipLaunchKernelGGL((halves ? kv_append_rotated_kernel<8, true> : kv_append_rotated_kernel<8, false>), grid, threads, 0, stream, c, r);
-    else if (r.rotated % 8 == 0) hipLaunchKernelGGL((halves ? kv_append_rotated_kernel<4, true> : kv_append_rotated_kernel<4, false>), grid, threads, 0, stream, c, r);
-    else hipLaunchKernelGGL((halves ? kv_append_rotated_kernel<1, true> : kv_append_rotated_kernel<1, false>), grid, threads, 0, stream, c, r);
+    // wavefronts to a token: as many as have work, while there are fewer than the chip holds
+    int split = 1;
+    while (split < 8 && (long long)r.n_tokens * split * 2 <= 2048 && split * 128 < (r.heads + c.kv_heads) * (r.rotated / 16 + 1)) split *= 2;
+    const long long blocks = ((long long)r.n_tokens * split + kTurnWaves - 1) / kTurnWaves;
+    const unsigned grid = (unsigned)std::min<long long>(blocks, 1 << 20);
+    // as many pairs to a lane as come in aligned pieces of 16 or 8 bytes
+    if (r.rotated % 16 == 0) launch_rotated<8>(c, r, split, grid, stream);
+    else if (r.rotated % 8 == 0) launch_rotated<4>(c, r, split, grid, stream);
+    else launch_rotated<1>(c, r, split, grid, stream);
     return hipGetLastError();
 }
 

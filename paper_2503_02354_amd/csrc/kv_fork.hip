@@ -16,142 +16,220 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 // What a request's rows were and become; in LDS.
 struct Family {
     int parent[kBeamMax];                     // row of the request that row i continues; -1: none
-    int blocks[kBeamMax], tail[kBeamMax];     // of the old rows: blocks, and tokens of the last one if it is not full
+    int blocks[kBeamMax], length[kBeamMax];   // of the old rows: blocks, tokens
     int last[kBeamMax];                       // the old rows' last block where it is not full and lies in the cache, else -1
     int place[kBeamMax];                      // row i's copy among the request's, or -1
     uint32_t lives;                           // old rows that are continued
-    int copies, most;                         // copies, most blocks of a row that is dropped
+    int copies, most, longest;                // copies, most blocks of a row that is dropped, and of any row
 };
 struct Counts { int32_t copies, freed; };     // of a request; the workspace holds them
 
 __device__ __forceinline__ int length_of(const KvFork& f, int64_t row) { return max(0, min(f.seq_len[row], f.max_blocks << f.block_shift)); }
 
-// by all threads of the workgroup
-__device__ __forceinline__ void read_family(Family& o, const KvFork& f, int r)
+// A thread's column of the old rows' tables: their blocks at one place, in LDS, all on their way together; of any value behind a row's blocks.
+typedef int32_t Column[kBeamMax][kThreads];
+__device__ __forceinline__ void read_column(Column& ids, const KvFork& f, const int32_t* table, int j)
 {
-    const int tid = threadIdx.x;
+    int32_t v[kBeamMax];
+    const bool there = j < f.max_blocks;
+#pragma unroll
+    for (int w = 0; w < kBeamMax; ++w)
+        if (w < f.beams) v[w] = there ? table[(int64_t)w * f.max_blocks + j] : -1;
+#pragma unroll
+    for (int w = 0; w < kBeamMax; ++w)
+        if (w < f.beams) ids[w][threadIdx.x] = v[w];
+}
+
+// By all threads of the workgroup; a row to a lane of its first wavefront.  `ids` holds the first kThreads columns, whose loads share a round trip with
+// the rows' own.
+__device__ __forceinline__ void read_family(Family& o, Column& ids, const KvFork& f, int r)
+{
+    const int lane = threadIdx.x;
     const int64_t row0 = (int64_t)r * f.beams;
-    if (tid < f.beams) {
-        const int p = f.parent[row0 + tid], len = length_of(f, row0 + tid), size = 1 << f.block_shift;
-        o.parent[tid] = p >= row0 && p < row0 + f.beams ? (int)(p - row0) : -1;
-        const int blocks = (len + size - 1) >> f.block_shift, tail = len & (size - 1);
-        o.blocks[tid] = blocks;
-        o.tail[tid] = tail;
-        const int id = tail ? f.table[(row0 + tid) * f.max_blocks + blocks - 1] : -1;
-        o.last[tid] = (uint32_t)id < (uint32_t)f.n_blocks ? id : -1;
-    }
+    const int32_t* const table = f.table + row0 * f.max_blocks;
+    const bool is = lane < f.beams;
+    const int given = is ? f.parent[row0 + lane] : -1, len = is ? length_of(f, row0 + lane) : 0, size = 1 << f.block_shift;
+    read_column(ids, f, table, threadIdx.x);
     __syncthreads();
-    if (tid == 0) {
-        uint32_t lives = 0;
-        int copies = 0, most = 0;
-        for (int i = 0; i < f.beams; ++i) {
-            const int p = o.parent[i];
-            o.place[i] = p >= 0 && (lives >> p & 1) && o.last[p] >= 0 ? copies++ : -1;
-            if (p >= 0) lives |= 1u << p;
+    if (lane < 64) {
+        const int p = given >= row0 && given < row0 + f.beams ? (int)(given - row0) : -1, blocks = (len + size - 1) >> f.block_shift;
+        int id = -1;
+        if (len & (size - 1)) id = blocks <= kThreads ? ids[lane][blocks - 1] : table[(int64_t)lane * f.max_blocks + blocks - 1];
+        const int last = (uint32_t)id < (uint32_t)f.n_blocks ? id : -1;
+        uint32_t lives = p >= 0 ? 1u << p : 0u;
+        bool first = true;
+        for (int s = 0; s < f.beams; ++s) {
+            const int other = __shfl(p, s, 64);
+            first &= s >= lane || other != p;
         }
-        for (int i = 0; i < f.beams; ++i)
-            if (!(lives >> i & 1)) most = max(most, o.blocks[i]);
-        o.lives = lives;
-        o.copies = copies;
-        o.most = most;
+        const int parents_last = __shfl(last, max(p, 0), 64);
+        for (int d = 1; d < kBeamMax; d <<= 1) lives |= (uint32_t)__shfl_xor((int)lives, d, 64);
+        const bool copied = is && p >= 0 && !first && parents_last >= 0;
+        const unsigned long long copies = __ballot(copied);
+        int longest = blocks, most = lives >> (lane & 31) & 1 ? 0 : blocks;
+        for (int d = 1; d < kBeamMax; d <<= 1) {
+            longest = max(longest, __shfl_xor(longest, d, 64));
+            most = max(most, __shfl_xor(most, d, 64));
+        }
+        if (is) {
+            o.parent[lane] = p;
+            o.blocks[lane] = blocks;
+            o.length[lane] = len;
+            o.last[lane] = last;
+            o.place[lane] = copied ? __popcll(copies & ((1ull << lane) - 1)) : -1;
+        }
+        if (lane == 0) {
+            o.lives = lives;
+            o.copies = __popcll(copies);
+            o.most = most;
+            o.longest = longest;
+        }
     }
     __syncthreads();
 }
-// the old rows whose block at place j is free: nobody continues the row, no row that is continued holds it, and none before it is dropped with it
-__device__ __forceinline__ uint32_t freed_at(const Family& o, const KvFork& f, const int32_t* table, int j)
+// The rows whose block at place j, this thread's column, is free: nobody continues the row, no row that is continued holds it, and none before it
+// is dropped with it.
+__device__ __forceinline__ uint32_t freed_in(const Column& ids, const Family& o, const KvFork& f, int j)
 {
-    uint32_t freed = 0;
-    for (int d = 0; d < f.beams; ++d) {
-        if ((o.lives >> d & 1) || j >= o.blocks[d]) continue;
-        const int id = table[(int64_t)d * f.max_blocks + j];
-        bool held = (uint32_t)id >= (uint32_t)f.n_blocks;
-        for (int s = 0; s < f.beams && !held; ++s)
-            if (j < o.blocks[s] && ((o.lives >> s & 1) || s < d)) held = table[(int64_t)s * f.max_blocks + j] == id;
-        freed |= held ? 0u : 1u << d;
+    uint32_t there = 0, freed = 0;
+    for (int s = 0; s < f.beams; ++s) there |= j < o.blocks[s] ? 1u << s : 0u;
+    for (uint32_t dropped = there & ~o.lives; dropped; dropped &= dropped - 1) {
+        const int d = __builtin_ctz(dropped), id = ids[d][threadIdx.x];
+        const uint32_t others = there & (o.lives | ((1u << d) - 1));
+        uint32_t same = 0;
+        for (int s = 0; s < f.beams; ++s) same |= ids[s][threadIdx.x] == id ? 1u << s : 0u;
+        freed |= (uint32_t)id < (uint32_t)f.n_blocks && !(same & others) ? 1u << d : 0u;
     }
     return freed;
+}
+
+// what a request copies and frees; by all threads of the workgroup
+__device__ __forceinline__ Counts count_request(Column& ids, const Family& o, const KvFork& f, const int32_t* table, int* part)
+{
+    const int tid = threadIdx.x;
+    int freed = 0;
+    for (int j = tid; j < o.most; j += kThreads) {
+        if (j >= kThreads) read_column(ids, f, table, j);
+        freed += __popc(freed_in(ids, o, f, j));
+    }
+    for (int d = 32; d > 0; d >>= 1) freed += __shfl_xor(freed, d, 64);
+    if ((tid & 63) == 0) part[tid >> 6] = freed;
+    __syncthreads();
+    freed = 0;
+    for (int w = 0; w < kWaves; ++w) freed += part[w];
+    return {o.copies, freed};
 }
 
 __global__ __launch_bounds__(kThreads) void kv_fork_count_kernel(KvFork f, Counts* counts)
 {
     __shared__ Family o;
+    __shared__ Column ids;
     __shared__ int part[kWaves];
-    const int tid = threadIdx.x, r = blockIdx.x;
-    read_family(o, f, r);
-    const int32_t* const table = f.table + (int64_t)r * f.beams * f.max_blocks;
-    int freed = 0;
-    for (int j = tid; j < o.most; j += kThreads) freed += __popc(freed_at(o, f, table, j));
-    for (int d = 32; d > 0; d >>= 1) freed += __shfl_xor(freed, d, 64);
-    if ((tid & 63) == 0) part[tid >> 6] = freed;
-    __syncthreads();
-    if (tid == 0) {
-        freed = 0;
-        for (int w = 0; w < kWaves; ++w) freed += part[w];
-        counts[r] = {o.copies, freed};
-    }
+    read_family(o, ids, f, blockIdx.x);
+    const Counts c = count_request(ids, o, f, f.table + (int64_t)blockIdx.x * f.beams * f.max_blocks, part);
+    if (threadIdx.x == 0) counts[blockIdx.x] = c;
 }
 
 __device__ __forceinline__ int ring_at(uint32_t head, long long i, int n) { return (int)((head + (unsigned long long)i) % (uint32_t)n); }
+__device__ __forceinline__ int taken_by(const Counts& c) { return max(0, c.copies - c.freed); }
+__device__ __forceinline__ int given_by(const Counts& c) { return max(0, c.freed - c.copies); }
 
-// the sum over the workgroup of two values per thread
-__device__ __forceinline__ void sum2(long long (&v)[2], long long (*part)[2])
+// the sums over the workgroup of three values per thread
+__device__ __forceinline__ void sum3(long long (&v)[3], long long (*part)[3])
 {
     for (int d = 32; d > 0; d >>= 1)
-        for (int e = 0; e < 2; ++e) v[e] += __shfl_xor(v[e], d, 64);
+        for (int e = 0; e < 3; ++e) v[e] += __shfl_xor(v[e], d, 64);
     __syncthreads();
     if ((threadIdx.x & 63) == 0)
-        for (int e = 0; e < 2; ++e) part[threadIdx.x >> 6][e] = v[e];
+        for (int e = 0; e < 3; ++e) part[threadIdx.x >> 6][e] = v[e];
     __syncthreads();
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < 3; ++e) {
         v[e] = 0;
         for (int w = 0; w < kWaves; ++w) v[e] += part[w][e];
     }
 }
 
-// A workgroup per request, and one more for the state.
+// The first request that needs more than `count` ids with those before it; by all threads of the workgroup.
+__device__ __forceinline__ int first_closed(const Counts* counts, int n, long long count, long long (*part)[3])
+{
+    __shared__ int closed;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    if (tid == 0) closed = n;
+    long long carry = 0;
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+        long long sum = i0 + tid < n ? taken_by(counts[i0 + tid]) : 0;
+        for (int d = 1; d < 64; d <<= 1) {
+            const long long u = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += u;
+        }
+        __syncthreads();
+        if (lane == 63) part[wid][0] = sum;
+        __syncthreads();
+        sum += carry;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wid) sum += part[w][0];
+            carry += part[w][0];
+        }
+        if (i0 + tid < n && sum > count) atomicMin(&closed, i0 + tid);
+    }
+    __syncthreads();
+    return closed;
+}
+
+// A workgroup per request, and one more for the state; with one request its counts are taken here (counts: null), and there is one workgroup.
 __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Counts* counts)
 {
     __shared__ Family o;
-    __shared__ long long part[kWaves][2];
+    __shared__ Column ids;
+    __shared__ long long part[kWaves][3];
     __shared__ int own[kBeamMax], wave_sum[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, r = blockIdx.x;
     const long long count = max(0, min(f.ring_state[1], f.n_blocks));
     const uint32_t head = (uint32_t)f.ring_state[0] % (uint32_t)f.n_blocks;
     if (r == f.n_requests) {
-        // the requests in order, until one needs more than is left
+        const int closed = first_closed(counts, f.n_requests, count, part);
+        long long sums[3] = {0, 0, 0};        // taken, given, copies
+        for (int i = tid; i < closed; i += kThreads) {
+            const Counts c = counts[i];
+            sums[0] += taken_by(c), sums[1] += given_by(c), sums[2] += c.copies;
+        }
+        sum3(sums, part);
         if (tid == 0) {
-            long long taken = 0, given = 0, copies = 0;
-            int i = 0;
-            for (; i < f.n_requests; ++i) {
-                const Counts c = counts[i];
-                if (taken + max(0, c.copies - c.freed) > count) break;
-                taken += max(0, c.copies - c.freed);
-                given += max(0, c.freed - c.copies);
-                copies += c.copies;
-            }
-            f.next_state[0] = ring_at(head, taken, f.n_blocks);
-            f.next_state[1] = (int32_t)(count - taken + given);
-            f.next_state[2] = i;
-            f.next_state[3] = (int32_t)copies;
+            f.next_state[0] = ring_at(head, sums[0], f.n_blocks);
+            f.next_state[1] = (int32_t)(count - sums[0] + sums[1]);
+            f.next_state[2] = closed;
+            f.next_state[3] = (int32_t)sums[2];
         }
         return;
     }
-    read_family(o, f, r);
-    const Counts mine = counts[r];
-    long long before[2] = {0, 0};             // taken from the ring, and given to it, by the requests before this one
-    for (int i = tid; i < r; i += kThreads) {
-        const Counts c = counts[i];
-        before[0] += max(0, c.copies - c.freed);
-        before[1] += max(0, c.freed - c.copies);
+    long long before[3] = {0, 0, 0};          // taken from the ring, and given to it, by the requests before this one
+    Counts mine{0, 0};
+    if (counts) {
+        mine = counts[r];
+        for (int i = tid; i < r; i += kThreads) {
+            const Counts c = counts[i];
+            before[0] += taken_by(c), before[1] += given_by(c);
+        }
     }
-    sum2(before, part);
-    const bool open = before[0] + max(0, mine.copies - mine.freed) <= count;
+    read_family(o, ids, f, r);
     const int64_t row0 = (int64_t)r * f.beams;
     const int32_t* const table = f.table + row0 * f.max_blocks;
-    if (open) {                               // blocks that are free, in order
-        int carry = 0;
-        for (int j0 = 0; j0 < o.most; j0 += kThreads) {
-            uint32_t freed = j0 + tid < o.most ? freed_at(o, f, table, j0 + tid) : 0u;
+    if (counts) sum3(before, part);
+    else mine = count_request(ids, o, f, table, wave_sum);
+    const bool open = before[0] + taken_by(mine) <= count;
+    if (!counts && tid == 0) {
+        f.next_state[0] = ring_at(head, open ? taken_by(mine) : 0, f.n_blocks);
+        f.next_state[1] = (int32_t)(count + (open ? given_by(mine) - taken_by(mine) : 0));
+        f.next_state[2] = open;
+        f.next_state[3] = open ? mine.copies : 0;
+    }
+    // a column to a thread: what is free of it, in order, and what the new rows take over
+    int carry = 0;
+    for (int j0 = 0; j0 < o.longest; j0 += kThreads) {
+        const int j = j0 + tid;
+        if (j0 > 0 || (!counts && o.most > kThreads)) read_column(ids, f, table, j);       // the first are there, but where later ones were counted
+        if (open && j0 < o.most) {
+            uint32_t freed = freed_in(ids, o, f, j);
             int sum = __popc(freed);
             const int v = sum;
             for (int d = 1; d < 64; d <<= 1) {
@@ -167,41 +245,61 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
                 carry += wave_sum[w];
             }
             for (; freed; freed &= freed - 1, ++at) {
-                const int id = table[(int64_t)__builtin_ctz(freed) * f.max_blocks + j0 + tid];
+                const int id = ids[__builtin_ctz(freed)][tid];
                 if (at < mine.copies) own[at] = id;
                 else f.ring[ring_at(head, count + before[1] + (at - mine.copies), f.n_blocks)] = id;
             }
         }
+        for (int i = 0; i < f.beams; ++i) {
+            const int p = open ? o.parent[i] : i;
+            if (p >= 0 && j < o.blocks[p] && !(open && o.place[i] >= 0 && j == o.blocks[p] - 1)) f.next_table[(row0 + i) * f.max_blocks + j] = ids[p][tid];
+        }
     }
     __syncthreads();
-    for (int i = 0; i < f.beams; ++i) {
-        const int p = open ? o.parent[i] : i, place = open ? o.place[i] : -1;
-        const int blocks = p >= 0 ? o.blocks[p] : 0;
-        int id = -1;                          // of the row's own last block
-        if (place >= 0) id = place < mine.freed ? own[place] : f.ring[ring_at(head, before[0] + (place - mine.freed), f.n_blocks)];
-        for (int j = tid; j < blocks; j += kThreads) f.next_table[(row0 + i) * f.max_blocks + j] = place >= 0 && j == blocks - 1 ? id : table[(int64_t)p * f.max_blocks + j];
-        if (tid == 0) {
-            f.next_len[row0 + i] = p >= 0 ? length_of(f, row0 + p) : 0;
-            f.copy[2 * (row0 + i)] = place >= 0 ? o.last[p] : -1;
-            f.copy[2 * (row0 + i) + 1] = place >= 0 ? id : -1;
+    if (tid < f.beams) {
+        const int p = open ? o.parent[tid] : tid, place = open ? o.place[tid] : -1;
+        int id = -1;                          // the row's own last block
+        if (place >= 0) {
+            id = place < mine.freed ? own[place] : f.ring[ring_at(head, before[0] + (place - mine.freed), f.n_blocks)];
+            f.next_table[(row0 + tid) * f.max_blocks + o.blocks[p] - 1] = id;
         }
+        f.next_len[row0 + tid] = p >= 0 ? o.length[p] : 0;
+        *(int2*)(f.copy + 2 * (row0 + tid)) = make_int2(place >= 0 ? o.last[p] : -1, place >= 0 ? id : -1);
     }
 }
 
-// A workgroup per row and layer.
+// A workgroup per row and layer; what bounds it is memory, so a thread has several pieces on their way at once.
+constexpr int kPieces = 4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __global__ __launch_bounds__(kThreads) void kv_copy_kernel(KvCaches caches, const int32_t* __restrict__ copy, const int32_t* __restrict__ seq_len)
 {
     const KvCache& c = caches.c[blockIdx.y];
-    const int i = blockIdx.x, from = copy[2 * i], to = copy[2 * i + 1];
-    if ((uint32_t)from >= (uint32_t)c.n_blocks || (uint32_t)to >= (uint32_t)c.n_blocks) return;
-    const int size = 1 << c.block_shift, tail = seq_len[i] & (size - 1), rows = tail ? tail : size;
-    const int per_head = c.head_dim >> 3, per_row = per_head * c.kv_heads;
-    for (int u = threadIdx.x; u < rows * per_row; u += kThreads) {
-        const int row = u / per_row, rest = u - row * per_row, head = rest / per_head, ch = (rest - head * per_head) * 8;
-        const int64_t at = row * c.token_stride + head * c.head_stride + ch;
-        const uint4 a = *(const uint4*)(c.k + from * c.block_stride + at), b = *(const uint4*)(c.v + from * c.block_stride + at);
-        *(uint4*)(c.k + to * c.block_stride + at) = a;
-        *(uint4*)(c.v + to * c.block_stride + at) = b;
+    const int i = blockIdx.x, length = seq_len[i], from_id = copy[2 * i], to_id = copy[2 * i + 1];
+    if ((uint32_t)from_id >= (uint32_t)c.n_blocks || (uint32_t)to_id >= (uint32_t)c.n_blocks) return;
+    const int size = 1 << c.block_shift, tail = length & (size - 1), rows = tail ? tail : size;
+    const int per_head = c.head_dim >> 3, per_row = per_head * c.kv_heads, n = rows * per_row;
+    const int64_t block = c.block_stride, token = c.token_stride, head_step = c.head_stride;
+    const uint16_t *const k_from = c.k + from_id * block, *const v_from = c.v + from_id * block;
+    uint16_t *const k_to = c.k + to_id * block, *const v_to = c.v + to_id * block;
+    auto place = [&](int u) {
+        const int row = u / per_row, rest = u - row * per_row, head = rest / per_head;
+        return row * token + head * head_step + (rest - head * per_head) * 8;
+    };
+    for (int u0 = threadIdx.x; u0 < n; u0 += kPieces * kThreads) {
+        u32x4 a[kPieces], b[kPieces];
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const int64_t at = place(min(u0 + p * kThreads, n - 1));
+            a[p] = *(const u32x4*)(k_from + at);
+            b[p] = *(const u32x4*)(v_from + at);
+        }
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            if (u0 + p * kThreads >= n) break;
+            const int64_t at = place(u0 + p * kThreads);
+            *(u32x4*)(k_to + at) = a[p];
+            *(u32x4*)(v_to + at) = b[p];
+        }
     }
 }
 
@@ -211,6 +309,10 @@ int64_t kv_fork_workspace(int32_t n_requests, int32_t) { return (int64_t)n_reque
 
 hipError_t kv_fork(const KvFork& f, void* workspace, hipStream_t stream)
 {
+    if (f.n_requests == 1) {
+        hipLaunchKernelGGL(kv_fork_kernel, dim3(1), dim3(kThreads), 0, stream, f, (const Counts*)nullptr);
+        return hipGetLastError();
+    }
     if (f.n_requests > 0) {
         hipLaunchKernelGGL(kv_fork_count_kernel, dim3((unsigned)f.n_requests), dim3(kThreads), 0, stream, f, (Counts*)workspace);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;

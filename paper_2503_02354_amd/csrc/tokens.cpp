@@ -303,6 +303,7 @@ int coe_kv_fork(int32_t n_requests, int32_t beams, int32_t block_size, int32_t n
     if ((long long)max_blocks * beams > 0x3FFFFFFFll) return fail(COE_EINVAL, "%s: max_blocks * beams must be below 2^30", call);
     if (!ring || !ring_state || !next_state || (n_requests > 0 && (!parent || !seq_len || !table || !next_table || !next_len || !copy)))
         return fail(COE_EINVAL, "%s: null argument", call);
+    if ((uintptr_t)copy & 7) return fail(COE_EINVAL, "%s: copy must be 8-byte aligned", call);
     if (next_state == ring_state || (n_requests > 0 && (next_table == table || next_len == seq_len || next_len == parent))) return fail(COE_EINVAL, "%s: outputs must not alias inputs", call);
     const int64_t need = coe::k::kv_fork_workspace(n_requests, beams);
     if (workspace_bytes < need) return fail(COE_ERANGE, "%s: workspace of %lld bytes, %lld needed", call, (long long)workspace_bytes, (long long)need);

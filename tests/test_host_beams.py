@@ -115,7 +115,7 @@ def test_fork_refuses(B):
     bad("max_blocks", width=0), bad("max_blocks", width=2 ** 28), bad("max_blocks * beams", block=8, width=2 ** 27, beams=32)
     for name in ("parent", "len", "table", "ring", "state", "next_table", "next_len", "copy", "next"):
         bad("null", **{name: 0})
-    bad("alias", next_table=P), bad("alias", next_len=P), bad("alias", next=P)
+    bad("alias", next_table=P), bad("alias", next_len=P), bad("alias", next=P), bad("aligned", copy=P + 4)
     need = B.coe_kv_fork_workspace(2, 4)
     assert need >= 0
     if need:
