@@ -23,7 +23,9 @@ namespace {
 constexpr int kKeys = 32;                 // keys of a tile of the kernels for few rows
 constexpr int kFewRows = 32;              // query rows of a source and head that they take at a time
 constexpr int kFewWaves = 4;
-constexpr int kFewGroups = 512;           // workgroups: two per compute unit
+// workgroups: two, three or four per compute unit, as many as registers allow
+template <int D> constexpr int kFewGroups = D <= 32 ? 1024 : D <= 64 ? 768 : 512;
+constexpr int kMostFewGroups = 1024;
 
 // A source's queries and rows, within the arrays.
 struct Source {
@@ -265,7 +267,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cross_attention_few_kernel(
         for (int s = tid; s <= n; s += 64 * kFewWaves) h->base[s] = base[s];
         if (tid == 0) h->per = per;
     }
-    unsigned long long now = blockIdx.x * per;
+    const unsigned index = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+    unsigned long long now = index * per;
     const unsigned long long stop = min(total, now + per);
     if (now >= stop) return;
     int s = 0;
@@ -290,7 +293,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cross_attention_few_kernel(
         const int kvh = (int)(into / (unsigned)tiles), t_begin = (int)(into - (unsigned long long)kvh * (unsigned)tiles);
         const int t_end = (int)min((unsigned long long)tiles, t_begin + (stop - now));
         const bool whole = t_begin == 0 && t_end == tiles;
-        float* const part = (float*)(workspace + few_header_bytes(n)) + ((size_t)blockIdx.x * 2 + (now != start)) * kPartFloats<D>;
+        float* const part = (float*)(workspace + few_header_bytes(n)) + ((size_t)index * 2 + (now != start)) * kPartFloats<D>;
         few_rows<D, PAD, kFewWaves>(st, a, o, kvh, 0, o.m * group, t_begin, t_end, lds, stat, [&](int rw, int ch, float mx, float sum, float4 acc) __attribute__((always_inline)) {
             if (whole) finish_row(st, a, o.q0, kvh, rw, ch, mx, sum, acc);
             else {
@@ -308,15 +311,34 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cross_attention_few_kernel(
 #endif
 }
 
-// Where sources are short, or many: a workgroup per source, head and 32 query rows, one launch, and no parts to join.
-template <int D, bool PAD, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void cross_attention_whole_kernel(States st, CrossAttention a)
+// Where sources are short, or many: a workgroup per source, head and 32 query rows, one launch, and no parts to join.  All heads of a source go to one
+// of the chip's eight dies, to which workgroups are dealt in turn: their rows' bytes lie side by side.  ORDERED: the longest sources first (every
+// workgroup ranks them all, at most kRanked), so that those which start last are short, and that every die gets its share.
+constexpr int kRanked = 256;
+template <int D, bool PAD, int WAVES, bool ORDERED>
+__global__ __launch_bounds__(64 * WAVES, 2) void cross_attention_whole_kernel(States st, CrossAttention a, int dies)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     extern __shared__ __attribute__((aligned(4096))) char lds[];
     __shared__ float stat[2][WAVES][kFewRows];
-    const int s = blockIdx.x / st.kv_heads, kvh = blockIdx.x - s * st.kv_heads, row0 = (int)blockIdx.y * kFewRows, group = a.heads / st.kv_heads;
-    const Source o = source_of(st, a, s);
+    const int turn = blockIdx.x / dies, s = turn / st.kv_heads * dies + blockIdx.x % dies, kvh = turn % st.kv_heads, row0 = (int)blockIdx.y * kFewRows, group = a.heads / st.kv_heads;
+    if (s >= a.n_sources) return;
+    Source o;
+    if (ORDERED) {
+        int4* const sources = (int4*)lds;     // [n_sources], and the one that this workgroup takes
+        const int tid = threadIdx.x, n = a.n_sources;
+        if (tid < n) o = source_of(st, a, tid);
+        if (tid < n) sources[tid] = make_int4(o.q0, o.m, o.first, o.keys);
+        __syncthreads();
+        int before = 0;
+        if (tid < n)
+            for (int i = 0; i < n; ++i) before += sources[i].w > o.keys || (sources[i].w == o.keys && i < tid);
+        if (tid < n && before == s) sources[n] = make_int4(o.q0, o.m, o.first, o.keys);
+        __syncthreads();
+        const int4 v = sources[n];
+        o = {__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), __builtin_amdgcn_readfirstlane(v.w)};
+        __syncthreads();
+    } else o = source_of(st, a, s);
     const int all = o.m * group;
     if (row0 >= all) return;
     few_rows<D, PAD, WAVES>(st, a, o, kvh, row0, min(kFewRows, all - row0), 0, o.tiles(), lds, stat,
@@ -858,20 +880,31 @@ struct Sizes {                            // what the choice of a kernel goes by
     int64_t groups() const { return n_sources * kv_heads * row_blocks(); }
 };
 bool is_few(const Sizes& z) { return z.rows() <= kFewRows; }
+// Whether a workgroup of its own for every source and head is faster than equal stretches and a join, by the longest source and the number of
+// workgroups.  Single tokens of four beams in a graph, whole / stretches, us, sources of equal lengths, then of lengths from one up: 16 heads of 64, 1 source
+// 1000 rows 11.4 / 13.6, 2000 18.2 / 15.8; 4 sources 2000 19.4 / 20.1 and 19.2 / 16.7; 8 sources 2000 19.8 / 23.7 and 19.4 / 20.4, 4000 37.5 / 35.1 and
+// 32.8 / 23.9; 16 sources 2000 27.4 / 35.5 and 20.6 / 25.0, 4000 64.7 / 69.1 and 44.9 / 40.6; 32 sources 2000 64.0 / 70.8 and 39.2 / 55.8, 4000 125 / 120 and
+// 100 / 81; 64 sources 2000 118 / 120 and 72 / 83.  8 heads of 128: 8 sources 500 rows 13.6 / 15.5, 1000 21.0 / 16.4; 16 sources 1000 21.4 / 21.2 and 20.0 /
+// 27.8, 2000 37.1 / 32.6; 32 sources 1000 26.8 / 31.8 and 21.8 / 38.1, 4000 116 / 118 and 102 / 70; 64 sources 1000 60.4 / 62.6 and 37.0 / 56.2.
+// Chunks, a workgroup for 32 rows of each / units and a join: 1000 tokens on 1000 rows, 16 heads of 64, 20.0 / 25.0, 4 x 400 tokens on 1500 rows 49 / 36;
+// 30 x 20 to 40 tokens on 100 to 1000 rows, 12 heads of 64, 21.6 / 24.6.
 bool is_whole(const Sizes& z)
 {
     const int64_t longest = z.max_rows * z.dim;
-    if (z.row_blocks() == 1) return longest <= (z.groups() >= 128 ? 98304 : 40960);
+    if (z.row_blocks() == 1) return longest <= (z.groups() >= 256 ? 229376 : z.groups() >= 128 ? 163840 : 81920);
     return z.groups() <= 2048 && longest <= 131072 && z.groups() * longest <= 52ll << 20;
 }
 
-template <int D, bool PAD, int WAVES> hipError_t launch_whole(const Sizes& z, const States& st, const CrossAttention& a, hipStream_t stream)
+template <int D, bool PAD, int WAVES, bool ORDERED> hipError_t launch_whole(const Sizes& z, const States& st, const CrossAttention& a, hipStream_t stream)
 {
     constexpr size_t kLds = kFewLds<D, WAVES>;
+    static_assert(!ORDERED || (kLds >= (kRanked + 1) * sizeof(int4) && 64 * WAVES >= kRanked), "a source to a thread");
     static const hipError_t configured =
-        hipFuncSetAttribute((const void*)cross_attention_whole_kernel<D, PAD, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+        hipFuncSetAttribute((const void*)cross_attention_whole_kernel<D, PAD, WAVES, ORDERED>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
     if (configured != hipSuccess) return configured;
-    hipLaunchKernelGGL((cross_attention_whole_kernel<D, PAD, WAVES>), dim3((unsigned)(a.n_sources * st.kv_heads), (unsigned)z.row_blocks()), dim3(64 * WAVES), kLds, stream, st, a);
+    const int dies = a.n_sources >= 32 || a.n_sources % 8 == 0 ? 8 : 1;       // where each has about as many
+    hipLaunchKernelGGL((cross_attention_whole_kernel<D, PAD, WAVES, ORDERED>), dim3((unsigned)((a.n_sources + dies - 1) / dies * dies * st.kv_heads), (unsigned)z.row_blocks()),
+                       dim3(64 * WAVES), kLds, stream, st, a, dies);
     return hipGetLastError();
 }
 
@@ -880,7 +913,7 @@ template <int D, bool PAD> hipError_t launch_few(const Sizes& z, const States& s
     const size_t lds = std::max(kFewLds<D>, ((size_t)a.n_sources + 1) * 8);
     static const hipError_t configured = hipFuncSetAttribute((const void*)cross_attention_few_kernel<D, PAD>, hipFuncAttributeMaxDynamicSharedMemorySize, 144 * 1024);
     if (configured != hipSuccess) return configured;
-    hipLaunchKernelGGL((cross_attention_few_kernel<D, PAD>), dim3(kFewGroups), dim3(64 * kFewWaves), lds, stream, st, a, workspace);
+    hipLaunchKernelGGL((cross_attention_few_kernel<D, PAD>), dim3(kFewGroups<D>), dim3(64 * kFewWaves), lds, stream, st, a, workspace);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(cross_attention_join_kernel<D>, dim3((unsigned)(a.n_sources * st.kv_heads), (unsigned)z.rows()), dim3(256), 0, stream, st, a, workspace);
     return hipGetLastError();
@@ -909,8 +942,11 @@ template <int D> hipError_t launch(const Sizes& z, const States& st, const Cross
 {
     const bool exact = st.head_dim == D;
     if (is_whole(z)) {                        // eight wavefronts while there is a compute unit for every workgroup
-        if (z.groups() <= kFewGroups / 2) return exact ? launch_whole<D, false, 8>(z, st, a, stream) : launch_whole<D, true, 8>(z, st, a, stream);
-        return exact ? launch_whole<D, false, kFewWaves>(z, st, a, stream) : launch_whole<D, true, kFewWaves>(z, st, a, stream);
+        if (z.groups() <= 256) return exact ? launch_whole<D, false, 8, false>(z, st, a, stream) : launch_whole<D, true, 8, false>(z, st, a, stream);
+        // ranked while the last workgroups matter: 64 sources of 60 to 1500 rows, 16 heads of 64, 63 -> 56 us; 150 of 500 to 1000 98 -> 104
+        if (z.n_sources <= kRanked && z.groups() > 512 && z.groups() <= 2048)
+            return exact ? launch_whole<D, false, kFewWaves, true>(z, st, a, stream) : launch_whole<D, true, kFewWaves, true>(z, st, a, stream);
+        return exact ? launch_whole<D, false, kFewWaves, false>(z, st, a, stream) : launch_whole<D, true, kFewWaves, false>(z, st, a, stream);
     }
     if (!is_few(z)) return launch_many<D>(st, a, workspace, stream);
     return exact ? launch_few<D, false>(z, st, a, workspace, stream) : launch_few<D, true>(z, st, a, workspace, stream);
@@ -923,7 +959,7 @@ int64_t cross_attention_workspace(int32_t n_sources, int32_t n_tokens, int32_t m
     const int dim = padded_dim(head_dim);
     const Sizes z{n_sources, max_new, max_rows, heads, kv_heads, dim};
     if (is_whole(z)) return 0;
-    if (is_few(z)) return few_header_bytes(n_sources) + (int64_t)kFewGroups * 2 * (2 * kFewRows + kFewRows * dim) * 4;
+    if (is_few(z)) return few_header_bytes(n_sources) + (int64_t)kMostFewGroups * 2 * (2 * kFewRows + kFewRows * dim) * 4;
     return many_layout(n_sources, n_tokens, heads, kv_heads, dim).end;
 }
 
