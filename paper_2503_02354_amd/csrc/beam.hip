@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -263,42 +264,32 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
     long long at = begin + (long long)wid * kPieces * 64;
 #pragma unroll
     for (int d = 0; d < kDepth; ++d) fetch(next[d], at + d * kStride);
-    {                                         // the first step: the lanes' maxima stand for it
-        float x[kPerLane], most = -INFINITY;
-        if (at < end) {
-            unpack(x, next[0], at);
-            fetch(next[0], at + kDepth * kStride);
-            most = most_of(x);
-            weigh(x, most);
-        }
-        const uint32_t key[1] = {most > -INFINITY ? key_of(most) : 0u};
-        const uint32_t least = wave_min(key[0]), high = wave_max(key[0]), mine = least ? reached(key, share, share / 2, least, high) : 0u;
-        if (lane == 0) quarter[wid] = mine;
-        __syncthreads();
-        const uint32_t q = all_reach();
-        if (q) threshold = below(q);
-        else if (least) threshold = below(reached(key, picks, picks, least, high));
-        if (at < end) put(x, at);
-    }
-    int step = 1;
+    int step = 0;
     auto go = [&](Piece (&from)[kPieces]) __attribute__((always_inline)) {
-        const uint32_t q = all_reach();
         float x[kPerLane];
         unpack(x, from, at);
         fetch(from, at + kDepth * kStride);
         const float most = most_of(x);
-        weigh(x, most);
+        if (step == 0) {                      // the lanes' maxima stand for the first step
+            const uint32_t key[1] = {most > -INFINITY ? key_of(most) : 0u};
+            const uint32_t least = wave_min(key[0]), high = wave_max(key[0]), mine = least ? reached(key, share, share / 2, least, high) : 0u;
+            if (lane == 0) quarter[wid] = mine;
+            weigh(x, most);
+            __syncthreads();
+            if (all_reach() == 0 && least) threshold = below(reached(key, picks, picks, least, high));
+        } else weigh(x, most);
+        const uint32_t q = all_reach();
         if (q) threshold = fmaxf(threshold, below(q));
         if (__any(most > threshold)) put(x, at);
-        if ((step & (step + 1)) == 0 && n >= share) tell();
+        if (step > 0 && (step & (step + 1)) == 0 && n >= share) tell();
         at += kStride;
         ++step;
     };
-    at += kStride;
+    if (at >= end) __syncthreads();
 #pragma nounroll
     while (at < end) {
-        go(next[kDepth - 1]);
-        if (kDepth > 1 && at < end) go(next[0]);
+        go(next[0]);
+        if (kDepth > 1 && at < end) go(next[kDepth - 1]);
     }
     if (step > 2 && n >= share) tell();
     // the lanes' sums
@@ -387,7 +378,8 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
 // ---- requests -----------------------------------------------------------------------------------------------------
 // A workgroup per request: the rows' sums, then the best of all lists.  From a score on that enough of the threads' best reach, candidates are listed and
 // counted against each other; where that is too many (an order that no list of a row has by chance), they are found one after the other.
-constexpr int kMeet = 1024, kHeld = 4;        // candidates that are listed; keys that a thread holds, more are read again
+// (A launch of few workgroups is bound by latency, that of its instructions' first use among it: its loops are left as they are.)
+constexpr int kMeet = 512, kHeld = 1024;      // candidates that are listed; keys that are kept in LDS, more are read again
 struct Candidate {
     unsigned long long score;                 // fp64 as an integer that grows with it; 0: none
     unsigned long long key;                   // of the row
@@ -404,15 +396,15 @@ __device__ __forceinline__ bool before(const Candidate& a, const Candidate& b)
     if (a.score != b.score) return a.score > b.score;     // equal ones are rare
     return a.row != b.row ? a.row < b.row : a.key > b.key;
 }
-__device__ __forceinline__ void write_pick(const BeamSelection& s, int r, int place, const Candidate& c)
+// done: the row has ended
+__device__ __forceinline__ void write_pick(const BeamSelection& s, int r, int place, const Candidate& c, bool done)
 {
     const int64_t at = (int64_t)r * s.picks + place, row = (int64_t)r * s.beams + c.row;
-    const bool done = c.score && s.ended && s.ended[row];
     const int token = c.score == 0 ? -1 : done ? s.end_token : (int)~(uint32_t)c.key;
     s.next_score[at] = c.score ? (float)score_of(c.score) : -INFINITY;
     s.next_row[at] = c.score ? (int)row : -1;
     s.next_token[at] = token;
-    if (s.next_ended) s.next_ended[at] = c.score && (done || token == s.end_token);
+    if (s.next_ended) s.next_ended[at] = c.score != 0 && (done || token == s.end_token);
 }
 
 __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, int parts, const RowPart* __restrict__ stats, const unsigned long long* __restrict__ lists)
@@ -422,41 +414,51 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
     __shared__ double row_log[kBeamMax], row_score[kBeamMax];
     __shared__ int row_state[kBeamMax];       // 0: not there, 1: candidates, 2: ended
     __shared__ __attribute__((aligned(16))) uint32_t best[kThreads];
-    __shared__ Candidate met[kMeet];
+    __shared__ unsigned long long held[kHeld], scores[kHeld];
+    __shared__ unsigned long long met_score[kMeet], met_key[kMeet];
+    __shared__ int met_row[kMeet];
+    __shared__ Candidate found[kThreads];
     __shared__ int n_met;
-    const int tid = threadIdx.x, lane = tid & 63, r = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
     const size_t first = (size_t)r * s.beams;
     const int per_row = parts * s.picks, n = s.beams * per_row;
     const unsigned long long* const keys = lists + first * per_row;
-    unsigned long long held[kHeld];
-#pragma unroll
-    for (int c = 0; c < kHeld; ++c) held[c] = tid + c * kThreads < n ? keys[tid + c * kThreads] : 0;
     {
         const int b = tid / kLanes, sub = tid % kLanes;
-        float top = -INFINITY;
-        double sum = 0;
-        int state = 0;
-        float so_far = 0.f;
-        if (b < s.beams) {
-            RowPart v = stats[(first + b) * parts + min(sub, parts - 1)];     // of any bits where the row has none; on its way with the row's state
+        RowPart v{0, -INFINITY, 0};
+        float so_far = -INFINITY;
+        int ended = 0;
+        if (b < s.beams) {                    // a row's parts are of any bits where it has none; all on their way together
+            v = stats[(first + b) * parts + min(sub, parts - 1)];
             so_far = s.score[first + b];
-            state = !(so_far > -INFINITY) ? 0 : s.ended && s.ended[first + b] ? 2 : 1;
-            if (state == 1)
-                for (int p = sub; p < parts; p += kLanes) {
-                    if (p != sub) v = stats[(first + b) * parts + p];
-                    const float t = fmaxf(top, v.top);
-                    sum = (top == t ? sum : sum * exp((double)top - (double)t)) + (v.top == t ? v.sum : v.sum * exp((double)v.top - (double)t));
-                    top = t;
-                }
+            if (s.ended) ended = s.ended[first + b];
         }
-        float all = top;
+        {
+            unsigned long long k[kHeld / kThreads];
 #pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) all = fmaxf(all, __shfl_xor(all, d, 64));
-        sum = top == all ? sum : sum * exp((double)top - (double)all);
+            for (int c = 0; c < kHeld / kThreads; ++c) k[c] = keys[min(tid + c * kThreads, n - 1)];
+#pragma unroll
+            for (int c = 0; c < kHeld / kThreads; ++c) held[tid + c * kThreads] = k[c];
+        }
+        const int state = !(so_far > -INFINITY) ? 0 : ended ? 2 : 1, mine = state == 1 && sub < parts;
+        float top = mine ? v.top : -INFINITY;
+        double sum = 0;
+        const int rounds = state == 1 ? (parts + kLanes - 1) / kLanes : 0;
+#pragma nounroll
+        for (int p = 1; p < rounds; ++p)
+            if (p * kLanes + sub < parts) top = fmaxf(top, stats[(first + b) * parts + p * kLanes + sub].top);
+#pragma unroll
+        for (int d = 1; d < kLanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+#pragma nounroll
+        for (int p = 0; p < rounds; ++p) {
+            if (p * kLanes + sub >= parts) break;
+            if (p > 0) v = stats[(first + b) * parts + p * kLanes + sub];
+            sum += v.top == top ? v.sum : v.sum * exp((double)v.top - (double)top);
+        }
 #pragma unroll
         for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d, 64);
         if (sub == 0 && b < s.beams) {
-            row_top[b] = all;
+            row_top[b] = top;
             row_log[b] = log(sum);
             row_score[b] = so_far;
             row_state[b] = state;
@@ -464,23 +466,29 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
     }
     if (tid == 0) n_met = 0;
     __syncthreads();
-    auto candidate = [&](int i, unsigned long long key) {
-        Candidate c{0, key, i / per_row};
-        const float x = logit_of((uint32_t)(key >> 32)), top = row_top[c.row];
-        if (row_state[c.row] == 1 && key != 0 && (x == top || top < INFINITY))
-            c.score = order_of(row_score[c.row] + ((x == top ? 0. : (double)x - (double)top) - row_log[c.row]));
-        return c;
-    };
-    // every candidate of this thread's: its keys, then a row that has ended
-    auto each = [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-        for (int c = 0; c < kHeld; ++c)
-            if (tid + c * kThreads < n) f(candidate(tid + c * kThreads, held[c]));
-        for (int i = tid + kHeld * kThreads; i < n; i += kThreads) f(candidate(i, keys[i]));
-        if (tid < s.beams && row_state[tid] == 2) f(Candidate{order_of(row_score[tid]), 0, tid});
+    // f(candidate) for all of this thread's: rows by wavefronts, a row's keys by lanes, and the row itself where it has ended.  known: not the first time
+    auto each = [&](auto known, auto f) __attribute__((always_inline)) {
+#pragma nounroll
+        for (int b = wid; b < s.beams; b += kWaves) {
+            const int state = row_state[b];
+            const float top = row_top[b];
+            const double base = row_score[b], less = row_log[b];
+            if (state == 2 && lane == 0) f(Candidate{order_of(base), 0, b});
+            if (state != 1) continue;
+#pragma nounroll
+            for (int i = b * per_row + lane; i < (b + 1) * per_row; i += 64) {
+                const unsigned long long key = i < kHeld ? held[i] : keys[i];
+                const float x = logit_of((uint32_t)(key >> 32));
+                unsigned long long score = 0;
+                if (known && i < kHeld) score = scores[i];
+                else if (key != 0 && (x == top || top < INFINITY)) score = order_of(base + ((x == top ? 0. : (double)x - (double)top) - less));
+                if (!known && i < kHeld) scores[i] = score;
+                if (score) f(Candidate{score, key, b});
+            }
+        }
     };
     unsigned long long mine = 0;
-    each([&](const Candidate& c) { mine = max(mine, c.score); });
+    each(std::false_type(), [&](const Candidate& c) { mine = max(mine, c.score); });
     best[tid] = (uint32_t)(mine >> 32);
     __syncthreads();
     uint32_t low;
@@ -488,40 +496,48 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
         const uint4 four = *(const uint4*)(best + 4 * lane);
         const uint32_t key[4] = {four.x, four.y, four.z, four.w};
         const uint32_t most = max(max(key[0], key[1]), max(key[2], key[3]));
-        low = max(reached(key, s.picks, 16, wave_min(most), wave_max(most)), 1u);             // no score's upper half is 0
+        low = max(reached(key, s.picks, 24, wave_min(most), wave_max(most)), 1u);             // no score's upper half is 0
     }
-    each([&](const Candidate& c) {
+    each(std::true_type(), [&](const Candidate& c) {
         if ((uint32_t)(c.score >> 32) < low) return;
         const int at = atomicAdd(&n_met, 1);
-        if (at < kMeet) met[at] = c;
+        if (at < kMeet) met_score[at] = c.score, met_key[at] = c.key, met_row[at] = c.row;
     });
     __syncthreads();
     const int all = n_met;
     if (all <= kMeet) {
-        for (int i = tid; i < all; i += kThreads) {
-            const Candidate c = met[i];
-            int place = 0;
-            for (int j = 0; j < all; ++j) place += before(met[j], c);
-            if (place < s.picks) write_pick(s, r, place, c);
+        for (int i = tid; i < max(all, s.picks); i += kThreads) {
+            Candidate c{0, 0, 0};
+            int place = i;
+            if (i < all) {
+                c = {met_score[i], met_key[i], met_row[i]};
+                place = 0;
+#pragma unroll 4
+                for (int j = 0; j < all; ++j) {           // before(), without a branch
+                    const unsigned long long v = met_score[j], k = met_key[j];
+                    const int w = met_row[j];
+                    place += (v > c.score) | ((v == c.score) & ((w < c.row) | ((w == c.row) & (k > c.key))));
+                }
+            }
+            if (place < s.picks) write_pick(s, r, place, c, row_state[c.row] == 2);
         }
-        for (int i = all + tid; i < s.picks; i += kThreads) write_pick(s, r, i, Candidate{0, 0, 0});
         return;
     }
     Candidate last{~0ull, ~0ull, -1};
     for (int p = 0; p < s.picks; ++p) {
         Candidate c{0, 0, 0};
-        each([&](const Candidate& v) {
-            if (v.score != 0 && before(last, v) && before(v, c)) c = v;
+        each(std::true_type(), [&](const Candidate& v) {
+            if (before(last, v) && before(v, c)) c = v;
         });
         __syncthreads();
-        met[tid] = c;
+        found[tid] = c;
         __syncthreads();
         for (int d = kThreads / 2; d > 0; d >>= 1) {
-            if (tid < d && before(met[tid + d], met[tid])) met[tid] = met[tid + d];
+            if (tid < d && before(found[tid + d], found[tid])) found[tid] = found[tid + d];
             __syncthreads();
         }
-        last = met[0];
-        if (tid == 0) write_pick(s, r, p, last);
+        last = found[0];
+        if (tid == 0) write_pick(s, r, p, last, row_state[last.row] == 2);
     }
 }
 

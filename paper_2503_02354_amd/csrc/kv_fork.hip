@@ -19,6 +19,7 @@ struct Family {
     int blocks[kBeamMax], length[kBeamMax];   // of the old rows: blocks, tokens
     int last[kBeamMax];                       // the old rows' last block where it is not full and lies in the cache, else -1
     int place[kBeamMax];                      // row i's copy among the request's, or -1
+    int taken[kBeamMax];                      // blocks that row i takes over as they are
     uint32_t lives;                           // old rows that are continued
     int copies, most, longest;                // copies, most blocks of a row that is dropped, and of any row
 };
@@ -26,18 +27,44 @@ struct Counts { int32_t copies, freed; };     // of a request; the workspace hol
 
 __device__ __forceinline__ int length_of(const KvFork& f, int64_t row) { return max(0, min(f.seq_len[row], f.max_blocks << f.block_shift)); }
 
-// A thread's column of the old rows' tables: their blocks at one place, in LDS, all on their way together; of any value behind a row's blocks.
-typedef int32_t Column[kBeamMax][kThreads];
+// A barrier that LDS is ready behind; stores to memory need not have ended.
+__device__ __forceinline__ void lds_barrier()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+#endif
+}
+// inclusive sums over a wavefront's lanes, by register operations
+__device__ __forceinline__ int wave_sums(int v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // one lane up, two, four, eight in a row of 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // a row's last lane to the next row, the second row's to the last two
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+#endif
+    return v;
+}
+
+// A thread's column of the old rows' tables: their blocks at one place, in LDS, eight rows' on their way together; of any value behind a row's blocks.
+// (Small launches like these are bound by latency, that of their instructions' first use among it: loops are left as they are.)
+typedef int32_t Column[kBeamMax][kThreads];           // kBeamMax is a multiple of eight
 __device__ __forceinline__ void read_column(Column& ids, const KvFork& f, const int32_t* table, int j)
 {
-    int32_t v[kBeamMax];
     const bool there = j < f.max_blocks;
+    const int32_t* const from = table + (there ? j : 0);
+#pragma nounroll
+    for (int w0 = 0; w0 < f.beams; w0 += 8) {
+        int32_t v[8];
 #pragma unroll
-    for (int w = 0; w < kBeamMax; ++w)
-        if (w < f.beams) v[w] = there ? table[(int64_t)w * f.max_blocks + j] : -1;
+        for (int w = 0; w < 8; ++w) v[w] = from[(int64_t)min(w0 + w, f.beams - 1) * f.max_blocks];
 #pragma unroll
-    for (int w = 0; w < kBeamMax; ++w)
-        if (w < f.beams) ids[w][threadIdx.x] = v[w];
+        for (int w = 0; w < 8; ++w) ids[w0 + w][threadIdx.x] = v[w];
+    }
 }
 
 // By all threads of the workgroup; a row to a lane of its first wavefront.  `ids` holds the first kThreads columns, whose loads share a round trip with
@@ -56,22 +83,25 @@ __device__ __forceinline__ void read_family(Family& o, Column& ids, const KvFork
         int id = -1;
         if (len & (size - 1)) id = blocks <= kThreads ? ids[lane][blocks - 1] : table[(int64_t)lane * f.max_blocks + blocks - 1];
         const int last = (uint32_t)id < (uint32_t)f.n_blocks ? id : -1;
-        uint32_t lives = p >= 0 ? 1u << p : 0u;
+        uint32_t lives = 0;
+        int longest = 0, most = 0;
         bool first = true;
-        for (int s = 0; s < f.beams; ++s) {
-            const int other = __shfl(p, s, 64);
-            first &= s >= lane || other != p;
+#pragma nounroll
+        for (int w = 0; w < f.beams; ++w) {
+            const int other = __builtin_amdgcn_readlane(p, w);
+            first &= w >= lane || other != p;
+            lives |= other >= 0 ? 1u << other : 0u;
+            longest = max(longest, __builtin_amdgcn_readlane(blocks, w));
         }
+#pragma nounroll
+        for (int w = 0; w < f.beams; ++w)
+            if (!(lives >> w & 1)) most = max(most, __builtin_amdgcn_readlane(blocks, w));
         const int parents_last = __shfl(last, max(p, 0), 64);
-        for (int d = 1; d < kBeamMax; d <<= 1) lives |= (uint32_t)__shfl_xor((int)lives, d, 64);
         const bool copied = is && p >= 0 && !first && parents_last >= 0;
         const unsigned long long copies = __ballot(copied);
-        int longest = blocks, most = lives >> (lane & 31) & 1 ? 0 : blocks;
-        for (int d = 1; d < kBeamMax; d <<= 1) {
-            longest = max(longest, __shfl_xor(longest, d, 64));
-            most = max(most, __shfl_xor(most, d, 64));
-        }
+        const int parents_blocks = __shfl(blocks, max(p, 0), 64);
         if (is) {
+            o.taken[lane] = p < 0 ? 0 : parents_blocks - (copied ? 1 : 0);
             o.parent[lane] = p;
             o.blocks[lane] = blocks;
             o.length[lane] = len;
@@ -92,11 +122,14 @@ __device__ __forceinline__ void read_family(Family& o, Column& ids, const KvFork
 __device__ __forceinline__ uint32_t freed_in(const Column& ids, const Family& o, const KvFork& f, int j)
 {
     uint32_t there = 0, freed = 0;
+#pragma nounroll
     for (int s = 0; s < f.beams; ++s) there |= j < o.blocks[s] ? 1u << s : 0u;
+#pragma nounroll
     for (uint32_t dropped = there & ~o.lives; dropped; dropped &= dropped - 1) {
         const int d = __builtin_ctz(dropped), id = ids[d][threadIdx.x];
         const uint32_t others = there & (o.lives | ((1u << d) - 1));
         uint32_t same = 0;
+#pragma nounroll
         for (int s = 0; s < f.beams; ++s) same |= ids[s][threadIdx.x] == id ? 1u << s : 0u;
         freed |= (uint32_t)id < (uint32_t)f.n_blocks && !(same & others) ? 1u << d : 0u;
     }
@@ -108,12 +141,13 @@ __device__ __forceinline__ Counts count_request(Column& ids, const Family& o, co
 {
     const int tid = threadIdx.x;
     int freed = 0;
+#pragma nounroll
     for (int j = tid; j < o.most; j += kThreads) {
         if (j >= kThreads) read_column(ids, f, table, j);
         freed += __popc(freed_in(ids, o, f, j));
     }
-    for (int d = 32; d > 0; d >>= 1) freed += __shfl_xor(freed, d, 64);
-    if ((tid & 63) == 0) part[tid >> 6] = freed;
+    freed = wave_sums(freed);
+    if ((tid & 63) == 63) part[tid >> 6] = freed;
     __syncthreads();
     freed = 0;
     for (int w = 0; w < kWaves; ++w) freed += part[w];
@@ -130,13 +164,21 @@ __global__ __launch_bounds__(kThreads) void kv_fork_count_kernel(KvFork f, Count
     if (threadIdx.x == 0) counts[blockIdx.x] = c;
 }
 
-__device__ __forceinline__ int ring_at(uint32_t head, long long i, int n) { return (int)((head + (unsigned long long)i) % (uint32_t)n); }
+// place i behind head in a ring of n entries; i passes n only where the state is none of a ring
+__device__ __forceinline__ int ring_at(uint32_t head, long long i, uint32_t n)
+{
+    uint32_t at = (uint32_t)i;
+    if (at >= n) at %= n;
+    at += head;
+    return (int)(at >= n ? at - n : at);
+}
 __device__ __forceinline__ int taken_by(const Counts& c) { return max(0, c.copies - c.freed); }
 __device__ __forceinline__ int given_by(const Counts& c) { return max(0, c.freed - c.copies); }
 
 // the sums over the workgroup of three values per thread
 __device__ __forceinline__ void sum3(long long (&v)[3], long long (*part)[3])
 {
+#pragma nounroll
     for (int d = 32; d > 0; d >>= 1)
         for (int e = 0; e < 3; ++e) v[e] += __shfl_xor(v[e], d, 64);
     __syncthreads();
@@ -156,8 +198,10 @@ __device__ __forceinline__ int first_closed(const Counts* counts, int n, long lo
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     if (tid == 0) closed = n;
     long long carry = 0;
+#pragma nounroll
     for (int i0 = 0; i0 < n; i0 += kThreads) {
         long long sum = i0 + tid < n ? taken_by(counts[i0 + tid]) : 0;
+#pragma nounroll
         for (int d = 1; d < 64; d <<= 1) {
             const long long u = __shfl_up(sum, d, 64);
             if (lane >= d) sum += u;
@@ -189,6 +233,7 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
     if (r == f.n_requests) {
         const int closed = first_closed(counts, f.n_requests, count, part);
         long long sums[3] = {0, 0, 0};        // taken, given, copies
+#pragma nounroll
         for (int i = tid; i < closed; i += kThreads) {
             const Counts c = counts[i];
             sums[0] += taken_by(c), sums[1] += given_by(c), sums[2] += c.copies;
@@ -202,10 +247,11 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
         }
         return;
     }
-    long long before[3] = {0, 0, 0};          // taken from the ring, and given to it, by the requests before this one
     Counts mine{0, 0};
+    long long before[3] = {0, 0, 0};          // taken from the ring, and given to it, by the requests before this one
     if (counts) {
         mine = counts[r];
+#pragma nounroll
         for (int i = tid; i < r; i += kThreads) {
             const Counts c = counts[i];
             before[0] += taken_by(c), before[1] += given_by(c);
@@ -214,9 +260,11 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
     read_family(o, ids, f, r);
     const int64_t row0 = (int64_t)r * f.beams;
     const int32_t* const table = f.table + row0 * f.max_blocks;
-    if (counts) sum3(before, part);
-    else mine = count_request(ids, o, f, table, wave_sum);
+    if (!counts) mine = count_request(ids, o, f, table, wave_sum);
+    else if (r > 0) sum3(before, part);
     const bool open = before[0] + taken_by(mine) <= count;
+    // ids that this request takes from the ring, should it
+    const int ring_id = tid < taken_by(mine) && open ? f.ring[ring_at(head, before[0] + tid, f.n_blocks)] : -1;
     if (!counts && tid == 0) {
         f.next_state[0] = ring_at(head, open ? taken_by(mine) : 0, f.n_blocks);
         f.next_state[1] = (int32_t)(count + (open ? given_by(mine) - taken_by(mine) : 0));
@@ -225,44 +273,42 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
     }
     // a column to a thread: what is free of it, in order, and what the new rows take over
     int carry = 0;
+#pragma nounroll
     for (int j0 = 0; j0 < o.longest; j0 += kThreads) {
         const int j = j0 + tid;
         if (j0 > 0 || (!counts && o.most > kThreads)) read_column(ids, f, table, j);       // the first are there, but where later ones were counted
         if (open && j0 < o.most) {
             uint32_t freed = freed_in(ids, o, f, j);
-            int sum = __popc(freed);
-            const int v = sum;
-            for (int d = 1; d < 64; d <<= 1) {
-                const int u = __shfl_up(sum, d, 64);
-                if (lane >= d) sum += u;
-            }
-            __syncthreads();
+            const int v = __popc(freed), sum = wave_sums(v);
+            lds_barrier();
             if (lane == 63) wave_sum[wid] = sum;
-            __syncthreads();
+            lds_barrier();
             int at = carry + sum - v;
+#pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                if (w < wid) at += wave_sum[w];
-                carry += wave_sum[w];
+                const int u = wave_sum[w];
+                at += w < wid ? u : 0;
+                carry += u;
             }
+#pragma nounroll
             for (; freed; freed &= freed - 1, ++at) {
                 const int id = ids[__builtin_ctz(freed)][tid];
                 if (at < mine.copies) own[at] = id;
                 else f.ring[ring_at(head, count + before[1] + (at - mine.copies), f.n_blocks)] = id;
             }
         }
+#pragma nounroll
         for (int i = 0; i < f.beams; ++i) {
-            const int p = open ? o.parent[i] : i;
-            if (p >= 0 && j < o.blocks[p] && !(open && o.place[i] >= 0 && j == o.blocks[p] - 1)) f.next_table[(row0 + i) * f.max_blocks + j] = ids[p][tid];
+            const int p = open ? o.parent[i] : i, blocks = open ? o.taken[i] : o.blocks[i];
+            if (j < blocks) f.next_table[(row0 + i) * f.max_blocks + j] = ids[p][tid];
         }
     }
-    __syncthreads();
+    if (open && tid < taken_by(mine)) own[mine.freed + tid] = ring_id;
+    lds_barrier();
     if (tid < f.beams) {
         const int p = open ? o.parent[tid] : tid, place = open ? o.place[tid] : -1;
-        int id = -1;                          // the row's own last block
-        if (place >= 0) {
-            id = place < mine.freed ? own[place] : f.ring[ring_at(head, before[0] + (place - mine.freed), f.n_blocks)];
-            f.next_table[(row0 + tid) * f.max_blocks + o.blocks[p] - 1] = id;
-        }
+        const int id = place >= 0 ? own[place] : -1;          // the row's own last block
+        if (place >= 0) f.next_table[(row0 + tid) * f.max_blocks + o.blocks[p] - 1] = id;
         f.next_len[row0 + tid] = p >= 0 ? o.length[p] : 0;
         *(int2*)(f.copy + 2 * (row0 + tid)) = make_int2(place >= 0 ? o.last[p] : -1, place >= 0 ? id : -1);
     }
