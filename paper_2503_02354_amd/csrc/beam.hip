@@ -2,9 +2,11 @@
 //
 // A row's candidates come in the order of their logits, and what they are short of the score, ln sum exp x, is one number for all of them.  So
 // one pass over a row finds both that sum and its best logits, and the rows of a request meet afterwards with a few candidates each:
-//   score(row, v) = score[row] + ((x_v - m) - ln S)      m = max x,  S = sum exp(x - m)
-// Candidates of different rows may be as near to each other as their logits' last bits, so scores are fp64, and so are S (from fp32 sums of a lane's
-// terms relative to the lane's largest, whose errors are independent) and its logarithm.
+//   score(row, v) = score[row] + (x_v - lse)      lse = (log2 S - c) / L      S = sum 2^(x L + c)      c = -m L, rounded      m = max x
+// L is log2 e as fp32 has it, 1.3e-8 (relative) off, which puts that times the row's entropy on lse: below 2e-7, and the same to a tenth of that for rows as
+// alike as a request's.  x L + c is rounded once, in the multiply-add.  Candidates of different rows may be as near to each other as their
+// logits' last bits, so scores are fp64, and so are S (from fp32 sums of a lane's terms relative to the lane's largest, whose errors are
+// independent) and its logarithm.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -40,13 +42,28 @@ __device__ __forceinline__ uint32_t key_of(float x)
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-__device__ __forceinline__ float exp_fast(float v)
+__device__ __forceinline__ float exp2_fast(float v)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f);
+    return __builtin_amdgcn_exp2f(v);
 #else
     return v;
 #endif
+}
+constexpr float kLog2e = 1.44269504088896340736f;
+// c = -m L; 0 where there is no m.  Beyond kHuge its rounding is no longer small beside 1, and sums are relative to e^m.
+constexpr float kHuge = 0x1p16f;
+__device__ __forceinline__ bool is_huge(float m) { return fabsf(m) > kHuge; }
+__device__ __forceinline__ float offset_of(float m) { return m == -INFINITY ? 0.f : -(m * kLog2e); }
+// what a sum relative to the maximum `from` weighs in one relative to `to`, the larger
+__device__ __forceinline__ double weight_of(float from, float to)
+{
+    if (from == to) return 1.;
+    if (from == -INFINITY) return 0.;
+    const double c = offset_of(from), L = kLog2e;
+    if (!is_huge(to) && !is_huge(from)) return exp2((double)offset_of(to) - c);
+    // by way of e^m
+    return exp2(((double)from - (double)to) * 1.44269504088896340736 - (is_huge(from) ? 0. : from * L + c) + (is_huge(to) ? 0. : to * L + (double)offset_of(to)));
 }
 // the largest of three; a signalling NaN among them makes it NaN (fmaxf would quiet every operand first, an instruction each)
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -93,6 +110,7 @@ __device__ __forceinline__ uint32_t wave_min(uint32_t v) { return ~wave_max(~v);
 // equal logit that comes later in the same wavefront is never wanted, but in another it may be.
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kPerLane = 16, kStep = 64 * kPerLane, kSlack = 32, kGrow = 64;
 constexpr int kList = kBeamPicksMax + kGrow + kStep;
+static_assert(kBeamPicksMax + kGrow <= 128 && kWaves * 128 <= kList, "two keys of a list to a lane, all lists in the place of one");
 struct RowPart {                              // the workspace: [rows][parts] of these, then as many lists of `picks` keys
     double sum;
     float top;
@@ -176,7 +194,7 @@ __device__ int cut_list(unsigned long long* list, int n, int picks, uint32_t& lo
 }
 
 // One wavefront's share of a part of a row, its 16-byte pieces [begin, end); all of the workgroup's wavefronts call this together.  SAFE: NaN counts as
-// -inf, and equal infinities weigh 1; without it they make the sum NaN.  quarter: [kWaves] what every wavefront's quarter of the picks reaches, 0 for
+// -inf, and equal infinities weigh 1; without it they, and maxima beyond kHuge, make the sum NaN.  quarter: [kWaves] what every wavefront's quarter of the picks reaches, 0 for
 // not yet.
 template <typename T, bool SAFE>
 __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int end, int wid, int picks, unsigned long long* list, volatile uint32_t* quarter, int& n, float& top, double& sum)
@@ -222,11 +240,17 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
         return max3(most, x[kPerLane - 1], x[0]);
     };
     auto weigh = [&](const float (&x)[kPerLane], float most) __attribute__((always_inline)) {
-        const float m_new = max3(m, most, m), m_use = m_new == -INFINITY ? 0.f : m_new;
-        s = m == m_new ? s : s * exp_fast(m - m_new);
+        const float m_new = max3(m, most, m), c = offset_of(m_new);
         float part[4] = {0.f, 0.f, 0.f, 0.f};
+        if (SAFE) {
+            s = m == m_new ? s : s * exp2_fast((m - m_new) * kLog2e);
 #pragma unroll
-        for (int e = 0; e < kPerLane; ++e) part[e & 3] += SAFE && x[e] == m_new && x[e] > -INFINITY ? 1.f : exp_fast(x[e] - m_use);
+            for (int e = 0; e < kPerLane; ++e) part[e & 3] += x[e] == -INFINITY ? 0.f : x[e] == m_new ? 1.f : exp2_fast((x[e] - m_new) * kLog2e);
+        } else {
+            s = m == m_new ? s : s * exp2_fast(c - offset_of(m));
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e) part[e & 3] += exp2_fast(__builtin_fmaf(x[e], kLog2e, c));
+        }
         s += (part[0] + part[1]) + (part[2] + part[3]);
         m = m_new;
     };
@@ -293,14 +317,15 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
     }
     if (step > 2 && n >= share) tell();
     // the lanes' sums
+    if (SAFE && m > -INFINITY && !is_huge(m)) s *= exp2_fast(__builtin_fmaf(m, kLog2e, offset_of(m)));      // they were relative to e^m
     float wave_top = m;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) wave_top = fmaxf(wave_top, __shfl_xor(wave_top, d, 64));
-    double v = m == wave_top ? (double)s : (double)s * exp((double)m - (double)wave_top);
+    double v = (double)s * weight_of(m, wave_top);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
     top = wave_top;
-    sum = __any(s != s) ? __longlong_as_double(0x7FF8000000000000ll) : v;
+    sum = __any(s != s || (!SAFE && m > -INFINITY && is_huge(m))) ? __longlong_as_double(0x7FF8000000000000ll) : v;
     wave_sync();
 }
 
@@ -333,23 +358,11 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
         __syncthreads();
         scan_row<T, true>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
     }
-    if ((tid & 63) == 0) {
-        tops[wid] = top;
-        sums[wid] = sum;
-    }
-    __syncthreads();
-    unsigned long long* const out = lists + (size_t)blockIdx.x * s.picks;
-    if (tid == 0) {
-        float t = tops[0];
-        for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
-        double v = 0;
-        for (int w = 0; w < kWaves; ++w) v += tops[w] == t ? sums[w] : sums[w] * exp((double)tops[w] - (double)t);
-        stats[blockIdx.x] = {v, t, 0};
-    }
-    // the wavefronts' lists without what the quarters pass, then a key to a thread: its place is the number of larger ones
+    // the wavefronts' lists without what the quarters pass, behind each other; then a key to a thread: its place is the number of larger ones
     const int lane = tid & 63;
     const uint32_t q = min(min(quarter[0], quarter[1]), min(quarter[2], quarter[3]));
     int mine = 0;
+#pragma nounroll
     for (int i = 0; i < n; i += 64) {
         const unsigned long long k = i + lane < n ? list[wid][i + lane] : 0;
         const bool keep = k != 0 && (uint32_t)(k >> 32) >= q;
@@ -359,17 +372,40 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
         wave_sync();
         mine += __popcll(b);
     }
-    if (lane == 0) lengths[wid] = mine;
+    if (lane == 0) {
+        lengths[wid] = mine;
+        tops[wid] = top;
+        sums[wid] = sum;
+    }
     __syncthreads();
-    int all = 0;
-    for (int w = 0; w < kWaves; ++w) all += lengths[w];
+    int all = 0, ahead = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        ahead += w < wid ? lengths[w] : 0;
+        all += lengths[w];
+    }
+    unsigned long long own[2];                // a list is at most picks + kGrow long
+#pragma unroll
+    for (int i = 0; i < 2; ++i) own[i] = i * 64 + lane < mine ? list[wid][i * 64 + lane] : 0;
+    __syncthreads();
+    unsigned long long* const joined = &list[0][0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (own[i]) joined[ahead + i * 64 + lane] = own[i];
+    __syncthreads();
+    unsigned long long* const out = lists + (size_t)blockIdx.x * s.picks;
+    if (tid == kThreads - 1) {
+        float t = tops[0];
+        for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
+        double v = 0;
+#pragma nounroll
+        for (int w = 0; w < kWaves; ++w) v += sums[w] * weight_of(tops[w], t);
+        stats[blockIdx.x] = {v, t, 0};
+    }
     for (int i = tid; i < all; i += kThreads) {
-        int w = 0, at = i;
-        while (at >= lengths[w]) at -= lengths[w++];
-        const unsigned long long key = list[w][at];
+        const unsigned long long key = joined[i];
         int place = 0;
-        for (w = 0; w < kWaves; ++w)
-            for (int j = 0; j < lengths[w]; ++j) place += list[w][j] > key;
+#pragma unroll 4
+        for (int j = 0; j < all; ++j) place += joined[j] > key;
         if (place < s.picks) out[place] = key;
     }
     for (int i = all + tid; i < s.picks; i += kThreads) out[i] = 0;
@@ -453,13 +489,14 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
         for (int p = 0; p < rounds; ++p) {
             if (p * kLanes + sub >= parts) break;
             if (p > 0) v = stats[(first + b) * parts + p * kLanes + sub];
-            sum += v.top == top ? v.sum : v.sum * exp((double)v.top - (double)top);
+            sum += v.sum * weight_of(v.top, top);
         }
 #pragma unroll
         for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d, 64);
         if (sub == 0 && b < s.beams) {
+            // a candidate's logit less this: lse, or what is on top of a huge maximum
             row_top[b] = top;
-            row_log[b] = log(sum);
+            row_log[b] = is_huge(top) ? log(sum) : (log2(sum) - (double)offset_of(top)) / (double)kLog2e;
             row_score[b] = so_far;
             row_state[b] = state;
         }
@@ -473,6 +510,7 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
             const int state = row_state[b];
             const float top = row_top[b];
             const double base = row_score[b], less = row_log[b];
+            const bool huge = is_huge(top);
             if (state == 2 && lane == 0) f(Candidate{order_of(base), 0, b});
             if (state != 1) continue;
 #pragma nounroll
@@ -481,7 +519,7 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
                 const float x = logit_of((uint32_t)(key >> 32));
                 unsigned long long score = 0;
                 if (known && i < kHeld) score = scores[i];
-                else if (key != 0 && (x == top || top < INFINITY)) score = order_of(base + ((x == top ? 0. : (double)x - (double)top) - less));
+                else if (key != 0 && (x == top || top < INFINITY)) score = order_of(base + ((!huge ? (double)x : x == top ? 0. : (double)x - (double)top) - less));
                 if (!known && i < kHeld) scores[i] = score;
                 if (score) f(Candidate{score, key, b});
             }

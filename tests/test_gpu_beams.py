@@ -485,6 +485,28 @@ def test_select_odd_values(B, dtype):
             _check_select(B, bits, score.astype(np.float32), np.ones(12), 4, 9, -7, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_select_large_logits(B, dtype):
+    """Maxima on both sides of 2^16, up to the largest, apart in a row's parts and among a request's rows: sums change their reference there."""
+    rng = np.random.default_rng(8)
+    to = (lambda a: _bf16(a)) if dtype == "bf16" else (lambda a: np.asarray(a, np.float32))
+    for vocab in (700, 5000, 50000):
+        x = 3 * rng.standard_normal((12, vocab))
+        x[1] += 65530
+        x[2] += 65545
+        x[3] -= 65540
+        x[4] += 1e6
+        x[5, ::2] += 1e6
+        x[6, vocab // 2:] += 65540
+        x[7, vocab // 2:] -= 65540
+        x[8] *= 1e30
+        x[9, 5] = 3e38
+        x[10] = -3e38
+        x[11, :vocab // 3] = -1e5
+        _check_select(B, to(x), np.linspace(-4, -1, 12).astype(np.float32), None, 4, 9, 2, dtype)
+        _check_select(B, to(x), np.zeros(12, np.float32), None, 12, 40, 2, dtype)
+
+
 def test_select_misaligned_rows(B):
     """Rows that begin anywhere: odd strides and bases."""
     import torch
