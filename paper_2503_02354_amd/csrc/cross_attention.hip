@@ -619,8 +619,13 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kerne
     const uint8_t* const seen = st.seen ? st.seen + first : nullptr;
     // Which keys of a tile are there and not hidden; a byte to a lane, on its way before the tile's turn.
     auto fetch_seen = [&](int t) {
-        const int key = (tile0 + t) * kManyKeys + lane;
-        return (int)(key < keys && t < tiles ? (seen ? seen[key] : 1) : 0);
+        int byte = 1;
+        if (seen) byte = seen[max(0, min((tile0 + t) * kManyKeys + lane, keys - 1))];
+        return byte;
+    };
+    auto shown_of = [&](int t, int byte) {
+        asm volatile("" : "+v"(byte));        // not looked at before its turn
+        return __ballot((tile0 + t) * kManyKeys + lane < keys && t < tiles && byte != 0);
     };
     unsigned long long shown[3];              // of tiles t, t + 1 and t + 2, in turn
     // K of tile t goes to buffer t % 2, V to buffer t % 3: while tile t is worked on, K and V of t + 1 are there or on their way.
@@ -770,10 +775,10 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kerne
 
     if (tiles > 0) {
         const int s0 = fetch_seen(0), s1 = fetch_seen(1), s2 = fetch_seen(2);
-        shown[0] = __ballot(s0);
+        shown[0] = shown_of(0, s0);
         load(0, shown[0]);
-        shown[1] = __ballot(s1);
-        shown[2] = __ballot(s2);
+        shown[1] = shown_of(1, s1);
+        shown[2] = shown_of(2, s2);
         const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
         for (int ks = 0; ks < kSteps; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, row_ok && 2 * ks + half < chunks ? q_raw[ks] ^ flip : u32x4{0, 0, 0, 0});
@@ -801,7 +806,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kerne
         else if (t + 2 < tiles) load(t + 2, shown[2]);
         shown[0] = shown[1];
         shown[1] = shown[2];
-        shown[2] = __ballot(ahead);
+        shown[2] = shown_of(t + 3, ahead);
     }
     l = sum_halves(l);
     if (!row_ok) return;
