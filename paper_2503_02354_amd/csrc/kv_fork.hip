@@ -36,19 +36,22 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 #endif
 }
-// inclusive sums over a wavefront's lanes, by register operations
-__device__ __forceinline__ int wave_sums(int v)
+// f over a wavefront's lanes up to each, by register operations; lane 63 has all.  0 changes nothing to f.
+template <class F> __device__ __forceinline__ int wave_scan(int v, F f)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // one lane up, two, four, eight in a row of 16
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // a row's last lane to the next row, the second row's to the last two
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));      // one lane up, two, four, eight in a row of 16
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));      // a row's last lane to the next row, the second row's to the last two
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));
 #endif
     return v;
 }
+__device__ __forceinline__ int wave_sums(int v) { return wave_scan(v, [](int a, int b) { return a + b; }); }
+__device__ __forceinline__ int wave_max(int v) { return __builtin_amdgcn_readlane(wave_scan(v, [](int a, int b) { return max(a, b); }), 63); }
+__device__ __forceinline__ uint32_t wave_or(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)v, [](int a, int b) { return a | b; }), 63); }
 
 // A thread's column of the old rows' tables: their blocks at one place, in LDS, eight rows' on their way together; of any value behind a row's blocks.
 // (Small launches like these are bound by latency, that of their instructions' first use among it: loops are left as they are.)
@@ -83,19 +86,11 @@ __device__ __forceinline__ void read_family(Family& o, Column& ids, const KvFork
         int id = -1;
         if (len & (size - 1)) id = blocks <= kThreads ? ids[lane][blocks - 1] : table[(int64_t)lane * f.max_blocks + blocks - 1];
         const int last = (uint32_t)id < (uint32_t)f.n_blocks ? id : -1;
-        uint32_t lives = 0;
-        int longest = 0, most = 0;
+        const uint32_t lives = wave_or(p >= 0 ? 1u << p : 0u);
+        const int longest = wave_max(blocks), most = wave_max(lane < kBeamMax && (lives >> lane & 1) ? 0 : blocks);
         bool first = true;
 #pragma nounroll
-        for (int w = 0; w < f.beams; ++w) {
-            const int other = __builtin_amdgcn_readlane(p, w);
-            first &= w >= lane || other != p;
-            lives |= other >= 0 ? 1u << other : 0u;
-            longest = max(longest, __builtin_amdgcn_readlane(blocks, w));
-        }
-#pragma nounroll
-        for (int w = 0; w < f.beams; ++w)
-            if (!(lives >> w & 1)) most = max(most, __builtin_amdgcn_readlane(blocks, w));
+        for (int w = 0; w < f.beams; ++w) first &= w >= lane || __builtin_amdgcn_readlane(p, w) != p;
         const int parents_last = __shfl(last, max(p, 0), 64);
         const bool copied = is && p >= 0 && !first && parents_last >= 0;
         const unsigned long long copies = __ballot(copied);
@@ -164,10 +159,9 @@ __global__ __launch_bounds__(kThreads) void kv_fork_count_kernel(KvFork f, Count
     if (threadIdx.x == 0) counts[blockIdx.x] = c;
 }
 
-// place i behind head in a ring of n entries; i passes n only where the state is none of a ring
-__device__ __forceinline__ int ring_at(uint32_t head, long long i, uint32_t n)
+// place `at` behind head in a ring of n entries; it passes n only where the state is none of a ring
+__device__ __forceinline__ int ring_at(uint32_t head, uint32_t at, uint32_t n)
 {
-    uint32_t at = (uint32_t)i;
     if (at >= n) at %= n;
     at += head;
     return (int)(at >= n ? at - n : at);
@@ -175,39 +169,36 @@ __device__ __forceinline__ int ring_at(uint32_t head, long long i, uint32_t n)
 __device__ __forceinline__ int taken_by(const Counts& c) { return max(0, c.copies - c.freed); }
 __device__ __forceinline__ int given_by(const Counts& c) { return max(0, c.freed - c.copies); }
 
-// the sums over the workgroup of three values per thread
-__device__ __forceinline__ void sum3(long long (&v)[3], long long (*part)[3])
+// The sums over the workgroup of three values per thread.  A request takes 31 ids at most, and gives what it holds: in a pool all of them fit 32 bits.
+__device__ __forceinline__ void sum3(uint32_t (&v)[3], uint32_t (*part)[3])
 {
-#pragma nounroll
-    for (int d = 32; d > 0; d >>= 1)
-        for (int e = 0; e < 3; ++e) v[e] += __shfl_xor(v[e], d, 64);
+#pragma unroll
+    for (int e = 0; e < 3; ++e) v[e] = (uint32_t)wave_sums((int)v[e]);
     __syncthreads();
-    if ((threadIdx.x & 63) == 0)
+    if ((threadIdx.x & 63) == 63)
+#pragma unroll
         for (int e = 0; e < 3; ++e) part[threadIdx.x >> 6][e] = v[e];
     __syncthreads();
+#pragma unroll
     for (int e = 0; e < 3; ++e) {
         v[e] = 0;
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) v[e] += part[w][e];
     }
 }
 
 // The first request that needs more than `count` ids with those before it; by all threads of the workgroup.
-__device__ __forceinline__ int first_closed(const Counts* counts, int n, long long count, long long (*part)[3])
+__device__ __forceinline__ int first_closed(const Counts* counts, int n, uint32_t count, uint32_t (*part)[3])
 {
     __shared__ int closed;
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    const int tid = threadIdx.x, wid = tid >> 6;
     if (tid == 0) closed = n;
-    long long carry = 0;
+    uint32_t carry = 0;
 #pragma nounroll
     for (int i0 = 0; i0 < n; i0 += kThreads) {
-        long long sum = i0 + tid < n ? taken_by(counts[i0 + tid]) : 0;
-#pragma nounroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const long long u = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += u;
-        }
+        uint32_t sum = (uint32_t)wave_sums(i0 + tid < n ? taken_by(counts[i0 + tid]) : 0);
         __syncthreads();
-        if (lane == 63) part[wid][0] = sum;
+        if ((tid & 63) == 63) part[wid][0] = sum;
         __syncthreads();
         sum += carry;
         for (int w = 0; w < kWaves; ++w) {
@@ -225,14 +216,14 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
 {
     __shared__ Family o;
     __shared__ Column ids;
-    __shared__ long long part[kWaves][3];
+    __shared__ uint32_t part[kWaves][3];
     __shared__ int own[kBeamMax], wave_sum[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, r = blockIdx.x;
-    const long long count = max(0, min(f.ring_state[1], f.n_blocks));
+    const uint32_t count = (uint32_t)max(0, min(f.ring_state[1], f.n_blocks));
     const uint32_t head = (uint32_t)f.ring_state[0] % (uint32_t)f.n_blocks;
     if (r == f.n_requests) {
         const int closed = first_closed(counts, f.n_requests, count, part);
-        long long sums[3] = {0, 0, 0};        // taken, given, copies
+        uint32_t sums[3] = {0, 0, 0};         // taken, given, copies
 #pragma nounroll
         for (int i = tid; i < closed; i += kThreads) {
             const Counts c = counts[i];
@@ -248,7 +239,7 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
         return;
     }
     Counts mine{0, 0};
-    long long before[3] = {0, 0, 0};          // taken from the ring, and given to it, by the requests before this one
+    uint32_t before[3] = {0, 0, 0};           // taken from the ring, and given to it, by the requests before this one
     if (counts) {
         mine = counts[r];
 #pragma nounroll
@@ -297,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
                 else f.ring[ring_at(head, count + before[1] + (at - mine.copies), f.n_blocks)] = id;
             }
         }
-#pragma nounroll
+#pragma unroll 4
         for (int i = 0; i < f.beams; ++i) {
             const int p = open ? o.parent[i] : i, blocks = open ? o.taken[i] : o.blocks[i];
             if (j < blocks) f.next_table[(row0 + i) * f.max_blocks + j] = ids[p][tid];
