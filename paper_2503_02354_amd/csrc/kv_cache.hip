@@ -205,15 +205,17 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, int n_tokens,
 // pair's sine and cosine each and leave them in LDS for all heads, while the first channels are on their way; then a lane turns V pairs of a head
 // at a time, or copies what is not turned.  The angle in turns, p f / 2 pi, is an fp64 product whose nearest integer is taken off there: what is left is
 // exact to 2^-22 of a turn at positions of 2^31, and its sine and cosine are fp32.
-constexpr int kTurnWaves = 4, kTurnAhead = 4;             // pieces that a lane has on their way
+constexpr int kTurnWaves = 4;
 
 template <int V> struct Packed;               // V bf16 values
 template <> struct Packed<8> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 template <> struct Packed<4> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Packed<2> { typedef uint32_t type; };
 template <> struct Packed<1> { typedef uint16_t type; };
 template <int V> __device__ __forceinline__ float value_of(const typename Packed<V>::type& p, int i)
 {
     if constexpr (V == 1) return __uint_as_float((uint32_t)p << 16);
+    else if constexpr (V == 2) return __uint_as_float(i & 1 ? p & 0xFFFF0000u : p << 16);
     else return __uint_as_float(i & 1 ? p[i / 2] & 0xFFFF0000u : p[i / 2] << 16);
 }
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -226,7 +228,9 @@ template <int V> __device__ __forceinline__ typename Packed<V>::type packed(cons
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
             const f32x2 two = {v[i], v[i + 1]};
-            p[i / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+            const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+            if constexpr (V == 2) p = w;
+            else p[i / 2] = w;
         }
     return p;
 }
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(64 * kTurnWaves) void kv_append_rotated_kernel(KvCa
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float2* const turn = turns[wid];
     const int half = r.rotated >> 1, units = half / V;            // of a head
-    constexpr int kRest = V == 1 ? 2 : 8;     // channels behind the rotated ones that a lane copies
+    constexpr int kRest = V >= 4 ? 8 : 2 * V; // channels behind the rotated ones that a lane copies
     const int per_head = units + (c.head_dim - r.rotated) / kRest, chunks = c.head_dim >> 3;
     const float f = lane < half ? r.frequency[lane] : 0.f;
     const long long waves = (long long)gridDim.x * kTurnWaves, wave = (long long)blockIdx.x * kTurnWaves + wid;
@@ -255,18 +259,12 @@ __global__ __launch_bounds__(64 * kTurnWaves) void kv_append_rotated_kernel(KvCa
         int head = first / per_head, u = first - head * per_head;
         bool turned = false;
         while (__any(head < heads)) {
-            Pack a[kTurnAhead], b[kTurnAhead];
-            int at_head[kTurnAhead], at_unit[kTurnAhead];
-#pragma unroll
-            for (int i = 0; i < kTurnAhead; ++i) {
-                at_head[i] = head, at_unit[i] = u;
-                const uint16_t* const from = head < r.heads ? q + head * r.q_head_stride : k + (head - r.heads) * r.k_head_stride;
-                if (head < heads && u < units) {
-                    a[i] = *(const Pack*)(from + (HALVES ? u * V : 2 * u * V));
-                    b[i] = *(const Pack*)(from + (HALVES ? half + u * V : 2 * u * V + V));
-                }
-                head += step_heads, u += step_units;
-                if (u >= per_head) u -= per_head, ++head;
+            const bool is = head < heads, rotates = u < units;
+            const uint16_t* const from = head < r.heads ? q + head * r.q_head_stride : k + (head - r.heads) * r.k_head_stride;
+            Pack a = {}, b = {};
+            if (is && rotates) {
+                a = *(const Pack*)(from + (HALVES ? u * V : 2 * u * V));
+                b = *(const Pack*)(from + (HALVES ? half + u * V : 2 * u * V + V));
             }
             if (!turned) {
                 turned = true;
@@ -278,43 +276,32 @@ __global__ __launch_bounds__(64 * kTurnWaves) void kv_append_rotated_kernel(KvCa
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
             }
-#pragma unroll
-            for (int i = 0; i < kTurnAhead; ++i) {
-                const int h = at_head[i], w = at_unit[i];
-                if (h >= heads) continue;
-                uint16_t* const to = h < r.heads ? q_out + h * r.q_out_head_stride : c.k + to_cache + (h - r.heads) * c.head_stride;
-                if (w >= units) {             // channels that are not turned
-                    const uint16_t* const from = h < r.heads ? q + h * r.q_head_stride : k + (h - r.heads) * r.k_head_stride;
-                    const int ch = r.rotated + (w - units) * kRest;
-                    if (V == 1) *(uint32_t*)(to + ch) = *(const uint32_t*)(from + ch);
-                    else *(uint4*)(to + ch) = *(const uint4*)(from + ch);
-                    continue;
-                }
-                float x[V], y[V];
-                if (HALVES) {
+            if (is) {
+                uint16_t* const to = head < r.heads ? q_out + head * r.q_out_head_stride : c.k + to_cache + (head - r.heads) * c.head_stride;
+                if (rotates) {
+                    float x[2 * V];           // the unit's channels in the order of their addresses
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float2 cs = turn[w * V + j];
-                        const float p = value_of<V>(a[i], j), m = value_of<V>(b[i], j);
-                        x[j] = p * cs.x - m * cs.y;
-                        y[j] = m * cs.x + p * cs.y;
+                        const int ia = HALVES ? j : 2 * j, ib = HALVES ? V + j : 2 * j + 1;
+                        const float2 cs = turn[u * V + j];
+                        const float p = ia < V ? value_of<V>(a, ia) : value_of<V>(b, ia - V), m = ib < V ? value_of<V>(a, ib) : value_of<V>(b, ib - V);
+                        x[ia] = p * cs.x - m * cs.y;
+                        x[ib] = m * cs.x + p * cs.y;
                     }
-                } else {                      // the unit's channels in the order of their addresses: x, then y
-                    float z[2 * V];
+                    float first_half[V], second_half[V];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float2 cs = turn[w * V + j];
-                        const float p = 2 * j < V ? value_of<V>(a[i], 2 * j) : value_of<V>(b[i], 2 * j - V);
-                        const float m = 2 * j + 1 < V ? value_of<V>(a[i], 2 * j + 1) : value_of<V>(b[i], 2 * j + 1 - V);
-                        z[2 * j] = p * cs.x - m * cs.y;
-                        z[2 * j + 1] = m * cs.x + p * cs.y;
-                    }
-#pragma unroll
-                    for (int j = 0; j < V; ++j) x[j] = z[j], y[j] = z[V + j];
+                    for (int j = 0; j < V; ++j) first_half[j] = x[j], second_half[j] = x[V + j];
+                    *(Pack*)(to + (HALVES ? u * V : 2 * u * V)) = packed<V>(first_half);
+                    *(Pack*)(to + (HALVES ? half + u * V : 2 * u * V + V)) = packed<V>(second_half);
+                } else {                      // channels that are not turned
+                    const int ch = r.rotated + (u - units) * kRest;
+                    if (kRest == 8) *(uint4*)(to + ch) = *(const uint4*)(from + ch);
+                    else if (kRest == 4) *(uint2*)(to + ch) = *(const uint2*)(from + ch);
+                    else *(uint32_t*)(to + ch) = *(const uint32_t*)(from + ch);
                 }
-                *(Pack*)(to + (HALVES ? w * V : 2 * w * V)) = packed<V>(x);
-                *(Pack*)(to + (HALVES ? half + w * V : 2 * w * V + V)) = packed<V>(y);
             }
+            head += step_heads, u += step_units;
+            if (u >= per_head) u -= per_head, ++head;
         }
         if (!kept) continue;
         for (int i = first; i < c.kv_heads * chunks; i += step) {
@@ -361,14 +348,19 @@ template <int V> void launch_rotated(const KvCache& c, const Rotation& r, int sp
 
 hipError_t kv_append_rotated(const KvCache& c, const Rotation& r, hipStream_t stream)
 {
-    // wavefronts to a token: as many as have work, while there are fewer than the chip holds
+    // as many pairs to a lane as come in aligned pieces of 16, 8 or 4 bytes
+    const int pairs = r.rotated % 16 == 0 ? 8 : r.rotated % 8 == 0 ? 4 : r.rotated % 4 == 0 ? 2 : 1;
+    // Wavefronts to a token: those that have two rounds of pieces each, so that the last to start are short; up to eight while there are fewer than the
+    // chip holds.  7000 tokens, 32 heads and 8 of 128 channels, one wavefront 45 us, two 39, four 38; 12 and 12 of 64 15.0, 14.7, 18.0.  Four pieces of a
+    // lane on their way instead of one cost registers, and with them wavefronts: 43.
+    const long long pieces = (long long)(r.heads + c.kv_heads) * (r.rotated / (2 * pairs) + (c.head_dim - r.rotated) / (pairs >= 4 ? 8 : 2 * pairs));
     int split = 1;
-    while (split < 8 && (long long)r.n_tokens * split * 2 <= 2048 && split * 128 < (r.heads + c.kv_heads) * (r.rotated / 16 + 1)) split *= 2;
+    while (split < 8 && (split * 256 <= pieces || (split * 64 < pieces && (long long)r.n_tokens * split * 2 <= 2048))) split *= 2;
     const long long blocks = ((long long)r.n_tokens * split + kTurnWaves - 1) / kTurnWaves;
     const unsigned grid = (unsigned)std::min<long long>(blocks, 1 << 20);
-    // as many pairs to a lane as come in aligned pieces of 16 or 8 bytes
-    if (r.rotated % 16 == 0) launch_rotated<8>(c, r, split, grid, stream);
-    else if (r.rotated % 8 == 0) launch_rotated<4>(c, r, split, grid, stream);
+    if (pairs == 8) launch_rotated<8>(c, r, split, grid, stream);
+    else if (pairs == 4) launch_rotated<4>(c, r, split, grid, stream);
+    else if (pairs == 2) launch_rotated<2>(c, r, split, grid, stream);
     else launch_rotated<1>(c, r, split, grid, stream);
     return hipGetLastError();
 }
