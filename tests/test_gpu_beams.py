@@ -779,3 +779,66 @@ def test_calls_on_another_stream_and_in_graphs(B):
         torch.cuda.synchronize()
         assert all(torch.equal(t, w) for t, w in zip(outputs, want))
         torch.randn(1000, device="cuda").sum().item()
+
+
+# ---- the example that puts them together ------------------------------------------------------------------------------------------
+def _dense_decoder(d, states, ids):
+    """The decoder's logits at every place of ids: whole rows of scores, fp32 on the CPU, nothing cached, positions turned in fp64."""
+    import torch
+    f = lambda w: w.float().cpu()
+    norm = lambda x: x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-5)
+    n, group = len(ids), d.heads // d.kv_heads
+    x, seen = f(d.embedding)[ids], f(states)
+    mask = torch.full((n, n), -np.inf).triu(1)
+
+    def turn(a):
+        out, _ = T.rotate(a.double().numpy(), np.arange(n), d.frequency.cpu().numpy(), d.rotated, False)
+        return torch.from_numpy(out).float()
+
+    def attend(q, k, v, mask):
+        k, v = (a.repeat_interleave(group, 1) for a in (k, v))
+        s = torch.einsum("qhd,khd->hqk", q, k) * d.head_dim ** -0.5 + mask
+        return torch.einsum("hqk,khd->qhd", s.softmax(-1), v).reshape(n, -1)
+    for layer in range(d.layers):
+        q, k, v = (norm(x) @ f(d.qkv[layer])).view(n, -1, d.head_dim).split([d.heads, d.kv_heads, d.kv_heads], 1)
+        x = x + attend(turn(q), turn(k), v, mask) @ f(d.o[layer])
+        k, v = (seen @ f(d.cross_kv[layer])).view(len(seen), -1, d.head_dim).split([d.kv_heads, d.kv_heads], 1)
+        x = x + attend((norm(x) @ f(d.cross_q[layer])).view(n, d.heads, d.head_dim), k, v, 0.0) @ f(d.cross_o[layer])
+        x = x + torch.nn.functional.gelu(norm(x) @ f(d.up[layer])) @ f(d.down[layer])
+    return norm(x) @ f(d.head)
+
+
+def test_example_writes_what_the_dense_model_scores(B):
+    """Beams over states and prompts of different lengths, blocks shared and copied: every beam's score is what whole forwards without a cache give its
+    tokens, the search with one beam takes the best token at every place, and all blocks come back."""
+    import importlib.util
+    import pathlib
+    import torch
+    spec = importlib.util.spec_from_file_location("describe", pathlib.Path(__file__).parent.parent / "examples" / "describe.py")
+    describe = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(describe)
+    d = describe.Decoder(rotated=16)
+    rng = np.random.default_rng(0)
+    g = torch.Generator().manual_seed(2)
+    states = [torch.randn(m, d.width, generator=g).bfloat16().cuda() for m in (1, 197, 30, 64, 300)]
+    prompts = [rng.integers(2, d.vocab, m).tolist() for m in (1, 20, 7, 16, 33)]
+    writer = describe.Writer(d, n_blocks=80, block_size=8, max_len=48)
+    for beams, new in ((4, 10), (1, 6), (7, 3)):
+        found = writer.write(states, prompts, beams, new)
+        assert sorted(writer.ring[(int(writer.state[0]) + torch.arange(80, device="cuda")) % 80].tolist()) == list(range(80)) and int(writer.state[1]) == 80
+        for s, prompt, list_ in zip(states, prompts, found):
+            assert len(list_) == beams and len({tuple(t) for t, _ in list_}) == beams
+            scores = [v for _, v in list_]
+            assert scores == sorted(scores, reverse=True)
+            for tokens, score in list_:
+                logits = _dense_decoder(d, s, prompt + tokens)[len(prompt) - 1:-1]
+                lp = logits.log_softmax(-1)[torch.arange(len(tokens)), tokens]
+                # a bf16 rounding is at most 2^-8 of a value, uniform inside that: 2^-8 / sqrt(3) in the root mean square.  Some fifteen of them on
+                # the way through each of two layers add up to 2^-8 sqrt(30 / 3) = 1.2 % of the state, the logits are of deviation 1 (weights:
+                # variance 1 / fan-in): 0.012 each, 0.12 is ten deviations of a token
+                assert abs(float(lp.sum()) - score) <= 0.12 * len(tokens)
+                if beams == 1:
+                    assert (logits[torch.arange(len(tokens)), tokens] >= logits.max(-1).values - 0.12).all()
+    small = describe.Writer(d, n_blocks=20, block_size=8, max_len=48)
+    with pytest.raises(RuntimeError, match="too small"):
+        small.write(states, prompts, 4, 10)
