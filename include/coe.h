@@ -417,8 +417,8 @@ typedef struct {
  * NaN gets NaN for both.  Hidden rows do not reach it, whatever their bits.  Of a source with more than max_new queries the first max_new
  * are served; rows of q that belong to no source are not read, and theirs of out and lse not written.  length is limited to max_rows and
  * to the rows that there are behind first; a negative first or length counts as a source without rows.
- * q, out and lse as in coe_kv_attention (lse may be NULL); scale, numerics and limits too.  heads: a multiple of kv_heads; n_tokens * heads and
- * max_rows at most 2^31 - 4096; n_sources * beams at most COE_KV_MAX_REQUESTS.  The same inputs give the same bits.
+ * q, out and lse as in coe_kv_attention (lse may be NULL); scale, numerics and limits too.  heads: a multiple of kv_heads; n_tokens * heads at most
+ * 2^30, n_sources * kv_heads 2^22, max_rows 2^31 - 4096, n_sources * beams COE_KV_MAX_REQUESTS.  The same inputs give the same bits.
  * workspace: coe_cross_attention_workspace bytes for the same sizes (may be 0), 16-byte aligned. */
 int64_t coe_cross_attention_workspace(int32_t n_sources, int32_t n_tokens, int32_t max_new, int32_t max_rows, int32_t heads, int32_t kv_heads,
                                       int32_t head_dim);
@@ -470,8 +470,8 @@ int coe_kv_fork(int32_t n_requests, int32_t beams, int32_t block_size, int32_t n
                 const int32_t* table, int32_t* ring, const int32_t* ring_state, int32_t* next_table, int32_t* next_len, int32_t* copy,
                 int32_t* next_state, void* workspace, int64_t workspace_bytes, void* stream);
 
-/* Brings the rows of blocks that are not full to their copies, in every layer's cache at once: for every i < n with copy[i] = {from, to}, both in the
- * cache, the first seq_len[i] % block_size rows of block `from` (all of them where that is 0) go to block `to`; other entries are skipped.
+/* Brings the rows of blocks that are not full to their copies, in every layer's cache at once: for every i < n (at most COE_KV_MAX_REQUESTS) with copy[i] = {from, to},
+ * both in the cache, the first seq_len[i] % block_size rows of block `from` (all of them where that is 0) go to block `to`; other entries are skipped.
  * caches: [n_caches] host values, read during the call; they may differ in heads, channels, layout and number of blocks, not in block_size.  No block may be the
  * target of two entries, or the target of one and the source of another. */
 int coe_kv_copy(int32_t n_caches, const coe_kv_cache* caches, int32_t n, const int32_t* copy, const int32_t* seq_len, void* stream);

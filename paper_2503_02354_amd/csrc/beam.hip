@@ -415,7 +415,8 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
 // A workgroup per request: the rows' sums, then the best of all lists.  From a score on that enough of the threads' best reach, candidates are listed and
 // counted against each other; where that is too many (an order that no list of a row has by chance), they are found one after the other.
 // (A launch of few workgroups is bound by latency, that of its instructions' first use among it: its loops are left as they are.)
-constexpr int kMeet = 512, kHeld = 2048;      // candidates that are listed; keys that are kept in LDS, more are read again
+constexpr int kMeet = 512, kHeld = 2048;      // candidates that are listed; a request's keys, which are kept in LDS
+static_assert(kBeamMax * kBeamPicksMax <= kHeld, "one part of a row at least");
 struct Candidate {
     unsigned long long score;                 // fp64 as an integer that grows with it; 0: none
     unsigned long long key;                   // of the row
@@ -522,12 +523,12 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
             if (state != 1) continue;
 #pragma nounroll
             for (int i = b * per_row + lane; i < (b + 1) * per_row; i += 64) {
-                const unsigned long long key = i < kHeld ? held[i] : keys[i];
+                const unsigned long long key = held[i];
                 const float x = logit_of((uint32_t)(key >> 32));
                 unsigned long long score = 0;
-                if (known && i < kHeld) score = scores[i];
+                if (known) score = scores[i];
                 else if (key != 0 && (x == top || top < INFINITY)) score = order_of(base + ((!huge ? (double)x : x == top ? 0. : (double)x - (double)top) - less));
-                if (!known && i < kHeld) scores[i] = score;
+                if (!known) scores[i] = score;
                 if (score) f(Candidate{score, key, b});
             }
         }
@@ -606,7 +607,6 @@ hipError_t beam_select(int dtype, const BeamSelection& s, void* workspace, hipSt
 {
     const int64_t rows = (int64_t)s.n_requests * s.beams;
     const int parts = row_parts(rows, s.beams, s.picks, s.vocab);
-    if (rows * parts > 0x7FFFFFFFll / kThreads) return hipErrorInvalidValue;
     RowPart* const stats = (RowPart*)workspace;
     unsigned long long* const lists = (unsigned long long*)(stats + rows * parts);
     if (dtype == 0) hipLaunchKernelGGL(beam_rows_kernel<float>, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, s, parts, stats, lists);

@@ -933,7 +933,6 @@ template <int D> hipError_t launch_many(const States& st, const CrossAttention& 
         hipFuncSetAttribute((const void*)cross_attention_schedule_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSchedLds)};
     if (configured[0] != hipSuccess || configured[1] != hipSuccess) return configured[0] != hipSuccess ? configured[0] : configured[1];
     const ManyLayout at = many_layout(a.n_sources, a.n_tokens, a.heads, st.kv_heads, D);
-    if (at.most_units * st.kv_heads > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const size_t sched_lds = ((size_t)a.n_sources + 4) * 4 + (a.n_sources <= kSchedInLds ? (size_t)a.n_sources * 16 : 0);
     hipLaunchKernelGGL(cross_attention_schedule_kernel, dim3(1), dim3(kSchedThreads), sched_lds, stream, st, a, workspace, at);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;

@@ -195,12 +195,14 @@ int coe_kv_append_rotated(const coe_kv_cache* cache, int32_t n_tokens, int32_t h
     return launched(call, coe::k::kv_append_rotated(c, r, (hipStream_t)stream));
 }
 
+// a launch of a workgroup to 128 query rows of a head, and one more to a source and head, holds fewer than 2^32 threads
+constexpr long long kMostCrossRows = 1ll << 30, kMostCrossHeads = 1ll << 22;
 int64_t coe_cross_attention_workspace(int32_t n_sources, int32_t n_tokens, int32_t max_new, int32_t max_rows, int32_t heads, int32_t kv_heads,
                                       int32_t head_dim)
 {
     if (n_sources < 0 || n_sources > COE_KV_MAX_REQUESTS || n_tokens < 0 || max_new < 0 || max_rows < 0 || max_rows > kMostRows || kv_heads <= 0 ||
-        kv_heads > 65535 || heads <= 0 || heads % kv_heads || heads > 65535 || (long long)n_tokens * heads > kMostRows || head_dim < 8 || head_dim > 128 ||
-        head_dim % 8)
+        kv_heads > 65535 || heads <= 0 || heads % kv_heads || heads > 65535 || (long long)n_tokens * heads > kMostCrossRows ||
+        (long long)n_sources * kv_heads > kMostCrossHeads || head_dim < 8 || head_dim > 128 || head_dim % 8)
         return fail(COE_EINVAL, "coe_cross_attention_workspace: bad size");
     return coe::k::cross_attention_workspace(n_sources, n_tokens, max_new < n_tokens ? max_new : n_tokens, max_rows, heads, kv_heads, head_dim);
 }
@@ -228,8 +230,8 @@ int coe_cross_attention(const coe_states* states, int32_t n_sources, int32_t n_t
     if (n_sources < 0 || beams <= 0 || n_tokens < 0 || max_new < 0 || max_rows < 0 || max_rows > kMostRows || (long long)n_sources * beams > COE_KV_MAX_REQUESTS)
         return fail(COE_EINVAL, "%s: a size is out of range (n_sources * beams: at most %d)", call, COE_KV_MAX_REQUESTS);
     if (heads <= 0 || heads > 65535 || heads % states->kv_heads) return fail(COE_EINVAL, "%s: heads %d is not a multiple of kv_heads %d", call, heads, states->kv_heads);
-    if ((long long)n_tokens * heads > kMostRows || (long long)n_sources * states->kv_heads > 0x7FFFFFFFll)
-        return fail(COE_EINVAL, "%s: n_tokens * heads must be at most 2^31 - 4096", call);
+    if ((long long)n_tokens * heads > kMostCrossRows) return fail(COE_EINVAL, "%s: n_tokens * heads must be at most 2^30", call);
+    if ((long long)n_sources * states->kv_heads > kMostCrossHeads) return fail(COE_EINVAL, "%s: n_sources * kv_heads must be at most 2^22", call);
     if (!(scale == scale) || scale - scale != 0.f) return fail(COE_EINVAL, "%s: scale must be finite", call);
     if (n_sources == 0 || n_tokens == 0 || max_new == 0) return COE_OK;
     if (!q || !q_off || !first || !length || !out) return fail(COE_EINVAL, "%s: null argument", call);
@@ -265,7 +267,6 @@ int coe_beam_select(int32_t n_requests, int32_t beams, int32_t picks, int32_t vo
     if (n_requests < 0 || vocab <= 0) return fail(COE_EINVAL, "%s: n_requests %d, vocab %d", call, n_requests, vocab);
     if (beams <= 0 || beams > COE_BEAM_MAX) return fail(COE_EINVAL, "%s: beams %d outside 1..%d", call, beams, COE_BEAM_MAX);
     if (picks <= 0 || picks > COE_BEAM_PICKS_MAX) return fail(COE_EINVAL, "%s: picks %d outside 1..%d", call, picks, COE_BEAM_PICKS_MAX);
-    if ((long long)n_requests * beams > 0x7FFFFFFFll || (long long)n_requests * picks > 0x7FFFFFFFll) return fail(COE_EINVAL, "%s: n_requests * beams and n_requests * picks must be below 2^31", call);
     if ((long long)n_requests * beams >= 1 << 23) return fail(COE_EINVAL, "%s: n_requests * beams must be below 2^23", call);
     if (dtype != COE_DT_F32 && dtype != COE_DT_BF16) return fail(COE_EINVAL, "%s: unknown dtype %d", call, dtype);
     if (n_requests == 0) return COE_OK;
@@ -316,6 +317,7 @@ int coe_kv_copy(int32_t n_caches, const coe_kv_cache* caches, int32_t n, const i
 {
     const char* const call = "coe_kv_copy";
     if (n_caches < 0 || n < 0) return fail(COE_EINVAL, "%s: n_caches %d, n %d", call, n_caches, n);
+    if (n > COE_KV_MAX_REQUESTS) return fail(COE_EINVAL, "%s: n %d exceeds %d", call, n, COE_KV_MAX_REQUESTS);
     if (n_caches > 0 && !caches) return fail(COE_EINVAL, "%s: null caches", call);
     coe::k::KvCache c;
     for (int32_t i = 0; i < n_caches; ++i) {  // all of them before the first launch

@@ -357,6 +357,60 @@ def test_cross_limits_of_sizes(B):
         assert (got[c.off[last]:c.off[last + 1]] == 0).all()
 
 
+def test_cross_longest_sources_first(B):
+    """Between one and a few workgroups to a place on the chip sources are ranked by length: equal ones, empty ones, ones without queries among them."""
+    rng = np.random.default_rng(12)
+    for n, heads, kv, dim, beams in ((100, 16, 8, 64, 2), (256, 4, 4, 32, 1), (70, 8, 8, 128, 3), (129, 10, 5, 40, 1)):
+        sources = [(int(a), tuple(int(m) for m in rng.integers(0, 3, beams))) for a in rng.choice([0, 1, 31, 64, 64, 65, 200, 333], n)]
+        for hidden in (0.0, 0.4):
+            c = Cross(sources, heads, kv, dim, beams=beams, seed=n, hidden=hidden)
+            c.check(*c.run(B))
+
+
+def test_cross_most_sources(B):
+    """As many sources as a call takes, single tokens and chunks, a long one among them: the lists of tiles and units at their longest."""
+    rng = np.random.default_rng(13)
+    rows = rng.integers(0, 3, 16384)
+    rows[[0, 7000, 16383]] = 9000, 40, 5000
+    c = Cross([(int(n), 1) for n in rows], 2, 2, 32, seed=6, gap=0)
+    c.check(*c.run(B))
+    new = rng.integers(0, 2, 16384)
+    new[[5, 16380]] = 400, 90
+    rows[5] = 2000
+    c = Cross([(int(n), int(m)) for n, m in zip(rows, new)], 2, 1, 32, seed=7, gap=0)
+    c.check(*c.run(B))
+    c = Cross([(5, 1)] * 8192, 2, 2, 32, beams=2, seed=8, gap=0)
+    c.check(*c.run(B))
+
+
+@pytest.mark.parametrize("sources,max_rows", [([(9000, 2), (30, 3), (500, 1)], 9000), ([(90, 2), (30, 3), (50, 1)], 90), ([(2000, 200), (3000, 90), (64, 300)], 3000), ([(60, 60), (33, 40), (9, 50)], 60)])
+def test_cross_offsets_that_are_no_offsets(B, sources, max_rows):
+    """q_off that runs backwards, outside q or over itself: nothing beside q's rows is touched, and the call ends."""
+    c = Cross(sources, 4, 2, 64, seed=1)
+    tokens, good = int(c.off[-1]), c.off.copy()
+    for off in ([tokens, tokens // 2, 0, -5], [0, tokens, 0, tokens], [-7, 2 ** 31 - 1, -2 ** 31, tokens], [0, 1, 2 ** 31 - 1, 3], [tokens, tokens, tokens, 0]):
+        c.off = np.asarray(off, np.int32)
+        got = _cross_with_offsets(B, c, good, max_rows)
+        assert (got[tokens:] == 0xFFC0).all()
+
+
+def _cross_with_offsets(B, c, good, max_rows):
+    """A run whose arrays have the sizes of the good offsets; returns out with rows behind the tokens."""
+    import torch
+    tokens = int(good[-1])
+    both = _dev(c.kv_bits.transpose(1, 0, 2, 3))
+    st = B.coe_states(1, c.rows, c.kv, c.dim, both.data_ptr(), both[:, 1].data_ptr(), *both.stride()[0:1], both.stride(2), both.stride(0), both.stride(2), 0)
+    q, out = _dev(c.q), _dev(np.full((tokens + 8, c.heads, c.dim), 0xFFC0, np.uint16))
+    need = B.coe_cross_attention_workspace(len(c.length), tokens, c.most, max_rows, c.heads, c.kv, c.dim)
+    work = torch.full((need + 256,), 0xAB, dtype=torch.uint8, device="cuda")
+    d = [_dev(a) for a in (c.off, c.first, c.length)]
+    B.coe_cross_attention(st, len(c.length), tokens, 1, c.most, max_rows, c.heads, c.scale, q.data_ptr(), *q.stride()[:2], *(t.data_ptr() for t in d), out.data_ptr(), *out.stride()[:2], 0,
+                          work.data_ptr(), need, _stream())
+    torch.cuda.synchronize()
+    assert (work[need:] == 0xAB).all()
+    return _bits(out)
+
+
 def test_cross_far_rows(B):
     """States of more than 2^32 bytes."""
     import torch
@@ -716,6 +770,107 @@ def test_copy(B, layers, kv, dim, block, layout):
                 rows = seq_len[i] % block or block
                 b[:, copy[i, 1], :rows] = b[:, copy[i, 0], :rows]
         assert np.array_equal(_bits(k), b[0]) and np.array_equal(_bits(v), b[1])
+
+
+def test_rows_beyond_32_bits(B):
+    """Caches, tokens and logits whose offsets pass 2^32 bytes."""
+    import torch
+    big = torch.zeros(3 * 2 ** 30 + 64, dtype=torch.bfloat16, device="cuda")         # 6 GiB
+    # a cache of 3000 blocks, 2^21 bytes apart; the tokens' rows lie in a tensor of their own, 2^23 bytes apart
+    n, stride, block = 3000, 2 ** 20, 8
+    kv = big[:n * stride].view(n, stride)
+    cache = B.coe_kv_cache(B.COE_DT_BF16, n, block, 2, 64, kv.data_ptr(), kv[:, 4096:].data_ptr(), stride, 128, 64)
+    rot = Rotate(600, 4, 2, 64, 64, False, seed=4)
+    x, q_out = _dev(rot.x), torch.zeros(600, 4, 64, dtype=torch.int16, device="cuda")
+    rot.slot = (n * block - 1 - 39 * np.arange(600)).astype(np.int32)     # the last rows of the cache, one in 39
+    rot.position = np.arange(600).astype(np.int32)
+    rot.device = [_dev(rot.slot), _dev(rot.position), _dev(rot.frequency)]
+    rot.call(B, x, q_out, cache)
+    torch.cuda.synchronize()
+    at = _dev((rot.slot // block).astype(np.int64)) * stride + _dev((rot.slot % block).astype(np.int64)) * 128
+    take = lambda off: big[(at + off)[:, None] + torch.arange(128, device="cuda")].view(600, 2, 64)
+    want, size = T.rotate(T.bf16_to_f64(rot.x[:, 4:6]), rot.position, rot.frequency, 64, False)
+    assert (np.abs(take(0).double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2e-6 * size + 1e-38).all()          # as in Rotate.check
+    assert np.array_equal(_bits(take(4096).view(torch.int16)), rot.x[:, 6:])
+    # blocks to others on both sides of 2^32 bytes
+    copy, length = _dev(np.array([[n - 1, 0], [n - 6, 1], [10, n - 2]], np.int32)), _dev(np.array([8, 3, 5], np.int32))
+    kv[10, :1024], kv[10, 4096:5120] = 3.0, 5.0
+    before = kv[[n - 1, n - 6], :5120].clone()
+    B.coe_kv_copy([cache], 3, copy.data_ptr(), length.data_ptr(), _stream())
+    torch.cuda.synchronize()
+    assert torch.equal(kv[0, :1024], before[0, :1024]) and torch.equal(kv[0, 4096:5120], before[0, 4096:])
+    assert torch.equal(kv[1, :384], before[1, :384]) and (kv[1, 384:1024] == 0).all()
+    assert (kv[n - 2, :640] == 3).all() and (kv[n - 2, 4096:4736] == 5).all() and (kv[n - 2, 640:1024] == 0).all()
+    # tokens far apart, in and out
+    rows = big[:700 * 2 ** 22].view(700, 2 ** 22)
+    rows[:600, :512] = x.view(torch.bfloat16).reshape(600, 512)
+    rows[:, 1024:1280] = 7.0
+    small_k, small_v, small = _make_cache(B, rot.old, "token")
+    rot.slot = np.arange(600).astype(np.int32)
+    rot.device = [_dev(rot.slot), _dev(rot.position), _dev(rot.frequency)]
+    d = rot.device
+    B.coe_kv_append_rotated(small, 600, 4, rows.data_ptr(), 2 ** 22, 64, rows[:, 1024:].data_ptr(), 2 ** 22, 64, rows[:, 256:].data_ptr(), 2 ** 22, 64, rows[:, 384:].data_ptr(), 2 ** 22, 64,
+                            *(t.data_ptr() for t in d), 64, 0, _stream())
+    torch.cuda.synchronize()
+    rot.check(_bits(rows[:600, 1024:1280].contiguous().view(torch.int16)).reshape(600, 4, 64), _bits(small_k), _bits(small_v), np.zeros((600, 4, 64), np.uint16))
+    assert (rows[600:, 1024:1280] == 7).all()
+    # and logits
+    logits = big[:16 * 190000000].view(16, 190000000)
+    bits = _bf16(2 * np.random.default_rng(0).standard_normal((16, 5003)))
+    logits[:, 1:5004] = _dev(bits).view(torch.bfloat16)
+    out = [torch.zeros(4, 8, dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32, torch.int32)]
+    need = B.coe_beam_workspace(4, 4, 8, 5003)
+    work, score = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"), torch.zeros(16, device="cuda")
+    B.coe_beam_select(4, 4, 8, 5003, B.COE_DT_BF16, logits[:, 1:].data_ptr(), 190000000, score.data_ptr(), 0, 2, *(t.data_ptr() for t in out), work.data_ptr(), need, _stream())
+    torch.cuda.synchronize()
+    want = T.beam(T.bf16_to_f64(bits), np.zeros(16), None, 4, 8, 2)
+    assert all(np.array_equal(o.cpu().numpy(), w) for o, w in zip(out[1:], want[1:]))
+
+
+def test_select_long_rows(B):
+    """Millions of tokens in a row; the best at its ends and where parts meet."""
+    rng = np.random.default_rng(14)
+    for dtype in ("f32", "bf16"):
+        x = rng.standard_normal((2, 5000001))
+        x[0, [0, -1, 2500000]], x[1, 1234567] = 9.0, 8.0
+        _check_select(B, _bf16(x) if dtype == "bf16" else x.astype(np.float32), np.array([-1, -1.5], np.float32), None, 2, 32, 2, dtype)
+
+
+def test_calls_at_once(B):
+    """Calls on two streams together, each with a workspace of its own, give what they give alone."""
+    import torch
+    rng = np.random.default_rng(15)
+    x = [_dev((2 * rng.standard_normal((16, 50000))).astype(np.float32)) for _ in range(2)]
+    score = torch.zeros(16, device="cuda")
+    c = Cross([(900, 90), (3000, 1), (500, 200)], 8, 2, 64, seed=3)
+    both = _dev(c.kv_bits.transpose(1, 0, 2, 3))
+    st = B.coe_states(1, c.rows, 2, 64, both.data_ptr(), both[:, 1].data_ptr(), 256, 64, 256, 64, 0)
+    qs = [_dev(c.q), _dev(c.q[::-1].copy())]
+    d = [_dev(a) for a in (c.off, c.first, c.length)]
+    needs = B.coe_beam_workspace(4, 4, 8, 50000), B.coe_cross_attention_workspace(3, len(c.q), c.most, 3000, 8, 2, 64)
+
+    def room():
+        return [torch.full((max(n, 16),), 0xFF, dtype=torch.uint8, device="cuda") for n in needs]
+
+    def outputs():
+        return [torch.zeros(4, 8, dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32)] + [torch.zeros(len(c.q), 8, 64, dtype=torch.int16, device="cuda")]
+
+    def go(i, work, out, stream):
+        B.coe_cross_attention(st, 3, len(c.q), 1, c.most, 3000, 8, 0.125, qs[i].data_ptr(), 512, 64, *(t.data_ptr() for t in d), out[3].data_ptr(), 512, 64, 0, work[1].data_ptr(), needs[1], stream)
+        B.coe_beam_select(4, 4, 8, 50000, 0, x[i].data_ptr(), 50000, score.data_ptr(), 0, 2, *(t.data_ptr() for t in out[:3]), 0, work[0].data_ptr(), needs[0], stream)
+    alone, work = [], room()
+    for i in range(2):
+        out = outputs()
+        go(i, work, out, _stream())
+        alone.append(out)
+    torch.cuda.synchronize()
+    streams, works, outs = [torch.cuda.Stream() for _ in range(2)], [room() for _ in range(2)], [outputs() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i in range(2):
+            go(i, works[i], outs[i], streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for a, b in zip(alone[i], outs[i]))
 
 
 # ---- streams, graphs ------------------------------------------------------------------------------------------------------------

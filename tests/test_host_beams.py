@@ -63,7 +63,8 @@ def test_cross_attention_refuses(B):
     for kw in (dict(sources=-1), dict(beams=0), dict(beams=-2), dict(tokens=-1), dict(new=-1), dict(rows=-1), dict(rows=2 ** 31 - 4095),
                dict(sources=B.COE_KV_MAX_REQUESTS, beams=2), dict(sources=2 ** 20, beams=2 ** 20)):
         bad("size", **kw)
-    bad("heads", heads=0), bad("heads", heads=3), bad("2^31", tokens=2 ** 30), bad("scale", scale=float("nan")), bad("scale", scale=float("-inf"))
+    bad("heads", heads=0), bad("heads", heads=3), bad("2^30", tokens=2 ** 28 + 1), bad("scale", scale=float("nan")), bad("scale", scale=float("-inf"))
+    bad("2^22", states=_states(B, kv_heads=300), heads=300, sources=14000, beams=1)
     for name in ("q", "off", "first", "length", "out"):
         bad("null", **{name: 0})
     for kw in (dict(q=P + 8), dict(qt=100), dict(qh=-8), dict(out=P + 2), dict(ot=4), dict(oh=63)):
@@ -78,7 +79,7 @@ def test_cross_attention_refuses(B):
             kw = dict(zip(("sources", "tokens", "new", "rows"), sizes), beams=1)
             bad("workspace", B.COE_ERANGE, bytes=need - 1, **kw), bad("workspace", work=0, **kw), bad("workspace", work=P + 8, **kw)
     for args in ((-1, 1, 1, 9, 4, 2, 64), (1, -1, 1, 9, 4, 2, 64), (1, 1, -1, 9, 4, 2, 64), (1, 1, 1, -1, 4, 2, 64), (1, 1, 1, 9, 3, 2, 64), (1, 1, 1, 9, 4, 0, 64),
-                 (1, 1, 1, 9, 4, 2, 65), (1, 1, 1, 2 ** 31 - 1, 4, 2, 64), (1, 2 ** 30, 1, 9, 4, 2, 64), (B.COE_KV_MAX_REQUESTS + 1, 1, 1, 9, 4, 2, 64)):
+                 (1, 1, 1, 9, 4, 2, 65), (1, 1, 1, 2 ** 31 - 1, 4, 2, 64), (1, 2 ** 28 + 1, 1, 9, 4, 2, 64), (14000, 1, 1, 9, 300, 300, 64), (B.COE_KV_MAX_REQUESTS + 1, 1, 1, 9, 4, 2, 64)):
         _refused(B, B.COE_EINVAL, "bad size", B.coe_cross_attention_workspace, *args)
 
 
@@ -89,7 +90,7 @@ def test_beam_select_refuses(B):
     def bad(text, code=B.COE_EINVAL, **kw):
         _refused(B, code, text, B.coe_beam_select, *{**ok, **kw}.values())
     bad("n_requests", requests=-1), bad("vocab", vocab=0), bad("beams", beams=0), bad("beams", beams=B.COE_BEAM_MAX + 1), bad("picks", picks=0)
-    bad("picks", picks=B.COE_BEAM_PICKS_MAX + 1), bad("dtype", dtype=2), bad("2^31", requests=2 ** 30)
+    bad("picks", picks=B.COE_BEAM_PICKS_MAX + 1), bad("dtype", dtype=2), bad("2^23", requests=2 ** 30), bad("2^23", requests=2 ** 21)
     for name in ("logits", "score", "next_score", "row", "token"):
         bad("null", **{name: 0})
     bad("misaligned", logits=P + 2), bad("misaligned", logits=P + 1, dtype=1), bad("stride", stride=99), bad("alias", next_score=P), bad("alias", next_ended=P)
@@ -100,7 +101,7 @@ def test_beam_select_refuses(B):
         if need:
             kw = dict(zip(("requests", "beams", "picks", "vocab"), sizes), stride=sizes[3])
             bad("workspace", B.COE_ERANGE, bytes=need - 1, **kw), bad("workspace", work=0, **kw), bad("workspace", work=P + 8, **kw)
-    for args in ((-1, 4, 8, 100), (1, 0, 8, 100), (1, 33, 8, 100), (1, 4, 0, 100), (1, 4, 65, 100), (1, 4, 8, 0), (2 ** 30, 4, 8, 10)):
+    for args in ((-1, 4, 8, 100), (1, 0, 8, 100), (1, 33, 8, 100), (1, 4, 0, 100), (1, 4, 65, 100), (1, 4, 8, 0), (2 ** 30, 4, 8, 10), (2 ** 21, 4, 8, 10)):
         _refused(B, B.COE_EINVAL, "bad size", B.coe_beam_workspace, *args)
 
 
@@ -127,6 +128,7 @@ def test_fork_refuses(B):
 def test_copy_refuses(B):
     c = _cache(B)
     _refused(B, B.COE_EINVAL, "n -1", B.coe_kv_copy, [c], -1, P, P, 0)
+    _refused(B, B.COE_EINVAL, "exceeds", B.coe_kv_copy, [c], B.COE_KV_MAX_REQUESTS + 1, P, P, 0)
     _refused(B, B.COE_EINVAL, "null", B.coe_kv_copy, [c], 1, 0, P, 0)
     _refused(B, B.COE_EINVAL, "null", B.coe_kv_copy, [c], 1, P, 0, 0)
     _refused(B, B.COE_EINVAL, "aligned", B.coe_kv_copy, [c], 1, P + 4, P, 0)
