@@ -412,13 +412,14 @@ __global__ __launch_bounds__(256) void cross_attention_join_kernel(States st, Cr
 }
 
 // ---- many query rows (prompts, answers that are scored): more than 32 per source and head --------------------------------------------
-// Units of work are tiles of 128 query rows (32 to a wavefront) of a source and head, with all its 64-key tiles.  A scheduling launch lists
-// them, longest first, so that the last workgroups to start are short ones; where there are too few units to fill the chip it cuts long ones
-// into parts over the keys, which cross_attention_join_units_kernel adds up.  Block b takes head b % kv_heads, so that with eight of them
+// Units of work are tiles of 128 query rows (32 to a wavefront) of a source and head, with all its 64-key tiles, the longest first, so that the last
+// workgroups to start are short ones.  Every workgroup finds its own where there are few sources; else a scheduling launch lists them, which also cuts
+// long ones into parts over the keys where there are too few to fill the chip; cross_attention_join_units_kernel adds those up.  Block b takes head b % kv_heads, so that with eight of them
 // (or four, or two) the units of one head meet in the same second-level caches.  K tiles go from memory into two LDS buffers by DMA, V
 // tiles into three, in turn; a wavefront reads every key and value of a tile for its 32 rows.
 constexpr int kManyRows = 128, kManyKeys = 64, kManyWaves = 4;
 constexpr int kManyGroups = 512;          // two workgroups per compute unit
+constexpr int kListed = 64;               // sources that a workgroup looks at for its unit: one to a lane
 
 struct Unit {
     int32_t first_row, tile, tiles, part;      // first query row; 64-key tiles; -1, or the part of the workspace that takes the result (times kv_heads)
@@ -523,8 +524,9 @@ __global__ __launch_bounds__(kSchedThreads) void cross_attention_schedule_kernel
     };
     const Segment own = tid < count ? find(tid) : Segment{};             // the only one in most calls
     auto segment = [&](int i) { return i == tid ? own : find(i); };
-    // no part is shorter than 8 tiles, or than what fills the chip once
-    const int most = (int)min(1ull << 30, max(8ull, (total * (unsigned)st.kv_heads + kManyGroups - 1) / kManyGroups));
+    // No part is shorter than 8 tiles, or than twice a workgroup's share: at one share 8 sources of 200 tokens and 600 rows, 32 heads on 8 of 128, took 61 us
+    // instead of 41, one and a half or twice make no difference.
+    const int most = (int)min(1ull << 30, max(8ull, (2 * total * (unsigned)st.kv_heads + kManyGroups - 1) / kManyGroups));
     // longest first: by length, the longer halves of the range in coarser steps
     int scale = 0;
     while ((most >> scale) >= kSchedBins) ++scale;
@@ -574,7 +576,7 @@ __global__ __launch_bounds__(kSchedThreads) void cross_attention_schedule_kernel
 template <int D> constexpr int kManyTile = kManyKeys * kRow<D> * 2;  // bytes of a K (or V) tile
 
 template <int D>
-__global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kernel(States st, CrossAttention a, char* workspace, ManyLayout layout)
+__global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kernel(States st, CrossAttention a, char* workspace, ManyLayout layout, bool listed)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int DH = kRow<D>, kSteps = D / 16, kBlocks = D / 32, kTile = kManyTile<D>;
@@ -582,14 +584,31 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kerne
     extern __shared__ __attribute__((aligned(4096))) char lds[];          // two buffers of K tiles, three of V
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     const int kvh = blockIdx.x % st.kv_heads, index = blockIdx.x / st.kv_heads;
-    // one round trip for the number of units and the unit, whose place is there in any case
-    const int units = ((const ManyHeader*)workspace)->units;
-    const int4 *const up = (const int4*)((const Unit*)(workspace + layout.units) + index), u0 = up[0], u1 = up[1];
-    if (index >= units) return;
-    const int row0 = __builtin_amdgcn_readfirstlane(u0.x), tile0 = __builtin_amdgcn_readfirstlane(u0.y), part = __builtin_amdgcn_readfirstlane(u0.w);
-    const int q0 = __builtin_amdgcn_readfirstlane(u1.x), group = a.heads / st.kv_heads, rows = __builtin_amdgcn_readfirstlane(u1.y) * group;
-    const int first = __builtin_amdgcn_readfirstlane(u1.z), keys = __builtin_amdgcn_readfirstlane(u1.w);
-    const int tiles = keys == 0 ? 0 : __builtin_amdgcn_readfirstlane(u0.z);
+    const int group = a.heads / st.kv_heads;
+    int row0, tile0 = 0, part = -1, q0, rows, first, keys, tiles;
+    if (listed) {                             // a source to a lane; the unit is one of the source that `index` falls to
+        const int n = a.n_sources, s = min(lane, n - 1);
+        const Source o = source_of(st, a, s);
+        const int length = (int)(((unsigned)o.keys + kManyKeys - 1) / kManyKeys), order = length << 6 | (63 - lane);         // unequal, below 2^31
+        const int segments = lane < n ? (int)(((unsigned)(o.m * group) + kManyRows - 1) / kManyRows) : 0;
+        int before = 0;
+        for (int i = 0; i < n; ++i) before += __builtin_amdgcn_readlane(order, i) > order ? __builtin_amdgcn_readlane(segments, i) : 0;
+        const unsigned long long owner = __ballot(index >= before && index < before + segments);
+        if (!owner) return;
+        const int from = __builtin_ctzll(owner);
+        row0 = (index - __builtin_amdgcn_readlane(before, from)) * kManyRows;
+        q0 = __builtin_amdgcn_readlane(o.q0, from), rows = __builtin_amdgcn_readlane(o.m, from) * group;
+        first = __builtin_amdgcn_readlane(o.first, from), keys = __builtin_amdgcn_readlane(o.keys, from), tiles = __builtin_amdgcn_readlane(length, from);
+    } else {
+        // one round trip for the number of units and the unit, whose place is there in any case
+        const int units = ((const ManyHeader*)workspace)->units;
+        const int4 *const up = (const int4*)((const Unit*)(workspace + layout.units) + index), u0 = up[0], u1 = up[1];
+        if (index >= units) return;
+        row0 = __builtin_amdgcn_readfirstlane(u0.x), tile0 = __builtin_amdgcn_readfirstlane(u0.y), part = __builtin_amdgcn_readfirstlane(u0.w);
+        q0 = __builtin_amdgcn_readfirstlane(u1.x), rows = __builtin_amdgcn_readfirstlane(u1.y) * group;
+        first = __builtin_amdgcn_readfirstlane(u1.z), keys = __builtin_amdgcn_readfirstlane(u1.w);
+        tiles = keys == 0 ? 0 : __builtin_amdgcn_readfirstlane(u0.z);
+    }
     const int chunks = st.head_dim >> 3;
 
     // this lane's query row; a negative scale moves to the queries
@@ -891,13 +910,34 @@ bool is_few(const Sizes& z) { return z.rows() <= kFewRows; }
 // 32.8 / 23.9; 16 sources 2000 27.4 / 35.5 and 20.6 / 25.0, 4000 64.7 / 69.1 and 44.9 / 40.6; 32 sources 2000 64.0 / 70.8 and 39.2 / 55.8, 4000 125 / 120 and
 // 100 / 81; 64 sources 2000 118 / 120 and 72 / 83.  8 heads of 128: 8 sources 500 rows 13.6 / 15.5, 1000 21.0 / 16.4; 16 sources 1000 21.4 / 21.2 and 20.0 /
 // 27.8, 2000 37.1 / 32.6; 32 sources 1000 26.8 / 31.8 and 21.8 / 38.1, 4000 116 / 118 and 102 / 70; 64 sources 1000 60.4 / 62.6 and 37.0 / 56.2.
-// Chunks, a workgroup for 32 rows of each / units and a join: 1000 tokens on 1000 rows, 16 heads of 64, 20.0 / 25.0, 4 x 400 tokens on 1500 rows 49 / 36;
-// 30 x 20 to 40 tokens on 100 to 1000 rows, 12 heads of 64, 21.6 / 24.6.
+// Chunks of tokens, a workgroup for 32 rows of each / units, listed or scheduled, whichever is faster (us), 16 heads of 64: one source 40 tokens 1000 rows
+// 12.2 / 17.7, 4000 33.8 / 22.9, 300 tokens 1000 rows 12.8 / 19.6, 1000 tokens (512 workgroups) 500 rows 13.6 / 13.2; 4 sources 100 tokens 2000 rows 21.4 / 26.0,
+// 4000 35.7 / 32.8; 300 tokens (640) 200 rows 11.6 / 10.1, 1000 28.6 / 21.3; 16 sources 300 tokens 1000 rows 95 / 36.  32 heads on 8 of 128: one source 100 tokens
+// 1000 rows 21.7 / 26.6, 2000 35.4 / 29.7; 300 tokens (304) 500 rows 22.0 / 17.5.  Above kListed sources units are scheduled, which costs more: 640
+// workgroups 1000 rows of 64 28.6 / 29.8, 1024 200 rows 15.7 / 18.7, 500 rows 23.0 / 22.2.
 bool is_whole(const Sizes& z)
 {
-    const int64_t longest = z.max_rows * z.dim;
-    if (z.row_blocks() == 1) return longest <= (z.groups() >= 256 ? 229376 : z.groups() >= 128 ? 163840 : 81920);
-    return z.groups() <= 2048 && longest <= 131072 && z.groups() * longest <= 52ll << 20;
+    const int64_t longest = z.max_rows * z.dim, groups = z.groups();
+    if (z.row_blocks() == 1) return longest <= (groups >= 256 ? 229376 : groups >= 128 ? 163840 : 81920);
+    if (groups <= 256) return longest <= 163840;
+    return z.n_sources > kListed && groups <= 1536 && groups * longest <= 16ll << 20;
+}
+
+// units of a call, at most
+int64_t most_units(const Sizes& z, int64_t n_tokens)
+{
+    return std::min(z.n_sources * ((z.rows() + kManyRows - 1) / kManyRows), n_tokens * (z.heads / z.kv_heads) / kManyRows + z.n_sources);
+}
+// Whether units are listed by their own workgroups and none is cut: where the scheduling launch and the join, which cost 7 to 10 us, would not shorten the longest
+// by more than 12 tiles (by what the states' rows say of their mean length).  Listed / scheduled, us, 16 heads of 64: 4 sources 300 tokens 500 rows 14.1 /
+// 21.4, 2000 rows (192 units of 32 tiles) 34.7 / 38.9, 4000 60 / 56; one source 1000 tokens 2000 rows (128 of 32) 34.8 / 33.0; 32 sources 20 to 500 tokens on 200 to
+// 3000 rows 105 / 108.  32 heads on 8 of 128: one source 300 tokens 1000 rows (80 of 16) 27 / 31, 2000 47 / 39; 8 sources 1000 tokens 4000 rows 265 / 273.
+bool is_listed(const Sizes& z, int64_t n_tokens, int64_t n_rows)
+{
+    if (z.n_sources > kListed) return false;
+    auto tiles = [](int64_t rows) { return (rows + kManyKeys - 1) / kManyKeys; };
+    const int64_t share = most_units(z, n_tokens) * z.kv_heads * tiles(std::min(z.max_rows, n_rows / z.n_sources)) / kManyGroups;
+    return tiles(z.max_rows) - std::max<int64_t>(8, 2 * share) <= 12;
 }
 
 template <int D, bool PAD, int WAVES, bool ORDERED> hipError_t launch_whole(const Sizes& z, const States& st, const CrossAttention& a, hipStream_t stream)
@@ -924,7 +964,7 @@ template <int D, bool PAD> hipError_t launch_few(const Sizes& z, const States& s
     return hipGetLastError();
 }
 
-template <int D> hipError_t launch_many(const States& st, const CrossAttention& a, char* workspace, hipStream_t stream)
+template <int D> hipError_t launch_many(const Sizes& z, const States& st, const CrossAttention& a, char* workspace, hipStream_t stream)
 {
     constexpr int kLds = 5 * kManyTile<D>;
     constexpr size_t kSchedLds = std::max((size_t)(kPlanMaxRequests + 4) * 4, (size_t)(kSchedInLds + 4) * 4 + kSchedInLds * 16);
@@ -933,10 +973,14 @@ template <int D> hipError_t launch_many(const States& st, const CrossAttention& 
         hipFuncSetAttribute((const void*)cross_attention_schedule_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSchedLds)};
     if (configured[0] != hipSuccess || configured[1] != hipSuccess) return configured[0] != hipSuccess ? configured[0] : configured[1];
     const ManyLayout at = many_layout(a.n_sources, a.n_tokens, a.heads, st.kv_heads, D);
+    if (is_listed(z, a.n_tokens, st.n_rows)) {
+        hipLaunchKernelGGL(cross_attention_many_kernel<D>, dim3((unsigned)(most_units(z, a.n_tokens) * st.kv_heads)), dim3(64 * kManyWaves), kLds, stream, st, a, workspace, at, true);
+        return hipGetLastError();
+    }
     const size_t sched_lds = ((size_t)a.n_sources + 4) * 4 + (a.n_sources <= kSchedInLds ? (size_t)a.n_sources * 16 : 0);
     hipLaunchKernelGGL(cross_attention_schedule_kernel, dim3(1), dim3(kSchedThreads), sched_lds, stream, st, a, workspace, at);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(cross_attention_many_kernel<D>, dim3((unsigned)(at.most_units * st.kv_heads)), dim3(64 * kManyWaves), kLds, stream, st, a, workspace, at);
+    hipLaunchKernelGGL(cross_attention_many_kernel<D>, dim3((unsigned)(at.most_units * st.kv_heads)), dim3(64 * kManyWaves), kLds, stream, st, a, workspace, at, false);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(cross_attention_join_units_kernel<D>, dim3((unsigned)(at.most_joined * st.kv_heads), kManyRows / kUnitRows), dim3(kUnitThreads<D>), 0, stream, st, a, workspace, at);
     return hipGetLastError();
@@ -952,7 +996,7 @@ template <int D> hipError_t launch(const Sizes& z, const States& st, const Cross
             return exact ? launch_whole<D, false, kFewWaves, true>(z, st, a, stream) : launch_whole<D, true, kFewWaves, true>(z, st, a, stream);
         return exact ? launch_whole<D, false, kFewWaves, false>(z, st, a, stream) : launch_whole<D, true, kFewWaves, false>(z, st, a, stream);
     }
-    if (!is_few(z)) return launch_many<D>(st, a, workspace, stream);
+    if (!is_few(z)) return launch_many<D>(z, st, a, workspace, stream);
     return exact ? launch_few<D, false>(z, st, a, workspace, stream) : launch_few<D, true>(z, st, a, workspace, stream);
 }
 
