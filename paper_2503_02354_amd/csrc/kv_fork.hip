@@ -53,26 +53,33 @@ __device__ __forceinline__ int wave_sums(int v) { return wave_scan(v, [](int a, 
 __device__ __forceinline__ int wave_max(int v) { return __builtin_amdgcn_readlane(wave_scan(v, [](int a, int b) { return max(a, b); }), 63); }
 __device__ __forceinline__ uint32_t wave_or(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)v, [](int a, int b) { return a | b; }), 63); }
 
-// A thread's column of the old rows' tables: their blocks at one place, in LDS, eight rows' on their way together; of any value behind a row's blocks.
-// (Small launches like these are bound by latency, that of their instructions' first use among it: loops are left as they are.)
-typedef int32_t Column[kBeamMax][kThreads];           // kBeamMax is a multiple of eight
-__device__ __forceinline__ void read_column(Column& ids, const KvFork& f, const int32_t* table, int j)
+// A thread's column of the old rows' tables: their blocks at one place, in LDS, a group of rows on their way together; of any value behind a row's blocks.
+// ROWS: room for that many, kGroup or kBeamMax.  (Small launches like these are bound by latency, that of their instructions' first use among it, some 150 ns
+// for every 128 bytes: loops over groups and rows are left as they are.)
+constexpr int kGroup = 8;
+static_assert(kBeamMax % (2 * kGroup) == 0, "whole groups");
+template <int ROWS> struct Columns {
+    static constexpr int kTogether = ROWS < 2 * kGroup ? ROWS : 2 * kGroup;
+    int32_t id[ROWS][kThreads];
+};
+template <int ROWS> __device__ __forceinline__ void read_column(Columns<ROWS>& ids, const KvFork& f, const int32_t* table, int j)
 {
+    constexpr int T = Columns<ROWS>::kTogether;
     const bool there = j < f.max_blocks;
     const int32_t* const from = table + (there ? j : 0);
 #pragma nounroll
-    for (int w0 = 0; w0 < f.beams; w0 += 8) {
-        int32_t v[8];
+    for (int w0 = 0; w0 < f.beams; w0 += T) {
+        int32_t v[T];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) v[w] = from[(int64_t)min(w0 + w, f.beams - 1) * f.max_blocks];
+        for (int w = 0; w < T; ++w) v[w] = from[(int64_t)min(w0 + w, f.beams - 1) * f.max_blocks];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) ids[w0 + w][threadIdx.x] = v[w];
+        for (int w = 0; w < T; ++w) ids.id[w0 + w][threadIdx.x] = v[w];
     }
 }
 
 // By all threads of the workgroup; a row to a lane of its first wavefront.  `ids` holds the first kThreads columns, whose loads share a round trip with
 // the rows' own.
-__device__ __forceinline__ void read_family(Family& o, Column& ids, const KvFork& f, int r)
+template <int ROWS> __device__ __forceinline__ void read_family(Family& o, Columns<ROWS>& ids, const KvFork& f, int r)
 {
     const int lane = threadIdx.x;
     const int64_t row0 = (int64_t)r * f.beams;
@@ -84,18 +91,18 @@ __device__ __forceinline__ void read_family(Family& o, Column& ids, const KvFork
     if (lane < 64) {
         const int p = given >= row0 && given < row0 + f.beams ? (int)(given - row0) : -1, blocks = (len + size - 1) >> f.block_shift;
         int id = -1;
-        if (len & (size - 1)) id = blocks <= kThreads ? ids[lane][blocks - 1] : table[(int64_t)lane * f.max_blocks + blocks - 1];
+        if (len & (size - 1)) id = blocks <= kThreads ? ids.id[lane][blocks - 1] : table[(int64_t)lane * f.max_blocks + blocks - 1];
         const int last = (uint32_t)id < (uint32_t)f.n_blocks ? id : -1;
         const uint32_t lives = wave_or(p >= 0 ? 1u << p : 0u);
         const int longest = wave_max(blocks), most = wave_max(lane < kBeamMax && (lives >> lane & 1) ? 0 : blocks);
         bool first = true;
 #pragma nounroll
-        for (int w = 0; w < f.beams; ++w) first &= w >= lane || __builtin_amdgcn_readlane(p, w) != p;
+        for (int w = 0; w < f.beams; ++w) first &= (w >= lane) | (__builtin_amdgcn_readlane(p, w) != p);
         const int parents_last = __shfl(last, max(p, 0), 64);
         const bool copied = is && p >= 0 && !first && parents_last >= 0;
         const unsigned long long copies = __ballot(copied);
         const int parents_blocks = __shfl(blocks, max(p, 0), 64);
-        if (is) {
+        if (lane < kBeamMax) {                // what is no row has no blocks
             o.taken[lane] = p < 0 ? 0 : parents_blocks - (copied ? 1 : 0);
             o.parent[lane] = p;
             o.blocks[lane] = blocks;
@@ -112,34 +119,52 @@ __device__ __forceinline__ void read_family(Family& o, Column& ids, const KvFork
     }
     __syncthreads();
 }
-// The rows whose block at place j, this thread's column, is free: nobody continues the row, no row that is continued holds it, and none before it
-// is dropped with it.
-__device__ __forceinline__ uint32_t freed_in(const Column& ids, const Family& o, const KvFork& f, int j)
+// Looking for free blocks is what these launches compute most, of rows by rows in every column; threads that have no column share those of others.
+struct Share {
+    int column, part, parts;                  // of `parts` threads with this column, the part-th
+    uint32_t rows;                            // that it looks at
+};
+__device__ __forceinline__ Share share_of(int columns)
 {
+    const int parts = columns <= kThreads / 4 ? 4 : columns <= kThreads / 2 ? 2 : 1, part = (int)threadIdx.x / (kThreads / parts);
+    return {(int)threadIdx.x % (kThreads / parts), part, parts, (parts == 4 ? 0x11111111u : parts == 2 ? 0x55555555u : ~0u) << part};
+}
+// Those of a share's rows whose block at place j, in `column`, is free: nobody continues the row, no row that is continued holds it, and none before it
+// is dropped with it.
+template <int ROWS> __device__ __forceinline__ uint32_t freed_in(const Columns<ROWS>& ids, const Family& o, const KvFork& f, int j, int column, uint32_t rows)
+{
+    constexpr int T = Columns<ROWS>::kTogether;
     uint32_t there = 0, freed = 0;
 #pragma nounroll
-    for (int s = 0; s < f.beams; ++s) there |= j < o.blocks[s] ? 1u << s : 0u;
+    for (int s0 = 0; s0 < f.beams; s0 += T)
+#pragma unroll
+        for (int s = 0; s < T; ++s) there |= (j < o.blocks[s0 + s] ? 1u << s : 0u) << s0;
 #pragma nounroll
-    for (uint32_t dropped = there & ~o.lives; dropped; dropped &= dropped - 1) {
-        const int d = __builtin_ctz(dropped), id = ids[d][threadIdx.x];
-        const uint32_t others = there & (o.lives | ((1u << d) - 1));
-        uint32_t same = 0;
+    for (uint32_t dropped = there & ~o.lives & rows; dropped; dropped &= dropped - 1) {
+        const int d = __builtin_ctz(dropped), id = ids.id[d][column];
+        uint32_t same = 0;                    // rows that are not there have any bits
 #pragma nounroll
-        for (int s = 0; s < f.beams; ++s) same |= ids[s][threadIdx.x] == id ? 1u << s : 0u;
-        freed |= (uint32_t)id < (uint32_t)f.n_blocks && !(same & others) ? 1u << d : 0u;
+        for (int s0 = 0; s0 < f.beams; s0 += T) {
+            uint32_t some = 0;
+#pragma unroll
+            for (int s = 0; s < T; ++s) some |= ids.id[s0 + s][column] == id ? 1u << s : 0u;
+            same |= some << s0;
+        }
+        freed |= ((uint32_t)id < (uint32_t)f.n_blocks) & !(same & there & (o.lives | ((1u << d) - 1))) ? 1u << d : 0u;
     }
     return freed;
 }
 
 // what a request copies and frees; by all threads of the workgroup
-__device__ __forceinline__ Counts count_request(Column& ids, const Family& o, const KvFork& f, const int32_t* table, int* part)
+template <int ROWS> __device__ __forceinline__ Counts count_request(Columns<ROWS>& ids, const Family& o, const KvFork& f, const int32_t* table, int* part)
 {
     const int tid = threadIdx.x;
+    const Share share = share_of(o.most);
     int freed = 0;
 #pragma nounroll
-    for (int j = tid; j < o.most; j += kThreads) {
+    for (int j = share.column; j < o.most; j += kThreads) {
         if (j >= kThreads) read_column(ids, f, table, j);
-        freed += __popc(freed_in(ids, o, f, j));
+        freed += __popc(freed_in(ids, o, f, j, share.column, share.rows));
     }
     freed = wave_sums(freed);
     if ((tid & 63) == 63) part[tid >> 6] = freed;
@@ -149,10 +174,10 @@ __device__ __forceinline__ Counts count_request(Column& ids, const Family& o, co
     return {o.copies, freed};
 }
 
-__global__ __launch_bounds__(kThreads) void kv_fork_count_kernel(KvFork f, Counts* counts)
+template <int ROWS> __global__ __launch_bounds__(kThreads) void kv_fork_count_kernel(KvFork f, Counts* counts)
 {
     __shared__ Family o;
-    __shared__ Column ids;
+    __shared__ Columns<ROWS> ids;
     __shared__ int part[kWaves];
     read_family(o, ids, f, blockIdx.x);
     const Counts c = count_request(ids, o, f, f.table + (int64_t)blockIdx.x * f.beams * f.max_blocks, part);
@@ -212,12 +237,13 @@ __device__ __forceinline__ int first_closed(const Counts* counts, int n, uint32_
 }
 
 // A workgroup per request, and one more for the state; with one request its counts are taken here (counts: null), and there is one workgroup.
-__global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Counts* counts)
+template <int ROWS> __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Counts* counts)
 {
     __shared__ Family o;
-    __shared__ Column ids;
+    __shared__ Columns<ROWS> ids;
     __shared__ uint32_t part[kWaves][3];
     __shared__ int own[kBeamMax], wave_sum[kWaves];
+    __shared__ uint32_t some[kThreads];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, r = blockIdx.x;
     const uint32_t count = (uint32_t)max(0, min(f.ring_state[1], f.n_blocks));
     const uint32_t head = (uint32_t)f.ring_state[0] % (uint32_t)f.n_blocks;
@@ -263,13 +289,21 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
         f.next_state[3] = open ? mine.copies : 0;
     }
     // a column to a thread: what is free of it, in order, and what the new rows take over
+    const Share share = share_of(o.most);
     int carry = 0;
 #pragma nounroll
     for (int j0 = 0; j0 < o.longest; j0 += kThreads) {
         const int j = j0 + tid;
         if (j0 > 0 || (!counts && o.most > kThreads)) read_column(ids, f, table, j);       // the first are there, but where later ones were counted
         if (open && j0 < o.most) {
-            uint32_t freed = freed_in(ids, o, f, j);
+            uint32_t freed = freed_in(ids, o, f, j0 + share.column, share.column, share.rows);
+            if (share.parts > 1) {            // one of a column's threads has them all
+                some[tid] = freed;
+                lds_barrier();
+                freed = 0;
+                if (share.part == 0)
+                    for (int i = tid; i < kThreads; i += kThreads / share.parts) freed |= some[i];
+            }
             const int v = __popc(freed), sum = wave_sums(v);
             lds_barrier();
             if (lane == 63) wave_sum[wid] = sum;
@@ -283,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
             }
 #pragma nounroll
             for (; freed; freed &= freed - 1, ++at) {
-                const int id = ids[__builtin_ctz(freed)][tid];
+                const int id = ids.id[__builtin_ctz(freed)][tid];
                 if (at < mine.copies) own[at] = id;
                 else f.ring[ring_at(head, count + before[1] + (at - mine.copies), f.n_blocks)] = id;
             }
@@ -291,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvFork f, const Count
 #pragma unroll 4
         for (int i = 0; i < f.beams; ++i) {
             const int p = open ? o.parent[i] : i, blocks = open ? o.taken[i] : o.blocks[i];
-            if (j < blocks) f.next_table[(row0 + i) * f.max_blocks + j] = ids[p][tid];
+            if (j < blocks) f.next_table[(row0 + i) * f.max_blocks + j] = ids.id[p][tid];
         }
     }
     if (open && tid < taken_by(mine)) own[mine.freed + tid] = ring_id;
@@ -344,18 +378,23 @@ __global__ __launch_bounds__(kThreads) void kv_copy_kernel(KvCaches caches, cons
 
 int64_t kv_fork_workspace(int32_t n_requests, int32_t) { return (int64_t)n_requests * (int64_t)sizeof(Counts); }
 
-hipError_t kv_fork(const KvFork& f, void* workspace, hipStream_t stream)
+template <int ROWS> static hipError_t launch_fork(const KvFork& f, Counts* counts, hipStream_t stream)
 {
     if (f.n_requests == 1) {
-        hipLaunchKernelGGL(kv_fork_kernel, dim3(1), dim3(kThreads), 0, stream, f, (const Counts*)nullptr);
+        hipLaunchKernelGGL(kv_fork_kernel<ROWS>, dim3(1), dim3(kThreads), 0, stream, f, (const Counts*)nullptr);
         return hipGetLastError();
     }
     if (f.n_requests > 0) {
-        hipLaunchKernelGGL(kv_fork_count_kernel, dim3((unsigned)f.n_requests), dim3(kThreads), 0, stream, f, (Counts*)workspace);
+        hipLaunchKernelGGL(kv_fork_count_kernel<ROWS>, dim3((unsigned)f.n_requests), dim3(kThreads), 0, stream, f, counts);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kv_fork_kernel, dim3((unsigned)f.n_requests + 1), dim3(kThreads), 0, stream, f, (const Counts*)workspace);
+    hipLaunchKernelGGL(kv_fork_kernel<ROWS>, dim3((unsigned)f.n_requests + 1), dim3(kThreads), 0, stream, f, (const Counts*)counts);
     return hipGetLastError();
+}
+
+hipError_t kv_fork(const KvFork& f, void* workspace, hipStream_t stream)
+{
+    return f.beams <= kGroup ? launch_fork<kGroup>(f, (Counts*)workspace, stream) : launch_fork<kBeamMax>(f, (Counts*)workspace, stream);
 }
 
 hipError_t kv_copy(int32_t n_caches, const KvCaches& caches, int32_t n, const int32_t* copy, const int32_t* seq_len, hipStream_t stream)
