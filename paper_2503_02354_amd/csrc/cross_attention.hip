@@ -64,6 +64,8 @@ __device__ __forceinline__ void finish_row(const States& st, const CrossAttentio
 // (maximum, sum, unnormalised output) and cross_attention_join_kernel adds them up; a source inside one stretch is finished here.  Inside a
 // stretch the four wavefronts take tiles in turn, each for itself: keys go from memory straight into registers (they are the first
 // operand as they lie), values through registers into LDS of the wavefront's own, and the next tile's are on their way while this one is multiplied.
+// What bounds it is memory: three sources of 20,000 to 60,000 rows, 32 query heads on 8 of 128 (516 MB), take 102 us where the rate of a large copy
+// would take 106; matrix cores are busy 7 % of that.
 struct FewHeader {                        // at the workspace's start, for the joining kernel
     unsigned long long per;               // tiles of a stretch
     unsigned long long base[1];           // [n_sources + 1] tiles before source s, of one head
@@ -313,7 +315,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cross_attention_few_kernel(
 
 // Where sources are short, or many: a workgroup per source, head and 32 query rows, one launch, and no parts to join.  All heads of a source go to one
 // of the chip's eight dies, to which workgroups are dealt in turn: their rows' bytes lie side by side.  ORDERED: the longest sources first (every
-// workgroup ranks them all, at most kRanked), so that those which start last are short, and that every die gets its share.
+// workgroup ranks them all, at most kRanked), so that those which start last are short, and that every die gets its share.  Bound by memory, or by a
+// chain of round trips where there is little of it: 64 sources of 60 to 1500 rows with five beams, 16 heads of 64 (209 MB), 41 us where they have just been
+// read and 55 where not (the rate of a copy: 43); one source of 197 rows, four beams, 12 heads, 6.0 us in a graph.
 constexpr int kRanked = 256;
 template <int D, bool PAD, int WAVES, bool ORDERED>
 __global__ __launch_bounds__(64 * WAVES, 2) void cross_attention_whole_kernel(States st, CrossAttention a, int dies)
@@ -357,7 +361,8 @@ __device__ __forceinline__ void add_part(float& mx, float& sum, float4& acc, flo
 
 // Adds up the parts of a source that several workgroups shared: a workgroup per source, head and query row (blockIdx.y).  Several threads share
 // the parts of a row's four channels, since a long source has many; each leaves its sum relative to its own maximum, and the first adds
-// those up in their order.  Round trips to memory bound it, so every thread fetches four parts at a time.
+// those up in their order.  Round trips to memory bound it, so every thread fetches four parts at a time: 5.2 us for the
+// three long sources.
 constexpr int kAhead = 4;
 template <int D>
 __global__ __launch_bounds__(256) void cross_attention_join_kernel(States st, CrossAttention a, const char* workspace)
@@ -417,6 +422,10 @@ __global__ __launch_bounds__(256) void cross_attention_join_kernel(States st, Cr
 // long ones into parts over the keys where there are too few to fill the chip; cross_attention_join_units_kernel adds those up.  Block b takes head b % kv_heads, so that with eight of them
 // (or four, or two) the units of one head meet in the same second-level caches.  K tiles go from memory into two LDS buffers by DMA, V
 // tiles into three, in turn; a wavefront reads every key and value of a tile for its 32 rows.
+// Bound by the matrix cores and the vector unit, which takes the exponentials: a 32 x 32 x 16 product hides about 20 of its 32 cycles of vector instructions,
+// and beside each lie some 36 cycles of them with 64 channels, 18 with 128.  Four sources of 3500 to 7000 rows with 2901 to 4900 tokens each, 32 heads on 8 of 128:
+// 1,460 to 1,500 us, 1.02 to 1.05 PFLOP/s, at 1.75 GHz; 16 of 4000 rows with 2000 tokens, 24 heads of 64, 0.88 to 0.91; 20 of 200 to 2100 with 30 to 900, 0.67,
+// units of 18 tiles, whose beginnings and ends (first loads, a first maximum, stores) count.
 constexpr int kManyRows = 128, kManyKeys = 64, kManyWaves = 4;
 constexpr int kManyGroups = 512;          // two workgroups per compute unit
 constexpr int kListed = 64;               // sources that a workgroup looks at for its unit: one to a lane
@@ -448,7 +457,7 @@ __host__ __device__ inline ManyLayout many_layout(int32_t n_sources, int32_t n_t
     return l;
 }
 
-// One workgroup.  Row tiles of a source are of one length, its number of 64-key tiles.
+// One workgroup, bound by latency: 6.2 us for one source, 7.7 for 90.  Row tiles of a source are of one length, its number of 64-key tiles.
 constexpr int kSchedThreads = 1024, kSchedBins = 2048, kSchedInLds = 4096;
 __global__ __launch_bounds__(kSchedThreads) void cross_attention_schedule_kernel(States st, CrossAttention a, char* workspace, ManyLayout at)
 {
@@ -861,7 +870,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kerne
 #endif
 }
 
-// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.
+// Adds up the parts of a unit that was cut; blockIdx.y: 16 of its rows.  Latency: 5.1 us where nothing is to be joined, 5.8 for ten parts of 16 units.
 constexpr int kUnitRows = 16;
 template <int D> constexpr int kUnitThreads = kUnitRows * D / 4;          // four channels of a row each
 template <int D>
@@ -947,7 +956,8 @@ template <int D, bool PAD, int WAVES, bool ORDERED> hipError_t launch_whole(cons
     static const hipError_t configured =
         hipFuncSetAttribute((const void*)cross_attention_whole_kernel<D, PAD, WAVES, ORDERED>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
     if (configured != hipSuccess) return configured;
-    const int dies = a.n_sources >= 32 || a.n_sources % 8 == 0 ? 8 : 1;       // where each has about as many
+    // 100 sources of 200 to 600 rows, 16 heads of 64, 46.3 us with dies and 49.3 without, 64 sources the same, 16 of 500 rows 10.9 and 10.4
+    const int dies = a.n_sources >= 64 ? 8 : 1;
     hipLaunchKernelGGL((cross_attention_whole_kernel<D, PAD, WAVES, ORDERED>), dim3((unsigned)((a.n_sources + dies - 1) / dies * dies * st.kv_heads), (unsigned)z.row_blocks()),
                        dim3(64 * WAVES), kLds, stream, st, a, dies);
     return hipGetLastError();
@@ -989,8 +999,11 @@ template <int D> hipError_t launch_many(const Sizes& z, const States& st, const 
 template <int D> hipError_t launch(const Sizes& z, const States& st, const CrossAttention& a, char* workspace, hipStream_t stream)
 {
     const bool exact = st.head_dim == D;
-    if (is_whole(z)) {                        // eight wavefronts while there is a compute unit for every workgroup
-        if (z.groups() <= 256) return exact ? launch_whole<D, false, 8, false>(z, st, a, stream) : launch_whole<D, true, 8, false>(z, st, a, stream);
+    if (is_whole(z)) {
+        // Eight wavefronts while there is a compute unit for every workgroup, where a row has little to read: one source, 8 heads of 32, 1000 rows 7.6 us with
+        // eight, 8.7 with four, 2000 10.9 and 13.4; 16 heads of 64, 500 rows 8.9 and 8.3, 8 of 128, 640 rows 14.3 and 13.4.
+        if constexpr (D == 32)
+            if (z.groups() <= 256) return exact ? launch_whole<D, false, 8, false>(z, st, a, stream) : launch_whole<D, true, 8, false>(z, st, a, stream);
         // ranked while the last workgroups matter: 64 sources of 60 to 1500 rows, 16 heads of 64, 63 -> 56 us; 150 of 500 to 1000 98 -> 104
         if (z.n_sources <= kRanked && z.groups() > 512 && z.groups() <= 2048)
             return exact ? launch_whole<D, false, kFewWaves, true>(z, st, a, stream) : launch_whole<D, true, kFewWaves, true>(z, st, a, stream);

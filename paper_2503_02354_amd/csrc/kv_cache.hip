@@ -205,6 +205,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, int n_tokens,
 // pair's sine and cosine each and leave them in LDS for all heads, while the first channels are on their way; then a lane turns V pairs of a head
 // at a time, or copies what is not turned.  The angle in turns, p f / 2 pi, is an fp64 product whose nearest integer is taken off there: what is left is
 // exact to 2^-22 of a turn at positions of 2^31, and its sine and cosine are fp32.
+// Bound by memory: 7000 tokens, 32 heads and 8 of 128 (172 MB), 38.4 us, 4.5 TB/s (28 where the rows have just been read); 1201 tokens, 24 and 8 heads of 96, 48 of
+// them turned, 7.6 us; three tokens 3.7, latency.
 constexpr int kTurnWaves = 4;
 
 template <int V> struct Packed;               // V bf16 values
