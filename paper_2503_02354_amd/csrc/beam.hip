@@ -113,7 +113,10 @@ __device__ __forceinline__ uint32_t wave_min(uint32_t v) { return ~wave_max(~v);
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kPerLane = 16, kStep = 64 * kPerLane, kSlack = 32, kGrow = 64;
 constexpr int kList = kBeamPicksMax + kGrow + kStep;
 static_assert(kBeamPicksMax + kGrow <= 128 && kWaves * 128 <= kList, "two keys of a list to a lane, all lists in the place of one");
-struct RowPart {                              // the workspace: [rows][parts] of these, then as many lists of `picks` keys
+// The workspace: [rows][parts] of these, then a request's lists of keys across each other: all parts' best, all parts' second, ...; an odd number of keys from
+// one to the next, so that no thread of those that share them out meets a list twice before all others have.
+__host__ __device__ constexpr int pitch_of(int beams, int parts) { return beams * parts | 1; }
+struct RowPart {
     double sum;
     float top;
     int32_t pad;
@@ -235,11 +238,10 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
 #pragma unroll
             for (int e = 0; e < kPerLane; ++e) x[e] = x[e] == x[e] ? x[e] : -INFINITY;
     };
-    auto most_of = [&](const float (&x)[kPerLane]) __attribute__((always_inline)) {
-        float most = x[0];
+    auto most_of = [&](const float (&x)[kPerLane], float (&four)[kPerLane / 4]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 1; e + 1 < kPerLane; e += 2) most = max3(most, x[e], x[e + 1]);
-        return max3(most, x[kPerLane - 1], x[0]);
+        for (int g = 0; g < kPerLane / 4; ++g) four[g] = max3(max3(x[4 * g], x[4 * g + 1], x[4 * g + 2]), x[4 * g + 3], x[4 * g + 3]);
+        return max3(max3(four[0], four[1], four[2]), four[3], four[3]);
     };
     auto weigh = [&](const float (&x)[kPerLane], float most) __attribute__((always_inline)) {
         const float m_new = max3(m, most, m), c = offset_of(m_new);
@@ -259,17 +261,20 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
     n = 0;
     uint32_t low = kLeast;                    // what the list's logits lie at or above
     float threshold = -INFINITY;              // what is wanted lies above
-    auto put = [&](const float (&x)[kPerLane], long long at) __attribute__((always_inline)) {
+    auto put = [&](const float (&x)[kPerLane], const float (&four)[kPerLane / 4], long long at) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < kPerLane; ++e) {
-            const bool take = x[e] > threshold;
-            const unsigned long long b = __ballot(take);
-            if (b) {
-                const uint32_t i = (uint32_t)((at + e / W * 64 + lane) * W + e % W);
-                if (take) list[n + __popcll(b & ((1ull << lane) - 1))] = (unsigned long long)key_of(x[e]) << 32 | (uint32_t)~i;
-                n += __popcll(b);
-            }
-        }
+        for (int g = 0; g < kPerLane / 4; ++g)
+            if (__any(four[g] > threshold))
+#pragma unroll
+                for (int e = 4 * g; e < 4 * g + 4; ++e) {
+                    const bool take = x[e] > threshold;
+                    const unsigned long long b = __ballot(take);
+                    if (b) {
+                        const uint32_t i = (uint32_t)((at + e / W * 64 + lane) * W + e % W);
+                        if (take) list[n + __popcll(b & ((1ull << lane) - 1))] = (unsigned long long)key_of(x[e]) << 32 | (uint32_t)~i;
+                        n += __popcll(b);
+                    }
+                }
         if (n > picks + kGrow) {
             n = cut_list(list, n, picks, low);
             threshold = fmaxf(threshold, logit_of(low));
@@ -295,7 +300,8 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
         float x[kPerLane];
         unpack(x, from, at);
         fetch(from, at + kDepth * kStride);
-        const float most = most_of(x);
+        float four[kPerLane / 4];
+        const float most = most_of(x, four);
         if (step == 0) {                      // the lanes' maxima stand for the first step
             const uint32_t key[1] = {most > -INFINITY ? key_of(most) : 0u};
             const uint32_t least = wave_min(key[0]), high = wave_max(key[0]), mine = least ? reached(key, share, share / 2, least, high) : 0u;
@@ -306,7 +312,7 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
         } else weigh(x, most);
         const uint32_t q = all_reach();
         if (q) threshold = fmaxf(threshold, below(q));
-        if (__any(most > threshold)) put(x, at);
+        if (__any(most > threshold)) put(x, four, at);
         if (step > 0 && (step & (step + 1)) == 0 && n >= share) tell();
         at += kStride;
         ++step;
@@ -394,7 +400,9 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
     for (int i = 0; i < 2; ++i)
         if (own[i]) joined[ahead + i * 64 + lane] = own[i];
     __syncthreads();
-    unsigned long long* const out = lists + (size_t)blockIdx.x * s.picks;
+    const int64_t request = row / s.beams;
+    const int pitch = pitch_of(s.beams, parts);
+    unsigned long long* const out = lists + request * pitch * s.picks + (blockIdx.x - request * s.beams * parts);
     if (tid == kThreads - 1) {
         float t = tops[0];
         for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
@@ -408,17 +416,20 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
         int place = 0;
 #pragma unroll 4
         for (int j = 0; j < all; ++j) place += joined[j] > key;
-        if (place < s.picks) out[place] = key;
+        if (place < s.picks) out[(int64_t)place * pitch] = key;
     }
-    for (int i = all + tid; i < s.picks; i += kThreads) out[i] = 0;
+    for (int i = all + tid; i < s.picks; i += kThreads) out[(int64_t)i * pitch] = 0;
 }
 
 // ---- requests -----------------------------------------------------------------------------------------------------
 // A workgroup per request: the rows' sums, then the best of all lists.  From a score on that enough of the threads' best reach, candidates are listed and
-// counted against each other; where that is too many (an order that no list of a row has by chance), they are found one after the other.
-// Bound by latency, that of its instructions' first use among it, so its loops are left as they are: 6.3 us for one request of four beams, 7.9 for 64 of eight.
-constexpr int kMeet = 512, kHeld = 2048;      // candidates that are listed; a request's keys, which are kept in LDS
-static_assert(kBeamMax * kBeamPicksMax <= kHeld, "one part of a row at least");
+// counted against each other.  Where that is too many, since few lists have the best of all, the score is searched for among all candidates; where those that
+// are equal are too many still (rows of one value), they are found one after the other, at 8 us each.
+// Bound by latency, that of its instructions' first use among it, so its loops are left as they are: 6.3 us for one request of four beams, 7.9 for 64 of eight,
+// 10 to 12 for 2048 keys.
+constexpr int kMeet = 512, kKeys = 2048;      // candidates that are listed; a request's keys, which are kept in LDS
+static_assert(kBeamMax * kBeamPicksMax <= kKeys, "one part of a row at least");
+constexpr int kHeld = (kKeys + kBeamPicksMax + kThreads - 1) / kThreads * kThreads;       // with one of every pitch that is none
 struct Candidate {
     unsigned long long score;                 // fp64 as an integer that grows with it; 0: none
     unsigned long long key;                   // of the row
@@ -460,8 +471,8 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
     __shared__ int n_met;
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
     const size_t first = (size_t)r * s.beams;
-    const int per_row = parts * s.picks, n = s.beams * per_row;
-    const unsigned long long* const keys = lists + first * per_row;
+    const int segments = s.beams * parts, pitch = pitch_of(s.beams, parts), n = pitch * s.picks;
+    const unsigned long long* const keys = lists + (size_t)r * n;
     {
         const int b = tid / kLanes, sub = tid % kLanes;
         RowPart v{0, -INFINITY, 0};
@@ -513,26 +524,28 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
     }
     if (tid == 0) n_met = 0;
     __syncthreads();
-    // f(candidate) for all of this thread's: rows by wavefronts, a row's keys by lanes, and the row itself where it has ended.  known: not the first time
+    // f(candidate) for all of this thread's, and the row itself where it has ended.  known: not the first time
+    const float per_part = 1.f / (float)parts;
     auto each = [&](auto known, auto f) __attribute__((always_inline)) {
+        if (tid < s.beams && row_state[tid] == 2) f(Candidate{order_of(row_score[tid]), 0, tid});
+        int segment = tid % pitch;
+        const int step = kThreads % pitch;
 #pragma nounroll
-        for (int b = wid; b < s.beams; b += kWaves) {
-            const int state = row_state[b];
-            const float top = row_top[b];
-            const double base = row_score[b], less = row_log[b];
-            const bool huge = is_huge(top);
-            if (state == 2 && lane == 0) f(Candidate{order_of(base), 0, b});
-            if (state != 1) continue;
-#pragma nounroll
-            for (int i = b * per_row + lane; i < (b + 1) * per_row; i += 64) {
-                const unsigned long long key = held[i];
-                const float x = logit_of((uint32_t)(key >> 32));
-                unsigned long long score = 0;
-                if (known) score = scores[i];
-                else if (key != 0 && (x == top || top < INFINITY)) score = order_of(base + ((!huge ? (double)x : x == top ? 0. : (double)x - (double)top) - less));
-                if (!known) scores[i] = score;
-                if (score) f(Candidate{score, key, b});
+        for (int i = tid; i < n; i += kThreads) {
+            const bool is = segment < segments;
+            const int b = is ? (int)(((float)segment + 0.5f) * per_part) : 0;         // segment / parts: both are below 2^12
+            segment += step;
+            if (segment >= pitch) segment -= pitch;
+            const unsigned long long key = held[i];
+            unsigned long long score = 0;
+            if (known) score = scores[i];
+            else {
+                const float x = logit_of((uint32_t)(key >> 32)), top = row_top[b];
+                const double of = is_huge(top) ? x == top ? 0. : (double)x - (double)top : (double)x;
+                if (is & (row_state[b] == 1) & (key != 0) & ((x == top) | (top < INFINITY))) score = order_of(row_score[b] + (of - row_log[b]));
+                scores[i] = score;
             }
+            if (score) f(Candidate{score, key, b});
         }
     };
     unsigned long long mine = 0;
@@ -546,13 +559,38 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
         const uint32_t most = max(max(key[0], key[1]), max(key[2], key[3]));
         low = max(reached(key, s.picks, 24, wave_min(most), wave_max(most)), 1u);             // no score's upper half is 0
     }
-    each(std::true_type(), [&](const Candidate& c) {
-        if ((uint32_t)(c.score >> 32) < low) return;
-        const int at = atomicAdd(&n_met, 1);
-        if (at < kMeet) met_score[at] = c.score, met_key[at] = c.key, met_row[at] = c.row;
-    });
-    __syncthreads();
-    const int all = n_met;
+    auto list = [&]() __attribute__((always_inline)) {
+        each(std::true_type(), [&](const Candidate& c) {
+            if ((uint32_t)(c.score >> 32) < low) return;
+            const int at = atomicAdd(&n_met, 1);
+            if (at < kMeet) met_score[at] = c.score, met_key[at] = c.key, met_row[at] = c.row;
+        });
+        __syncthreads();
+        return n_met;
+    };
+    int all = list();
+    if (all > kMeet) {                        // one list has most of the best: a threshold that all candidates are counted against
+        uint32_t high = 0;
+        for (int i = 0; i < kThreads; ++i) high = max(high, best[i]);
+#pragma nounroll
+        while (all > kMeet && low < high) {
+            const uint32_t mid = low + (high - low) / 2 + 1;
+            int more = 0;
+            each(std::true_type(), [&](const Candidate& c) { more += (uint32_t)(c.score >> 32) >= mid; });
+            __syncthreads();
+            if (tid == 0) n_met = 0;
+            __syncthreads();
+            if (more) atomicAdd(&n_met, more);
+            __syncthreads();
+            const int now = n_met;
+            if (now >= s.picks) low = mid, all = now;
+            else high = mid - 1;
+        }
+        __syncthreads();
+        if (tid == 0) n_met = 0;
+        __syncthreads();
+        all = list();
+    }
     if (all <= kMeet) {
         for (int i = tid; i < max(all, s.picks); i += kThreads) {
             Candidate c{0, 0, 0};
@@ -593,7 +631,7 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
 // keys.  512 rows of 128,000 in bf16, 16 picks, 512 / 768 / 1024 / 2048 workgroups 54.9 / 45.0 / 45.0 / 52.6 us; 400 rows, 8 picks 41 / 41 / 47 / 49.
 int row_parts(int64_t rows, int32_t beams, int32_t picks, int32_t vocab)
 {
-    const int64_t fill = (768 + rows - 1) / std::max<int64_t>(rows, 1), length = ((int64_t)vocab + 4095) / 4096, held = kHeld / ((int64_t)beams * picks);
+    const int64_t fill = (768 + rows - 1) / std::max<int64_t>(rows, 1), length = ((int64_t)vocab + 4095) / 4096, held = kKeys / ((int64_t)beams * picks);
     return (int)std::max<int64_t>(1, std::min(std::min(fill, length), held));
 }
 
@@ -602,7 +640,8 @@ int row_parts(int64_t rows, int32_t beams, int32_t picks, int32_t vocab)
 int64_t beam_workspace(int32_t n_requests, int32_t beams, int32_t picks, int32_t vocab)
 {
     const int64_t rows = (int64_t)n_requests * beams;
-    return rows * row_parts(rows, beams, picks, vocab) * (int64_t)(sizeof(RowPart) + 8 * picks);
+    const int parts = row_parts(rows, beams, picks, vocab);
+    return rows * parts * (int64_t)sizeof(RowPart) + (int64_t)n_requests * pitch_of(beams, parts) * picks * 8;
 }
 
 hipError_t beam_select(int dtype, const BeamSelection& s, void* workspace, hipStream_t stream)

@@ -561,6 +561,24 @@ def test_select_large_logits(B, dtype):
         _check_select(B, to(x), np.zeros(12, np.float32), None, 12, 40, 2, dtype)
 
 
+@pytest.mark.parametrize("beams,picks", [(1, 64), (2, 64), (3, 64), (1, 40), (7, 50), (32, 64)])
+def test_select_best_in_few_places(B, beams, picks):
+    """Many picks of few rows: random ones, all in one part of a row, all in one row, a part's best spread over the others'."""
+    rng = np.random.default_rng(beams + picks)
+    for vocab in (3000, 130000 if beams < 8 else 20000):
+        x = 3 * rng.standard_normal((2 * beams, vocab))
+        score = -rng.uniform(0, 1, 2 * beams).astype(np.float32)
+        for bits, dtype in ((_bf16(x), "bf16"), (x.astype(np.float32), "f32")):
+            _check_select(B, bits, score, None, beams, picks, 2, dtype)
+            _check_select(B, bits, score - 50 * (np.arange(2 * beams) % beams != 0).astype(np.float32), None, beams, picks, 2, dtype)
+        rising = (np.arange(vocab) / 1000.0 + np.arange(2 * beams)[:, None] % beams).astype(np.float32)
+        _check_select(B, rising, score, None, beams, picks, 2)
+        _check_select(B, rising[:, ::-1].copy(), score, None, beams, picks, 2)
+        one = x.astype(np.float32)
+        one[:, vocab // 2:vocab // 2 + 100] += 20
+        _check_select(B, one, score, None, beams, picks, 2)
+
+
 def test_select_misaligned_rows(B):
     """Rows that begin anywhere: odd strides and bases."""
     import torch
