@@ -304,11 +304,13 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
         const float most = most_of(x, four);
         if (step == 0) {                      // the lanes' maxima stand for the first step
             const uint32_t key[1] = {most > -INFINITY ? key_of(most) : 0u};
-            const uint32_t least = wave_min(key[0]), high = wave_max(key[0]), mine = least ? reached(key, share, share / 2, least, high) : 0u;
+            const uint32_t least = wave_min(key[0] - 1) + 1, high = wave_max(key[0]);       // of those that are there, `some`
+            const int some = count_of(key[0] != 0);
+            const uint32_t mine = some >= share ? reached(key, share, share / 2, least, high) : 0u;
             if (lane == 0) quarter[wid] = mine;
             weigh(x, most);
             __syncthreads();
-            if (all_reach() == 0 && least) threshold = below(reached(key, picks, picks, least, high));
+            if (all_reach() == 0 && some >= picks) threshold = below(reached(key, picks, picks, least, high));
         } else weigh(x, most);
         const uint32_t q = all_reach();
         if (q) threshold = fmaxf(threshold, below(q));
@@ -469,7 +471,7 @@ __global__ __launch_bounds__(kThreads) void beam_meet_kernel(BeamSelection s, in
     __shared__ int met_row[kMeet];
     __shared__ Candidate found[kThreads];
     __shared__ int n_met;
-    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, r = blockIdx.x;
     const size_t first = (size_t)r * s.beams;
     const int segments = s.beams * parts, pitch = pitch_of(s.beams, parts), n = pitch * s.picks;
     const unsigned long long* const keys = lists + (size_t)r * n;
