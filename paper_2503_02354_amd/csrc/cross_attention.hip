@@ -915,15 +915,15 @@ struct Sizes {                            // what the choice of a kernel goes by
 bool is_few(const Sizes& z) { return z.rows() <= kFewRows; }
 // Whether a workgroup of its own for every source and head is faster than equal stretches and a join, by the longest source and the number of
 // workgroups.  Single tokens of four beams in a graph, whole / stretches, us, sources of equal lengths, then of lengths from one up: 16 heads of 64, 1 source
-// 1000 rows 11.4 / 13.6, 2000 18.2 / 15.8; 4 sources 2000 19.4 / 20.1 and 19.2 / 16.7; 8 sources 2000 19.8 / 23.7 and 19.4 / 20.4, 4000 37.5 / 35.1 and
-// 32.8 / 23.9; 16 sources 2000 27.4 / 35.5 and 20.6 / 25.0, 4000 64.7 / 69.1 and 44.9 / 40.6; 32 sources 2000 64.0 / 70.8 and 39.2 / 55.8, 4000 125 / 120 and
-// 100 / 81; 64 sources 2000 118 / 120 and 72 / 83.  8 heads of 128: 8 sources 500 rows 13.6 / 15.5, 1000 21.0 / 16.4; 16 sources 1000 21.4 / 21.2 and 20.0 /
-// 27.8, 2000 37.1 / 32.6; 32 sources 1000 26.8 / 31.8 and 21.8 / 38.1, 4000 116 / 118 and 102 / 70; 64 sources 1000 60.4 / 62.6 and 37.0 / 56.2.
-// Chunks of tokens, a workgroup for 32 rows of each / units, listed or scheduled, whichever is faster (us), 16 heads of 64: one source 40 tokens 1000 rows
-// 12.2 / 17.7, 4000 33.8 / 22.9, 300 tokens 1000 rows 12.8 / 19.6, 1000 tokens (512 workgroups) 500 rows 13.6 / 13.2; 4 sources 100 tokens 2000 rows 21.4 / 26.0,
-// 4000 35.7 / 32.8; 300 tokens (640) 200 rows 11.6 / 10.1, 1000 28.6 / 21.3; 16 sources 300 tokens 1000 rows 95 / 36.  32 heads on 8 of 128: one source 100 tokens
-// 1000 rows 21.7 / 26.6, 2000 35.4 / 29.7; 300 tokens (304) 500 rows 22.0 / 17.5.  Above kListed sources units are scheduled, which costs more: 640
-// workgroups 1000 rows of 64 28.6 / 29.8, 1024 200 rows 15.7 / 18.7, 500 rows 23.0 / 22.2.
+// 1000 rows 11.0 / 13.5, 2000 17.9 / 15.6; 4 sources 2000 19.0 / 19.7 and 18.9 / 16.0; 8 sources 2000 19.3 / 23.7 and 18.9 / 20.4, 4000 50.5 / 41.2 and
+// 32.5 / 23.9; 16 sources 2000 32.4 / 43.1 and 19.5 / 25.0, 4000 60.1 / 68.8 and 50.5 / 45.2; 32 sources 2000 61.7 / 69.3 and 48.3 / 55.0, 4000 120 / 121 and
+// 93 / 77; 64 sources 2000 118 / 119 and 71 / 99.  8 heads of 128: 8 sources 500 rows 12.9 / 15.0, 1000 20.0 / 16.1; 16 sources 1000 20.3 / 21.2 and 19.7 /
+// 24.3, 2000 50.4 / 38.9; 32 sources 1000 33.1 / 37.8 and 20.9 / 41.9, 4000 113 / 117 and 96 / 70; 64 sources 1000 61.2 / 62.5 and 44.1 / 53.5.
+// Chunks of tokens, a workgroup for 32 rows of each / units, listed or scheduled, 16 heads of 64: one source 40 tokens 1000 rows 11.6 / 17.5, 4000 33.0 / 22.9,
+// 300 tokens 1000 rows 12.1 / 19.4, 1000 tokens (512 workgroups) 500 rows 13.4 / 13.1; 4 sources 100 tokens 2000 rows 20.6 / 25.9, 4000 34.1 / 33.1; 300 tokens
+// (640) 200 rows 11.3 / 9.8, 1000 28.0 / 20.8; 16 sources 300 tokens 1000 rows 103 / 38.  32 heads on 8 of 128: one source 100 tokens 1000 rows 20.1 / 26.1, 2000
+// 33.5 / 29.2; 300 tokens (304) 500 rows 21.9 / 17.4.  Above kListed sources units are scheduled, which costs more: 70 sources of 33 tokens (980) 200 rows of 64
+// 18.3 / 19.5, 500 rows 26.2 / 23.9.
 bool is_whole(const Sizes& z)
 {
     const int64_t longest = z.max_rows * z.dim, groups = z.groups();
@@ -945,7 +945,7 @@ bool is_listed(const Sizes& z, int64_t n_tokens, int64_t n_rows)
 {
     if (z.n_sources > kListed) return false;
     auto tiles = [](int64_t rows) { return (rows + kManyKeys - 1) / kManyKeys; };
-    const int64_t share = most_units(z, n_tokens) * z.kv_heads * tiles(std::min(z.max_rows, n_rows / z.n_sources)) / kManyGroups;
+    const int64_t share = most_units(z, n_tokens) * z.kv_heads * tiles(std::min(z.max_rows, n_rows / std::max<int64_t>(z.n_sources, 1))) / kManyGroups;
     return tiles(z.max_rows) - std::max<int64_t>(8, 2 * share) <= 12;
 }
 
@@ -1020,6 +1020,7 @@ int64_t cross_attention_workspace(int32_t n_sources, int32_t n_tokens, int32_t m
     const int dim = padded_dim(head_dim);
     const Sizes z{n_sources, max_new, max_rows, heads, kv_heads, dim};
     if (is_whole(z)) return 0;
+    if (!is_few(z) && is_listed(z, n_tokens, 0)) return 0;      // and so with any number of rows
     if (is_few(z)) return few_header_bytes(n_sources) + (int64_t)kMostFewGroups * 2 * (2 * kFewRows + kFewRows * dim) * 4;
     return many_layout(n_sources, n_tokens, heads, kv_heads, dim).end;
 }
