@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256) void cross_attention_join_kernel(States st, Cr
 // tiles into three, in turn; a wavefront reads every key and value of a tile for its 32 rows.
 // Bound by the matrix cores and the vector unit, which takes the exponentials: a 32 x 32 x 16 product hides about 20 of its 32 cycles of vector instructions,
 // and beside each lie some 36 cycles of them with 64 channels, 18 with 128.  Four sources of 3500 to 7000 rows with 2901 to 4900 tokens each, 32 heads on 8 of 128:
-// 1,460 to 1,500 us, 1.02 to 1.05 PFLOP/s, at 1.75 GHz; 16 of 4000 rows with 2000 tokens, 24 heads of 64, 0.88 to 0.91; 20 of 200 to 2100 with 30 to 900, 0.67,
+// 1,460 to 1,620 us by card, 0.94 to 1.04 PFLOP/s, at 1.66 to 1.75 GHz; 16 of 4000 rows with 2000 tokens, 24 heads of 64, 0.88 to 0.91; 20 of 200 to 2100 with 30 to 900, 0.67,
 // units of 18 tiles, whose beginnings and ends (first loads, a first maximum, stores) count.
 constexpr int kManyRows = 128, kManyKeys = 64, kManyWaves = 4;
 constexpr int kManyGroups = 512;          // two workgroups per compute unit
