@@ -357,6 +357,121 @@ def test_cross_limits_of_sizes(B):
         assert (got[c.off[last]:c.off[last + 1]] == 0).all()
 
 
+# Sizes at which units of 128 query rows are taken: more than 256 workgroups of 32 rows.  A limit of 50000 rows has them scheduled and cut, and single tokens
+# split into stretches; without it short sources' units are found by their workgroups.
+LIMITS = [None, 50000]
+
+
+@pytest.mark.parametrize("max_rows", LIMITS)
+@pytest.mark.parametrize("heads,kv,dim", [(16, 8, 64), (32, 8, 128), (24, 12, 96), (10, 10, 80), (16, 8, 24), (9, 9, 40), (8, 8, 8), (32, 32, 32)])
+def test_cross_units(B, heads, kv, dim, max_rows):
+    for sources in ([(300, 150), (1, 90), (129, 1), (64, 257), (0, 70), (65, 0), (1064, 130), (63, 33)], [(127, 500), (128, 300), (640, 129)]):
+        for hidden in (0.0, 0.2):
+            c = Cross(sources, heads, kv, dim, seed=len(sources) + dim, hidden=hidden)
+            c.check(*c.run(B, max_rows=max_rows))
+
+
+@pytest.mark.parametrize("max_rows", LIMITS)
+@pytest.mark.parametrize("heads,kv,dim,m", [(32, 8, 128, 150), (16, 16, 64, 150), (8, 2, 128, 1), (4, 4, 64, 5)])
+def test_cross_hidden_rows_by_form(B, heads, kv, dim, m, max_rows):
+    """As test_cross_hidden_rows, in the forms that its sizes do not take."""
+    c = Cross([(300, m), (200, m), (64, m), (1, m)], heads, kv, dim, seed=m, hidden=0.1)
+    c.seen[c.first[0]:c.first[0] + 300] = 0
+    c.seen[c.first[0] + 217] = 9
+    c.seen[c.first[1]:c.first[1] + 200] = 0
+    c.seen[c.first[2]:c.first[2] + 32] = 0
+    got, logs = c.run(B, max_rows=max_rows)
+    c.check(got, logs)
+    for value in (0x7F80, 0xFF80, 0x7FC0, 0x7F7F, 0xFF7F):
+        c.kv_bits[:, np.flatnonzero(c.seen == 0)] = value
+        again, logs_again = c.run(B, max_rows=max_rows)
+        assert np.array_equal(got, again) and np.array_equal(logs, logs_again)
+
+
+@pytest.mark.parametrize("max_rows", LIMITS)
+@pytest.mark.parametrize("heads,kv,dim,n,m", [(16, 8, 64, 300, 400), (32, 8, 128, 1500, 400), (8, 2, 128, 300, 1), (6, 6, 64, 300, 4)])
+def test_cross_infinite_scores_by_form(B, heads, kv, dim, n, m, max_rows):
+    """Scores of -inf and NaN, as test_cross_infinite_scores, in the forms that its sizes do not take; and scores of some hundreds."""
+    c = Cross([(n, m), (50, m)], heads, kv, dim, seed=m)
+    c.q[:] = _bf16(np.abs(T.bf16_to_f64(c.q)) + 0.01)
+    f, group = int(c.first[0]), heads // kv
+    c.kv_bits[0, [f + 3, f + n - 7], 0] = 0xFF80
+    got, logs = c.run(B, max_rows=max_rows)
+    seen = np.ones(c.rows, np.uint8)
+    seen[[f + 3, f + n - 7]] = 0
+    out, lse, _, _ = T.cross(T.bf16_to_f64(c.q[:, :group]), *T.bf16_to_f64(c.kv_bits[:, :, :1]), c.off, c.first, c.length, 1, c.scale, seen)
+    # probabilities of at most 1 rounded to bf16 and values of a few units: 2^-8 of each, 0.02 at most
+    assert (np.abs(T.bf16_to_f64(got[:, :group]) - out) <= 0.02).all() and np.allclose(logs[:, :group], lse, atol=2e-4)
+    keep = c.kv_bits.copy()
+    c.kv_bits[0, int(c.first[1]):int(c.first[1]) + 50, 1] = 0xFF80
+    got, logs = c.run(B, max_rows=max_rows)
+    rows = slice(group, 2 * group)
+    assert (got[m:, rows] == 0).all() and (logs[m:, rows] == -np.inf).all() and (T.bf16_to_f64(got[m:, :group]) != 0).any()
+    c.kv_bits[:] = keep
+    c.kv_bits[0, f + n - 1, 0] = 0x7FC0
+    got, logs = c.run(B, max_rows=max_rows)
+    assert np.isnan(T.bf16_to_f64(got[:m, :group])).all() and np.isnan(logs[:m, :group]).all()
+    assert np.isfinite(T.bf16_to_f64(got[:m, group:])).all() and np.isfinite(T.bf16_to_f64(got[m:])).all()
+    c = Cross([(n, m), (200, m)], heads, kv, dim, seed=1, sharp=40.0, scale=0.5)
+    got, logs = c.run(B, max_rows=max_rows)
+    out, lse, size, _ = T.cross(T.bf16_to_f64(c.q), *T.bf16_to_f64(c.kv_bits), c.off, c.first, c.length, 1, c.scale)
+    # as in test_cross_sharp_and_flat_scores
+    assert (np.abs(T.bf16_to_f64(got) - out) <= 2.0 ** -8 * np.abs(out) + (2.0 ** -8 + 0.026) * size + 1e-30).all()
+    assert (np.abs(logs - lse) <= 0.013 + 1e-6 * np.abs(lse)).all()
+
+
+@pytest.mark.parametrize("max_rows", LIMITS)
+def test_cross_large_values_and_limits_by_form(B, max_rows):
+    """Values of 2^110; a maximum that rises with every row; scales of zero and below; max_new; rows of no source; no lse."""
+    for heads, kv, m in ((16, 8, 300), (3, 3, 1)):
+        c = Cross([(1200, m), (9, m)], heads, kv, 64, seed=m, scale=0.0)
+        c.kv_bits[1] = _bf16(np.full(c.kv_bits[1].shape, 2.0 ** 110))
+        assert (T.bf16_to_f64(c.run(B, max_rows=max_rows)[0]) == 2.0 ** 110).all()
+        for scale in (0.0, -0.2):
+            c = Cross([(400, m), (300, m)], heads, kv, 64, seed=2, scale=scale)
+            c.check(*c.run(B, max_rows=max_rows))
+        for sign in (1.0, -1.0):
+            c = Cross([(700, m), (280, m)], heads, kv, 64, seed=3)
+            c.q[:] = _bf16(np.ones_like(c.q, np.float64))
+            for f, n in zip(c.first, c.length):
+                c.kv_bits[0, f:f + n] = _bf16(sign * np.arange(n)[:, None, None] / 64.0 * np.ones((n, kv, 64)))
+            c.check(*c.run(B, max_rows=max_rows))
+        c = Cross([(300, m), (200, m + 9), (10, 3)], heads, kv, 64, seed=4)
+        got, logs = c.run(B, max_new=m, max_rows=max_rows, extra=3)
+        c.check(got, logs, max_new=m, max_rows=max_rows)
+        assert np.array_equal(got, c.run(B, max_new=m, max_rows=max_rows, lse=False)[0])
+
+
+@pytest.mark.parametrize("max_rows", [1200, 50000])
+def test_cross_units_in_graphs(B, max_rows):
+    """Captured and replayed over changed lengths, eager work between: every replay gives what an eager call gives."""
+    import torch
+    c = Cross([(700, 200), (300, 300), (1200, 90)], 16, 8, 64, seed=11)
+    both, q = _dev(c.kv_bits.transpose(1, 0, 2, 3)), _dev(c.q)
+    st = B.coe_states(1, c.rows, 8, 64, both.data_ptr(), both[:, 1].data_ptr(), 1024, 64, 1024, 64, 0)
+    need = B.coe_cross_attention_workspace(3, len(c.q), c.most, max_rows, 16, 8, 64)
+    work, other = (torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(2))
+    d = [_dev(a) for a in (c.off, c.first, c.length)]
+    out, want = (torch.zeros(c.q.shape, dtype=torch.int16, device="cuda") for _ in range(2))
+
+    def call(to, room):
+        B.coe_cross_attention(st, 3, len(c.q), 1, c.most, max_rows, 16, c.scale, q.data_ptr(), 1024, 64, *(t.data_ptr() for t in d), to.data_ptr(), 1024, 64, 0, room.data_ptr(), need,
+                              _stream())
+    call(out, work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, work)
+    for lengths in ([700, 300, 1200], [1, 0, 40], [699, 300, 1130], [700, 300, 1200]):
+        d[2].copy_(torch.tensor(lengths, dtype=torch.int32))
+        out.zero_()
+        graph.replay()
+        call(want, other)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        torch.randn(1000, device="cuda").sum().item()
+
+
 def test_cross_longest_sources_first(B):
     """Between one and a few workgroups to a place on the chip sources are ranked by length: equal ones, empty ones, ones without queries among them."""
     rng = np.random.default_rng(12)
@@ -383,10 +498,12 @@ def test_cross_most_sources(B):
     c.check(*c.run(B))
 
 
-@pytest.mark.parametrize("sources,max_rows", [([(9000, 2), (30, 3), (500, 1)], 9000), ([(90, 2), (30, 3), (50, 1)], 90), ([(2000, 200), (3000, 90), (64, 300)], 3000), ([(60, 60), (33, 40), (9, 50)], 60)])
-def test_cross_offsets_that_are_no_offsets(B, sources, max_rows):
+@pytest.mark.parametrize("heads,sources,max_rows", [
+    (4, [(9000, 2), (30, 3), (500, 1)], 9000), (4, [(90, 2), (30, 3), (50, 1)], 90), (4, [(2000, 200), (3000, 90), (64, 300)], 3000), (4, [(60, 60), (33, 40), (9, 50)], 60),
+    (16, [(600, 200), (700, 90), (64, 300)], 700), (16, [(2000, 200), (3000, 90), (64, 300)], 50000), (2, [(2000, 200), (3000, 90), (64, 300)], 50000)])
+def test_cross_offsets_that_are_no_offsets(B, heads, sources, max_rows):
     """q_off that runs backwards, outside q or over itself: nothing beside q's rows is touched, and the call ends."""
-    c = Cross(sources, 4, 2, 64, seed=1)
+    c = Cross(sources, heads, heads // 2, 64, seed=1)
     tokens, good = int(c.off[-1]), c.off.copy()
     for off in ([tokens, tokens // 2, 0, -5], [0, tokens, 0, tokens], [-7, 2 ** 31 - 1, -2 ** 31, tokens], [0, 1, 2 ** 31 - 1, 3], [tokens, tokens, tokens, 0]):
         c.off = np.asarray(off, np.int32)
