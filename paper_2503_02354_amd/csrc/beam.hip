@@ -325,7 +325,6 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
         go(next[0]);
         if (kDepth > 1 && at < end) go(next[kDepth - 1]);
     }
-    if (step > 2 && n >= share) tell();
     // the lanes' sums
     if (SAFE && m > -INFINITY && !is_huge(m)) s *= exp2_fast(__builtin_fmaf(m, kLog2e, offset_of(m)));      // they were relative to e^m
     float wave_top = m;

@@ -315,12 +315,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cross_attention_few_kernel(
 
 // Where sources are short, or many: a workgroup per source, head and 32 query rows, one launch, and no parts to join.  All heads of a source go to one
 // of the chip's eight dies, to which workgroups are dealt in turn: their rows' bytes lie side by side.  ORDERED: the longest sources first (every
-// workgroup ranks them all, at most kRanked), so that those which start last are short, and that every die gets its share.  Bound by memory, or by a
+// workgroup ranks them all, at most kRanked), so that those which start last are short, and that every die gets its share; each second round of
+// workgroups (one to a compute unit) the other way round, so that every unit gets long and short ones.  Bound by memory, or by a
 // chain of round trips where there is little of it: 64 sources of 60 to 1500 rows with five beams, 16 heads of 64 (209 MB), 41 us where they have just been
 // read and 55 where not (the rate of a copy: 43); one source of 197 rows, four beams, 12 heads, 6.0 us in a graph.
 constexpr int kRanked = 256;
 template <int D, bool PAD, int WAVES, bool ORDERED>
-__global__ __launch_bounds__(64 * WAVES, 2) void cross_attention_whole_kernel(States st, CrossAttention a, int dies)
+__global__ __launch_bounds__(64 * WAVES, 2) void cross_attention_whole_kernel(States st, CrossAttention a, int dies, int per_round)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     extern __shared__ __attribute__((aligned(4096))) char lds[];
@@ -329,17 +330,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cross_attention_whole_kernel(St
     if (s >= a.n_sources) return;
     Source o;
     if (ORDERED) {
-        int4* const sources = (int4*)lds;     // [n_sources], and the one that this workgroup takes
-        const int tid = threadIdx.x, n = a.n_sources;
+        int* const keys = (int*)lds;          // [kRanked]: lengths and, among equal ones, places
+        int4* const chosen = (int4*)(keys + kRanked);
+        const int tid = threadIdx.x, n = a.n_sources, chunk = s / per_round, place = chunk & 1 ? min(chunk * per_round + per_round, n) - 1 - (s - chunk * per_round) : s;
         if (tid < n) o = source_of(st, a, tid);
-        if (tid < n) sources[tid] = make_int4(o.q0, o.m, o.first, o.keys);
+        const int key = tid < n ? o.keys << 8 | (kRanked - 1 - tid) : -1;
+        keys[tid] = key;
         __syncthreads();
         int before = 0;
-        if (tid < n)
-            for (int i = 0; i < n; ++i) before += sources[i].w > o.keys || (sources[i].w == o.keys && i < tid);
-        if (tid < n && before == s) sources[n] = make_int4(o.q0, o.m, o.first, o.keys);
+#pragma unroll 4
+        for (int i = 0; i < n; i += 4) {      // without a branch, so that many reads are on their way
+            const int4 four = *(const int4*)(keys + i);
+            before += (four.x > key) + (four.y > key) + (four.z > key) + (four.w > key);
+        }
+        if (tid < n && before == place) *chosen = make_int4(o.q0, o.m, o.first, o.keys);
         __syncthreads();
-        const int4 v = sources[n];
+        const int4 v = *chosen;
         o = {__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), __builtin_amdgcn_readfirstlane(v.w)};
         __syncthreads();
     } else o = source_of(st, a, s);
@@ -952,14 +958,14 @@ bool is_listed(const Sizes& z, int64_t n_tokens, int64_t n_rows)
 template <int D, bool PAD, int WAVES, bool ORDERED> hipError_t launch_whole(const Sizes& z, const States& st, const CrossAttention& a, hipStream_t stream)
 {
     constexpr size_t kLds = kFewLds<D, WAVES>;
-    static_assert(!ORDERED || (kLds >= (kRanked + 1) * sizeof(int4) && 64 * WAVES >= kRanked), "a source to a thread");
+    static_assert(!ORDERED || (kLds >= (kRanked + 4) * 4 && 64 * WAVES == kRanked), "a source to a thread");
     static const hipError_t configured =
         hipFuncSetAttribute((const void*)cross_attention_whole_kernel<D, PAD, WAVES, ORDERED>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
     if (configured != hipSuccess) return configured;
     // 100 sources of 200 to 600 rows, 16 heads of 64, 46.3 us with dies and 49.3 without, 64 sources the same, 16 of 500 rows 10.9 and 10.4
     const int dies = a.n_sources >= 64 ? 8 : 1;
     hipLaunchKernelGGL((cross_attention_whole_kernel<D, PAD, WAVES, ORDERED>), dim3((unsigned)((a.n_sources + dies - 1) / dies * dies * st.kv_heads), (unsigned)z.row_blocks()),
-                       dim3(64 * WAVES), kLds, stream, st, a, dies);
+                       dim3(64 * WAVES), kLds, stream, st, a, dies, (int)std::max<int64_t>(1, 256 / st.kv_heads));
     return hipGetLastError();
 }
 
@@ -1004,8 +1010,10 @@ template <int D> hipError_t launch(const Sizes& z, const States& st, const Cross
         // eight, 8.7 with four, 2000 10.9 and 13.4; 16 heads of 64, 500 rows 8.9 and 8.3, 8 of 128, 640 rows 14.3 and 13.4.
         if constexpr (D == 32)
             if (z.groups() <= 256) return exact ? launch_whole<D, false, 8, false>(z, st, a, stream) : launch_whole<D, true, 8, false>(z, st, a, stream);
-        // ranked while the last workgroups matter: 64 sources of 60 to 1500 rows, 16 heads of 64, 63 -> 56 us; 150 of 500 to 1000 98 -> 104
-        if (z.n_sources <= kRanked && z.groups() > 512 && z.groups() <= 2048)
+        // Ranked / as they come, us, 16 heads of 64 and four beams: 24 sources of 60 to 1500 rows 18.7 / 24.9, 64 53.1 / 62.0, 64 of 197 16.6 / 15.0, 80 of 1 to
+        // 600 28.1 / 29.7, 100 of 60 to 1500 73 / 88, 125 of 1 to 600 43.1 / 39.6 (every workgroup ranks them all), 150 of 500 to 1000 99 / 98.
+        const int64_t groups = z.groups(), longest = z.max_rows * z.dim;
+        if (z.n_sources <= kRanked && groups > 256 && (groups <= 1024 || (groups <= 2048 && longest >= 49152)))
             return exact ? launch_whole<D, false, kFewWaves, true>(z, st, a, stream) : launch_whole<D, true, kFewWaves, true>(z, st, a, stream);
         return exact ? launch_whole<D, false, kFewWaves, false>(z, st, a, stream) : launch_whole<D, true, kFewWaves, false>(z, st, a, stream);
     }
