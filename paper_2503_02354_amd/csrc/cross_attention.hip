@@ -317,8 +317,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cross_attention_few_kernel(
 // of the chip's eight dies, to which workgroups are dealt in turn: their rows' bytes lie side by side.  ORDERED: the longest sources first (every
 // workgroup ranks them all, at most kRanked), so that those which start last are short, and that every die gets its share; each second round of
 // workgroups (one to a compute unit) the other way round, so that every unit gets long and short ones.  Bound by memory, or by a
-// chain of round trips where there is little of it: 64 sources of 60 to 1500 rows with five beams, 16 heads of 64 (209 MB), 41 us where they have just been
-// read and 55 where not (the rate of a copy: 43); one source of 197 rows, four beams, 12 heads, 6.0 us in a graph.
+// chain of round trips where there is little of it: 64 sources of 60 to 1500 rows with five beams, 16 heads of 64 (209 MB), 40 us where they have just been
+// read and 51 where not (the rate of a copy: 43); one source of 197 rows, four beams, 12 heads, 6.0 us in a graph.
 constexpr int kRanked = 256;
 template <int D, bool PAD, int WAVES, bool ORDERED>
 __global__ __launch_bounds__(64 * WAVES, 2) void cross_attention_whole_kernel(States st, CrossAttention a, int dies, int per_round)
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cross_attention_whole_kernel(St
         int4* const chosen = (int4*)(keys + kRanked);
         const int tid = threadIdx.x, n = a.n_sources, chunk = s / per_round, place = chunk & 1 ? min(chunk * per_round + per_round, n) - 1 - (s - chunk * per_round) : s;
         if (tid < n) o = source_of(st, a, tid);
-        const int key = tid < n ? o.keys << 8 | (kRanked - 1 - tid) : -1;
+        const int key = tid < n ? o.keys << 8 | (kRanked - 1 - tid) : -1;          // is_whole() has at most 8192 rows
         keys[tid] = key;
         __syncthreads();
         int before = 0;
@@ -922,9 +922,10 @@ bool is_few(const Sizes& z) { return z.rows() <= kFewRows; }
 // Whether a workgroup of its own for every source and head is faster than equal stretches and a join, by the longest source and the number of
 // workgroups.  Single tokens of four beams in a graph, whole / stretches, us, sources of equal lengths, then of lengths from one up: 16 heads of 64, 1 source
 // 1000 rows 11.0 / 13.5, 2000 17.9 / 15.6; 4 sources 2000 19.0 / 19.7 and 18.9 / 16.0; 8 sources 2000 19.3 / 23.7 and 18.9 / 20.4, 4000 50.5 / 41.2 and
-// 32.5 / 23.9; 16 sources 2000 32.4 / 43.1 and 19.5 / 25.0, 4000 60.1 / 68.8 and 50.5 / 45.2; 32 sources 2000 61.7 / 69.3 and 48.3 / 55.0, 4000 120 / 121 and
-// 93 / 77; 64 sources 2000 118 / 119 and 71 / 99.  8 heads of 128: 8 sources 500 rows 12.9 / 15.0, 1000 20.0 / 16.1; 16 sources 1000 20.3 / 21.2 and 19.7 /
-// 24.3, 2000 50.4 / 38.9; 32 sources 1000 33.1 / 37.8 and 20.9 / 41.9, 4000 113 / 117 and 96 / 70; 64 sources 1000 61.2 / 62.5 and 44.1 / 53.5.
+// 32.5 / 23.9; 16 sources 2000 32.4 / 43.1 and 19.5 / 25.0, 4000 60.1 / 68.8 and 50.5 / 45.2; 32 sources 2000 62.4 / 69.5 and 36.3 / 54.6, 4000 123 / 121 and
+// 67 / 79; 64 sources 2000 118 / 118 and 67 / 101, 4000 237 / 230 and 129 / 152.  8 heads of 128: 8 sources 500 rows 12.9 / 15.0, 1000 20.0 / 16.1; 16 sources
+// 1000 20.3 / 21.2 and 19.7 / 24.3, 2000 50.4 / 38.9; 32 sources 1000 33.1 / 37.8 and 21.0 / 42.2, 4000 113 / 117 and 96 / 70; 64 sources 1000 63.7 / 62.6 and
+// 36.9 / 53.6, 2000 117 / 115 and 67 / 87, 4000 from one up 122 / 118.
 // Chunks of tokens, a workgroup for 32 rows of each / units, listed or scheduled, 16 heads of 64: one source 40 tokens 1000 rows 11.6 / 17.5, 4000 33.0 / 22.9,
 // 300 tokens 1000 rows 12.1 / 19.4, 1000 tokens (512 workgroups) 500 rows 13.4 / 13.1; 4 sources 100 tokens 2000 rows 20.6 / 25.9, 4000 34.1 / 33.1; 300 tokens
 // (640) 200 rows 11.3 / 9.8, 1000 28.0 / 20.8; 16 sources 300 tokens 1000 rows 103 / 38.  32 heads on 8 of 128: one source 100 tokens 1000 rows 20.1 / 26.1, 2000
@@ -933,7 +934,7 @@ bool is_few(const Sizes& z) { return z.rows() <= kFewRows; }
 bool is_whole(const Sizes& z)
 {
     const int64_t longest = z.max_rows * z.dim, groups = z.groups();
-    if (z.row_blocks() == 1) return longest <= (groups >= 256 ? 229376 : groups >= 128 ? 163840 : 81920);
+    if (z.row_blocks() == 1) return longest <= (groups > 256 ? 262144 : groups >= 128 ? 163840 : 81920);
     if (groups <= 256) return longest <= 163840;
     return z.n_sources > kListed && groups <= 1536 && groups * longest <= 16ll << 20;
 }
