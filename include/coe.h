@@ -438,8 +438,8 @@ int coe_cross_attention(const coe_states* states, int32_t n_sources, int32_t n_t
  * -1, -1, 0.  With picks == beams, next_score and next_ended are the next step's score and ended, and next_row coe_kv_fork's parent; outputs
  * must not alias inputs.
  * beams in 1..COE_BEAM_MAX, picks in 1..COE_BEAM_PICKS_MAX, n_requests * beams below 2^23.
- * Numerics: exponentials and their sums over a few hundred tokens in fp32, sums over a row, logarithms and scores in fp64, in which candidates
- * are compared; one rounding of next_score to fp32.  The same inputs give the same outputs, and rows of equal bits equal scores.
+ * Numerics: exponentials and their sums over a lane's tokens (a few hundred of a vocabulary of 128,000) in fp32, sums over a row, logarithms and scores in
+ * fp64, in which candidates are compared; one rounding of next_score to fp32.  The same inputs give the same outputs, and rows of equal bits equal scores.
  * workspace: coe_beam_workspace bytes (may be 0), 16-byte aligned. */
 #define COE_BEAM_MAX 32
 #define COE_BEAM_PICKS_MAX 64

@@ -317,7 +317,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void cross_attention_few_kernel(
 // of the chip's eight dies, to which workgroups are dealt in turn: their rows' bytes lie side by side.  ORDERED: the longest sources first (every
 // workgroup ranks them all, at most kRanked), so that those which start last are short, and that every die gets its share; each second round of
 // workgroups (one to a compute unit) the other way round, so that every unit gets long and short ones.  Bound by memory, or by a
-// chain of round trips where there is little of it: 64 sources of 60 to 1500 rows with five beams, 16 heads of 64 (209 MB), 40 us where they have just been
+// chain of round trips where there is little of it: 64 sources of 60 to 1500 rows with five beams, 16 heads of 64 (209 MB), 38 us where they have just been
 // read and 51 where not (the rate of a copy: 43); one source of 197 rows, four beams, 12 heads, 6.0 us in a graph.
 constexpr int kRanked = 256;
 template <int D, bool PAD, int WAVES, bool ORDERED>
