@@ -425,7 +425,7 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
 // ---- requests -----------------------------------------------------------------------------------------------------
 // A workgroup per request: the rows' sums, then the best of all lists.  From a score on that enough of the threads' best reach, candidates are listed and
 // counted against each other.  Where that is too many, since few lists have the best of all, the score is searched for among all candidates; where those that
-// are equal are too many still (rows of one value), they are found one after the other, at 8 us each.
+// are equal are too many still (rows of one value), they are found one after the other, at 6 us each.
 // Bound by latency, that of its instructions' first use among it, so its loops are left as they are: 5.9 us for one request of four beams, 7.0 for 64 of eight,
 // 10 to 12 for 2048 keys.
 constexpr int kMeet = 512, kKeys = 2048;      // candidates that are listed; a request's keys, which are kept in LDS
