@@ -201,7 +201,7 @@ __device__ int cut_list(unsigned long long* list, int n, int picks, uint32_t& lo
 // One wavefront's share of a part of a row, its 16-byte pieces [begin, end); all of the workgroup's wavefronts call this together.  SAFE: NaN counts as
 // -inf, and equal infinities weigh 1; without it they, and maxima beyond kHuge, make the sum NaN.  quarter: [kWaves] what every wavefront's quarter of the picks reaches, 0 for
 // not yet.
-template <typename T, bool SAFE>
+template <typename T, bool SAFE, bool STREAM>
 __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int end, int wid, int picks, unsigned long long* list, volatile uint32_t* quarter, int& n, float& top, double& sum)
 {
     typedef typename Vec<T>::type Piece;
@@ -215,7 +215,10 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             const long long piece = at + j * 64 + lane;
-            if (piece < whole) to[j] = *(const Piece*)(row + piece * W);
+            if (piece < whole) {
+                if constexpr (STREAM) to[j] = __builtin_nontemporal_load((const Piece*)(row + piece * W));
+                else to[j] = *(const Piece*)(row + piece * W);
+            }
         }
     };
     auto unpack = [&](float (&x)[kPerLane], const Piece (&from)[kPieces], long long at) __attribute__((always_inline)) {
@@ -340,7 +343,7 @@ __device__ __forceinline__ void scan_row(const T* row, int vocab, int begin, int
 
 __device__ __forceinline__ bool is_there(const BeamSelection& s, int64_t row) { return s.score[row] > -INFINITY; }
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s, int parts, RowPart* stats, unsigned long long* lists)
 {
     constexpr int W = Vec<T>::kWidth;
@@ -361,11 +364,11 @@ __global__ __launch_bounds__(kThreads, 4) void beam_rows_kernel(BeamSelection s,
     double sum;
     if (tid < kWaves) quarter[tid] = 0;
     __syncthreads();
-    scan_row<T, false>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
+    scan_row<T, false, STREAM>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
     if (__syncthreads_or(sum != sum)) {       // a quarter that counted NaN or signs of them holds for nobody
         if (tid < kWaves) quarter[tid] = 0;
         __syncthreads();
-        scan_row<T, true>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
+        scan_row<T, true, STREAM>(x, s.vocab, begin, end, wid, s.picks, list[wid], quarter, n, top, sum);
     }
     // the wavefronts' lists without what the quarters pass, behind each other; then a key to a thread: its place is the number of larger ones
     const int lane = tid & 63;
@@ -651,8 +654,12 @@ hipError_t beam_select(int dtype, const BeamSelection& s, void* workspace, hipSt
     const int parts = row_parts(rows, s.beams, s.picks, s.vocab);
     RowPart* const stats = (RowPart*)workspace;
     unsigned long long* const lists = (unsigned long long*)(stats + rows * parts);
-    if (dtype == 0) hipLaunchKernelGGL(beam_rows_kernel<float>, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, s, parts, stats, lists);
-    else hipLaunchKernelGGL(beam_rows_kernel<uint16_t>, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, s, parts, stats, lists);
+    // Logits that would fill the second-level caches pass by them: 512 rows of 128,000 in bf16 44.5 -> 42.2 us, of 64,000 in fp32 38.3 -> 35.0, 64 rows 22.6 ->
+    // 21.8; 32 rows, 8 MB, 37.7 -> 39.8 with 32 picks.
+    const bool stream_by = rows * s.vocab * (dtype == 0 ? 4 : 2) >= 12ll << 20;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, s, parts, stats, lists); };
+    if (dtype == 0) stream_by ? launch(beam_rows_kernel<float, true>) : launch(beam_rows_kernel<float, false>);
+    else stream_by ? launch(beam_rows_kernel<uint16_t, true>) : launch(beam_rows_kernel<uint16_t, false>);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(beam_meet_kernel, dim3((unsigned)s.n_requests), dim3(kThreads), 0, stream, s, parts, stats, lists);
     return hipGetLastError();
