@@ -812,6 +812,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kerne
         shown[0] = shown_of(0, s0);
         load(0, shown[0]);
         shown[1] = shown_of(1, s1);
+        if (tiles > 1) load(1, shown[1]);
         shown[2] = shown_of(2, s2);
         const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
@@ -821,13 +822,11 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void cross_attention_many_kerne
         if (works) {
             read_half(v0, 0, 0);
             read_half(v1, 0, 1);
-        }
-        if (tiles > 1) load(1, shown[1]);
-        if (works) {
             u32x4 k[kSteps];
             read_keys(k, 0);
             scores(sc, k);
             mask(sc, shown[0], 0);
+            m = highest(sc);                  // what the first half would move the reference to
         }
     }
     for (int t = 0; t < tiles; ++t) {
