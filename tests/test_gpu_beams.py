@@ -371,6 +371,18 @@ def test_cross_units(B, heads, kv, dim, max_rows):
             c.check(*c.run(B, max_rows=max_rows))
 
 
+@pytest.mark.parametrize("n,beams", [(1, 1), (2, 3), (64, 1), (65, 1), (64, 2), (130, 2)])
+def test_cross_units_of_many_sources(B, n, beams):
+    """On both sides of the number of sources whose units their workgroups find; sources and beams without rows or tokens among them."""
+    rng = np.random.default_rng(n + beams)
+    sources = [(int(r), tuple(int(m) for m in rng.choice([0, 1, 17, 40, 70], beams))) for r in rng.choice([0, 1, 63, 64, 65, 200], n)]
+    sources[n // 2] = (1100, (300,) * beams)
+    for heads, kv, dim in ((16, 16, 64), (16, 4, 128)):
+        c = Cross(sources, heads, kv, dim, beams=beams, seed=n, hidden=0.1)
+        for max_rows in (1200, 6000):
+            c.check(*c.run(B, max_rows=max_rows))
+
+
 @pytest.mark.parametrize("max_rows", LIMITS)
 @pytest.mark.parametrize("heads,kv,dim,m", [(32, 8, 128, 150), (16, 16, 64, 150), (8, 2, 128, 1), (4, 4, 64, 5)])
 def test_cross_hidden_rows_by_form(B, heads, kv, dim, m, max_rows):
