@@ -58,9 +58,11 @@ __device__ __forceinline__ bool is_empty(float mx, float sum) { return mx == -IN
 [[maybe_unused]] __device__ __forceinline__ float weight_of_part(float from, float to) { return from == to ? 1.f : exp2f(from - to); }
 
 // Room for values of 2^110: the weights that meet in a sum of fp32 add up to 2^17, so that they and the values stay below 2^128.  A part's
-// own do: the few-rows kernel's are 1 at most (and its stretches hold 2^17 keys of a history at most, unless a step has 2^26 cached tokens x cache heads), the
-// many-rows kernel moves its reference.  Joining adds up to some 512 parts: their outputs are taken times 2^-10 and the result back.
-[[maybe_unused]] constexpr float kJoinRoom = 0x1p-10f;
+// own do: the few-rows kernels' are 1 at most (and their stretches hold 2^17 keys of a history or source at most, unless a step has 2^26 cached tokens x cache
+// heads, or rows x heads of states), the many-rows kernels move their reference.  Joining adds up kMostParts parts at most: their outputs are
+// taken times 1 / kMostParts, so that all of them together are no more than one, and the result back.
+[[maybe_unused]] constexpr int kMostParts = 1024;
+[[maybe_unused]] constexpr float kJoinRoom = 1.f / kMostParts;
 
 // Where 16-byte chunk c of row r of a V tile lies: chunks in an order that spreads both the writes (sixteen rows of
 // one chunk) and the transposing reads (four rows of four chunks) over all LDS banks.

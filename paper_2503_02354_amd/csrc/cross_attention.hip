@@ -26,6 +26,7 @@ constexpr int kFewWaves = 4;
 // workgroups: two, three or four per compute unit, as many as registers allow
 template <int D> constexpr int kFewGroups = D <= 32 ? 1024 : D <= 64 ? 768 : 512;
 constexpr int kMostFewGroups = 1024;
+static_assert(kMostFewGroups <= kMostParts, "a part of every stretch at most");
 
 // A source's queries and rows, within the arrays.
 struct Source {
@@ -433,7 +434,8 @@ __global__ __launch_bounds__(256) void cross_attention_join_kernel(States st, Cr
 // 1,460 to 1,620 us by card, 0.94 to 1.04 PFLOP/s, at 1.66 to 1.75 GHz; 16 of 4000 rows with 2000 tokens, 24 heads of 64, 0.88 to 0.91; 20 of 200 to 2100 with 30 to 900, 0.67,
 // units of 18 tiles, whose beginnings and ends (first loads, a first maximum, stores) count.
 constexpr int kManyRows = 128, kManyKeys = 64, kManyWaves = 4;
-constexpr int kManyGroups = 512;          // two workgroups per compute unit
+constexpr int kManyGroups = 512;          // two workgroups per compute unit; a unit has no more parts
+static_assert(kManyGroups <= kMostParts, "joins have room for all of them");
 constexpr int kListed = 64;               // sources that a workgroup looks at for its unit: one to a lane
 
 struct Unit {

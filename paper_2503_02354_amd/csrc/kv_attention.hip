@@ -22,6 +22,7 @@ constexpr int kKeys = 32;                 // keys of a tile
 constexpr int kFewRows = 32;              // query rows of a request and cache head that the kernel for few rows takes
 constexpr int kFewWaves = 4;
 constexpr int kFewGroups = 512;           // its workgroups: two per compute unit
+static_assert(kFewGroups <= kMostParts, "a part of every stretch at most");
 
 // A request's new tokens and the cached tokens [begin, end) that at least one of them sees.
 struct Span {

@@ -1144,3 +1144,24 @@ def test_example_writes_what_the_dense_model_scores(B):
     small = describe.Writer(d, n_blocks=20, block_size=8, max_len=48)
     with pytest.raises(RuntimeError, match="too small"):
         small.write(states, prompts, 4, 10)
+
+
+@pytest.mark.parametrize("heads,dim", [(1, 32), (2, 64), (4, 128), (1, 24)])
+def test_cross_large_values_in_the_most_parts(B, heads, dim):
+    """Just below 2^26 rows, all in one place, of equal weight and with values of 2^110: as many parts as there are stretches, each with as many
+    weights as a call within its limits can give it.  Sums of equal powers of two are exact up to 2^24 weights and 2^-24 of them off beyond, far below the
+    half step of 2^-9 that a result of 2^110 has room for."""
+    import torch
+    n = 2 ** 26 - 1
+    k, v = torch.ones(dim, dtype=torch.bfloat16, device="cuda"), torch.full((dim,), 2.0 ** 110, dtype=torch.bfloat16, device="cuda")
+    q = torch.randn(heads, dim, generator=torch.Generator().manual_seed(dim)).bfloat16().cuda()
+    out, lse = torch.zeros(heads, dim, dtype=torch.bfloat16, device="cuda"), torch.zeros(heads, device="cuda")
+    need = B.coe_cross_attention_workspace(1, 1, 1, n, heads, 1, dim)
+    assert need > 0
+    work, d = torch.empty(need, dtype=torch.uint8, device="cuda"), [_dev(np.array(a, np.int32)) for a in ([0, 1], [0], [n])]
+    B.coe_cross_attention(B.coe_states(1, n, 1, dim, k.data_ptr(), v.data_ptr(), 0, 0, 0, 0, 0), 1, 1, 1, 1, n, heads, 0.0, q.data_ptr(), heads * dim, dim, *(t.data_ptr() for t in d),
+                          out.data_ptr(), heads * dim, dim, lse.data_ptr(), work.data_ptr(), need, _stream())
+    torch.cuda.synchronize()
+    assert (out.float() == 2.0 ** 110).all()
+    # log2 of the sum within a step of its 26 (2^-19), times ln 2 1.3e-6; ln 2 itself 5e-7 of 18, the product's rounding 2^-20: 2.8e-6 in all
+    assert (lse.double() - math.log(n)).abs().max() <= 4 * 18 * 2.0 ** -24
