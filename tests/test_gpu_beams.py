@@ -1165,3 +1165,55 @@ def test_cross_large_values_in_the_most_parts(B, heads, dim):
     assert (out.float() == 2.0 ** 110).all()
     # log2 of the sum within a step of its 26 (2^-19), times ln 2 1.3e-6; ln 2 itself 5e-7 of 18, the product's rounding 2^-20: 2.8e-6 in all
     assert (lse.double() - math.log(n)).abs().max() <= 4 * 18 * 2.0 ** -24
+
+
+# ---- forms that the sizes above do not choose --------------------------------------------------------------------------------
+def _is_whole(B, c, max_rows):
+    """Above 64 sources only the form with a workgroup for every 32 query rows needs no workspace; returns its workgroups."""
+    rows = c.most * (c.heads // c.kv)
+    assert len(c.length) > 64 and B.coe_cross_attention_workspace(len(c.length), int(c.off[-1]), c.most, max_rows, c.heads, c.kv, c.dim) == 0
+    return len(c.length) * c.kv * -(-rows // 32)
+
+
+@pytest.mark.parametrize("n,beams,heads,kv,dim,tokens,rows", [
+    (65, 1, 2, 2, 64, 100, 200), (100, 2, 2, 2, 64, 50, 200), (65, 1, 2, 2, 96, 100, 200), (81, 1, 2, 2, 128, 90, 120), (65, 4, 8, 2, 64, 10, 200), (70, 1, 8, 2, 128, 33, 180),
+    (65, 1, 8, 2, 96, 33, 200), (72, 1, 6, 3, 40, 40, 200)])
+def test_cross_ranked_sources_with_several_row_blocks(B, n, beams, heads, kv, dim, tokens, rows):
+    """More than 64 short sources with more than 32 query rows: ranked by length, a source's row blocks and heads on one die; sources without rows,
+    without tokens, with full and short last blocks among them."""
+    rng = np.random.default_rng(n + dim)
+    sources = [(int(a), tuple(int(m) for m in rng.choice([0, 1, tokens // 3, tokens - 1, tokens], beams))) for a in rng.choice([0, 1, 31, 32, 33, 100, rows - 1, rows], n)]
+    sources[n // 3], sources[n - 1], sources[0] = (rows, (tokens,) * beams), (rows, (tokens,) * beams), (0, (tokens,) * beams)
+    for hidden in (0.0, 0.3):
+        c = Cross(sources, heads, kv, dim, beams=beams, seed=n, hidden=hidden)
+        assert 256 < _is_whole(B, c, rows) <= 1024 and c.most * (heads // kv) > 32
+        got, logs = c.run(B)
+        c.check(got, logs)
+        for value in (0x7FC0, 0xFF80) if hidden else ():
+            c.kv_bits[:, np.flatnonzero(c.seen == 0)] = value
+            again, logs_again = c.run(B)
+            assert np.array_equal(got, again) and np.array_equal(logs, logs_again)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_cross_unranked_sources_with_several_row_blocks(B, dim):
+    """More sources than are ranked, two row blocks each."""
+    rng = np.random.default_rng(dim)
+    sources = [(int(a), int(m)) for a, m in zip(rng.choice([0, 1, 33, 64, 100], 300), rng.choice([0, 1, 32, 33, 40], 300))]
+    sources[7] = (100, 40)
+    for hidden in (0.0, 0.3):
+        c = Cross(sources, 2, 1, dim, seed=dim, hidden=hidden) if dim == 64 else Cross(sources, 1, 1, dim, seed=dim, hidden=hidden)
+        assert 256 < _is_whole(B, c, 100) <= 1536
+        c.check(*c.run(B))
+
+
+@pytest.mark.parametrize("n,heads,kv,dim,rows,beams", [(200, 16, 8, 64, 800, 2), (200, 8, 8, 96, 550, 1), (129, 12, 12, 128, 400, 2), (256, 8, 8, 64, 780, 1)])
+def test_cross_ranked_sources_beyond_a_thousand_workgroups(B, n, heads, kv, dim, rows, beams):
+    """Longer sources are ranked up to 2048 workgroups: several rounds of the chip's compute units, every second the other way round."""
+    rng = np.random.default_rng(n)
+    sources = [(int(a), tuple(int(m) for m in rng.integers(0, 3, beams))) for a in rng.choice([0, 1, 64, 64, 65, 300, rows], n)]
+    sources[n // 2] = (rows, (2,) * beams)
+    for hidden in (0.0, 0.4):
+        c = Cross(sources, heads, kv, dim, beams=beams, seed=n, hidden=hidden)
+        assert 1024 < _is_whole(B, c, rows) <= 2048 and rows * dim >= 49152
+        c.check(*c.run(B))
