@@ -1217,3 +1217,34 @@ def test_cross_ranked_sources_beyond_a_thousand_workgroups(B, n, heads, kv, dim,
         c = Cross(sources, heads, kv, dim, beams=beams, seed=n, hidden=hidden)
         assert 1024 < _is_whole(B, c, rows) <= 2048 and rows * dim >= 49152
         c.check(*c.run(B))
+
+
+@pytest.mark.parametrize("heads,kv,dim,m,max_rows", [
+    (8, 2, 128, 1, 640), (8, 2, 128, 1, 50000), (4, 4, 64, 40, 1200), (4, 1, 32, 8, 50000),          # a workgroup each; stretches
+    (16, 8, 64, 400, 1200), (32, 8, 128, 400, 1200), (32, 8, 128, 400, 50000), (2, 1, 64, 300, 50000)])       # units, listed; scheduled and cut
+def test_cross_bits_do_not_depend_on_the_others(B, heads, kv, dim, m, max_rows):
+    """At equal sizes a source's bits are the same whatever the other sources and their queries hold, and a query's whatever the queries beside it do: where
+    some need another reference than others, or are NaN, the rest keep theirs."""
+    rng = np.random.default_rng(dim + m)
+    rows = [min(n, max_rows) for n in (600, 333, 1200)]
+    for hidden in (0.0, 0.2):
+        c = Cross([(n, m) for n in rows], heads, kv, dim, seed=m, hidden=hidden)
+        want, logs = c.run(B, max_rows=max_rows)
+        c.check(want, logs)
+        q, states = c.q.copy(), c.kv_bits.copy()
+        own, mine = slice(int(c.off[1]), int(c.off[2])), slice(int(c.first[1]), int(c.first[1]) + rows[1])
+        for sharp, odd in ((30.0, None), (0.0, None), (1.0, 0x7FC0), (1.0, 0x7F80)):
+            c.q[:], c.kv_bits[:] = _bf16(sharp * rng.standard_normal(q.shape)), _bf16(sharp * rng.standard_normal(states.shape))
+            if odd is not None:
+                c.q[::3], c.kv_bits[:, ::5] = odd, odd
+            c.q[own], c.kv_bits[:, mine] = q[own], states[:, mine]
+            got, again = c.run(B, max_rows=max_rows)
+            assert np.array_equal(got[own], want[own]) and np.array_equal(again[own], logs[own])
+        c.kv_bits[:] = states
+        for sharp, odd in ((30.0, None), (0.0, None), (1.0, 0x7FC0)):
+            for kept in (0, 1):                                          # every second token, so that a tile of rows holds both sorts
+                other = np.arange(len(q)) % 2 != kept
+                c.q[:] = q
+                c.q[other] = _bf16(sharp * rng.standard_normal(q[other].shape)) if odd is None else odd
+                got, again = c.run(B, max_rows=max_rows)
+                assert np.array_equal(got[~other], want[~other]) and np.array_equal(again[~other], logs[~other])
