@@ -1248,3 +1248,37 @@ def test_cross_bits_do_not_depend_on_the_others(B, heads, kv, dim, m, max_rows):
                 c.q[other] = _bf16(sharp * rng.standard_normal(q[other].shape)) if odd is None else odd
                 got, again = c.run(B, max_rows=max_rows)
                 assert np.array_equal(got[~other], want[~other]) and np.array_equal(again[~other], logs[~other])
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 130001), ("f32", 60001)])
+def test_select_odd_values_in_large_batches(B, dtype, vocab):
+    """More than 12 MB of logits, which are loaded past the caches: what test_select_odd_values and test_select_large_logits hold, late in a row too,
+    masks of finite values over most of a vocabulary, ended and absent beams, rows at odd places."""
+    to = (lambda a: _bf16(a)) if dtype == "bf16" else (lambda a: np.asarray(a, np.float32))
+    rng = np.random.default_rng(vocab)
+    x = 3 * rng.standard_normal((64, vocab))
+    assert to(x[:1]).nbytes * 64 >= 12 << 20
+    hide = rng.random((64, vocab)) < 0.9
+    for row, value in ((8, -1e4), (9, -1e9), (10, -3.38e38), (11, -np.inf), (12, -100.0), (13, -65540.0)):
+        x[row, hide[row]] = value
+    x[16], x[17, 1:], x[18, :-1] = -np.inf, -np.inf, -np.inf
+    x[19, -2], x[20, [5, -1]] = np.inf, np.inf
+    x[21, -3] += 1e6
+    x[22] += 65545
+    x[23] -= 65540
+    x[24, vocab // 2:] += 65540
+    x[25, vocab // 2:] -= 1e6
+    x[26] *= 1e30
+    x[27] = -3e38
+    x[28, :vocab // 3] = -1e5
+    bits = to(x)
+    nan = (0x7FC0, 0xFFC1) if dtype == "bf16" else (np.float32(np.nan), -np.float32(np.nan))
+    bits[32, -1], bits[33, 7], bits[34, ::3], bits[35], bits[36, 1:] = nan[0], nan[1], nan[0], nan[1], nan[0]
+    bits[37, hide[37]] = nan[0]
+    score = -rng.uniform(0, 9, 64).astype(np.float32)
+    score[[3, 40]], score[[5, 50]] = -np.inf, np.nan
+    ended = np.zeros(64)
+    ended[[1, 14, 33, 41, 42, 63]] = 1
+    for picks in (9, 32):
+        _check_select(B, bits, score, ended, 8, picks, 2, dtype)
+    _check_select(B, bits, -rng.uniform(0, 9, 64).astype(np.float32), None, 16, 16, 2, dtype)
