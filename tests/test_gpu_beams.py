@@ -1282,3 +1282,28 @@ def test_select_odd_values_in_large_batches(B, dtype, vocab):
     for picks in (9, 32):
         _check_select(B, bits, score, ended, 8, picks, 2, dtype)
     _check_select(B, bits, -rng.uniform(0, 9, 64).astype(np.float32), None, 16, 16, 2, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_select_the_longest_row(B, dtype):
+    """A row of 2^31 - 1 tokens of one logit, and a few better ones: at its ends and next to 2^30.  Equal ones come by token."""
+    import torch
+    vocab, t = 2 ** 31 - 1, torch.float32 if dtype == "f32" else torch.bfloat16
+    x = torch.full((vocab,), -8.0, dtype=t, device="cuda")
+    best = {vocab - 1: 9.0, 2 ** 30: 8.5, 0: 8.0, 2 ** 30 - 1: 7.5, vocab - 8: 7.0, 123456789: 7.0}
+    for i, value in best.items():
+        x[i] = value
+    out, score = [torch.zeros(8, dtype=q, device="cuda") for q in (torch.float32, torch.int32, torch.int32)], torch.full((1,), -2.0, device="cuda")
+    need = B.coe_beam_workspace(1, 1, 8, vocab)
+    work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    B.coe_beam_select(1, 1, 8, vocab, B.COE_DT_F32 if dtype == "f32" else B.COE_DT_BF16, x.data_ptr(), vocab, score.data_ptr(), 0, 2, *(o.data_ptr() for o in out), 0, work.data_ptr(), need,
+                      _stream())
+    torch.cuda.synchronize()
+    del x
+    tokens = [vocab - 1, 2 ** 30, 0, 2 ** 30 - 1, 123456789, vocab - 8, 1, 2]
+    logits = np.array([9.0, 8.5, 8.0, 7.5, 7.0, 7.0, -8.0, -8.0])
+    lse = math.log(sum(math.exp(v) for v in best.values()) + (vocab - len(best)) * math.exp(-8.0))
+    assert out[2].tolist() == tokens and out[1].tolist() == [0] * 8
+    # as in _check_select: a lane's sum of 2^15 terms of one value is exact, or has one larger term, beside which each rounds by 2^-24 of the sum: 2^-9
+    # of that lane's sum at most, which is a term of 2^16 such sums
+    assert (np.abs(out[0].double().cpu().numpy() - (-2.0 + logits - lse)) <= 2.0 ** -24 * 32 + 2.0 ** -20).all()
