@@ -410,7 +410,8 @@ typedef struct {
 
 /* Attention of tokens over their source's states.  Source s is the rows first[s] .. first[s] + length[s] - 1 of the states, in any order and
  * overlapping as the caller likes; its queries are rows q_off[s * beams] .. q_off[(s + 1) * beams] - 1 of q, at most max_new of them (q_off:
- * [n_sources * beams + 1] as coe_kv_plan writes it; beams share their source's states, which are read once for all of them).  Every query sees
+ * [n_sources * beams + 1] as coe_kv_plan writes it; beams share their source's states, which are read once for all of them, where they make at most 32 query
+ * rows for a head of the states, else once for every 32 or 128).  Every query sees
  * every row of its source that is not hidden.  Query head h reads head h / (heads / kv_heads) of the states.
  *   out = softmax_j(scale * q . k_j) v_j      lse = ln sum_j exp(scale * q . k_j)
  * A query that sees nothing (length 0, every row hidden), or whose scores are all -inf, gets out = 0 and lse = -inf; one with a score that is
@@ -438,6 +439,8 @@ int coe_cross_attention(const coe_states* states, int32_t n_sources, int32_t n_t
  * -1, -1, 0.  With picks == beams, next_score and next_ended are the next step's score and ended, and next_row coe_kv_fork's parent; outputs
  * must not alias inputs.
  * beams in 1..COE_BEAM_MAX, picks in 1..COE_BEAM_PICKS_MAX, n_requests * beams below 2^23.
+ * Masks: -inf costs nothing.  Logits of -89 and below are as good as others, but rows that hold many are read twice, and long runs of one value take several times as
+ * long again.
  * Numerics: exponentials and their sums over a lane's tokens (a few hundred of a vocabulary of 128,000) in fp32, sums over a row, logarithms and scores in
  * fp64, in which candidates are compared; one rounding of next_score to fp32.  The same inputs give the same outputs, and rows of equal bits equal scores.
  * workspace: coe_beam_workspace bytes (may be 0), 16-byte aligned. */

@@ -108,8 +108,12 @@ __device__ __forceinline__ uint32_t wave_min(uint32_t v) { return ~wave_max(~v);
 // quarter of them in every wavefront (each says what its quarter reaches after its first step, its second, its fourth, ...; the lowest of the four holds), or
 // all of them in its own list.  A list that grows all the same is cut back to at most kSlack more than picks.  Indices ascend from step to step, so an
 // equal logit that comes later in the same wavefront is never wanted, but in another it may be.
-// What bounds it is waiting for memory, half of a wavefront's time: 512 rows of 128,000 in bf16, a seventh of them without a pass (113 MB), 34 us, 3.3 TB/s; four
-// rows of 50,001 fp32 7.0 us, of which a step's round trip, the threshold and the lists at the end are most.
+// What bounds it is waiting for memory, half of a wavefront's time: 512 rows of 128,000 in bf16 (131 MB) 35.8 us, 3.7 TB/s; where a seventh of them has no pass (113 MB) 34.6,
+// 3.3 TB/s, since their compute units have fewer wavefronts than others then.  Four rows of 50,001 fp32 7.0 us, of which a step's round trip, the threshold and the lists at
+// the end are most.
+// Finite masks cost a second pass: a lane that begins with nothing above -88.7 scales its sum, 0, by more than fp32 holds, and so does one whose maximum stays
+// beyond kHuge; both say NaN, and the part is read again with SAFE.  The same call with nine logits in ten masked, at random, by -88 or -inf 40 us, by -90 to -3e38 76 to 77;
+// four rows 12.0 and 16.3.  And a step of one value is a list of 1024 equal logits, to be cut: the last nine tenths of every row -50 143 us, -1e4 281, -inf 36.
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kPerLane = 16, kStep = 64 * kPerLane, kSlack = 32, kGrow = 64;
 constexpr int kList = kBeamPicksMax + kGrow + kStep;
 static_assert(kBeamPicksMax + kGrow <= 128 && kWaves * 128 <= kList, "two keys of a list to a lane, all lists in the place of one");

@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) void cross_attention_join_kernel(States st, Cr
 // tiles into three, in turn; a wavefront reads every key and value of a tile for its 32 rows.
 // Bound by the matrix cores and the vector unit, which takes the exponentials: a 32 x 32 x 16 product hides about 20 of its 32 cycles of vector instructions,
 // and beside each lie some 36 cycles of them with 64 channels, 18 with 128.  Four sources of 3500 to 7000 rows with 2901 to 4900 tokens each, 32 heads on 8 of 128:
-// 1,460 to 1,620 us by card, 0.94 to 1.04 PFLOP/s, at 1.66 to 1.75 GHz; 16 of 4000 rows with 2000 tokens, 24 heads of 64, 0.88 to 0.91; 20 of 200 to 2100 with 30 to 900, 0.67,
+// 1,420 to 1,620 us by card, 0.94 to 1.07 PFLOP/s, clocks of 1.66 to 1.75 GHz among them; 16 of 4000 rows with 2000 tokens, 24 heads of 64, 0.88 to 0.91; 20 of 200 to 2100 with 30 to 900, 0.67,
 // units of 18 tiles, whose beginnings and ends (first loads, a first maximum, stores) count.
 constexpr int kManyRows = 128, kManyKeys = 64, kManyWaves = 4;
 constexpr int kManyGroups = 512;          // two workgroups per compute unit; a unit has no more parts
@@ -1013,7 +1013,8 @@ template <int D> hipError_t launch(const Sizes& z, const States& st, const Cross
         if constexpr (D == 32)
             if (z.groups() <= 256) return exact ? launch_whole<D, false, 8, false>(z, st, a, stream) : launch_whole<D, true, 8, false>(z, st, a, stream);
         // Ranked / as they come, us, 16 heads of 64 and four beams: 24 sources of 60 to 1500 rows 18.7 / 24.9, 64 53.1 / 62.0, 64 of 197 16.6 / 15.0, 80 of 1 to
-        // 600 28.1 / 29.7, 100 of 60 to 1500 73 / 88, 125 of 1 to 600 43.1 / 39.6 (every workgroup ranks them all), 150 of 500 to 1000 99 / 98.
+        // 600 28.1 / 29.7, 100 of 60 to 1500 73 / 88, 125 of 1 to 600 43.1 / 39.6 (every workgroup ranks them all), 150 of 500 to 1000 99 / 98.  Sizes do not tell
+        // equal lengths, which are ranked for nothing: 64 of 197 is what that costs.
         const int64_t groups = z.groups(), longest = z.max_rows * z.dim;
         if (z.n_sources <= kRanked && groups > 256 && (groups <= 1024 || (groups <= 2048 && longest >= 49152)))
             return exact ? launch_whole<D, false, kFewWaves, true>(z, st, a, stream) : launch_whole<D, true, kFewWaves, true>(z, st, a, stream);
